@@ -103,8 +103,8 @@ def work(case):
     if case["op"] == "logprobs":  # tokens in; logprob, lse, entropy, alternatives out; sub, scale, exp, add, fma
         return {"bytes": rows * vocab * size + rows * (8 + 12 + 12 * k), "flops": 6 * rows * vocab}
     if case["op"] == "backward":
-        return {"bytes": (kept + rows) * vocab * size + rows * (8 + 8 + (8 if case["entropy"] else 0) + 12 * k),
-                "flops": 5 * kept * vocab}
+        return {"bytes": (kept + rows) * vocab * size + rows * (8 + 4 + (4 if case["entropy"] else 0) + 12 * k),
+                "flops": (11 if case["entropy"] else 8) * kept * vocab}
     out = rows * vocab * size if case["grad"] else 0
     return {"bytes": kept * vocab * size + out + rows * (8 + 12 * k), "flops": (9 if case["grad"] else 5) * kept * vocab}
 
@@ -153,16 +153,11 @@ def prepare(case, seed):
             s["top_token"] = torch.empty((rows, k), dtype=torch.int64, device="cuda")
             s["top_logprob"] = vector(rows, k)
     elif case["op"] == "backward":
-        # what the forward pass left, and the upstream gradients
-        s["lse"], s["entropy"] = vector(rows), vector(rows)
+        # upstream gradients, and the alternatives that the forward pass named
         if k:
             s["top_token"] = torch.empty((rows, k), dtype=torch.int64, device="cuda")
-        for a in range(0, rows, 512):
-            logp = torch.log_softmax(s["logits"][a:a + 512].float() / case["temperature"], 1)
-            s["lse"][a:a + 512] = torch.logsumexp(s["logits"][a:a + 512].float() / case["temperature"], 1)
-            s["entropy"][a:a + 512] = -(logp.exp() * logp).sum(1)
-            if k:
-                s["top_token"][a:a + 512] = logp.topk(k, 1).indices
+            for a in range(0, rows, 512):
+                s["top_token"][a:a + 512] = s["logits"][a:a + 512].topk(k, 1).indices
         s["d_logprob"] = upstream(rows).masked_fill(padding, 0.0)
         s["d_entropy"] = upstream(rows).masked_fill(padding, 0.0) if case["entropy"] else None
         s["d_top_logprob"] = upstream(rows, k).masked_fill(padding[:, None], 0.0) if k else None
@@ -214,14 +209,17 @@ def _plain_logprobs(s):
 def _plain_backward(s):
     case = s["case"]
     u = s["logits"].float() / case["temperature"]
-    logp = u - s["lse"][:, None]
-    p = torch.exp(logp)
+    u = u - u.amax(1, keepdim=True)
+    e = torch.exp(u)
+    total = e.sum(1, keepdim=True)
+    p = e / total
     a = -s["d_logprob"]
     if case["k"]:
         a = a - s["d_top_logprob"].sum(1)
     if s["d_entropy"] is not None:
-        a = a - s["d_entropy"] * s["entropy"]
-        d = p * (a[:, None] - s["d_entropy"][:, None] * logp)
+        logp = u - torch.log(total)
+        entropy = -(p * logp).sum(1, keepdim=True)
+        d = p * (a[:, None] - s["d_entropy"][:, None] * (logp + entropy))
     else:
         d = p * a[:, None]
     d.scatter_add_(1, s["tokens"][:, None], s["d_logprob"][:, None])
@@ -275,8 +273,8 @@ def _own_logprobs(s):
 
 
 def _own_backward(s):
-    _qn().qn_logprobs_backward(s["logits"], s["lse"], s["dlogits"], tokens=s["tokens"], d_logprob=s["d_logprob"],
-                               entropy=s["entropy"], d_entropy=s["d_entropy"], top_token=s.get("top_token"),
+    _qn().qn_logprobs_backward(s["logits"], s["dlogits"], tokens=s["tokens"], d_logprob=s["d_logprob"],
+                               d_entropy=s["d_entropy"], top_token=s.get("top_token"),
                                d_top_logprob=s["d_top_logprob"], temperature=s["case"]["temperature"])
     return {"dlogits": s["dlogits"]}
 
