@@ -351,6 +351,105 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
                                 void* cuda_stream);
 
 /*
+ * The Worker's side: losses over a vocabulary and their gradients (the paper takes grad J(theta_k) as given; for a
+ * language model it starts at the logits).  A Worker whose J is a token loss turns the dlogits of one of the calls below
+ * into its g_k with its model's own backward pass.
+ *
+ * Three calls without a handle: they need no workspace, keep nothing between calls and may overlap on different
+ * streams.  They run on the device that holds `logits`; every other pointer must be device memory of that device (or
+ * managed memory), and cuda_stream one of its streams.  Each call is one kernel launch, never waits for the device, and
+ * gives the same bits each time it is given the same inputs.  Pointers must be aligned to their element type; rows that
+ * start anywhere else than on 16 bytes lose no more than their first and last vector to element-wise loads.
+ *
+ * Common arguments
+ *   rows, vocab     the matrix of logits; rows >= 0 (0: nothing is done), 1 <= vocab < 2^31
+ *   dtype           storage type of logits and dlogits; all other real values are fp32
+ *   logits          DEVICE, element (r, i) at r * row_stride + i, row_stride >= vocab; read only
+ *   temperature     T > 0: the distribution is softmax(z / T), u_i = z_i / T, p_i = exp(u_i - lse)
+ *   tokens          int64, as torch indexes; tokens < 0 stand for "none"
+ * Arithmetic: fp32 with sums per thread, added over the row in a fixed order; one rounding to the storage type when
+ * dlogits is written.  Offsets are 64-bit.
+ *
+ * What a row may hold.  -inf is a masked token (probability 0); the type's lowest value is an ordinary, very small
+ * logit (a row that holds nothing else is uniform).  A row of -inf only is empty.  A row with a NaN or +inf has no
+ * distribution: its numbers, or its whole gradient, are NaN.  A given token >= vocab gives NaN in its row.  Nothing in
+ * one row reaches another.
+ *
+ * Errors: QN_ERR_INVALID for a bad argument, QN_ERR_CUDA for a failed launch; nothing is launched in the first case.
+ */
+#define QN_TOP_MAX 128           /* largest number of alternatives, and of a teacher's tokens in a row */
+#define QN_GRAD_MAX_VOCAB 393216 /* largest vocab of the calls that keep a row on the chip (1.5 MB of fp32) */
+
+/*
+ * Log probabilities of given tokens, with entropy and top alternatives.
+ *   tokens        int64[rows], may be NULL (then logprob must be NULL too)
+ *   logprob       [rows]  u_t - lse of the given token; 0 where the token is < 0; -inf for a masked token or an empty row
+ *   lse           [rows]  ln sum_i exp(u_i); -inf for an empty row
+ *   entropy       [rows]  -sum_i p_i ln p_i; 0 for an empty row
+ *   k             0 <= k <= QN_TOP_MAX alternatives
+ *   top_token     int64[rows][k]  tokens of the k largest logits, largest first, ties in order of their index
+ *   top_logprob   [rows][k]       their u_i - lse
+ *                 Masked tokens are no alternatives: where fewer than k are left, the rest is -1 and -inf.  A row without
+ *                 a distribution gives -1 and NaN.
+ * Each output may be NULL (top_token and top_logprob together, with k = 0), but not all of them.  Outputs must not
+ * overlap the logits.
+ */
+QN_API qn_status qn_logprobs(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
+                             const int64_t* tokens, double temperature, float* logprob, float* lse, float* entropy,
+                             int32_t k, int64_t* top_token, float* top_logprob, void* cuda_stream);
+
+/*
+ * The gradient of anything built from qn_logprobs' outputs, with respect to the logits:
+ *   dlogits_i = 1/T * [ d_logprob (1[i = t] - p_i) + d_lse p_i - d_entropy p_i (ln p_i + H)
+ *                       + sum_k d_top_k (1[i = top_k] - p_i) ]
+ * from the same logits, tokens and temperature, and the top_token that qn_logprobs wrote.  The distribution is
+ * recomputed from the row, which stays on the chip for it: nothing else has to be kept from the forward call, and ln p_i
+ * does not pass through a rounded lse.
+ *   d_logprob, d_lse, d_entropy   [rows], and d_top_logprob [rows][k]: upstream gradients, each may be NULL (zero), not all
+ *   tokens      needed with d_logprob; rows whose token is < 0 ignore their d_logprob
+ *   top_token   needed with d_top_logprob; entries < 0 ignore their gradient.  A token may occur more than once.
+ *   dlogits     DEVICE, [rows] of vocab elements dlogits_stride >= vocab apart, each element written; either `logits`
+ *               itself (same pointer and stride: the gradient takes the logits' place) or memory that does not overlap it
+ * A row whose upstream gradients are all 0 is padding: it is not read, whatever it holds, and its gradient is 0.  An
+ * empty row's gradient is 0 but for the 1[..] terms.  vocab <= QN_GRAD_MAX_VOCAB.
+ */
+QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits,
+                                      int64_t row_stride, const int64_t* tokens, double temperature,
+                                      const float* d_logprob, const float* d_lse, const float* d_entropy, int32_t k,
+                                      const int64_t* top_token, const float* d_top_logprob, void* dlogits,
+                                      int64_t dlogits_stride, void* cuda_stream);
+
+/*
+ * Distillation from a teacher's top logits: the loss of each row and, in the same call, its gradient (the row stays on
+ * the chip between the two, so it is read once; a backward pass is this call with dlogits).
+ *   k               1 <= k <= QN_TOP_MAX tokens of the teacher for each row
+ *   teacher_token   int64[rows][k]; < 0: absent.  The tokens of a row must differ from one another (not checked; a row
+ *                   that repeats one gets a finite but unspecified loss and gradient).  A token >= vocab makes the row's
+ *                   outputs NaN.
+ *   teacher_value   [rows][k] of teacher_dtype (QN_F32 or QN_BF16), by `teacher`:
+ *     QN_TEACHER_LOGITS     logits v_k: q = softmax(v / T) over the list alone,
+ *                           L = sum_k q_k (ln q_k - ln p_k)
+ *     QN_TEACHER_LOGPROBS   log probabilities at this temperature, as qn_logprobs writes them: q_k = exp(v_k); all other
+ *                           tokens are one more outcome, q_r = max(0, 1 - sum_k q_k) and p_r = sum of p_i off the list:
+ *                           L = sum_k q_k (ln q_k - ln p_k) + q_r (ln q_r - ln p_r)
+ *                           (a list that names the whole vocabulary has no such outcome)
+ *   weight          [rows], NULL = 1.  A row of weight 0 is padding: it is not read, its loss and gradient are 0.
+ *   loss            [rows]  L, without the weight
+ *   dlogits         NULL (the loss alone), or weight * dL/dlogits:
+ *                           weight / T * (Q p_i - q_i) on the list, weight / T * (Q p_i - q_r p_i / p_r) off it, Q = sum q
+ *                   placed as in qn_logprobs_backward (dlogits_stride, in place or apart)
+ * A row without any teacher token has loss 0 and gradient 0 and is not read.  A token that the student masks and the
+ * teacher does not makes the loss +inf (the gradient stays finite); an empty row of the student has loss +inf, gradient 0.
+ * vocab <= QN_GRAD_MAX_VOCAB.
+ */
+#define QN_TEACHER_LOGITS 0
+#define QN_TEACHER_LOGPROBS 1
+QN_API qn_status qn_distill(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
+                            int32_t k, const int64_t* teacher_token, qn_dtype teacher_dtype, const void* teacher_value,
+                            int32_t teacher, double temperature, const float* weight, float* loss, void* dlogits,
+                            int64_t dlogits_stride, void* cuda_stream);
+
+/*
  * Per-kernel timing, for benchmarks.  Between qn_timing_begin and qn_timing_end every kernel the
  * handle launches (up to max_kernels of them) is bracketed by two CUDA events recorded on the
  * stream of the call.  qn_timing_end waits for those events and returns, per kind of kernel,

@@ -9,11 +9,16 @@ from . import qn  # noqa: F401
 from .qn import (  # noqa: F401
     QN_BF16,
     QN_F32,
+    QN_TEACHER_LOGITS,
+    QN_TEACHER_LOGPROBS,
     QNError,
     Handle,
     qn_create,
     qn_destroy,
+    qn_distill,
     qn_gram,
+    qn_logprobs,
+    qn_logprobs_backward,
     qn_push,
     qn_rebuild,
     qn_status_sync,

@@ -7,6 +7,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "qn_host.h"
 #include "qn_internal.h"
 
 struct qn_ctx {
@@ -88,19 +89,6 @@ extern "C" const char* qn_strerror(qn_status s) {
 
 namespace {
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev) {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = (prev == dev) || cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard() {
-        int cur = -1;
-        if (prev >= 0 && cudaGetDevice(&cur) == cudaSuccess && cur != prev) cudaSetDevice(prev);
-    }
-};
-
 inline bool finite_d(double x) { return isfinite(x); }
 
 // Brackets one kernel launch with an NVTX range (visible to a profiler, free without one) and, when timing is on
@@ -149,23 +137,6 @@ qn_status check_step_args(qn_handle h, double tau, double lambda, const void* th
     if (!h || !theta_new) return QN_ERR_INVALID;
     if (!finite_d(tau) || !finite_d(lambda) || !(lambda > 0.0)) return QN_ERR_INVALID;
     return QN_OK;
-}
-
-// A pointer the kernels of this handle may dereference: device memory of the handle's device, or managed memory.
-// Anything else (host memory, another GPU's memory) would fault on the device, so it is refused on the host.
-bool on_device(const void* p, int dev) {
-    cudaPointerAttributes a;
-    if (cudaPointerGetAttributes(&a, p) != cudaSuccess) {
-        cudaGetLastError();
-        return false;
-    }
-    if (a.type == cudaMemoryTypeManaged) return true;
-    return a.type == cudaMemoryTypeDevice && a.device == dev;
-}
-
-bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
-    return a0 < b0 + nb && b0 < a0 + na;
 }
 
 // After the first solve of a step whose Gram pass had reduced precision: the same pass with every product in fp64,

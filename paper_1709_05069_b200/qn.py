@@ -17,6 +17,10 @@ QN_MAX_M = 64
 QN_GRAM_PATH_AUTO = 0
 QN_GRAM_PATH_PLAIN_ALU = 1
 QN_GRAM_PATH_FP64 = 2
+QN_TOP_MAX = 128
+QN_TEACHER_LOGITS = 0
+QN_TEACHER_LOGPROBS = 1
+QN_GRAD_MAX_VOCAB = 393216
 
 (QN_OK, QN_ERR_INVALID, QN_ERR_ALLOC, QN_ERR_CUDA, QN_ERR_STATE, QN_ERR_NOT_CONVERGED, QN_ERR_NONFINITE,
  QN_ERR_DEVICE_TIMEOUT) = range(8)
@@ -33,6 +37,7 @@ EXPORTS = (
     "qn_timing_begin",
     "qn_timing_end",
     "qn_gram_static", "qn_selftest_bounded_wait",
+    "qn_logprobs", "qn_logprobs_backward", "qn_distill",
 )
 TIME_KINDS = ("gram", "solve", "combine", "row")
 KERNEL_NAMES = {
@@ -91,6 +96,10 @@ def lib() -> ctypes.CDLL:
         L.qn_gram_static.argtypes, L.qn_gram_static.restype = [i64, i32, i32, vp, vp, vp], i32
         L.qn_timing_begin.argtypes, L.qn_timing_begin.restype = [vp, i32], i32
         L.qn_timing_end.argtypes, L.qn_timing_end.restype = [vp, vp, vp], i32
+        L.qn_logprobs.argtypes = [i64, i64, i32, vp, i64, vp, dbl, vp, vp, vp, i32, vp, vp, vp]
+        L.qn_logprobs_backward.argtypes = [i64, i64, i32, vp, i64, vp, dbl, vp, vp, vp, i32, vp, vp, vp, i64, vp]
+        L.qn_distill.argtypes = [i64, i64, i32, vp, i64, i32, vp, i32, vp, i32, dbl, vp, vp, vp, i64, vp]
+        L.qn_logprobs.restype = L.qn_logprobs_backward.restype = L.qn_distill.restype = i32
         _lib = L
     return _lib
 
@@ -427,3 +436,113 @@ def qn_gram_static(g: torch.Tensor, gram_out: torch.Tensor, stream=None) -> None
     with torch.cuda.device(g.device):
         _check(lib().qn_gram_static(int(n), int(m), dtype_code(g.dtype), g.data_ptr(), gram_out.data_ptr(),
                                     _stream_ptr(stream)), "qn_gram_static")
+
+
+# ---- losses over a vocabulary (no handle) ---------------------------------------------------------------------------
+
+
+def _logit_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
+    """rows, vocab, row stride, dtype code of a matrix of logits (or their gradient)."""
+    if not t.is_cuda or t.dim() != 2:
+        raise ValueError("%s must be a CUDA tensor [rows][vocab]" % name)
+    rows, vocab = t.shape
+    stride, inner = t.stride()
+    if rows <= 1 and stride < vocab:
+        stride = vocab
+    if vocab < 1 or (inner != 1 and vocab != 1) or stride < vocab:
+        raise ValueError("%s must have contiguous rows that do not overlap" % name)
+    return rows, vocab, stride, dtype_code(t.dtype)
+
+
+def _beside(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: torch.device, name: str) -> int:
+    """Address of a small array that goes with the logits (0 for None)."""
+    if t is None:
+        return 0
+    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, list(shape), device))
+    return t.data_ptr()
+
+
+def _gradient(t: torch.Tensor, logits: torch.Tensor, name: str) -> Tuple[int, int]:
+    """Address and row stride of the gradient of ``logits``."""
+    if t.shape != logits.shape or t.dtype != logits.dtype or t.device != logits.device:
+        raise ValueError("%s must have the shape, dtype and device of the logits" % name)
+    return t.data_ptr(), _logit_matrix(t, name)[2]
+
+
+def _stream_on(device: torch.device, stream) -> int:
+    return int((torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+
+
+def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+                lse: Optional[torch.Tensor] = None, entropy: Optional[torch.Tensor] = None,
+                top_token: Optional[torch.Tensor] = None, top_logprob: Optional[torch.Tensor] = None,
+                temperature: float = 1.0, stream=None) -> None:
+    """Log probability of one given token in each row of ``logits`` [rows][vocab], with lse, entropy and the ``k``
+    largest alternatives (k: the width of ``top_token``), in one launch.
+
+    Outputs are the tensors that are passed: ``logprob``, ``lse``, ``entropy`` float32 [rows], ``top_token`` int64 and
+    ``top_logprob`` float32 [rows][k]; ``tokens`` is int64 [rows], negative for "none".  Nothing waits for the device."""
+    rows, vocab, stride, code = _logit_matrix(logits, "logits")
+    dev, k = logits.device, 0
+    if top_token is not None or top_logprob is not None:
+        if top_token is None or top_logprob is None or top_token.dim() != 2:
+            raise ValueError("top_token and top_logprob go together, [rows][k] each")
+        k = top_token.shape[1]
+    f32, one = torch.float32, (rows,)
+    _check(lib().qn_logprobs(rows, vocab, code, logits.data_ptr(), stride,
+                             _beside(tokens, torch.int64, one, dev, "tokens"), temperature,
+                             _beside(logprob, f32, one, dev, "logprob"), _beside(lse, f32, one, dev, "lse"),
+                             _beside(entropy, f32, one, dev, "entropy"), k,
+                             _beside(top_token, torch.int64, (rows, k), dev, "top_token"),
+                             _beside(top_logprob, f32, (rows, k), dev, "top_logprob"), _stream_on(dev, stream)),
+           "qn_logprobs")
+
+
+def qn_logprobs_backward(logits: torch.Tensor, dlogits: torch.Tensor, tokens: Optional[torch.Tensor] = None,
+                         d_logprob: Optional[torch.Tensor] = None, d_lse: Optional[torch.Tensor] = None,
+                         d_entropy: Optional[torch.Tensor] = None, top_token: Optional[torch.Tensor] = None,
+                         d_top_logprob: Optional[torch.Tensor] = None, temperature: float = 1.0, stream=None) -> None:
+    """Gradient with respect to the logits, into ``dlogits`` (which may be ``logits`` itself), of a loss whose upstream
+    gradients with respect to ``qn_logprobs``' outputs are ``d_logprob``, ``d_lse``, ``d_entropy`` [rows] and
+    ``d_top_logprob`` [rows][k] (with the ``top_token`` that the forward call wrote), in one launch."""
+    rows, vocab, stride, code = _logit_matrix(logits, "logits")
+    dev, k = logits.device, 0
+    if d_top_logprob is not None:
+        if top_token is None or d_top_logprob.dim() != 2:
+            raise ValueError("d_top_logprob [rows][k] goes with top_token")
+        k = d_top_logprob.shape[1]
+    f32, one = torch.float32, (rows,)
+    out, out_stride = _gradient(dlogits, logits, "dlogits")
+    _check(lib().qn_logprobs_backward(rows, vocab, code, logits.data_ptr(), stride,
+                                      _beside(tokens, torch.int64, one, dev, "tokens"), temperature,
+                                      _beside(d_logprob, f32, one, dev, "d_logprob"),
+                                      _beside(d_lse, f32, one, dev, "d_lse"),
+                                      _beside(d_entropy, f32, one, dev, "d_entropy"), k,
+                                      _beside(top_token, torch.int64, (rows, k), dev, "top_token") if k else 0,
+                                      _beside(d_top_logprob, f32, (rows, k), dev, "d_top_logprob") if k else 0, out,
+                                      out_stride, _stream_on(dev, stream)), "qn_logprobs_backward")
+
+
+def qn_distill(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_value: torch.Tensor, loss: torch.Tensor,
+               dlogits: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None, temperature: float = 1.0,
+               teacher: int = QN_TEACHER_LOGPROBS, stream=None) -> None:
+    """Loss of each row of the student's ``logits`` against a teacher's top tokens (into ``loss`` float32 [rows]) and, if
+    ``dlogits`` is given (it may be ``logits`` itself), the gradient of sum(weight * loss), in one launch.
+
+    ``teacher_token`` int64 [rows][k] (negative: absent), ``teacher_value`` float32 or bfloat16 [rows][k]: log
+    probabilities as ``qn_logprobs`` writes them (``QN_TEACHER_LOGPROBS``: the rest of the vocabulary is one more outcome)
+    or logits (``QN_TEACHER_LOGITS``: normalised over the list).  ``weight`` float32 [rows], 0 for padding."""
+    rows, vocab, stride, code = _logit_matrix(logits, "logits")
+    dev = logits.device
+    if teacher_token is None or teacher_value is None or loss is None or teacher_token.dim() != 2:
+        raise ValueError("teacher_token and teacher_value [rows][k] and loss [rows] are required")
+    k = teacher_token.shape[1]
+    out, out_stride = _gradient(dlogits, logits, "dlogits") if dlogits is not None else (0, 0)
+    _check(lib().qn_distill(rows, vocab, code, logits.data_ptr(), stride, k,
+                            _beside(teacher_token, torch.int64, (rows, k), dev, "teacher_token"),
+                            dtype_code(teacher_value.dtype),
+                            _beside(teacher_value, teacher_value.dtype, (rows, k), dev, "teacher_value"), teacher,
+                            temperature, _beside(weight, torch.float32, (rows,), dev, "weight"),
+                            _beside(loss, torch.float32, (rows,), dev, "loss"), out, out_stride,
+                            _stream_on(dev, stream)), "qn_distill")
