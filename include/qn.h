@@ -358,7 +358,8 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  * Three calls without a handle: they need no workspace, keep nothing between calls and may overlap on different
  * streams.  They run on the device that holds `logits`; every other pointer must be device memory of that device (or
  * managed memory), and cuda_stream one of its streams.  Each call is one kernel launch, never waits for the device, and
- * gives the same bits each time it is given the same inputs.  Pointers must be aligned to their element type; rows that
+ * gives the same bits each time it is given the same inputs (at the same addresses modulo 16: the alignment of a row
+ * decides which elements are added first).  Pointers must be aligned to their element type; rows that
  * start anywhere else than on 16 bytes lose no more than their first and last vector to element-wise loads.
  *
  * Common arguments

@@ -12,7 +12,8 @@ LIB_PATH = os.path.join(_PKG, "libqn.so")
 
 SOURCES = ["qn_api.cu", "qn_gram.cu", "qn_solve.cu", "qn_combine.cu", "qn_row.cu", "qn_static.cu", "qn_gram_tc.cu",
            "qn_logprobs.cu", "qn_distill.cu"]
-HEADERS = ["qn_internal.h", "qn_device.cuh", "qn_host.h", "qn_vocab.cuh"]
+HEADERS = ["qn_internal.h", "qn_device.cuh", "qn_host.h", "qn_vocab.cuh",
+           "qn_vocab_grad.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

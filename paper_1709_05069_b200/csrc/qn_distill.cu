@@ -1,16 +1,14 @@
 // qn_distill: a student's loss against a teacher's top logits, and its gradient.
 //
-// One CTA takes a row.  With e_i = 2^((z_i - m) log2(e) / T) and the student's sums kept apart for the list (S_l) and the
+// An operator of the row-gradient kernel.  With e_i = 2^((z_i - m) log2(e) / T) and the student's sums kept apart for the list (S_l) and the
 // rest (S_r), S = S_l + S_r: p_k = e_k / S, and the mass off the list p_r = S_r / S comes without a subtraction.
 #include <nvtx3/nvToolsExt.h>
 
-#include "qn_vocab.cuh"
+#include "qn_vocab_grad.cuh"
 
 namespace {
 
 using namespace qn;
-
-constexpr int kThreads = 256;
 
 struct DistillParams {
     const void* logits;
@@ -26,83 +24,156 @@ struct DistillParams {
     int64_t dlogits_stride;
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) distill_kernel(const DistillParams p) {
-    __shared__ float scratch[kThreads / 32];
-    __shared__ double scratch_sum[kThreads / 32];
-    __shared__ int32_t list[QN_TOP_MAX];
-    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-        const T* z = static_cast<const T*>(p.logits) + r * p.row_stride;
-        T* out = p.dlogits ? static_cast<T*>(p.dlogits) + r * p.dlogits_stride : nullptr;
-        const float w = p.weight ? p.weight[r] : 1.0f;
-        __syncthreads();  // list of the last row
-        // thread j's entry of the teacher's list
-        const int j = threadIdx.x;
-        const int64_t at = j < p.k ? p.token[r * p.k + j] : -1;
-        const bool here = at >= 0 && at < p.vocab;
-        if (j < p.k) list[j] = here ? (int32_t)at : -1;
-        const bool wrong = __syncthreads_or(at >= p.vocab);
-        const int named = __syncthreads_count(here);
-        float v = -INFINITY;
-        if (here) {
-            v = p.value_bf16 ? Storage<__nv_bfloat16>::load1(static_cast<const __nv_bfloat16*>(p.value) + r * p.k + j)
-                             : __ldg(static_cast<const float*>(p.value) + r * p.k + j);
-        }
-        float logq = v, q_rest = 0.0f;
-        bool none = named == 0 && !wrong;
-        if (p.logprobs) {
-            // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
-            const double sum = block_reduce<double, add_op>(exp((double)v), scratch_sum);
-            if (named < p.vocab) q_rest = sum != sum ? NAN : (float)fmax(0.0, 1.0 - sum);
-        } else {
-            const float top = block_reduce<float, max_op>(v, scratch);
-            if (top == -INFINITY && !__syncthreads_or(v != v)) none = none || !wrong;
-            const float d = top == -INFINITY ? -INFINITY : (v - top) * p.inv_t;
-            logq = d - logf(block_reduce<float, add_op>(v != v ? NAN : expf(d), scratch));
-        }
-        if (w == 0.0f || none) {
-            if (threadIdx.x == 0) p.loss[r] = 0.0f;
-            if (out)
-                for (int i = threadIdx.x; i < p.vocab; i += kThreads) Storage<T>::store1(out + i, 0.0f);
-            continue;
-        }
-        const float q = wrong ? NAN : here ? expf(logq) : 0.0f;
-        const float mass = block_reduce<float, add_op>(q, scratch) + q_rest;
+struct Distill {
+    using Params = DistillParams;
+    struct Shared {
+        int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
+        float q[QN_TOP_MAX], z[QN_TOP_MAX];
+        float4 scratch[32];
+        double scratch_sum[32];
+        float scratch_max[32];
+        float q_sum, q_log_q, q_rest, weight;
+        float on, unit;  // gradient on the list: on * e_k - unit * q_k
+    };
+    struct Partial {
+        float m, rest, list, dot, q;  // a slice's maximum; sums of e_i off and on the list; sums of q_k u_k and q_k
+        __device__ void poison() { rest = NAN; }
+    };
+    __device__ static __forceinline__ bool moments(const Params&) { return false; }
+    __device__ static void nothing(const Params& p, int64_t r) { p.loss[r] = 0.0f; }
 
-        const float zj = here ? load_rw(z + at) : -INFINITY;
-        float m = -INFINITY;
-        for (int i = threadIdx.x; i < p.vocab; i += kThreads) m = fmaxf(m, load_rw(z + i));
-        m = block_reduce<float, max_op>(m, scratch);
-        const bool empty = m == -INFINITY;
-        if (empty) m = 0.0f;
-        float rest = 0.0f;
-        for (int i = threadIdx.x; i < p.vocab; i += kThreads) {
-            bool on = false;
-            for (int a = 0; a < p.k; ++a) on = on || list[a] == i;
-            if (!on) rest += exp2_approx((load_rw(z + i) - m) * p.scale);
+    template <int NT>
+    __device__ static bool begin(const Params& p, Shared& sh, int64_t r) {
+        const float w = p.weight ? p.weight[r] : 1.0f;
+        if (w == 0.0f) return false;
+        constexpr int kMine = (QN_TOP_MAX + NT - 1) / NT;
+        float v[kMine];
+        int named = 0;
+        bool wrong = false, finite = false;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int j = threadIdx.x + i * NT;
+            v[i] = -INFINITY;
+            if (j >= p.k) continue;
+            const int64_t at = p.token[r * p.k + j];
+            const bool here = at >= 0 && at < p.vocab;
+            sh.pos[j] = here ? static_cast<int32_t>(at) : -1;
+            wrong = wrong || at >= p.vocab;
+            if (!here) continue;
+            ++named;
+            v[i] = p.value_bf16 ? Storage<__nv_bfloat16>::load1(static_cast<const __nv_bfloat16*>(p.value) + r * p.k + j)
+                                : __ldg(static_cast<const float*>(p.value) + r * p.k + j);
+            finite = finite || v[i] != -INFINITY;
         }
-        rest = block_reduce<float, add_op>(rest, scratch);
-        const float ej = here ? exp2_approx((zj - m) * p.scale) : 0.0f;
-        const float s = rest + block_reduce<float, add_op>(ej, scratch);
-        const float log_s = logf(s);
-        // q ln q - q ln p, nothing where the teacher has nothing
-        float term = wrong ? NAN : q > 0.0f ? q * (logq - ((zj - m) * p.inv_t - log_s)) : q;
-        if (empty) term = q > 0.0f ? INFINITY : q;
-        if (j == 0 && q_rest > 0.0f) term += q_rest * (logf(q_rest) - (empty ? -INFINITY : logf(rest) - log_s));
-        if (j == 0 && q_rest != q_rest) term = NAN;
-        const float loss = block_reduce<float, add_op>(term, scratch);
-        if (threadIdx.x == 0) p.loss[r] = loss;
-        if (!out) continue;
-        const float unit = w * p.inv_t;
-        const float on_coef = empty ? 0.0f : mass / s;
-        const float off_coef = empty ? 0.0f : on_coef - (q_rest > 0.0f && rest > 0.0f ? q_rest / rest : 0.0f);
-        __syncthreads();  // every logit of the list is fetched before the row may be overwritten
-        for (int i = threadIdx.x; i < p.vocab; i += kThreads)
-            Storage<T>::store1(out + i, unit * off_coef * exp2_approx((load_rw(z + i) - m) * p.scale));
+        wrong = __syncthreads_or(wrong);
+        // a row without a teacher: no token at all, or (logits) none that weighs anything
+        if (!wrong && !__syncthreads_or(p.logprobs ? named > 0 : finite)) return false;
+        float top = 0.0f, log_norm = 0.0f, inv = 1.0f;
+        if (!p.logprobs) {
+            top = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) top = fmaxf(top, v[i]);
+            top = block_reduce<float, max_op>(top, sh.scratch_max);
+            if (top == -INFINITY) top = 0.0f;
+            inv = p.inv_t;
+            double norm = 0.0;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) norm += exp(static_cast<double>((v[i] - top) * inv));
+            log_norm = static_cast<float>(log(block_reduce<double, add_op>(norm, sh.scratch_sum)));
+        }
+        // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
+        double q_sum = 0.0;
+        float q_log_q = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int j = threadIdx.x + i * NT;
+            if (j >= p.k) continue;
+            const float log_q = (v[i] - top) * inv - log_norm;
+            const double q = exp(static_cast<double>(log_q));
+            q_sum += q;
+            if (q != 0.0) q_log_q += static_cast<float>(q) * log_q;
+            sh.q[j] = static_cast<float>(q);
+        }
+        q_sum = block_reduce<double, add_op>(q_sum, sh.scratch_sum);
+        const float4 x = block_sum4<NT>(make_float4(q_log_q, static_cast<float>(named), 0.0f, 0.0f), sh.scratch);
+        if (threadIdx.x == 0) {
+            sh.weight = w;
+            sh.q_sum = wrong ? NAN : static_cast<float>(q_sum);
+            sh.q_log_q = x.x;
+            sh.q_rest = 0.0f;
+            if (p.logprobs && x.y < static_cast<float>(p.vocab))
+                sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
+        }
         __syncthreads();
-        if (here) Storage<T>::store1(out + at, empty ? 0.0f : unit * (on_coef * ej - q));
+        return true;
     }
-}
+
+    // The list leaves the sums: its logits are kept, and masked in the slice.
+    template <typename T, int NT>
+    __device__ static void before_sums(const Params& p, Shared& sh, const Slice<T>& s) {
+        for (int j = threadIdx.x; j < p.k; j += NT)
+            if (s.holds(sh.pos[j])) sh.z[j] = load_rw(s.elements() + (sh.pos[j] - s.origin()));
+        __syncthreads();
+        for (int j = threadIdx.x; j < p.k; j += NT)
+            if (s.holds(sh.pos[j])) s.elements()[sh.pos[j] - s.origin()] = masked<T>();
+        __syncthreads();
+    }
+
+    template <typename T, int NT>
+    __device__ static float slice_max(const Params& p, Shared& sh, const Slice<T>& s, float mine) {
+        for (int j = threadIdx.x; j < p.k; j += NT)
+            if (s.holds(sh.pos[j])) mine = fmaxf(mine, sh.z[j]);
+        return block_reduce<float, max_op>(mine, sh.scratch_max);
+    }
+
+    template <typename T, int NT>
+    __device__ static Partial sums(const Params& p, Shared& sh, const Slice<T>& s, float m, float sum, float) {
+        const float ref = m == -INFINITY ? 0.0f : m;
+        float list = 0.0f, dot = 0.0f, q = 0.0f;
+        for (int j = threadIdx.x; j < p.k; j += NT) {
+            if (!s.holds(sh.pos[j])) continue;
+            const float d = sh.z[j] - ref;
+            list += exp2_approx(d * p.scale);
+            if (sh.q[j] > 0.0f) dot += sh.q[j] * (d * p.inv_t);
+            q += sh.q[j];
+        }
+        const float4 x = block_sum4<NT>(make_float4(sum, list, dot, q), sh.scratch);
+        return {m, x.x, x.y, x.z, x.w};
+    }
+
+    __device__ static Gradient finish(const Params& p, Shared& sh, const Partial* part, int n, int64_t r, bool first) {
+        float m = -INFINITY;
+        for (int c = 0; c < n; ++c) m = fmaxf(m, part[c].m);
+        float rest = 0.0f, list = 0.0f, dot = 0.0f;
+        for (int c = 0; c < n; ++c) {
+            const Partial x = part[c];
+            const float f = x.m == m || x.m == -INFINITY ? 1.0f : exp2_approx((x.m - m) * p.scale);
+            rest += f * x.rest, list += f * x.list;  // a masked slice's are 0, or NaN where it holds one
+            dot += x.dot;
+            if (x.q > 0.0f && x.m != m) dot += x.q * ((x.m - m) * p.inv_t);
+        }
+        const float s = m == INFINITY ? NAN : rest + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
+        const bool empty = s == 0.0f;
+        const float log_s = logf(s);
+        if (first) {
+            // sum q (ln q - ln p) with ln p = u - m/T - ln S
+            float loss = empty ? INFINITY : sh.q_log_q - dot + sh.q_sum * log_s;
+            if (!empty && q_rest != 0.0f) loss += q_rest * (logf(q_rest) - (logf(rest) - log_s));
+            p.loss[r] = mass != mass ? NAN : loss;
+        }
+        sh.unit = empty ? 0.0f : sh.weight * p.inv_t;
+        sh.on = empty ? 0.0f : sh.unit * (mass / s);
+        const float off = q_rest > 0.0f && rest > 0.0f ? mass / s - q_rest / rest : mass / s;
+        return {m == -INFINITY ? 0.0f : m, empty ? 0.0f : sh.unit * off, 0.0f};
+    }
+
+    template <typename T, int NT, typename Store>
+    __device__ static void fix(const Params& p, Shared& sh, const Slice<T>& s, const Gradient& g, Store store) {
+        for (int j = threadIdx.x; j < p.k; j += NT)
+            if (s.holds(sh.pos[j]))
+                store(sh.pos[j], sh.on * exp2_approx((sh.z[j] - g.m) * p.scale) - sh.unit * sh.q[j]);
+    }
+};
 
 }  // namespace
 
@@ -130,10 +201,9 @@ extern "C" qn_status qn_distill(int64_t rows, int64_t vocab, qn_dtype dtype, con
                           static_cast<float>(1.0 / temperature), static_cast<float>(1.4426950408889634 / temperature),
                           weight, loss, dlogits, dlogits_stride};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    const unsigned grid = static_cast<unsigned>(rows < INT32_MAX ? rows : INT32_MAX);
     nvtxRangePushA("qn:distill");
-    if (dtype == QN_F32) distill_kernel<float><<<grid, kThreads, 0, st>>>(p);
-    else distill_kernel<__nv_bfloat16><<<grid, kThreads, 0, st>>>(p);
+    const cudaError_t e = dtype == QN_F32 ? launch_gradient<float, Distill>(p, st)
+                                          : launch_gradient<__nv_bfloat16, Distill>(p, st);
     nvtxRangePop();
-    return cudaGetLastError() == cudaSuccess ? QN_OK : QN_ERR_CUDA;
+    return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }

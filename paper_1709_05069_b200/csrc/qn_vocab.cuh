@@ -87,6 +87,26 @@ __device__ __forceinline__ V warp_reduce(V x) {
     return x;
 }
 
+// Sums of four values over the CTA, in a fixed order, with one pair of barriers.
+template <int NT>
+__device__ __forceinline__ float4 block_sum4(float4 x, float4* scratch) {
+    x.x = warp_reduce<float, add_op>(x.x);
+    x.y = warp_reduce<float, add_op>(x.y);
+    x.z = warp_reduce<float, add_op>(x.z);
+    x.w = warp_reduce<float, add_op>(x.w);
+    if constexpr (NT == 32) return x;
+    __syncthreads();  // scratch may still be read from the last use
+    if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
+    __syncthreads();
+    x = scratch[0];
+#pragma unroll
+    for (int w = 1; w < NT / 32; ++w) {
+        const float4 y = scratch[w];
+        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+    }
+    return x;
+}
+
 // Over the CTA, in a fixed order; every thread gets the result.  `scratch`: one V for each warp.
 template <typename V, V (*op)(V, V)>
 __device__ __forceinline__ V block_reduce(V x, V* scratch) {

@@ -354,7 +354,7 @@ def check_distill(qn, z, token, value, logprobs, temperature=1.0, weight=None, p
         src = out
     else:
         src, out = z, o.new((rows, vocab), z.dtype, vocab + pad, offset)
-    qn.qn_distill(z, token, value, alone, weight=weight, temperature=temperature, teacher=mode)
+    qn.qn_distill(src, token, value, alone, weight=weight, temperature=temperature, teacher=mode)
     qn.qn_distill(src, token, value, loss, dlogits=out, weight=weight, temperature=temperature, teacher=mode)
     torch.cuda.synchronize()
     o.check()
