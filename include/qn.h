@@ -379,7 +379,7 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  * Errors: QN_ERR_INVALID for a bad argument, QN_ERR_CUDA for a failed launch; nothing is launched in the first case.
  */
 #define QN_TOP_MAX 128           /* largest number of alternatives, and of a teacher's tokens in a row */
-#define QN_GRAD_MAX_VOCAB 393216 /* largest vocab of the calls that keep a row on the chip (1.5 MB of fp32) */
+#define QN_GRAD_MAX_VOCAB 393208 /* largest vocab of the calls that keep a row on the chip: 16 x 24576 less a vector */
 
 /*
  * Log probabilities of given tokens, with entropy and top alternatives.

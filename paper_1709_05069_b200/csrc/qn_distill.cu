@@ -24,154 +24,182 @@ struct DistillParams {
     int64_t dlogits_stride;
 };
 
+// Out of line: it is called for every entry of the list, and instruction cache is scarce in this kernel.
+__device__ __noinline__ double exp64(double x) { return exp(x); }
+
 struct Distill {
     using Params = DistillParams;
+    static constexpr bool kMoments = false, kListMessage = true, kMask = true;
+    static constexpr int kMine = QN_TOP_MAX / 32;  // entries of the list a lane
     struct Shared {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
         float q[QN_TOP_MAX], z[QN_TOP_MAX];
-        float4 scratch[32];
-        double scratch_sum[32];
-        float scratch_max[32];
         float q_sum, q_log_q, q_rest, weight;
-        float on, unit;  // gradient on the list: on * e_k - unit * q_k
+        Gradient g;
+        float rest, s, dot;  // of the row, relative to its maximum
     };
-    struct Partial {
-        float m, rest, list, dot, q;  // a slice's maximum; sums of e_i off and on the list; sums of q_k u_k and q_k
-        __device__ void poison() { rest = NAN; }
-    };
-    __device__ static __forceinline__ bool moments(const Params&) { return false; }
-    __device__ static void nothing(const Params& p, int64_t r) { p.loss[r] = 0.0f; }
+    __device__ static void without(const Params& p, int64_t r, float loss) { p.loss[r] = loss; }
+    __device__ static __forceinline__ int entries(const Params& p) { return p.k; }
 
-    template <int NT>
-    __device__ static bool begin(const Params& p, Shared& sh, int64_t r) {
-        const float w = p.weight ? p.weight[r] : 1.0f;
-        if (w == 0.0f) return false;
-        constexpr int kMine = (QN_TOP_MAX + NT - 1) / NT;
-        float v[kMine];
-        int named = 0;
-        bool wrong = false, finite = false;
+    struct Fetched {
+        int64_t at[kMine];
+        float v[kMine], weight;
+    };
+    __device__ static __forceinline__ Fetched fetch(const Params& p, int64_t r) {
+        Fetched f;
+        const bool row = r < p.rows;
+        f.weight = row && p.weight ? p.weight[r] : 1.0f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            const int j = threadIdx.x + i * NT;
-            v[i] = -INFINITY;
-            if (j >= p.k) continue;
-            const int64_t at = p.token[r * p.k + j];
-            const bool here = at >= 0 && at < p.vocab;
-            sh.pos[j] = here ? static_cast<int32_t>(at) : -1;
-            wrong = wrong || at >= p.vocab;
-            if (!here) continue;
-            ++named;
-            v[i] = p.value_bf16 ? Storage<__nv_bfloat16>::load1(static_cast<const __nv_bfloat16*>(p.value) + r * p.k + j)
-                                : __ldg(static_cast<const float*>(p.value) + r * p.k + j);
-            finite = finite || v[i] != -INFINITY;
+            const int j = (threadIdx.x & 31) + 32 * i;
+            const int64_t entry = r * p.k + j;
+            f.at[i] = -1;
+            f.v[i] = -INFINITY;
+            if (!row || j >= p.k) continue;
+            f.at[i] = p.token[entry];
+            f.v[i] = p.value_bf16 ? Storage<__nv_bfloat16>::load1(static_cast<const __nv_bfloat16*>(p.value) + entry)
+                                  : __ldg(static_cast<const float*>(p.value) + entry);
         }
-        wrong = __syncthreads_or(wrong);
-        // a row without a teacher: no token at all, or (logits) none that weighs anything
-        if (!wrong && !__syncthreads_or(p.logprobs ? named > 0 : finite)) return false;
+        return f;
+    }
+
+    // false: weight 0, or no teacher (no token at all, or of logits none that weighs anything)
+    __device__ static __forceinline__ bool wanted(const Params& p, const Fetched& f) {
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i)
+            any = any || f.at[i] >= p.vocab || (f.at[i] >= 0 && (p.logprobs || f.v[i] != -INFINITY));
+        return __any_sync(0xffffffffu, any) && f.weight != 0.0f;
+    }
+
+    __device__ static __forceinline__ void begin(const Params& p, Shared& sh, const Fetched& f) {
+        const int lane = threadIdx.x & 31;
+        float v[kMine];
+        int named = 0;
+        bool wrong = false;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int j = lane + 32 * i;
+            const bool here = f.at[i] >= 0 && f.at[i] < p.vocab;
+            v[i] = here ? f.v[i] : -INFINITY;
+            wrong = wrong || f.at[i] >= p.vocab;
+            named += here;
+            if (j < p.k) sh.pos[j] = here ? static_cast<int32_t>(f.at[i]) : -1;
+        }
+        named = __reduce_add_sync(0xffffffffu, named);
+        wrong = __any_sync(0xffffffffu, wrong);
         float top = 0.0f, log_norm = 0.0f, inv = 1.0f;
         if (!p.logprobs) {
             top = -INFINITY;
 #pragma unroll
             for (int i = 0; i < kMine; ++i) top = fmaxf(top, v[i]);
-            top = block_reduce<float, max_op>(top, sh.scratch_max);
+            top = warp_reduce<float, max_op>(top);
             if (top == -INFINITY) top = 0.0f;
             inv = p.inv_t;
             double norm = 0.0;
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) norm += exp(static_cast<double>((v[i] - top) * inv));
-            log_norm = static_cast<float>(log(block_reduce<double, add_op>(norm, sh.scratch_sum)));
+            for (int i = 0; i < kMine; ++i) norm += exp64(static_cast<double>((v[i] - top) * inv));
+            log_norm = static_cast<float>(log(warp_reduce<double, add_op>(norm)));
         }
         // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
         double q_sum = 0.0;
         float q_log_q = 0.0f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-            const int j = threadIdx.x + i * NT;
+            const int j = lane + 32 * i;
             if (j >= p.k) continue;
             const float log_q = (v[i] - top) * inv - log_norm;
-            const double q = exp(static_cast<double>(log_q));
+            const double q = exp64(static_cast<double>(log_q));
             q_sum += q;
             if (q != 0.0) q_log_q += static_cast<float>(q) * log_q;
             sh.q[j] = static_cast<float>(q);
         }
-        q_sum = block_reduce<double, add_op>(q_sum, sh.scratch_sum);
-        const float4 x = block_sum4<NT>(make_float4(q_log_q, static_cast<float>(named), 0.0f, 0.0f), sh.scratch);
-        if (threadIdx.x == 0) {
-            sh.weight = w;
+        q_sum = warp_reduce<double, add_op>(q_sum);
+        q_log_q = warp_reduce<float, add_op>(q_log_q);
+        if (lane == 0) {
+            sh.weight = f.weight;
             sh.q_sum = wrong ? NAN : static_cast<float>(q_sum);
-            sh.q_log_q = x.x;
+            sh.q_log_q = q_log_q;
             sh.q_rest = 0.0f;
-            if (p.logprobs && x.y < static_cast<float>(p.vocab))
-                sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
+            if (p.logprobs && named < p.vocab) sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
         }
-        __syncthreads();
-        return true;
+        __syncwarp();
     }
 
-    // The list leaves the sums: its logits are kept, and masked in the slice.
-    template <typename T, int NT>
-    __device__ static void before_sums(const Params& p, Shared& sh, const Slice<T>& s) {
-        for (int j = threadIdx.x; j < p.k; j += NT)
-            if (s.holds(sh.pos[j])) sh.z[j] = load_rw(s.elements() + (sh.pos[j] - s.origin()));
-        __syncthreads();
-        for (int j = threadIdx.x; j < p.k; j += NT)
-            if (s.holds(sh.pos[j])) s.elements()[sh.pos[j] - s.origin()] = masked<T>();
-        __syncthreads();
-    }
-
-    template <typename T, int NT>
-    __device__ static float slice_max(const Params& p, Shared& sh, const Slice<T>& s, float mine) {
-        for (int j = threadIdx.x; j < p.k; j += NT)
-            if (s.holds(sh.pos[j])) mine = fmaxf(mine, sh.z[j]);
-        return block_reduce<float, max_op>(mine, sh.scratch_max);
-    }
-
-    template <typename T, int NT>
-    __device__ static Partial sums(const Params& p, Shared& sh, const Slice<T>& s, float m, float sum, float) {
-        const float ref = m == -INFINITY ? 0.0f : m;
-        float list = 0.0f, dot = 0.0f, q = 0.0f;
-        for (int j = threadIdx.x; j < p.k; j += NT) {
-            if (!s.holds(sh.pos[j])) continue;
-            const float d = sh.z[j] - ref;
+    // Of the list's entries in a warp's chunks: the largest logit; sums of e_k and q_k u_k relative to it; sum of q_k.
+    struct Extra {
+        float m = -INFINITY, list = 0.0f, dot = 0.0f, q = 0.0f;
+        __device__ __forceinline__ void down_to(const Params& p, float to) {
+            if (!(to > m)) return;
+            const float d = m - to;  // -inf at first, with nothing in the sums
+            list *= exp2_approx(d * p.scale);
+            if (q > 0.0f) dot += q * (d * p.inv_t);
+            m = to;
+        }
+        __device__ __forceinline__ void take(const Params& p, const Shared& sh, int k, float z) {
+            down_to(p, z);
+            const float d = z - (m == -INFINITY ? 0.0f : m), qk = sh.q[k];
             list += exp2_approx(d * p.scale);
-            if (sh.q[j] > 0.0f) dot += sh.q[j] * (d * p.inv_t);
-            q += sh.q[j];
+            if (qk > 0.0f) dot += qk * (d * p.inv_t);
+            q += qk;
         }
-        const float4 x = block_sum4<NT>(make_float4(sum, list, dot, q), sh.scratch);
-        return {m, x.x, x.y, x.z, x.w};
-    }
+        __device__ __forceinline__ float4 message(const Params& p) {
+            down_to(p, warp_max_f32(m));
+            return make_float4(m, warp_reduce<float, add_op>(list), warp_reduce<float, add_op>(dot),
+                               warp_reduce<float, add_op>(q));
+        }
+    };
 
-    __device__ static Gradient finish(const Params& p, Shared& sh, const Partial* part, int n, int64_t r, bool first) {
+    // messages: of a CTA's warps, their maximum and sum of e_i; then of each what Extra has
+    template <int kWarps>
+    __device__ static __forceinline__ void join(const Params& p, Shared& sh, const float4* in, int ctas) {
+        const int lane = threadIdx.x & 31, all = ctas * (2 * kWarps);
         float m = -INFINITY;
-        for (int c = 0; c < n; ++c) m = fmaxf(m, part[c].m);
+#pragma unroll 1
+        for (int i = lane; i < all; i += 32) m = fmaxf(m, in[i].x);
+        m = warp_max_f32(m);
         float rest = 0.0f, list = 0.0f, dot = 0.0f;
-        for (int c = 0; c < n; ++c) {
-            const Partial x = part[c];
-            const float f = x.m == m || x.m == -INFINITY ? 1.0f : exp2_approx((x.m - m) * p.scale);
-            rest += f * x.rest, list += f * x.list;  // a masked slice's are 0, or NaN where it holds one
-            dot += x.dot;
-            if (x.q > 0.0f && x.m != m) dot += x.q * ((x.m - m) * p.inv_t);
+#pragma unroll 1
+        for (int i = lane; i < all; i += 32) {
+            const float4 v = in[i];
+            const float f = v.x == m || v.x == -INFINITY ? 1.0f : exp2_approx((v.x - m) * p.scale);
+            if (i % (2 * kWarps) < kWarps) {
+                rest += f * v.y;  // masked elements only: 0, or NaN where there is one
+            } else {
+                list += f * v.y;
+                dot += v.z;
+                if (v.w > 0.0f && v.x != m) dot += v.w * ((v.x - m) * p.inv_t);
+            }
         }
+        rest = warp_reduce<float, add_op>(rest);
+        list = warp_reduce<float, add_op>(list);
+        dot = warp_reduce<float, add_op>(dot);
         const float s = m == INFINITY ? NAN : rest + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
-        const bool empty = s == 0.0f;
-        const float log_s = logf(s);
-        if (first) {
-            // sum q (ln q - ln p) with ln p = u - m/T - ln S
-            float loss = empty ? INFINITY : sh.q_log_q - dot + sh.q_sum * log_s;
-            if (!empty && q_rest != 0.0f) loss += q_rest * (logf(q_rest) - (logf(rest) - log_s));
-            p.loss[r] = mass != mass ? NAN : loss;
+        Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (s != 0.0f) {
+            g.m = m == -INFINITY ? 0.0f : m;
+            g.unit = sh.weight * p.inv_t;
+            g.on = g.unit * __fdividef(mass, s);
+            g.c0 = q_rest > 0.0f && rest > 0.0f ? g.on - g.unit * __fdividef(q_rest, rest) : g.on;
         }
-        sh.unit = empty ? 0.0f : sh.weight * p.inv_t;
-        sh.on = empty ? 0.0f : sh.unit * (mass / s);
-        const float off = q_rest > 0.0f && rest > 0.0f ? mass / s - q_rest / rest : mass / s;
-        return {m == -INFINITY ? 0.0f : m, empty ? 0.0f : sh.unit * off, 0.0f};
+        if (lane == 0) sh.g = g, sh.rest = rest, sh.s = s, sh.dot = dot;
     }
 
-    template <typename T, int NT, typename Store>
-    __device__ static void fix(const Params& p, Shared& sh, const Slice<T>& s, const Gradient& g, Store store) {
-        for (int j = threadIdx.x; j < p.k; j += NT)
-            if (s.holds(sh.pos[j]))
-                store(sh.pos[j], sh.on * exp2_approx((sh.z[j] - g.m) * p.scale) - sh.unit * sh.q[j]);
+    template <typename T>
+    __device__ static void fix(const Params& p, const Shared& sh, const Slice<T>& s, T* out, int64_t r, bool first) {
+        const Gradient g = sh.g;
+        if (out)
+#pragma unroll 1
+            for (int j = threadIdx.x & 31; j < p.k; j += 32)
+                if (s.holds(sh.pos[j]))
+                    Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - g.m) * p.scale) - g.unit * sh.q[j]);
+        if (first && (threadIdx.x & 31) == 0) {
+            // sum q (ln q - ln p) with ln p = u - m/T - ln S
+            const float log_s = logf(sh.s);
+            float loss = sh.s == 0.0f ? INFINITY : sh.q_log_q - sh.dot + sh.q_sum * log_s;
+            if (sh.s != 0.0f && sh.q_rest != 0.0f) loss += sh.q_rest * (logf(sh.q_rest) - (logf(sh.rest) - log_s));
+            p.loss[r] = sh.q_sum + sh.q_rest != sh.q_sum + sh.q_rest ? NAN : loss;
+        }
     }
 };
 

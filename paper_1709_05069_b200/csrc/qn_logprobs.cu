@@ -90,131 +90,119 @@ struct BackwardParams {
     int64_t dlogits_stride;
 };
 
-// dz_i = 1/T [ p_i (a + b ln p_i) + sparse_i ],  a = d_lse - sum of the sparse terms - d_H H,  b = -d_H.
-// The sums leave out one maximal element: S = 1 + s, ln S = log1p(s).  For a row whose maximum has nearly all the
-// probability, H and ln p then keep their relative accuracy (s is small and all of H comes from it).
+// dz_i = 1/T [ p_i (a - d_H (ln p_i + H)) + sparse_i ],  a = d_lse - sum of the sparse terms.
+// With E = sum e_i d_i, H = ln S - ln 2 E / S and ln p_i = ln 2 d_i - ln S: in their sum ln S cancels, and
+// ln p_i + H = ln 2 (d_i - E / S) keeps its relative accuracy in rows whose maximum has nearly all the probability.
+template <bool kEntropy>
 struct Backward {
     using Params = BackwardParams;
+    static constexpr bool kMoments = kEntropy;
+    static constexpr bool kListMessage = false, kMask = false;
     struct Shared {
         int32_t pos[QN_TOP_MAX + 1];  // sparse terms: 0 the given token, 1..k the alternatives; -1 for none
         float add[QN_TOP_MAX + 1], z[QN_TOP_MAX + 1];
-        float4 scratch[32];
-        float scratch_max[32];
-        float total;
-        int owner, skipped;
+        float total, d_lse, d_h;
+        Gradient g;
     };
-    struct Partial {
-        float m, s, e;  // a slice's maximum; sums of e_i and e_i d_i over the rest of it
-        __device__ void poison() { s = NAN; }
+    __device__ static void without(const Params&, int64_t, float) {}
+    __device__ static __forceinline__ int entries(const Params& p) { return p.k + 1; }
+    struct Extra {
+        __device__ __forceinline__ void take(const Params&, const Shared&, int, float) {}
     };
-    __device__ static __forceinline__ bool moments(const Params& p) { return p.d_entropy != nullptr; }
-    __device__ static void nothing(const Params&, int64_t) {}
 
-    template <int NT>
-    __device__ static bool begin(const Params& p, Shared& sh, int64_t r) {
-        float sum = 0.0f;
-        bool any = false;
-        for (int j = threadIdx.x; j <= p.k; j += NT) {
-            float mine = 0.0f;
-            int64_t at = -1;
-            if (j == 0) {
-                if (p.d_logprob) {
-                    at = p.tokens[r];
-                    if (at >= 0) mine = p.d_logprob[r];
-                }
-                any = (p.d_lse && p.d_lse[r] != 0.0f) || (p.d_entropy && p.d_entropy[r] != 0.0f);
-                sh.owner = NT;
-            } else if (p.d_top) {
-                at = p.top_token[r * p.k + j - 1];
-                if (at >= 0) mine = p.d_top[r * p.k + j - 1];
-            }
-            if (at >= p.vocab) mine = NAN;
-            sh.pos[j] = at >= 0 && at < p.vocab ? static_cast<int32_t>(at) : -1;
-            sh.add[j] = mine;
-            sum += mine;
-            any = any || mine != 0.0f;
-        }
-        const float total = block_sum4<NT>(make_float4(sum, 0.0f, 0.0f, 0.0f), sh.scratch).x;
-        if (threadIdx.x == 0) sh.total = total;
-        return __syncthreads_or(any);
-    }
-
-    template <typename T, int NT>
-    __device__ static void before_sums(const Params& p, Shared& sh, const Slice<T>& s) {
-        for (int j = threadIdx.x; j <= p.k; j += NT)
-            if (s.holds(sh.pos[j])) sh.z[j] = load_rw(s.elements() + (sh.pos[j] - s.origin()));
-        __syncthreads();
-    }
-
-    // The slice's maximum.  One element that has it (the first of the first thread that has one) leaves the sums.
-    template <typename T, int NT>
-    __device__ static float slice_max(const Params&, Shared& sh, const Slice<T>& s, float mine) {
-        const float m = block_reduce<float, max_op>(mine, sh.scratch_max);
-        if (m == -INFINITY) return m;
-        if (mine == m) atomicMin(&sh.owner, static_cast<int>(threadIdx.x));
-        __syncthreads();
-        if (sh.owner == static_cast<int>(threadIdx.x)) {
-            int at = s.count * Slice<T>::kVec;
-            for (int j = threadIdx.x; j < s.count; j += NT) {
+    static constexpr int kMine = QN_TOP_MAX / 32 + 1;  // sparse terms a lane
+    struct Fetched {
+        int64_t at[kMine];
+        float x[kMine], d_lse, d_h;
+    };
+    __device__ static __forceinline__ Fetched fetch(const Params& p, int64_t r) {
+        Fetched f;
+        const bool row = r < p.rows;
+        f.d_lse = row && p.d_lse ? p.d_lse[r] : 0.0f;
+        f.d_h = kEntropy && row ? p.d_entropy[r] : 0.0f;
 #pragma unroll
-                for (int e = 0; e < Slice<T>::kVec; ++e)
-                    if (Storage<T>::get(s.data[j], e) == m) at = min(at, j * Slice<T>::kVec + e);
-            }
-            sh.skipped = at;
-            if (at < s.count * Slice<T>::kVec) s.elements()[at] = masked<T>();
+        for (int i = 0; i < kMine; ++i) {
+            const int j = (threadIdx.x & 31) + 32 * i;
+            f.at[i] = -1;
+            f.x[i] = 0.0f;
+            if (row && j == 0 && p.d_logprob) f.at[i] = p.tokens[r], f.x[i] = p.d_logprob[r];
+            if (row && j >= 1 && j <= p.k) f.at[i] = p.top_token[r * p.k + j - 1], f.x[i] = p.d_top[r * p.k + j - 1];
         }
-        asm volatile("" ::: "memory");  // the owner itself reads the vector next, and no other thread does
-        return m;
+        return f;
+    }
+    // a sparse term's gradient: none for an absent token, NaN for one that is not in the vocabulary
+    __device__ static __forceinline__ float term(const Params& p, const Fetched& f, int i) {
+        return f.at[i] < 0 ? 0.0f : f.at[i] >= p.vocab ? NAN : f.x[i];
     }
 
-    template <typename T, int NT>
-    __device__ static Partial sums(const Params&, Shared& sh, const Slice<T>& s, float m, float sum, float moment) {
-        const float4 x = block_sum4<NT>(make_float4(sum, moment, 0.0f, 0.0f), sh.scratch);
-        if (m != -INFINITY && sh.owner == static_cast<int>(threadIdx.x) && sh.skipped < s.count * Slice<T>::kVec)
-            Storage<T>::store1(s.elements() + sh.skipped, m);
-        return {m, x.x, x.y};
+    __device__ static __forceinline__ bool wanted(const Params& p, const Fetched& f) {
+        bool any = f.d_lse != 0.0f || f.d_h != 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) any = any || term(p, f, i) != 0.0f;
+        return __any_sync(0xffffffffu, any);
     }
 
-    __device__ static Gradient finish(const Params& p, Shared& sh, const Partial* part, int n, int64_t r, bool) {
+    __device__ static __forceinline__ void begin(const Params& p, Shared& sh, const Fetched& f) {
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int j = (threadIdx.x & 31) + 32 * i;
+            if (j > p.k) continue;
+            sh.pos[j] = f.at[i] >= 0 && f.at[i] < p.vocab ? static_cast<int32_t>(f.at[i]) : -1;
+            sh.add[j] = term(p, f, i);
+            sum += sh.add[j];
+        }
+        sum = warp_reduce<float, add_op>(sum);
+        if ((threadIdx.x & 31) == 0) sh.total = sum, sh.d_lse = f.d_lse, sh.d_h = f.d_h;
+        __syncwarp();
+    }
+
+    // messages: a warp's maximum, sums of e_i and e_i d_i
+    template <int kWarps>
+    __device__ static __forceinline__ void join(const Params& p, Shared& sh, const float4* in, int ctas) {
+        const int lane = threadIdx.x & 31;
         float m = -INFINITY;
-        for (int c = 0; c < n; ++c) m = fmaxf(m, part[c].m);
+#pragma unroll 1
+        for (int i = lane; i < ctas * kWarps; i += 32) m = fmaxf(m, in[i].x);
+        m = warp_max_f32(m);
         float s = 0.0f, e = 0.0f;
-        bool left_out = false;
-        for (int c = 0; c < n; ++c) {
-            const Partial x = part[c];
-            if (x.m == -INFINITY) {
-                s += x.s;  // 0, or NaN where the slice holds one
-            } else if (x.m == m && !left_out) {
-                left_out = true;
-                s += x.s, e += x.e;
-            } else {
-                const float d = (x.m - m) * p.scale, f = exp2_approx(d);
-                s += f * (1.0f + x.s);
-                if (f != 0.0f) e += f * (x.e + d * (1.0f + x.s));
-            }
+#pragma unroll 1
+        for (int i = lane; i < ctas * kWarps; i += 32) {
+            const float4 v = in[i];
+            const float d = v.x == m || v.x == -INFINITY ? 0.0f : (v.x - m) * p.scale, f = exp2_approx(d);
+            s += f * v.y;  // masked elements only: 0, or NaN where there is one
+            if (kEntropy && f != 0.0f) e += f * (v.z + d * v.y);
         }
+        s = warp_reduce<float, add_op>(s);
+        if constexpr (kEntropy) e = warp_reduce<float, add_op>(e);
         if (m == INFINITY) s = NAN;
-        if (m == -INFINITY && s == 0.0f) return {0.0f, 0.0f, 0.0f};  // empty
-        const float d_lse = p.d_lse ? p.d_lse[r] : 0.0f, d_h = p.d_entropy ? p.d_entropy[r] : 0.0f;
-        // a + b ln p_i = d_lse - total - d_h (H + ln p_i), with H = ln S - ln 2 e / S and ln p_i = ln 2 d_i - ln S: ln S cancels
-        const float unit = p.inv_t / (1.0f + s);
-        return {m, unit * (d_lse - sh.total + d_h * (kLn2 * e / (1.0f + s))), -unit * d_h * kLn2};
+        Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (s != 0.0f) {  // not empty
+            const float unit = p.inv_t / s;
+            g.m = m == -INFINITY ? 0.0f : m;
+            g.c0 = unit * (sh.d_lse - sh.total + sh.d_h * (kLn2 * e / s));
+            g.c1 = -unit * sh.d_h * kLn2;
+        }
+        if (lane == 0) sh.g = g;
     }
 
-    template <typename T, int NT, typename Store>
-    __device__ static void fix(const Params& p, Shared& sh, const Slice<T>& s, const Gradient& g, Store store) {
-        for (int j = threadIdx.x; j <= p.k; j += NT) {
+    template <typename T>
+    __device__ static void fix(const Params& p, const Shared& sh, const Slice<T>& s, T* out, int64_t, bool) {
+        const Gradient g = sh.g;
+#pragma unroll 1
+        for (int j = threadIdx.x & 31; j <= p.k; j += 32) {
             const int32_t at = sh.pos[j];
             if (!s.holds(at)) continue;
             bool first = true;
             float extra = 0.0f;
+#pragma unroll 1
             for (int i = 0; i <= p.k; ++i) {  // a token that occurs more than once is written once, by its first entry
                 if (sh.pos[i] != at) continue;
                 if (i < j) first = false;
                 extra += sh.add[i];
             }
             const float d = (sh.z[j] - g.m) * p.scale;
-            if (first) store(at, exp2_approx(d) * (g.c0 + g.c1 * fmaxf(d, -1e30f)) + extra * p.inv_t);
+            if (first) Storage<T>::store1(out + at, exp2_approx(d) * (g.c0 + g.c1 * fmaxf(d, -1e30f)) + extra * p.inv_t);
         }
     }
 };
@@ -279,8 +267,11 @@ extern "C" qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype 
                            d_logprob, d_lse, d_entropy, top_token, d_top_logprob, dlogits, dlogits_stride};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:logprobs_backward");
-    const cudaError_t e = dtype == QN_F32 ? launch_gradient<float, Backward>(p, st)
-                                          : launch_gradient<__nv_bfloat16, Backward>(p, st);
+    const cudaError_t e =
+        d_entropy ? (dtype == QN_F32 ? launch_gradient<float, Backward<true>>(p, st)
+                                     : launch_gradient<__nv_bfloat16, Backward<true>>(p, st))
+                  : (dtype == QN_F32 ? launch_gradient<float, Backward<false>>(p, st)
+                                     : launch_gradient<__nv_bfloat16, Backward<false>>(p, st));
     nvtxRangePop();
     return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }

@@ -1,21 +1,35 @@
 // The kernel behind the calls that give the gradient of a row of logits: the row is read once, its softmax statistics are
 // taken, and the gradient is written, with the row in shared memory between the two.
 //
-// A cluster of C CTAs takes a row; each holds a slice of at most 192 KB.  A row is seen as 16-byte vectors that start at the
-// 16-byte boundary at or below its first element, so that whatever its alignment all but its first and last vector move as
-// one bulk copy; what those two hold outside the row is filled with -inf.  Each CTA takes its slice's maximum and sums
-// relative to it, tells the other CTAs (stores into their shared memory, one cluster barrier), and joins the C partials in
-// rank order, so every CTA arrives at the same numbers.  Two passes over shared memory before that barrier and one after
-// it cost about 3/128 of a cycle a byte, an eighth of what the bytes take from and to HBM.
+// A cluster of C CTAs takes a row; each holds a slice of at most 192 KB (128 KB unless the row is larger than 1 MB).  A row
+// is seen as 16-byte vectors that start at the 16-byte boundary at or below its first element, so that whatever its
+// alignment all but its first and last vector move as bulk copies; what those two hold outside the row is filled with -inf.
 //
-// An operator Op brings the few elements of a row that are special (a given token, alternatives, a teacher's list):
-//   Params, Shared        arguments; its shared memory
-//   begin                 reads them; false if the row is padding (its gradient is 0 and it is not read)
-//   before_sums           after the slice has arrived: may take elements out of the sums (by -inf in their place)
-//   Partial / sums        what a CTA tells the others
-//   finish                from the joined partials to the coefficients: gradient_i = e_i (c0 + c1 d_i) with
-//                         d_i = (z_i - m) log2(e) / T, e_i = 2^d_i
-//   fix                   the special elements' gradients, one after the other
+// There is one CTA on an SM, it stays, and its warps are stages of a pipeline over chunks of 4 KB in a ring of 48:
+//   list warps     a row each: read the few elements of it that are special (a given token, alternatives, a teacher's list),
+//                  work out what depends on them alone, and sort them by chunk; when the row has been written, write their
+//                  gradients
+//   copy warp      brings the slices of the coming rows in
+//   sum warps      a chunk each: fetch the special elements' logits, take them out where they must not be added, and add
+//                  e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative to a running maximum m of each thread; at the end of a
+//                  slice each sends its maximum and sums to every CTA of the cluster (asynchronous stores into shared
+//                  memory that count on a barrier there)
+//   join warp      from all messages, in the same order in every CTA, to the row's coefficients
+//   write warps    a chunk each: e_i times the coefficient; give the chunk back
+// So HBM is read and written at the same time, and the exchange of one row passes while others are summed and written.
+// Loops are short and rolled: a form that kept the slice in registers (unrolled over them) ran out of the instruction cache.
+// exp2 is taken twice for an element: at 16 a cycle and SM that is 73 % of the time in which bf16 logits come from HBM and
+// their gradient goes there.
+//
+// An operator Op brings:
+//   Params, Shared        arguments; what the warps tell one another of a row
+//   Fetched, fetch        a row's special elements as a lane of a list warp loads them, ahead of their use
+//   wanted                false if the row is padding: its gradient is 0 and it is not read
+//   begin                 list warp: what depends on the special elements alone, and their places (Shared::pos)
+//   kMask                 whether the special elements leave the sums
+//   Extra                 what a sum warp adds up over the special elements of its chunks (kListMessage: and sends)
+//   join                  from all messages to Shared::g
+//   fix                   list warp, at the end: the special elements' gradients, and the row's loss
 #pragma once
 
 #include "qn_vocab.cuh"
@@ -25,6 +39,12 @@ namespace {
 using namespace qn;
 
 constexpr int kMaxCluster = 8;
+constexpr int kChunk = 256;      // vectors in a chunk
+constexpr int kSlots = 48;       // chunks in the ring
+constexpr int kSumWarps = 11, kWriteWarps = 12;
+constexpr int kListWarps = 3;
+constexpr int kLists = 2 * kListWarps;  // rows between the list warps' beginning and end of them
+constexpr int kGradThreads = 32 * (kSumWarps + kWriteWarps + 2 + kListWarps);
 
 // ---- pairs of fp32 (one instruction for two) ---------------------------------------------------------------------
 
@@ -64,6 +84,12 @@ __device__ __forceinline__ f32x2 finite_pair(f32x2 d) {
     return pack2(fmaxf(lo, -1e30f), fmaxf(hi, -1e30f));
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
 template <typename T>
 struct Lanes;
 template <>
@@ -71,12 +97,13 @@ struct Lanes<float> {
     __device__ static __forceinline__ f32x2 pair(const uint4& v, int i) {
         return i == 0 ? pack2(__uint_as_float(v.x), __uint_as_float(v.y)) : pack2(__uint_as_float(v.z), __uint_as_float(v.w));
     }
-    // running maximum of a thread, several elements side by side; NaN is passed over (the sums keep it)
+    __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
+    // running maximum of a thread, several elements side by side; NaN if there is one
     struct Max {
         float m = -INFINITY;
         __device__ __forceinline__ void take(const uint4& v) {
-            m = fmaxf(fmaxf(m, fmaxf(__uint_as_float(v.x), __uint_as_float(v.y))),
-                      fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+            m = max_nan(max_nan(m, max_nan(__uint_as_float(v.x), __uint_as_float(v.y))),
+                        max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
         }
         __device__ __forceinline__ float get() const { return m; }
     };
@@ -87,18 +114,19 @@ struct Lanes<__nv_bfloat16> {
         const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
         return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
     }
+    __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     struct Max {
         uint32_t m = 0xff80ff80u;
         __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
             uint32_t r;
-            asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
             return r;
         }
         __device__ __forceinline__ void take(const uint4& v) {
             m = max2(max2(m, max2(v.x, v.y)), max2(v.z, v.w));
         }
         __device__ __forceinline__ float get() const {
-            return fmaxf(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
+            return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
         }
     };
 };
@@ -122,37 +150,71 @@ __device__ __forceinline__ uint32_t cluster_size() {
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
     return r;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// Store into the same variable of the CTA of rank `to`.
-__device__ __forceinline__ void store_remote(void* mine, uint32_t to, float x) {
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t map_remote(const void* mine, uint32_t cta) {
     uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(to));
-    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(x) : "memory");
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(cta));
+    return at;
+}
+// 16 bytes into the same variable of another CTA, counted on the same barrier of that CTA.
+__device__ __forceinline__ void store_async(const void* mine, const uint64_t* bar, uint32_t cta, float4 x) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
+                     map_remote(mine, cta)),
+                 "f"(x.x), "f"(x.y), "f"(x.z), "f"(x.w), "r"(map_remote(bar, cta))
+                 : "memory");
+}
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+// A bounded wait.  Its slow part is out of line (instruction cache), and leaves the warp suspended for up to 20 us at a time
+// instead of polling: with polls in their place half of the instructions that the SM issued were those of waiting warps.
+__device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    const uint64_t began = global_timer_ns();
+    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+        uint32_t passed;
+        asm volatile(
+            "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
+            : "=r"(passed)
+            : "r"(smem_u32(bar)), "r"(parity), "r"(20000u)
+            : "memory");
+        if (passed) return true;
+        if (*abort) return false;
+        if (global_timer_ns() - began > kWaitLimitNs) break;
+    }
+    *abort = 1;
+    return false;
+}
+__device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    return mbar_try(bar, parity) || wait_slow(bar, parity, abort);
 }
 
-// Before a barrier after which a bulk copy may write what this thread wrote.
+__device__ __forceinline__ float warp_max_f32(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));  // of numbers, if there are any
+    return r;
+}
+
+// Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // ---- geometry ------------------------------------------------------------------------------------------------------
 
-// A CTA's slice of a row: vectors [first, first + count) of the row, in shared memory.
+// A CTA's slice of a row: the row's vectors [first, first + count).
 template <typename T>
 struct Slice {
     static constexpr int kVec = Storage<T>::kVec;
-    uint4* data;
     int32_t vocab, phase;  // elements from the 16-byte boundary to the row's first
     int32_t first, count;
 
-    __device__ __forceinline__ void set(const T* row, int32_t vocab_, int32_t per_cta, uint32_t rank, uint4* data_) {
-        data = data_;
+    __device__ __forceinline__ Slice(const T* row, int32_t vocab_, int32_t per_cta, uint32_t rank) {
         vocab = vocab_;
         phase = static_cast<int32_t>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
         const int32_t all = (phase + vocab + kVec - 1) / kVec;
         first = static_cast<int32_t>(rank) * per_cta;
         count = max(0, min(per_cta, all - first));
     }
-    __device__ __forceinline__ T* elements() const { return reinterpret_cast<T*>(data); }
     // row index of the slice's element 0 (negative in a row's first vector)
     __device__ __forceinline__ int32_t origin() const { return first * kVec - phase; }
     __device__ __forceinline__ bool holds(int32_t i) const {
@@ -166,246 +228,504 @@ struct Slice {
     }
 };
 
-// Writes the slice's part of a row of zeros.
+// Writes one value over the slice's part of a row, by NT threads.
 template <typename T, int NT>
-__device__ __forceinline__ void write_zeros(T* out, const Slice<T>& s) {
+__device__ __noinline__ void write_constant(T* out, const Slice<T> s, int tid, float x) {
     const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
     if (lo >= hi) return;
     constexpr int kVec = Slice<T>::kVec;
     const int32_t head = min(hi - lo, static_cast<int32_t>((16 - (reinterpret_cast<uintptr_t>(out + lo) & 15)) / sizeof(T)) % kVec);
-    if (static_cast<int>(threadIdx.x) < head) Storage<T>::store1(out + lo + threadIdx.x, 0.0f);
+    if (tid < head) Storage<T>::store1(out + lo + tid, x);
     const int32_t n = (hi - lo - head) / kVec;
-    for (int j = threadIdx.x; j < n; j += NT) stg_stream16(out + lo + head + j * kVec, make_uint4(0, 0, 0, 0));
-    const int32_t tail = lo + head + n * kVec + threadIdx.x;
-    if (tail < hi && static_cast<int>(threadIdx.x) < kVec) Storage<T>::store1(out + tail, 0.0f);
+    float xs[kVec];
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) xs[e] = x;
+    const uint4 w = Storage<T>::pack(xs);
+#pragma unroll 1
+    for (int j = tid; j < n; j += NT) stg_stream16(out + lo + head + j * kVec, w);
+    const int32_t tail = lo + head + n * kVec + tid;
+    if (tail < hi && tid < kVec) Storage<T>::store1(out + tail, x);
 }
 
-// Copies the slice's elements to a row whose alignment is another than the slice's.
-template <int NT>
-__device__ __forceinline__ void write_shifted(float* out, const Slice<float>& s) {
-    const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * 4);
-    const float* from = s.elements() - s.origin();
-    for (int i = lo + threadIdx.x; i < hi; i += NT) out[i] = from[i];
-}
-template <int NT>
-__device__ __forceinline__ void write_shifted(__nv_bfloat16* out, const Slice<__nv_bfloat16>& s) {
-    const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * 8);
-    if (lo >= hi) return;
-    const uint16_t* from = reinterpret_cast<const uint16_t*>(s.data) - s.origin();
-    uint16_t* to = reinterpret_cast<uint16_t*>(out);
-    const int32_t head = (reinterpret_cast<uintptr_t>(to + lo) & 2) ? 1 : 0;
-    if (head && threadIdx.x == 0) to[lo] = from[lo];
-    const int32_t words = (hi - lo - head) / 2;
-    for (int w = threadIdx.x; w < words; w += NT) {
-        const int32_t i = lo + head + 2 * w;
-        *reinterpret_cast<uint32_t*>(to + i) = from[i] | (static_cast<uint32_t>(from[i + 1]) << 16);
+// The elements of one vector that lie inside the row, one at a time.
+template <typename T>
+__device__ __noinline__ void write_edge(T* out, int32_t origin, int32_t vocab, uint4 w) {
+#pragma unroll 1
+    for (int e = 0; e < Storage<T>::kVec; ++e) {
+        if (origin + e >= 0 && origin + e < vocab) Storage<T>::store1(out + origin + e, Storage<T>::get(w, 0));
+        if (sizeof(T) == 4) w = make_uint4(w.y, w.z, w.w, 0);
+        else w = make_uint4(w.x >> 16 | w.y << 16, w.y >> 16 | w.z << 16, w.z >> 16 | w.w << 16, w.w >> 16);
     }
-    const int32_t tail = lo + head + 2 * words;
-    if (tail < hi && threadIdx.x == 0) to[tail] = from[tail];
+}
+// 32 vectors of a warp, one run of the row from element `at` on, to a row that is not aligned as they are: through shared
+// memory to pieces of 4 bytes.
+__device__ __forceinline__ void write_run(float* out, int32_t at, const uint4* run) {
+    const int lane = threadIdx.x & 31;
+    const float* from = reinterpret_cast<const float*>(run);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[at + lane + 32 * i] = from[lane + 32 * i];
+}
+__device__ __forceinline__ void write_run(__nv_bfloat16* out_, int32_t at, const uint4* run) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t* from = reinterpret_cast<const uint32_t*>(run);
+    uint16_t* out = reinterpret_cast<uint16_t*>(out_) + at;
+    if (reinterpret_cast<uintptr_t>(out) & 2) {
+        uint32_t* words = reinterpret_cast<uint32_t*>(out + 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int w = lane + 32 * i;
+            const uint32_t x = from[w];
+            if (w == 0) out[0] = static_cast<uint16_t>(x);
+            if (w == 127) out[255] = static_cast<uint16_t>(x >> 16);
+            else words[w] = x >> 16 | from[w + 1] << 16;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(out)[lane + 32 * i] = from[lane + 32 * i];
+    }
 }
 
-// Coefficients of e_i and e_i d_i in the gradient, and the maximum they are relative to.
+// gradient_i = e_i (c0 + c1 d_i) with e_i and d_i relative to m; on and unit: for Op::fix.
 struct Gradient {
     float m, c0, c1;
+    float on, unit;
 };
 
-template <typename T, int NT, typename Op>
-__global__ void __launch_bounds__(NT) row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
+// kAligned: every row of the gradient starts as far from a 16-byte boundary as its row of logits.
+template <typename T, typename Op, bool kAligned>
+__global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
-    extern __shared__ __align__(128) uint4 slice_data[];
-    __shared__ typename Op::Shared sh;
-    __shared__ typename Op::Partial inbox[2][kMaxCluster];
-    __shared__ __align__(8) uint64_t bar;
+    constexpr int kMessages = kSumWarps * (Op::kListMessage ? 2 : 1);
+    constexpr bool moments = Op::kMoments;
+    extern __shared__ __align__(128) uint4 ring[];
+    __shared__ typename Op::Shared lists[kLists];
+    __shared__ __align__(16) float4 inbox[kLists][kMaxCluster * kMessages];
+    __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWriteWarps][32];
+    // a row's special elements in the order of their chunks, and where each chunk's begin
+    __shared__ uint8_t order[kLists][QN_TOP_MAX + 32], chunk_begin[kLists][64];
+    // full: a chunk has arrived; empty: it has been written.  By row: ready: begun; done: summed and written.  By row that is
+    // wanted: heard: all messages; joined: coefficients
+    __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists];
+    __shared__ bool wanted[kLists];
     __shared__ int abort;
-    __shared__ Gradient result;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
-    const int tid = threadIdx.x;
-    if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
-    if (tid == 0) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x == 0) {
         abort = 0;
-        mbar_init(&bar, 1);
+#pragma unroll 1
+        for (int i = 0; i < kSlots; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
+#pragma unroll 1
+        for (int i = 0; i < kLists; ++i) {
+            mbar_init(&ready[i], 1), mbar_init(&done[i], kSumWarps + kWriteWarps + 2);
+            mbar_init(&heard[i], 1), mbar_init(&joined[i], 1);
+        }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
-    uint32_t parity = 0;
-    int turn = 0;
-    bool first_row = true;
-    for (int64_t r = blockIdx.x / ctas; r < p.rows; r += gridDim.x / ctas) {
-        const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
-        T* out = p.dlogits ? static_cast<T*>(p.dlogits) + r * p.dlogits_stride : nullptr;
-        Slice<T> s;
-        s.set(row, p.vocab, per_cta, rank, slice_data);
-        if (!Op::template begin<NT>(p, sh, r)) {
-            if (out) write_zeros<T, NT>(out, s);
-            if (rank == 0 && tid == 0) Op::nothing(p, r);
-            __syncthreads();  // the operator's shared memory is free for the next row
-            continue;
-        }
+    if (ctas > 1) cluster_sync();  // every CTA's barriers are there before the first store into it
+    const int64_t row0 = blockIdx.x / ctas, row_step = gridDim.x / ctas;
+    auto row_of = [&](int64_t r) { return static_cast<const T*>(p.logits) + r * p.row_stride; };
+    auto out_of = [&](int64_t r) { return static_cast<T*>(p.dlogits) + r * p.dlogits_stride; };
+    auto slice_of = [&](int64_t r) { return Slice<T>(row_of(r), p.vocab, per_cta, rank); };
+    auto chunks_of = [](const Slice<T>& s) { return (s.count + kChunk - 1) / kChunk; };
+    // rounds of a ring: item n is in slot n % size, and is the (n / size)-th there
+    auto wait_item = [&](uint64_t* bars, uint32_t n, uint32_t size) { return wait(&bars[n % size], n / size & 1, &abort); };
+    auto wait_free = [&](uint64_t* bars, uint32_t n, uint32_t size) { return wait(&bars[n % size], (n / size & 1) ^ 1, &abort); };
+    // A CTA sends a row's messages once it has joined the row before the last.  So whoever has heard all of row u knows that
+    // every CTA has joined u - 2, and may send u + 2: four sets of messages never meet
+    auto may_send = [&](uint32_t u) { return u < 2 || wait_item(joined, u - 2, kLists); };
+    auto send = [&](uint32_t u, int index, float4 msg) {
+        if (lane < static_cast<int>(ctas))
+            store_async(&inbox[u % kLists][rank * kMessages + index], &heard[u % kLists], lane, msg);
+    };
 
-        // the slice: whole vectors as one bulk copy, the row's ends by elements
-        const T* base = row - s.phase + static_cast<int64_t>(s.first) * kVec;
-        const int32_t fb = s.full_begin(), fe = s.full_end();
-        if (tid == 0 && fe > fb) {
-            mbar_arrive_expect_tx(&bar, static_cast<uint32_t>(fe - fb) * 16u);
-            bulk_load(s.data + fb, base + fb * kVec, static_cast<uint32_t>(fe - fb) * 16u, &bar);
-        }
-        if (tid < 2 * kVec) {
-            const int32_t j = tid < kVec ? 0 : s.count - 1;
-            const int32_t e = j * kVec + tid % kVec;
-            const bool end = j >= 0 && (j < fb || j >= fe);
-            if (s.count > 0 && end) {
-                const int32_t i = s.origin() + e;
-                s.elements()[e] = i >= 0 && i < s.vocab ? row[i] : masked<T>();
-            }
-        }
-        if (fe > fb) {
-            if (!mbar_wait<false>(&bar, parity, &abort)) mbar_wait<false>(&bar, parity, &abort);
-            parity ^= 1;
-        }
-        __syncthreads();
-        Op::template before_sums<T, NT>(p, sh, s);  // ends with a barrier
-        typename Lanes<T>::Max top;
-        for (int j = tid; j < s.count; j += NT) top.take(s.data[j]);
-        const float m_all = Op::template slice_max<T, NT>(p, sh, s, top.get());
-        const float m = m_all == -INFINITY ? 0.0f : m_all;
-        f32x2 sum = 0, moment = 0;
-        const f32x2 minus_m = pack2(-m, -m), scale = pack2(p.scale, p.scale);
-        if (Op::moments(p)) {
-            for (int j = tid; j < s.count; j += NT) {
-                const uint4 v = s.data[j];
+    uint32_t n = 0;     // chunks so far
+    uint32_t turn = 0;  // rows so far
+    uint32_t u = 0;     // wanted rows so far
+    if (warp < kSumWarps) {
+#pragma unroll 1
+        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+            const int li = turn % kLists;
+            if (!wait_item(ready, turn, kLists)) return;
+            if (wanted[li]) {
+                const Slice<T> s = slice_of(r);
+                const int chunks = chunks_of(s);
+                const f32x2 scale = pack2(p.scale, p.scale);
+                typename Op::Shared& sh = lists[li];
+                typename Op::Extra extra;
+                float m = -INFINITY;
+                f32x2 sum = 0, moment = 0;
+                bool patched = false;  // a bulk copy may only write there again after a fence
+                // chunk c is for worker c % kSumWarps; which warp that is moves on from row to row
+                const int worker = (warp + kSumWarps - turn % kSumWarps) % kSumWarps;
+#pragma unroll 1
+                for (int c = worker; c < chunks; c += kSumWarps) {
+                    const uint32_t slot = (n + c) % kSlots;
+                    if (!wait_item(full, n + c, kSlots)) return;
+                    const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
+                    if (begin < end) {
+                        T* first = reinterpret_cast<T*>(ring + slot * kChunk) - (s.origin() + c * (kChunk * kVec));
+#pragma unroll 1
+                        for (int i = begin + lane; i < end; i += 32) {
+                            const int k = order[li][i];
+                            const float z = load_rw(first + sh.pos[k]);
+                            sh.z[k] = z;
+                            extra.take(p, sh, k, z);
+                        }
+                        if constexpr (Op::kMask) {
+                            __syncwarp();
+#pragma unroll 1
+                            for (int i = begin + lane; i < end; i += 32) first[sh.pos[order[li][i]]] = masked<T>();
+                            patched = true;
+                        }
+                        __syncwarp();
+                    }
+                    const uint4* data = ring + slot * kChunk + lane;
+                    const int count = min(kChunk, s.count - c * kChunk) - lane;
+#pragma unroll 1
+                    for (int j = 0; j < kChunk; j += 128, data += 128) {
+                        uint4 v[4];
+                        if (count + lane == kChunk) {
 #pragma unroll
-                for (int i = 0; i < kPairs; ++i) {
-                    const f32x2 d = mul2(add2(Lanes<T>::pair(v, i), minus_m), scale), e = exp2_pair(d);
-                    sum = add2(sum, e);
-                    moment = fma2(e, finite_pair(d), moment);
+                            for (int q = 0; q < 4; ++q) v[q] = data[32 * q];
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) v[q] = j + 32 * q < count ? data[32 * q] : Lanes<T>::masked4();
+                        }
+                        typename Lanes<T>::Max top;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) top.take(v[q]);
+                        const float most = top.get();
+                        if (!(most <= m)) {  // a new maximum, or NaN (then m and all sums become NaN)
+                            const float d = (m - most) * p.scale, f = exp2_approx(d);
+                            const f32x2 f2 = pack2(f, f);
+                            if (moments && f != 0.0f) moment = mul2(f2, fma2(sum, pack2(d, d), moment));
+                            sum = mul2(sum, f2);
+                            m = most;
+                        }
+                        const float ref = m == -INFINITY ? 0.0f : m;
+                        const f32x2 minus = pack2(-ref, -ref);
+#pragma unroll
+                        for (int q = 0; q < 4; ++q)
+#pragma unroll
+                            for (int i = 0; i < kPairs; ++i) {
+                                const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus), scale), e = exp2_pair(d);
+                                sum = add2(sum, e);
+                                if constexpr (moments) moment = fma2(e, finite_pair(d), moment);
+                            }
+                    }
+                    if (!p.dlogits) {  // nobody else needs the chunk
+                        if (patched) fence_async();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&empty[slot]);
+                    }
                 }
-            }
-        } else {
-            for (int j = tid; j < s.count; j += NT) {
-                const uint4 v = s.data[j];
-#pragma unroll
-                for (int i = 0; i < kPairs; ++i)
-                    sum = add2(sum, exp2_pair(mul2(add2(Lanes<T>::pair(v, i), minus_m), scale)));
-            }
-        }
-        float s0, s1, e0, e1;
-        unpack2(sum, s0, s1);
-        unpack2(moment, e0, e1);
-        typename Op::Partial mine = Op::template sums<T, NT>(p, sh, s, m_all, s0 + s1, e0 + e1);
-        if (abort) mine.poison();
-        // every CTA's partial to every CTA, by the first warp; the buffers alternate, so that the next row's partials do
-        // not meet a slower CTA that still reads this row's
-        if (ctas > 1) {
-            if (first_row) cluster_wait();
-            first_row = false;
-            if (tid < static_cast<int>(ctas)) {  // `mine` is the same in every thread
-                constexpr int kWords = sizeof(typename Op::Partial) / 4;
-                const float* words = reinterpret_cast<const float*>(&mine);
-                float* slot = reinterpret_cast<float*>(&inbox[turn][rank]);
-#pragma unroll
-                for (int i = 0; i < kWords; ++i) store_remote(slot + i, tid, words[i]);
+                n += chunks;
+                if (patched) fence_async();
+                // the warp's message: its maximum, and sums relative to it
+                float s0, s1;
+                unpack2(sum, s0, s1);
+                const float wm = warp_max_f32(m);
+                const float down = m == wm || m == -INFINITY ? 0.0f : (m - wm) * p.scale, f = exp2_approx(down);
+                float4 msg = make_float4(wm, f * (s0 + s1), 0.0f, 0.0f);
+                if constexpr (moments) {
+                    float e0, e1;
+                    unpack2(moment, e0, e1);
+                    if (f != 0.0f) msg.z = f * (e0 + e1) + down * msg.y;
+                    msg.z = warp_reduce<float, add_op>(msg.z);
+                }
+                msg.y = warp_reduce<float, add_op>(msg.y);
+                if (!may_send(u)) return;
+                send(u, worker, msg);
+                if constexpr (Op::kListMessage) send(u, kSumWarps + worker, extra.message(p));
+                ++u;
             }
             __syncwarp();
-            cluster_arrive();
-            cluster_wait();
-        } else {
-            if (tid == 0) inbox[turn][0] = mine;
+            if (lane == 0) mbar_arrive(&done[li]);
         }
-        if (tid == 0) result = Op::finish(p, sh, inbox[turn], static_cast<int>(ctas), r, rank == 0);
-        turn ^= 1;
-        fence_async();
-        __syncthreads();
-        if (!out) continue;
-        const Gradient g = result;
-
-        const bool aligned = (reinterpret_cast<uintptr_t>(out) & 15) / sizeof(T) == static_cast<uintptr_t>(s.phase);
-        T* out_base = out - s.phase + static_cast<int64_t>(s.first) * kVec;
-        const f32x2 minus = pack2(-g.m, -g.m), c0 = pack2(g.c0, g.c0), c1 = pack2(g.c1, g.c1);
-        const bool moments = Op::moments(p);
-        for (int j = tid; j < s.count; j += NT) {
-            const uint4 v = s.data[j];
-            float x[kVec];
-#pragma unroll
-            for (int i = 0; i < kPairs; ++i) {
-                const f32x2 d = mul2(add2(Lanes<T>::pair(v, i), minus), scale), e = exp2_pair(d);
-                const f32x2 y = moments ? mul2(e, fma2(finite_pair(d), c1, c0)) : mul2(e, c0);
-                unpack2(y, x[2 * i], x[2 * i + 1]);
-            }
-            const uint4 w = Storage<T>::pack(x);
-            if (aligned && j >= fb && j < fe) {
-                stg_stream16(out_base + j * kVec, w);
-            } else if (aligned) {
-#pragma unroll
-                for (int e = 0; e < kVec; ++e) {
-                    const int32_t i = s.origin() + j * kVec + e;
-                    if (i >= 0 && i < s.vocab) Storage<T>::store1(out + i, x[e]);
-                }
-            } else {
-                s.data[j] = w;
-            }
-        }
-        __syncthreads();
-        if (aligned) {
-            Op::template fix<T, NT>(p, sh, s, g, [&](int32_t i, float x) { Storage<T>::store1(out + i, x); });
-        } else {
-            Op::template fix<T, NT>(p, sh, s, g, [&](int32_t i, float x) { Storage<T>::store1(s.elements() + (i - s.origin()), x); });
-            __syncthreads();
-            write_shifted<NT>(out, s);
-        }
-        fence_async();
-        __syncthreads();  // shared memory is free for the next row
+        return;
     }
-    if (ctas > 1 && first_row) cluster_wait();
+    if (warp < kSumWarps + kWriteWarps) {
+        constexpr int NT = 32 * kWriteWarps;
+        const int w = warp - kSumWarps, tid = threadIdx.x - 32 * kSumWarps;
+#pragma unroll 1
+        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+            const int li = turn % kLists;
+            bool ok = wait_item(ready, turn, kLists);
+            if (ok && wanted[li]) ok = wait_item(joined, u, kLists);
+            if (!ok) {  // a wait ran out: what is left becomes NaN
+                if (p.dlogits)
+#pragma unroll 1
+                    for (; r < p.rows; r += row_step) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
+                return;
+            }
+            const Slice<T> s = slice_of(r);
+            if (!wanted[li]) {
+                if (p.dlogits) write_constant<T, NT>(out_of(r), s, tid, 0.0f);
+            } else {
+                ++u;
+                const int chunks = chunks_of(s);
+                if (p.dlogits) {
+                    T* out = out_of(r);
+                    const Gradient g = lists[li].g;
+                    const f32x2 minus = pack2(-g.m, -g.m), scale = pack2(p.scale, p.scale);
+                    const f32x2 c0 = pack2(g.c0, g.c0), c1 = pack2(g.c1, g.c1);
+                    const int32_t fb = s.full_begin(), fe = s.full_end();
+#pragma unroll 1
+                    for (int c = (w + kWriteWarps - turn % kWriteWarps) % kWriteWarps; c < chunks; c += kWriteWarps) {
+                        const uint32_t slot = (n + c) % kSlots;
+                        wait_item(full, n + c, kSlots);  // it has been: this thread sees the chunk too
+                        const uint4* data = ring + slot * kChunk + lane;
+                        auto gradient = [&](const uint4& v) {
+                            float y[kVec];
+#pragma unroll
+                            for (int i = 0; i < kPairs; ++i) {
+                                const f32x2 d = mul2(add2(Lanes<T>::pair(v, i), minus), scale), e = exp2_pair(d);
+                                unpack2(moments ? mul2(e, fma2(finite_pair(d), c1, c0)) : mul2(e, c0), y[2 * i], y[2 * i + 1]);
+                            }
+                            return Storage<T>::pack(y);
+                        };
+                        const int32_t at = s.origin() + (c * kChunk + lane) * kVec;
+                        if (kAligned && c * kChunk >= fb && (c + 1) * kChunk <= fe) {
+                            T* to = out + at;
+#pragma unroll 1
+                            for (int q = 0; q < kChunk / 32; q += 4, data += 128, to += 128 * kVec) {
+#pragma unroll
+                                for (int h = 0; h < 4; ++h) stg_stream16(to + 32 * kVec * h, gradient(data[32 * h]));
+                            }
+                        } else {
+                            const int count = min(kChunk, s.count - c * kChunk);
+#pragma unroll 1
+                            for (int q = 0; 32 * q < count; ++q) {
+                                const int j = 32 * q + lane, k = c * kChunk + j;
+                                const uint4 x = gradient(j < count ? data[32 * q] : Lanes<T>::masked4());
+                                if (kAligned) {
+                                    if (k >= fb && k < fe) stg_stream16(out + at + 32 * q * kVec, x);
+                                    else if (j < count) write_edge(out, at + 32 * q * kVec, s.vocab, x);
+                                } else if (k - lane >= fb && k - lane + 32 <= fe) {
+                                    __syncwarp();
+                                    stage[w][lane] = x;
+                                    __syncwarp();
+                                    write_run(out, at + (32 * q - lane) * kVec, stage[w]);
+                                } else if (j < count) {
+                                    write_edge(out, at + 32 * q * kVec, s.vocab, x);
+                                }
+                            }
+                        }
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(&empty[slot]);
+                    }
+                }
+                n += chunks;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&done[li]);
+        }
+        return;
+    }
+    if (warp == kSumWarps + kWriteWarps) {
+        // ---- copy warp
+#pragma unroll 1
+        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+            if (!wait_item(ready, turn, kLists)) return;
+            const bool want = wanted[turn % kLists];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&done[turn % kLists]);
+            if (!want) continue;
+            const T* row = row_of(r);
+            const Slice<T> s = slice_of(r);
+            const T* base = row + s.origin();
+            const int32_t fb = s.full_begin(), fe = s.full_end(), chunks = chunks_of(s);
+            // a chunk for each lane, issued as its slot comes free (one lane issuing all took 470 cycles a chunk, a third of
+            // what HBM delivers)
+#pragma unroll 1
+            for (int c0 = 0; c0 < chunks; c0 += 32) {
+                const int c = c0 + lane;
+                const uint32_t slot = (n + c) % kSlots, parity = ((n + c) / kSlots & 1) ^ 1;
+                uint4* to = ring + slot * kChunk;
+                const int32_t j0 = c * kChunk, j1 = min(j0 + kChunk, s.count), b0 = max(j0, fb), b1 = min(j1, fe);
+                const bool edge = c < chunks && (j0 < fb || j1 > max(fe, j0));
+                uint32_t pending = __ballot_sync(0xffffffffu, c < chunks);
+                while (pending) {
+                    const uint32_t first = n + c0 + __ffs(pending) - 1;  // slots come free in about this order
+                    if (!wait_free(empty, first, kSlots)) return;
+                    const bool mine = (pending >> lane & 1) && mbar_try(&empty[slot], parity);
+                    if (mine) {
+                        if (b1 > b0) {
+                            const uint32_t bytes = static_cast<uint32_t>(b1 - b0) * 16u;
+                            mbar_expect_tx(&full[slot], bytes);
+                            bulk_load(to + (b0 - j0), base + static_cast<int64_t>(b0) * kVec, bytes, &full[slot]);
+                        }
+                        if (!edge) mbar_arrive(&full[slot]);
+                    }
+                    pending &= ~__ballot_sync(0xffffffffu, mine);
+                }
+                if (edge) {  // a row's first and last vector, where they reach past it
+#pragma unroll 1
+                    for (int h = 0; h < 2; ++h) {
+                        const int32_t j = h == 0 ? j0 : j1 - 1;
+                        if (j >= fb && j < fe) continue;
+                        T x[kVec];
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) {
+                            const int32_t i = s.origin() + j * kVec + e;
+                            x[e] = i >= 0 && i < s.vocab ? row[i] : masked<T>();
+                        }
+#pragma unroll
+                        for (int e = 0; e < kVec; ++e) reinterpret_cast<T*>(to + (j - j0))[e] = x[e];
+                    }
+                    fence_async();
+                    mbar_arrive(&full[slot]);
+                }
+                __syncwarp();
+            }
+            n += chunks;
+        }
+        return;
+    }
+    if (warp == kSumWarps + kWriteWarps + 1) {
+        // ---- join warp
+#pragma unroll 1
+        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+            const int li = turn % kLists;
+            if (!wait_item(ready, turn, kLists)) return;
+            if (wanted[li]) {
+                const int set = u % kLists;
+                if (lane == 0) mbar_arrive_expect_tx(&heard[set], ctas * (kMessages * 16u));
+                __syncwarp();
+                if (!wait_item(heard, u, kLists)) return;
+                Op::template join<kSumWarps>(p, lists[li], inbox[set], static_cast<int>(ctas));
+                __syncwarp();
+                if (lane == 0) mbar_arrive(&joined[set]);
+                ++u;
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&done[li]);
+        }
+        return;
+    }
+    // ---- list warps
+    // what is left to do of a row once the others are through with it
+    auto retire = [&](uint32_t t) {
+        const int64_t r = row0 + static_cast<int64_t>(t) * row_step;
+        const int li = t % kLists;
+        if (!wait_item(done, t, kLists)) return false;
+        if (wanted[li]) Op::template fix<T>(p, lists[li], slice_of(r), p.dlogits ? out_of(r) : nullptr, r, rank == 0);
+        else if (rank == 0 && lane == 0) Op::without(p, r, 0.0f);
+        __syncwarp();
+        return true;
+    };
+    turn = warp - (kSumWarps + kWriteWarps + 2);
+    const int64_t mine = row0 + static_cast<int64_t>(turn) * row_step, mine_step = kListWarps * row_step;
+    uint32_t oldest = turn;  // not retired
+    bool ok = true;
+    typename Op::Fetched next = Op::fetch(p, mine);
+#pragma unroll 1
+    for (int64_t r = mine; r < p.rows; r += mine_step, turn += kListWarps) {
+        const int li = turn % kLists;
+        typename Op::Shared& sh = lists[li];
+        if (turn >= kLists) {
+            ok = retire(oldest);
+            if (!ok) break;
+            oldest += kListWarps;
+        }
+        const typename Op::Fetched now = next;
+        next = Op::fetch(p, r + mine_step);
+        const bool want = Op::wanted(p, now);
+        if (want) {
+            Op::begin(p, sh, now);
+            // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
+            const Slice<T> s = slice_of(r);
+            chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
+            __syncwarp();
+            int in[Op::kMine], place[Op::kMine];
+#pragma unroll
+            for (int i = 0; i < Op::kMine; ++i) {
+                const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
+                in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
+                place[i] = 0;
+                if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
+                const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
+                if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
+                __syncwarp();
+                if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
+                __syncwarp();
+            }
+            int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
+                if (lane >= o) a += up, b += up2;
+            }
+            b += __shfl_sync(0xffffffffu, a, 31);
+            __syncwarp();
+            chunk_begin[li][lane] = static_cast<uint8_t>(a);
+            chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < Op::kMine; ++i)
+                if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
+        }
+        if (lane == 0) wanted[li] = want;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ready[li]);
+    }
+#pragma unroll 1
+    for (; oldest < turn && ok; oldest += kListWarps) ok = retire(oldest);
+    if (!ok && rank == 0 && lane == 0)  // a wait ran out
+#pragma unroll 1
+        for (int64_t r = row0 + static_cast<int64_t>(oldest) * row_step; r < p.rows; r += mine_step) Op::without(p, r, NAN);
 }
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-// CTAs a row and vectors a CTA.
-struct RowSplit {
-    int ctas, per_cta;
-};
-inline RowSplit split_row(int64_t rows, int64_t vocab, int vec) {
-    const int64_t all = (vocab + 2 * vec - 2) / vec;  // vectors, whatever the alignment
-    auto per = [&](int c) { return (all + c - 1) / c; };
-    int c = 1;
-    while (c < kMaxCluster && per(c) * 16 > 72 * 1024) c *= 2;
-    while (c < kMaxCluster && rows * c < 2 * qn_sm_count() && per(c) > 512) c *= 2;
-    return {c, static_cast<int>(per(c))};
-}
-
-template <typename T, int NT, typename Op>
-cudaError_t launch_gradient_nt(const typename Op::Params& p, RowSplit split, cudaStream_t st) {
-    auto kernel = row_gradient_kernel<T, NT, Op>;
-    const size_t smem = static_cast<size_t>(split.per_cta) * 16;
-    static bool raised[64];
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
-    if (!raised[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
-        if (e != cudaSuccess) return e;
-        raised[dev] = true;
-    }
-    const int64_t clusters = p.rows < INT32_MAX / kMaxCluster ? p.rows : INT32_MAX / kMaxCluster;
+template <typename T, typename Op, bool kAligned>
+cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t st) {
+    auto kernel = row_gradient_kernel<T, Op, kAligned>;
+    // CTAs a row: slices of up to 128 KB, of up to 192 KB where 8 of them are not enough; where there are few rows, more and
+    // smaller ones, down to a chunk for every sum warp
+    constexpr int kVec = Storage<T>::kVec, kGood = 32 * kChunk;
+    const int64_t all = (static_cast<int64_t>(p.vocab) + 2 * kVec - 2) / kVec;  // vectors, whatever the alignment
+    int ctas = 1;
+    while (ctas < kMaxCluster && (all + ctas - 1) / ctas > kGood) ++ctas;
+    while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= qn_sm_count() && all / ctas > kSumWarps * kChunk) ctas *= 2;
+    const int per_cta = static_cast<int>((all + ctas - 1) / ctas);
+    if (per_cta > kSlots * kChunk) return cudaErrorInvalidValue;
+    constexpr int kBytes = kSlots * kChunk * 16;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(clusters * split.ctas));
-    cfg.blockDim = dim3(NT);
-    cfg.dynamicSmemBytes = smem;
+    cfg.gridDim = dim3(ctas);
+    cfg.blockDim = dim3(kGradThreads);
+    cfg.dynamicSmemBytes = kBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = split.ctas;
+    attr[0].val.clusterDim.x = ctas;
     attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(split.per_cta));
+    // clusters that fit on the device at once, by cluster size; asked for once
+    static int fit[64][kMaxCluster + 1];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    int& clusters = fit[dev][ctas];
+    if (clusters == 0) {
+        int found = 0;
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&found, kernel, &cfg);
+        if (e != cudaSuccess) return e;
+        if (found < 1) return cudaErrorInvalidConfiguration;
+        clusters = found;
+    }
+    cfg.gridDim = dim3(static_cast<unsigned>((p.rows < clusters ? p.rows : clusters) * ctas));
+    return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(per_cta));
 }
 
 template <typename T, typename Op>
 cudaError_t launch_gradient(const typename Op::Params& p, cudaStream_t st) {
-    const RowSplit split = split_row(p.rows, p.vocab, Storage<T>::kVec);
-    if (split.per_cta >= 1024) return launch_gradient_nt<T, 256, Op>(p, split, st);
-    if (split.per_cta >= 256) return launch_gradient_nt<T, 128, Op>(p, split, st);
-    return launch_gradient_nt<T, 32, Op>(p, split, st);
+    const auto off = [](const void* at) { return reinterpret_cast<uintptr_t>(at) % 16; };
+    const bool aligned = !p.dlogits || (off(p.logits) == off(p.dlogits) &&
+                                        (p.rows == 1 || (p.row_stride - p.dlogits_stride) * sizeof(T) % 16 == 0));
+    return aligned ? launch_gradient_aligned<T, Op, true>(p, st) : launch_gradient_aligned<T, Op, false>(p, st);
 }
 
 }  // namespace

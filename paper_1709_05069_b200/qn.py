@@ -20,7 +20,7 @@ QN_GRAM_PATH_FP64 = 2
 QN_TOP_MAX = 128
 QN_TEACHER_LOGITS = 0
 QN_TEACHER_LOGPROBS = 1
-QN_GRAD_MAX_VOCAB = 393216
+QN_GRAD_MAX_VOCAB = 393208
 
 (QN_OK, QN_ERR_INVALID, QN_ERR_ALLOC, QN_ERR_CUDA, QN_ERR_STATE, QN_ERR_NOT_CONVERGED, QN_ERR_NONFINITE,
  QN_ERR_DEVICE_TIMEOUT) = range(8)
