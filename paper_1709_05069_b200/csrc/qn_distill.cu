@@ -8,8 +8,6 @@
 
 namespace {
 
-using namespace qn;
-
 struct DistillParams {
     const void* logits;
     int64_t row_stride, rows;

@@ -1,8 +1,17 @@
 // qn_logprobs and qn_logprobs_backward: log probabilities over a vocabulary and their gradient.
 //
-// Forward: one CTA takes a row.  The maximum m, then S = sum e_i and E = sum e_i d_i with d_i = (z_i - m) log2(e) / T and
-// e_i = 2^d_i.  z - m is formed before the scale, so that a row of the type's lowest values does not overflow and large
-// logits lose nothing to the product's rounding.  lse = m / T + ln S, H = ln S - ln 2 * E / S.
+// Forward: one pass over the row by a CTA (or, where there are few rows, by a cluster of up to 8 whose results its first
+// CTA joins), 256 threads with 16-byte loads straight to registers, two batches of four ahead of their use.  Each thread
+// keeps a running maximum m, S = sum e_i and E = sum e_i d_i with d_i = (z_i - m) log2(e) / T and e_i = 2^d_i; z - m is
+// formed before the scale, so that large logits lose nothing to the product's rounding.  At the end
+// lse = m / T + ln S, H = ln S - ln 2 E / S.
+//
+// The k largest logits come out of the same pass: the k-th largest of the threads' maxima is a lower bound of the k-th
+// largest logit, and nearly a tight one (of 256 maxima and k = 64, 74 logits are expected at or above it).  Each thread has
+// also left the maxima of its batches in shared memory, so only the batches that hold such a logit are read again (from
+// L2); what is found is ranked by counting.  Where that finds too many (equal logits, or the large ones in few threads) or
+// too few, a slower selection that is exact for everything takes over.
+//
 // Backward: an operator of the row-gradient kernel.
 #include <nvtx3/nvToolsExt.h>
 
@@ -10,14 +19,20 @@
 
 namespace {
 
-using namespace qn;
-
 constexpr int kThreads = 256;
+constexpr int kBatch = 4;          // vectors of a thread at a time
+constexpr int kGroups = 16;        // groups of batches whose maxima a thread keeps
+constexpr int kCandidates = 1024;  // logits at or above the bound
+constexpr int kHot = 2048;         // groups that hold one
+constexpr int kTopCluster = 8;
+// Logits below this are passed over as if masked in the main pass (their probability is 0 beside any that is not, and a
+// product with 0 stays 0); a slice whose maximum is not well above it, or as large, is done again by slice_slow.
+constexpr float kFloor = -0x1p66f;
 
 struct LogprobParams {
     const void* logits;
     int64_t row_stride, rows;
-    int32_t vocab, k;
+    int32_t vocab, k, per_cta;
     const int64_t* tokens;
     float inv_t, scale;  // 1 / T, log2(e) / T
     float *logprob, *lse, *entropy;
@@ -25,56 +40,332 @@ struct LogprobParams {
     float* top_logprob;
 };
 
+struct LogprobShared {
+    float4 sums[kThreads / 32];
+    float max[kThreads / 32];
+    float4 part[kTopCluster];  // of the cluster's CTAs: maximum, S, E
+    int32_t count, hot_count;
+    uint32_t hot[kHot];
+    uint64_t candidate[kCandidates];
+    uint64_t best[QN_TOP_MAX * kTopCluster];  // the CTAs' alternatives, largest first
+    float group_max[kGroups][kThreads];
+};
+
+// A row's vector j of a slice, element by element; -inf outside the row.
 template <typename T>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const LogprobParams p) {
-    __shared__ float scratch[kThreads / 32];
-    __shared__ uint64_t scratch_key[kThreads / 32];
-    for (int64_t r = blockIdx.x; r < p.rows; r += gridDim.x) {
-        const T* z = static_cast<const T*>(p.logits) + r * p.row_stride;
-        float m = -INFINITY;
-        for (int i = threadIdx.x; i < p.vocab; i += kThreads) m = fmaxf(m, Storage<T>::load1(z + i));
-        m = block_reduce<float, max_op>(m, scratch);
-        const bool empty = m == -INFINITY;
-        if (empty) m = 0.0f;
-        float s = 0.0f, e = 0.0f;
-        for (int i = threadIdx.x; i < p.vocab; i += kThreads) {
-            const float zi = Storage<T>::load1(z + i);
-            const float d = (zi - m) * p.scale, x = exp2_approx(d);
-            s += x;
-            if (x != 0.0f) e += x * d;  // 0 * -inf
+__device__ __noinline__ uint4 load_edge(const T* row, int32_t origin, int32_t vocab) {
+    float x[Storage<T>::kVec];
+#pragma unroll
+    for (int e = 0; e < Storage<T>::kVec; ++e)
+        x[e] = origin + e >= 0 && origin + e < vocab ? Storage<T>::load1(row + origin + e) : -INFINITY;
+    return Storage<T>::pack(x);
+}
+
+// Vector j of a slice (-inf outside of it).
+template <typename T>
+__device__ __forceinline__ uint4 load_vector(const T* row, const Slice<T>& s, int32_t fb, int32_t fe, int32_t j) {
+    const int32_t at = s.origin() + j * Slice<T>::kVec;
+    if (j >= fb && j < fe) return ldg_stream16(row + at);
+    return j < s.count ? load_edge(row, at, s.vocab) : Lanes<T>::masked4();
+}
+
+// Of n keys, the k largest in order into `out` (0 where there are none).  All threads; n <= kCandidates, keys distinct.
+__device__ __noinline__ void rank_keys(const uint64_t* key, int n, int k, uint64_t* out) {
+#pragma unroll 1
+    for (int i = threadIdx.x; i < k; i += kThreads) out[i] = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < n; i += kThreads) {
+        const uint64_t mine = key[i];
+        int above = 0;
+#pragma unroll 4
+        for (int j = 0; j < n; ++j) above += key[j] > mine;
+        if (mine != 0 && above < k) out[above] = mine;
+    }
+    __syncthreads();
+}
+
+// The k largest of a slice, whatever it holds: in steps of a logit for each thread, those above the k-th of what there is.
+template <typename T>
+__device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, LogprobShared& sh, uint64_t* out) {
+    const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
+    uint64_t least = static_cast<uint64_t>(kOrderMasked) << 32 | 0xffffffffu;  // above every masked logit
+    if (threadIdx.x == 0) sh.count = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int32_t i0 = lo; i0 < hi; i0 += kThreads) {
+        const int32_t i = i0 + threadIdx.x;
+        const uint64_t key = i < hi ? key_of(Storage<T>::load1(row + i), i) : 0;
+        if (key > least) sh.candidate[atomicAdd(&sh.count, 1)] = key;
+        __syncthreads();
+        if (sh.count > kCandidates - kThreads) {
+            rank_keys(sh.candidate, sh.count, k, out);
+            least = out[k - 1];  // there are more than k
+            for (int j = threadIdx.x; j < k; j += kThreads) sh.candidate[j] = out[j];
+            if (threadIdx.x == 0) sh.count = k;
+            __syncthreads();
         }
-        s = block_reduce<float, add_op>(s, scratch);
-        e = block_reduce<float, add_op>(e, scratch);
-        const float log_s = logf(s);  // -inf for an empty row, NaN for a row without a distribution
-        const bool bad = s != s;
-        if (threadIdx.x == 0) {
-            if (p.lse) p.lse[r] = m * p.inv_t + log_s;
-            if (p.entropy) p.entropy[r] = s == 0.0f ? 0.0f : log_s - kLn2 * (e / s);
+        __syncthreads();
+    }
+    rank_keys(sh.candidate, sh.count, k, out);
+}
+
+// The sums of a slice whose distances from kFloor could come out infinite or 0 (see there; or by an extreme temperature).
+template <typename T>
+__device__ __noinline__ float4 slice_slow(const T* row, const Slice<T> s, float scale, LogprobShared& sh) {
+    const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
+    float m = -INFINITY;
+#pragma unroll 1
+    for (int32_t i = lo + threadIdx.x; i < hi; i += kThreads) m = fmaxf(m, Storage<T>::load1(row + i));
+    m = block_reduce<float, max_op>(m, sh.max);
+    const float ref = m == -INFINITY ? 0.0f : m;
+    float sum = 0.0f, moment = 0.0f;
+#pragma unroll 1
+    for (int32_t i = lo + threadIdx.x; i < hi; i += kThreads) {
+        const float d = (Storage<T>::load1(row + i) - ref) * scale, e = exp2_approx(d);
+        sum += e;
+        if (e != 0.0f) moment += e * d;
+    }
+    const float4 x = block_sum4<kThreads>(make_float4(sum, moment, 0.0f, 0.0f), sh.sums);
+    return make_float4(m, x.x, x.y, 0.0f);
+}
+
+// The k-th largest of the threads' maxima (as orders), or less; kFloor's order if fewer than k are above that.
+__device__ __forceinline__ uint32_t bound_of(uint32_t mine, int k) {
+    const uint32_t floor = order_of(kFloor);
+    if (__syncthreads_count(mine > floor) < k) return floor;
+    uint32_t bound = 0;
+#pragma unroll 1
+    for (int bit = 31; bit >= 12; --bit) {  // the last 12 bits only make the bound tighter by 2^-11 of itself
+        const uint32_t next = bound | 1u << bit;
+        if (__syncthreads_count(mine >= next) >= k) bound = next;
+    }
+    return max(bound, floor + 1);
+}
+
+template <typename T, bool kTop>
+__global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobParams p) {
+    constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
+    extern __shared__ __align__(16) unsigned char shared_bytes[];
+    LogprobShared& sh = *reinterpret_cast<LogprobShared*>(shared_bytes);
+    const uint32_t ctas = cluster_size(), rank = cluster_rank();
+    const int tid = threadIdx.x;
+    for (int64_t r = blockIdx.x / ctas; r < p.rows; r += gridDim.x / ctas) {
+        const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
+        const Slice<T> s(row, p.vocab, p.per_cta, rank);
+        const int32_t fb = s.full_begin(), fe = s.full_end();
+        const int batches = (s.count + kThreads * kBatch - 1) / (kThreads * kBatch);
+        const int per_group = (batches + kGroups - 1) / kGroups;
+        auto load = [&](int b, uint4* v) {
+            const int32_t j0 = b * (kThreads * kBatch);
+            if (j0 >= fb && j0 + kThreads * kBatch <= fe) {
+                const T* at = row + s.origin() + (j0 + tid) * kVec;
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) v[q] = ldg_stream16(at + q * (kThreads * kVec));
+            } else {
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) v[q] = load_vector(row, s, fb, fe, j0 + q * kThreads + tid);
+            }
+        };
+        float m = kFloor, group_top = kFloor;
+        f32x2 sum = 0, moment = 0;
+        const f32x2 scale = pack2(p.scale, p.scale);
+        int left = per_group, group = 0;
+        auto take = [&](uint4* v) {
+            typename Lanes<T>::Max top;
+            top.start(kFloor);
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q) {
+                v[q] = Lanes<T>::at_least(v[q], kFloor);
+                top.take(v[q]);
+            }
+            const float most = top.get();
+            if (!(most <= m)) {  // a new maximum, or NaN (then m and all sums become NaN)
+                const float d = (m - most) * p.scale, f = exp2_approx(d);
+                const f32x2 f2 = pack2(f, f);
+                moment = f != 0.0f ? mul2(f2, fma2(sum, pack2(d, d), moment)) : 0;
+                sum = mul2(sum, f2);
+                m = most;
+            }
+            if (kTop) {
+                group_top = fmaxf(group_top, most);
+                if (--left == 0) {
+                    sh.group_max[group++][tid] = group_top;
+                    left = per_group, group_top = kFloor;
+                }
+            }
+            const f32x2 minus = pack2(-m, -m);
+#pragma unroll
+            for (int q = 0; q < kBatch; ++q)
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) {
+                    const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus), scale), e = exp2_pair(d);
+                    sum = add2(sum, e);
+                    moment = fma2(e, d, moment);
+                }
+        };
+        uint4 a[kBatch], b[kBatch], c[kBatch];
+        if (batches > 0) load(0, a);
+        if (batches > 1) load(1, b);
+#pragma unroll 1
+        for (int i = 0; i < batches; i += 3) {
+            if (i + 2 < batches) load(i + 2, c);
+            take(a);
+            if (i + 1 >= batches) break;
+            if (i + 3 < batches) load(i + 3, a);
+            take(b);
+            if (i + 2 >= batches) break;
+            if (i + 4 < batches) load(i + 4, b);
+            take(c);
+        }
+        if (kTop && left != per_group) sh.group_max[group++][tid] = group_top;
+        // elements outside the slice were counted at the floor: in a slice with anything above it they are 0
+
+        float4 part;
+        part.x = block_reduce<float, max_op>(m, sh.max);
+        const bool slow = !__syncthreads_or(m != m) && (part.x <= kFloor / 2 || part.x >= -kFloor ||
+                                                          !(p.scale > 1e-15f && p.scale < 1e15f));
+        if (slow) {
+            part = slice_slow(row, s, p.scale, sh);
+        } else {
+            const float d = (m - part.x) * p.scale, f = exp2_approx(d);
+            float s0, s1, e0, e1;
+            unpack2(sum, s0, s1);
+            unpack2(moment, e0, e1);
+            const float4 x = block_sum4<kThreads>(
+                make_float4(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f, 0.0f, 0.0f), sh.sums);
+            part.y = x.x, part.z = x.y;
+        }
+        if (!(part.y == part.y)) part.x = INFINITY;  // NaN somewhere
+        if (kTop) {
+            bool exact = slow;
+            if (!exact) {
+                if (tid == 0) sh.count = 0, sh.hot_count = 0;
+                const uint32_t bound = bound_of(order_of(m), p.k);
+                const bool all = bound == order_of(kFloor);  // fewer than k threads have anything above the floor
+                const uint32_t above = all ? kOrderMasked : bound - 1;
+                auto collect = [&](int32_t j) {
+                    const uint4 v = load_vector(row, s, fb, fe, j);
+#pragma unroll
+                    for (int e = 0; e < kVec; ++e) {
+                        const float z = Storage<T>::get(v, e);
+                        if (order_of(z) > above) {
+                            const int at = atomicAdd(&sh.count, 1);
+                            if (at < kCandidates) sh.candidate[at] = key_of(z, s.origin() + j * kVec + e);
+                        }
+                    }
+                };
+                if (all) {
+#pragma unroll 1
+                    for (int j = tid; j < s.count; j += kThreads) collect(j);
+                } else {
+                    if (order_of(m) > above)
+#pragma unroll 1
+                        for (int g = 0; g < group; ++g)
+                            if (order_of(sh.group_max[g][tid]) > above) {
+                                const int h = atomicAdd(&sh.hot_count, 1);
+                                if (h < kHot) sh.hot[h] = g << 16 | tid;
+                            }
+                    __syncthreads();
+                    const int hot = sh.hot_count, vectors = per_group * kBatch;
+                    exact = hot > kHot;
+#pragma unroll 1
+                    for (int h = tid; !exact && h < hot * vectors; h += kThreads) {
+                        const uint32_t id = sh.hot[h / vectors];
+                        const int32_t j = ((id >> 16) * vectors + h % vectors) * kThreads + (id & 0xffff);
+                        if (j < s.count) collect(j);
+                    }
+                }
+                __syncthreads();
+                exact = exact || sh.count > kCandidates;
+            }
+            uint64_t* best = sh.best + rank * p.k;
+            if (exact) select_slow(row, s, p.k, sh, best);
+            else rank_keys(sh.candidate, sh.count, p.k, best);
+        }
+        if (ctas > 1) {  // to the cluster's first CTA
+            if (tid == 0) sh.part[rank] = part;
+            cluster_sync();
+            if (rank == 0) {
+                if (tid < static_cast<int>(ctas) && tid > 0) sh.part[tid] = load_remote(&sh.part[tid], tid);
+                if (kTop)
+                    for (int i = p.k + tid; i < p.k * static_cast<int>(ctas); i += kThreads)
+                        sh.best[i] = load_remote(&sh.best[i], i / p.k);
+                __syncthreads();
+                part = sh.part[0];
+                float top = -INFINITY;
+                for (uint32_t q = 0; q < ctas; ++q) top = fmaxf(top, sh.part[q].x);
+                float sums = 0.0f, moments = 0.0f;
+                for (uint32_t q = 0; q < ctas; ++q) {
+                    const float4 x = sh.part[q];
+                    const float d = x.x == top || x.x == -INFINITY ? 0.0f : (x.x - top) * p.scale, f = exp2_approx(d);
+                    sums += f * x.y;
+                    if (f != 0.0f) moments += f * fmaf(x.y, d, x.z);
+                }
+                part = make_float4(top, sums, moments, 0.0f);
+                if (kTop) {
+                    for (int i = tid; i < p.k * static_cast<int>(ctas); i += kThreads) sh.candidate[i] = sh.best[i];
+                    __syncthreads();
+                    rank_keys(sh.candidate, p.k * ctas, p.k, sh.best);
+                }
+            }
+            cluster_sync();  // nobody leaves, or goes on to another row, while its results are read
+            if (rank != 0) continue;
+        }
+        const bool bad = part.x == INFINITY, empty = part.x == -INFINITY;
+        const float top = empty ? 0.0f : part.x, log_s = bad ? NAN : logf(part.y);
+        if (tid == 0) {
+            if (p.lse) p.lse[r] = bad ? NAN : top * p.inv_t + log_s;
+            if (p.entropy) p.entropy[r] = empty ? 0.0f : log_s - kLn2 * (part.z / part.y);
             if (p.logprob) {
                 const int64_t t = p.tokens[r];
                 float out = 0.0f;
                 if (t >= p.vocab || (t >= 0 && bad)) out = NAN;
-                else if (t >= 0) out = empty ? -INFINITY : (Storage<T>::load1(z + t) - m) * p.inv_t - log_s;
+                else if (t >= 0) out = empty ? -INFINITY : (Storage<T>::load1(row + t) - top) * p.inv_t - log_s;
                 p.logprob[r] = out;
             }
         }
-        uint64_t last = ~0ull;
-        for (int j = 0; j < p.k; ++j) {
-            uint64_t best = 0;
-            if (last != 0 && !bad)
-                for (int i = threadIdx.x; i < p.vocab; i += kThreads) {
-                    const float zi = Storage<T>::load1(z + i);
-                    const uint64_t key = key_of(zi, i);
-                    if (zi > -INFINITY && key < last && key > best) best = key;
-                }
-            last = block_reduce<uint64_t, max_op>(best, scratch_key);
-            if (threadIdx.x == 0) {
-                p.top_token[r * p.k + j] = last ? (int64_t)key_index(last) : -1;
-                p.top_logprob[r * p.k + j] =
-                    bad ? NAN : last ? (key_value(last) - m) * p.inv_t - log_s : -INFINITY;
+        if (kTop) {
+            for (int i = tid; i < p.k; i += kThreads) {
+                const uint64_t key = sh.best[i];
+                p.top_token[r * p.k + i] = key && !bad ? static_cast<int64_t>(key_index(key)) : -1;
+                p.top_logprob[r * p.k + i] = bad ? NAN : key ? (key_value(key) - top) * p.inv_t - log_s : -INFINITY;
             }
         }
+        __syncthreads();
     }
+}
+
+template <typename T, bool kTop>
+cudaError_t launch_logprobs(LogprobParams& p, cudaStream_t st) {
+    auto kernel = logprobs_kernel<T, kTop>;
+    constexpr int kVec = Storage<T>::kVec;
+    const int64_t all = (static_cast<int64_t>(p.vocab) + 2 * kVec - 2) / kVec;  // vectors, whatever the alignment
+    int ctas = 1;
+    while (ctas < kTopCluster && p.rows * 2 * ctas <= 2 * qn_sm_count() && all / ctas > 2 * kThreads) ctas *= 2;
+    p.per_cta = static_cast<int32_t>((all + ctas - 1) / ctas);
+    int dev = 0;
+    static bool raised[64];
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (!raised[dev]) {
+        const cudaError_t e =
+            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(LogprobShared));
+        if (e != cudaSuccess) return e;
+        raised[dev] = true;
+    }
+    const int64_t most = INT32_MAX / kTopCluster;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>((p.rows < most ? p.rows : most) * ctas));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = sizeof(LogprobShared);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
 struct BackwardParams {
@@ -207,8 +498,6 @@ struct Backward {
     }
 };
 
-inline unsigned row_grid(int64_t rows) { return static_cast<unsigned>(rows < INT32_MAX ? rows : INT32_MAX); }
-
 }  // namespace
 
 extern "C" qn_status qn_logprobs(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
@@ -232,15 +521,16 @@ extern "C" qn_status qn_logprobs(int64_t rows, int64_t vocab, qn_dtype dtype, co
         return QN_ERR_INVALID;
     DeviceGuard guard(dev);
     if (!guard.ok) return QN_ERR_CUDA;
-    const LogprobParams p{logits, row_stride, rows, static_cast<int32_t>(vocab), k, tokens,
-                          static_cast<float>(1.0 / temperature), static_cast<float>(1.4426950408889634 / temperature),
-                          logprob, lse, entropy, top_token, top_logprob};
+    LogprobParams p{logits, row_stride, rows, static_cast<int32_t>(vocab), k, 0, tokens,
+                    static_cast<float>(1.0 / temperature), static_cast<float>(1.4426950408889634 / temperature),
+                    logprob, lse, entropy, top_token, top_logprob};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:logprobs");
-    if (dtype == QN_F32) logprobs_kernel<float><<<row_grid(rows), kThreads, 0, st>>>(p);
-    else logprobs_kernel<__nv_bfloat16><<<row_grid(rows), kThreads, 0, st>>>(p);
+    const cudaError_t e = dtype == QN_F32 ? (k ? launch_logprobs<float, true>(p, st) : launch_logprobs<float, false>(p, st))
+                                          : (k ? launch_logprobs<__nv_bfloat16, true>(p, st)
+                                               : launch_logprobs<__nv_bfloat16, false>(p, st));
     nvtxRangePop();
-    return cudaGetLastError() == cudaSuccess ? QN_OK : QN_ERR_CUDA;
+    return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }
 
 extern "C" qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits,

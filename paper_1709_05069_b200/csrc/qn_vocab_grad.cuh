@@ -36,8 +36,6 @@
 
 namespace {
 
-using namespace qn;
-
 constexpr int kMaxCluster = 8;
 constexpr int kChunk = 256;      // vectors in a chunk
 constexpr int kSlots = 48;       // chunks in the ring
@@ -46,118 +44,8 @@ constexpr int kListWarps = 3;
 constexpr int kLists = 2 * kListWarps;  // rows between the list warps' beginning and end of them
 constexpr int kGradThreads = 32 * (kSumWarps + kWriteWarps + 2 + kListWarps);
 
-// ---- pairs of fp32 (one instruction for two) ---------------------------------------------------------------------
-
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pack2(float lo, float hi) {
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
-    return r;
-}
-__device__ __forceinline__ void unpack2(f32x2 v, float& lo, float& hi) {
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v));
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f32x2 exp2_pair(f32x2 d) {
-    float lo, hi;
-    unpack2(d, lo, hi);
-    return pack2(exp2_approx(lo), exp2_approx(hi));
-}
-// -inf becomes a number that a zero can be multiplied with; NaN does too, but e_i keeps it.
-__device__ __forceinline__ f32x2 finite_pair(f32x2 d) {
-    float lo, hi;
-    unpack2(d, lo, hi);
-    return pack2(fmaxf(lo, -1e30f), fmaxf(hi, -1e30f));
-}
-
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-
-template <typename T>
-struct Lanes;
-template <>
-struct Lanes<float> {
-    __device__ static __forceinline__ f32x2 pair(const uint4& v, int i) {
-        return i == 0 ? pack2(__uint_as_float(v.x), __uint_as_float(v.y)) : pack2(__uint_as_float(v.z), __uint_as_float(v.w));
-    }
-    __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
-    // running maximum of a thread, several elements side by side; NaN if there is one
-    struct Max {
-        float m = -INFINITY;
-        __device__ __forceinline__ void take(const uint4& v) {
-            m = max_nan(max_nan(m, max_nan(__uint_as_float(v.x), __uint_as_float(v.y))),
-                        max_nan(__uint_as_float(v.z), __uint_as_float(v.w)));
-        }
-        __device__ __forceinline__ float get() const { return m; }
-    };
-};
-template <>
-struct Lanes<__nv_bfloat16> {
-    __device__ static __forceinline__ f32x2 pair(const uint4& v, int i) {
-        const uint32_t w = i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
-        return pack2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
-    }
-    __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
-    struct Max {
-        uint32_t m = 0xff80ff80u;
-        __device__ static __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
-            uint32_t r;
-            asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-            return r;
-        }
-        __device__ __forceinline__ void take(const uint4& v) {
-            m = max2(max2(m, max2(v.x, v.y)), max2(v.z, v.w));
-        }
-        __device__ __forceinline__ float get() const {
-            return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xffff0000u));
-        }
-    };
-};
-
-template <typename T>
-__device__ __forceinline__ T masked();
-template <>
-__device__ __forceinline__ float masked<float>() { return -INFINITY; }
-template <>
-__device__ __forceinline__ __nv_bfloat16 masked<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80u); }
-
 // ---- clusters ------------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ uint32_t cluster_rank() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ uint32_t cluster_size() {
-    uint32_t r;
-    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() {
-    asm volatile("barrier.cluster.arrive.release.aligned;\n barrier.cluster.wait.acquire.aligned;" ::: "memory");
-}
-__device__ __forceinline__ uint32_t map_remote(const void* mine, uint32_t cta) {
-    uint32_t at;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(cta));
-    return at;
-}
 // 16 bytes into the same variable of another CTA, counted on the same barrier of that CTA.
 __device__ __forceinline__ void store_async(const void* mine, const uint64_t* bar, uint32_t cta, float4 x) {
     asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v4.f32 [%0], {%1, %2, %3, %4}, [%5];" ::"r"(
@@ -199,34 +87,7 @@ __device__ __forceinline__ float warp_max_f32(float x) {
 // Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// ---- geometry ------------------------------------------------------------------------------------------------------
-
-// A CTA's slice of a row: the row's vectors [first, first + count).
-template <typename T>
-struct Slice {
-    static constexpr int kVec = Storage<T>::kVec;
-    int32_t vocab, phase;  // elements from the 16-byte boundary to the row's first
-    int32_t first, count;
-
-    __device__ __forceinline__ Slice(const T* row, int32_t vocab_, int32_t per_cta, uint32_t rank) {
-        vocab = vocab_;
-        phase = static_cast<int32_t>((reinterpret_cast<uintptr_t>(row) & 15) / sizeof(T));
-        const int32_t all = (phase + vocab + kVec - 1) / kVec;
-        first = static_cast<int32_t>(rank) * per_cta;
-        count = max(0, min(per_cta, all - first));
-    }
-    // row index of the slice's element 0 (negative in a row's first vector)
-    __device__ __forceinline__ int32_t origin() const { return first * kVec - phase; }
-    __device__ __forceinline__ bool holds(int32_t i) const {
-        const int32_t at = i - origin();
-        return i >= 0 && at >= 0 && at < count * kVec;
-    }
-    // vectors of the slice that lie wholly inside the row: [full_begin, full_end), slice-relative
-    __device__ __forceinline__ int32_t full_begin() const { return first == 0 && phase > 0 ? 1 : 0; }
-    __device__ __forceinline__ int32_t full_end() const {
-        return max(full_begin(), min(count, (phase + vocab) / kVec - first));
-    }
-};
+// ---- writing -------------------------------------------------------------------------------------------------------
 
 // Writes one value over the slice's part of a row, by NT threads.
 template <typename T, int NT>
