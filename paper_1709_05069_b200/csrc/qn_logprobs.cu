@@ -24,6 +24,8 @@ constexpr int kBatch = 4;          // vectors of a thread at a time
 constexpr int kGroups = 16;        // groups of batches whose maxima a thread keeps
 constexpr int kCandidates = 1024;  // logits at or above the bound
 constexpr int kHot = 2048;         // groups that hold one
+constexpr int kBins = 256;         // of the threads' maxima, from the row's on down, 64 bins to a factor of 2
+constexpr int kBinShift = 17;
 constexpr int kTopCluster = 8;
 // Logits below this are passed over as if masked in the main pass (their probability is 0 beside any that is not, and a
 // product with 0 stays 0); a slice whose maximum is not well above it, or as large, is done again by slice_slow.
@@ -45,6 +47,8 @@ struct LogprobShared {
     float max[kThreads / 32];
     float4 part[kTopCluster];  // of the cluster's CTAs: maximum, S, E
     int32_t count, hot_count;
+    uint32_t bound;
+    int32_t bins[kBins];
     uint32_t hot[kHot];
     uint64_t candidate[kCandidates];
     uint64_t best[QN_TOP_MAX * kTopCluster];  // the CTAs' alternatives, largest first
@@ -69,23 +73,23 @@ __device__ __forceinline__ uint4 load_vector(const T* row, const Slice<T>& s, in
     return j < s.count ? load_edge(row, at, s.vocab) : Lanes<T>::masked4();
 }
 
-// Of n keys, the k largest in order into `out` (0 where there are none).  All threads; n <= kCandidates, keys distinct.
-__device__ __noinline__ void rank_keys(const uint64_t* key, int n, int k, uint64_t* out) {
+// Gives the k largest of n keys (0 is none; the others are distinct) to `put(place, key)`, and 0 for the places that are
+// left.  All threads, after a barrier.
+template <typename Put>
+__device__ __forceinline__ void rank_keys(const uint64_t* key, int n, int k, Put put) {
 #pragma unroll 1
-    for (int i = threadIdx.x; i < k; i += kThreads) out[i] = 0;
-    __syncthreads();
-#pragma unroll 1
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint64_t mine = key[i];
-        int above = 0;
+    for (int i = threadIdx.x; i < n || i < k; i += kThreads) {
+        const uint64_t mine = i < n ? key[i] : 0;
+        int above = 0, any = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) above += key[j] > mine;
-        if (mine != 0 && above < k) out[above] = mine;
+        for (int j = 0; j < n; ++j) above += key[j] > mine, any += key[j] != 0;
+        if (mine != 0 && above < k) put(above, mine);
+        if (i >= any && i < k) put(i, 0);
     }
-    __syncthreads();
 }
 
-// The k largest of a slice, whatever it holds: in steps of a logit for each thread, those above the k-th of what there is.
+// At most kCandidates logits of a slice, the k largest among them, whatever it holds: in steps of a logit for each thread,
+// those above the k-th of what there is.
 template <typename T>
 __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, LogprobShared& sh, uint64_t* out) {
     const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
@@ -99,7 +103,8 @@ __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, 
         if (key > least) sh.candidate[atomicAdd(&sh.count, 1)] = key;
         __syncthreads();
         if (sh.count > kCandidates - kThreads) {
-            rank_keys(sh.candidate, sh.count, k, out);
+            rank_keys(sh.candidate, sh.count, k, [&](int at, uint64_t x) { out[at] = x; });
+            __syncthreads();
             least = out[k - 1];  // there are more than k
             for (int j = threadIdx.x; j < k; j += kThreads) sh.candidate[j] = out[j];
             if (threadIdx.x == 0) sh.count = k;
@@ -107,7 +112,6 @@ __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, 
         }
         __syncthreads();
     }
-    rank_keys(sh.candidate, sh.count, k, out);
 }
 
 // The sums of a slice whose distances from kFloor could come out infinite or 0 (see there; or by an extreme temperature).
@@ -131,12 +135,12 @@ __device__ __noinline__ float4 slice_slow(const T* row, const Slice<T> s, float 
 }
 
 // The k-th largest of the threads' maxima (as orders), or less; kFloor's order if fewer than k are above that.
-__device__ __forceinline__ uint32_t bound_of(uint32_t mine, int k) {
+__device__ __noinline__ uint32_t search_bound(uint32_t mine, int k) {
     const uint32_t floor = order_of(kFloor);
     if (__syncthreads_count(mine > floor) < k) return floor;
     uint32_t bound = 0;
 #pragma unroll 1
-    for (int bit = 31; bit >= 12; --bit) {  // the last 12 bits only make the bound tighter by 2^-11 of itself
+    for (int bit = 31; bit >= 0; --bit) {
         const uint32_t next = bound | 1u << bit;
         if (__syncthreads_count(mine >= next) >= k) bound = next;
     }
@@ -150,6 +154,7 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
     LogprobShared& sh = *reinterpret_cast<LogprobShared*>(shared_bytes);
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int tid = threadIdx.x;
+    if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
     for (int64_t r = blockIdx.x / ctas; r < p.rows; r += gridDim.x / ctas) {
         const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
         const Slice<T> s(row, p.vocab, p.per_cta, rank);
@@ -167,6 +172,17 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
                 for (int q = 0; q < kBatch; ++q) v[q] = load_vector(row, s, fb, fe, j0 + q * kThreads + tid);
             }
         };
+        // the given token's logit, long before it is needed
+        int64_t token = -1;
+        float token_z = 0.0f;
+        if (p.logprob && tid == 0 && rank == 0) {
+            token = p.tokens[r];
+            if (token >= 0 && token < p.vocab) token_z = Storage<T>::load1(row + token);
+        }
+        if (kTop) {
+            if (tid == 0) sh.count = 0, sh.hot_count = 0;
+            for (int i = tid; i < kBins; i += kThreads) sh.bins[i] = 0;
+        }
         float m = kFloor, group_top = kFloor;
         f32x2 sum = 0, moment = 0;
         const f32x2 scale = pack2(p.scale, p.scale);
@@ -221,27 +237,65 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
         if (kTop && left != per_group) sh.group_max[group++][tid] = group_top;
         // elements outside the slice were counted at the floor: in a slice with anything above it they are 0
 
-        float4 part;
-        part.x = block_reduce<float, max_op>(m, sh.max);
-        const bool slow = !__syncthreads_or(m != m) && (part.x <= kFloor / 2 || part.x >= -kFloor ||
-                                                          !(p.scale > 1e-15f && p.scale < 1e15f));
-        if (slow) {
-            part = slice_slow(row, s, p.scale, sh);
-        } else {
+        const int warp = tid >> 5, lane = tid & 31;
+        const float wm = warp_max_f32(m);
+        if (lane == 0) sh.max[warp] = wm;
+        __syncthreads();
+        float4 part = make_float4(kFloor, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) part.x = fmaxf(part.x, sh.max[w]);
+        {
             const float d = (m - part.x) * p.scale, f = exp2_approx(d);
             float s0, s1, e0, e1;
             unpack2(sum, s0, s1);
             unpack2(moment, e0, e1);
-            const float4 x = block_sum4<kThreads>(
-                make_float4(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f, 0.0f, 0.0f), sh.sums);
-            part.y = x.x, part.z = x.y;
+            float4 x = make_float4(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f, 0.0f, 0.0f);
+            x.x = warp_reduce<float, add_op>(x.x);
+            x.y = warp_reduce<float, add_op>(x.y);
+            if (lane == 0) sh.sums[warp] = x;
         }
+        const uint32_t most = order_of(part.x), mine = order_of(m);
+        if (kTop && m > kFloor) atomicAdd(&sh.bins[min((most - mine) >> kBinShift, kBins - 1u)], 1);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < kThreads / 32; ++w) part.y += sh.sums[w].x, part.z += sh.sums[w].y;
+        const bool slow = part.x <= kFloor / 2 || part.x >= -kFloor || !(p.scale > 1e-15f && p.scale < 1e15f);
+        if (slow) part = slice_slow(row, s, p.scale, sh);
         if (!(part.y == part.y)) part.x = INFINITY;  // NaN somewhere
+        const uint64_t* found = sh.candidate;
+        int n = 0;
         if (kTop) {
             bool exact = slow;
             if (!exact) {
-                if (tid == 0) sh.count = 0, sh.hot_count = 0;
-                const uint32_t bound = bound_of(order_of(m), p.k);
+                if (warp == 0) {
+                    // the bin in which the k-th largest maximum lies
+                    constexpr int kPer = kBins / 32;
+                    int c[kPer], total = 0;
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) c[i] = sh.bins[lane * kPer + i], total += c[i];
+                    int before = total;
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) {
+                        const int up = __shfl_up_sync(0xffffffffu, before, o);
+                        if (lane >= o) before += up;
+                    }
+                    const uint32_t reached = __ballot_sync(0xffffffffu, before >= p.k);
+                    before -= total;
+                    if (reached == 0) {
+                        if (lane == 0) sh.bound = 0;
+                    } else if (lane == __ffs(reached) - 1) {
+                        int bin = lane * kPer - 1;
+#pragma unroll
+                        for (int i = 0; i < kPer; ++i)
+                            if (before < p.k) before += c[i], ++bin;
+                        const uint32_t depth = static_cast<uint32_t>(bin + 1) << kBinShift;
+                        // the last bin has no lower end
+                        sh.bound = bin < kBins - 1 ? max(most - depth + 1, order_of(kFloor) + 1) : 0;
+                    }
+                }
+                __syncthreads();
+                uint32_t bound = sh.bound;
+                if (bound == 0) bound = search_bound(mine, p.k);
                 const bool all = bound == order_of(kFloor);  // fewer than k threads have anything above the floor
                 const uint32_t above = all ? kOrderMasked : bound - 1;
                 auto collect = [&](int32_t j) {
@@ -259,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
 #pragma unroll 1
                     for (int j = tid; j < s.count; j += kThreads) collect(j);
                 } else {
-                    if (order_of(m) > above)
+                    if (mine > above)
 #pragma unroll 1
                         for (int g = 0; g < group; ++g)
                             if (order_of(sh.group_max[g][tid]) > above) {
@@ -279,38 +333,27 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
                 __syncthreads();
                 exact = exact || sh.count > kCandidates;
             }
-            uint64_t* best = sh.best + rank * p.k;
-            if (exact) select_slow(row, s, p.k, sh, best);
-            else rank_keys(sh.candidate, sh.count, p.k, best);
+            if (exact) select_slow(row, s, p.k, sh, sh.best);
+            n = sh.count;
         }
-        if (ctas > 1) {  // to the cluster's first CTA
-            if (tid == 0) sh.part[rank] = part;
-            cluster_sync();
-            if (rank == 0) {
-                if (tid < static_cast<int>(ctas) && tid > 0) sh.part[tid] = load_remote(&sh.part[tid], tid);
-                if (kTop)
-                    for (int i = p.k + tid; i < p.k * static_cast<int>(ctas); i += kThreads)
-                        sh.best[i] = load_remote(&sh.best[i], i / p.k);
-                __syncthreads();
-                part = sh.part[0];
-                float top = -INFINITY;
-                for (uint32_t q = 0; q < ctas; ++q) top = fmaxf(top, sh.part[q].x);
-                float sums = 0.0f, moments = 0.0f;
-                for (uint32_t q = 0; q < ctas; ++q) {
-                    const float4 x = sh.part[q];
-                    const float d = x.x == top || x.x == -INFINITY ? 0.0f : (x.x - top) * p.scale, f = exp2_approx(d);
-                    sums += f * x.y;
-                    if (f != 0.0f) moments += f * fmaf(x.y, d, x.z);
-                }
-                part = make_float4(top, sums, moments, 0.0f);
-                if (kTop) {
-                    for (int i = tid; i < p.k * static_cast<int>(ctas); i += kThreads) sh.candidate[i] = sh.best[i];
-                    __syncthreads();
-                    rank_keys(sh.candidate, p.k * ctas, p.k, sh.best);
-                }
+        if (ctas > 1) {  // to the cluster's first CTA; there is one row for each cluster then
+            cluster_wait();
+            if (tid == 0) store_remote(&sh.part[rank], 0, part);
+            if (kTop) rank_keys(found, n, p.k, [&](int at, uint64_t x) { store_remote(&sh.best[rank * p.k + at], 0, x); });
+            cluster_arrive();
+            cluster_wait();
+            if (rank != 0) return;
+            float top = -INFINITY;
+            for (uint32_t q = 0; q < ctas; ++q) top = fmaxf(top, sh.part[q].x);
+            part = make_float4(top, 0.0f, 0.0f, 0.0f);
+            for (uint32_t q = 0; q < ctas; ++q) {
+                const float4 x = sh.part[q];
+                const float d = x.x == top || x.x == -INFINITY ? 0.0f : (x.x - top) * p.scale, f = exp2_approx(d);
+                part.y += f * x.y;
+                if (f != 0.0f) part.z += f * fmaf(x.y, d, x.z);
             }
-            cluster_sync();  // nobody leaves, or goes on to another row, while its results are read
-            if (rank != 0) continue;
+            found = sh.best;
+            n = ctas * p.k;
         }
         const bool bad = part.x == INFINITY, empty = part.x == -INFINITY;
         const float top = empty ? 0.0f : part.x, log_s = bad ? NAN : logf(part.y);
@@ -318,19 +361,17 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
             if (p.lse) p.lse[r] = bad ? NAN : top * p.inv_t + log_s;
             if (p.entropy) p.entropy[r] = empty ? 0.0f : log_s - kLn2 * (part.z / part.y);
             if (p.logprob) {
-                const int64_t t = p.tokens[r];
                 float out = 0.0f;
-                if (t >= p.vocab || (t >= 0 && bad)) out = NAN;
-                else if (t >= 0) out = empty ? -INFINITY : (Storage<T>::load1(row + t) - top) * p.inv_t - log_s;
+                if (token >= p.vocab || (token >= 0 && bad)) out = NAN;
+                else if (token >= 0) out = empty ? -INFINITY : (token_z - top) * p.inv_t - log_s;
                 p.logprob[r] = out;
             }
         }
         if (kTop) {
-            for (int i = tid; i < p.k; i += kThreads) {
-                const uint64_t key = sh.best[i];
-                p.top_token[r * p.k + i] = key && !bad ? static_cast<int64_t>(key_index(key)) : -1;
-                p.top_logprob[r * p.k + i] = bad ? NAN : key ? (key_value(key) - top) * p.inv_t - log_s : -INFINITY;
-            }
+            rank_keys(found, n, p.k, [&](int at, uint64_t key) {
+                p.top_token[r * p.k + at] = key && !bad ? static_cast<int64_t>(key_index(key)) : -1;
+                p.top_logprob[r * p.k + at] = bad ? NAN : key ? (key_value(key) - top) * p.inv_t - log_s : -INFINITY;
+            });
         }
         __syncthreads();
     }
@@ -342,7 +383,7 @@ cudaError_t launch_logprobs(LogprobParams& p, cudaStream_t st) {
     constexpr int kVec = Storage<T>::kVec;
     const int64_t all = (static_cast<int64_t>(p.vocab) + 2 * kVec - 2) / kVec;  // vectors, whatever the alignment
     int ctas = 1;
-    while (ctas < kTopCluster && p.rows * 2 * ctas <= 2 * qn_sm_count() && all / ctas > 2 * kThreads) ctas *= 2;
+    while (ctas < kTopCluster && p.rows * 2 * ctas <= 3 * qn_sm_count() && all / ctas > 2 * kThreads) ctas *= 2;
     p.per_cta = static_cast<int32_t>((all + ctas - 1) / ctas);
     int dev = 0;
     static bool raised[64];

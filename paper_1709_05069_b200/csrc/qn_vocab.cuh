@@ -227,6 +227,12 @@ __device__ __forceinline__ float masked<float>() { return -INFINITY; }
 template <>
 __device__ __forceinline__ __nv_bfloat16 masked<__nv_bfloat16>() { return __ushort_as_bfloat16(0xff80u); }
 
+__device__ __forceinline__ float warp_max_f32(float x) {
+    float r;
+    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));  // of numbers, if there are any
+    return r;
+}
+
 // ---- clusters ------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -247,19 +253,16 @@ __device__ __forceinline__ uint32_t map_remote(const void* mine, uint32_t cta) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(mine)), "r"(cta));
     return at;
 }
-// The same variable of another CTA of the cluster.
-__device__ __forceinline__ float4 load_remote(const float4* mine, uint32_t cta) {
-    float4 x;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w)
-                 : "r"(map_remote(mine, cta))
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// Store into the same variable of another CTA of the cluster.
+__device__ __forceinline__ void store_remote(const float4* mine, uint32_t cta, float4 x) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(map_remote(mine, cta)), "f"(x.x), "f"(x.y),
+                 "f"(x.z), "f"(x.w)
                  : "memory");
-    return x;
 }
-__device__ __forceinline__ uint64_t load_remote(const uint64_t* mine, uint32_t cta) {
-    uint64_t x;
-    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(x) : "r"(map_remote(mine, cta)) : "memory");
-    return x;
+__device__ __forceinline__ void store_remote(const uint64_t* mine, uint32_t cta, uint64_t x) {
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_remote(mine, cta)), "l"(x) : "memory");
 }
 
 // ---- geometry ------------------------------------------------------------------------------------------------------

@@ -78,11 +78,6 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
     return mbar_try(bar, parity) || wait_slow(bar, parity, abort);
 }
 
-__device__ __forceinline__ float warp_max_f32(float x) {
-    float r;
-    asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(x));  // of numbers, if there are any
-    return r;
-}
 
 // Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }

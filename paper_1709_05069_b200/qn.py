@@ -454,24 +454,30 @@ def _logit_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     return rows, vocab, stride, dtype_code(t.dtype)
 
 
-def _beside(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: torch.device, name: str) -> int:
+def _beside(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: int, name: str) -> int:
     """Address of a small array that goes with the logits (0 for None)."""
     if t is None:
         return 0
-    if t.dtype != dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on %s" % (name, dtype, list(shape), device))
+    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d" % (name, dtype, list(shape), device))
     return t.data_ptr()
 
 
 def _gradient(t: torch.Tensor, logits: torch.Tensor, name: str) -> Tuple[int, int]:
     """Address and row stride of the gradient of ``logits``."""
-    if t.shape != logits.shape or t.dtype != logits.dtype or t.device != logits.device:
+    if t.shape != logits.shape or t.dtype is not logits.dtype or t.get_device() != logits.get_device():
         raise ValueError("%s must have the shape, dtype and device of the logits" % name)
     return t.data_ptr(), _logit_matrix(t, name)[2]
 
 
-def _stream_on(device: torch.device, stream) -> int:
-    return int((torch.cuda.current_stream(device) if stream is None else stream).cuda_stream)
+# torch's current stream by device index without a Stream object around it (2 us a call); the public way otherwise
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_on(device: int, stream) -> int:
+    if stream is not None:
+        return int(stream.cuda_stream)
+    return _raw_stream(device) if _raw_stream is not None else int(torch.cuda.current_stream(device).cuda_stream)
 
 
 def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
@@ -484,7 +490,7 @@ def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, log
     Outputs are the tensors that are passed: ``logprob``, ``lse``, ``entropy`` float32 [rows], ``top_token`` int64 and
     ``top_logprob`` float32 [rows][k]; ``tokens`` is int64 [rows], negative for "none".  Nothing waits for the device."""
     rows, vocab, stride, code = _logit_matrix(logits, "logits")
-    dev, k = logits.device, 0
+    dev, k = logits.get_device(), 0
     if top_token is not None or top_logprob is not None:
         if top_token is None or top_logprob is None or top_token.dim() != 2:
             raise ValueError("top_token and top_logprob go together, [rows][k] each")
@@ -507,7 +513,7 @@ def qn_logprobs_backward(logits: torch.Tensor, dlogits: torch.Tensor, tokens: Op
     gradients with respect to ``qn_logprobs``' outputs are ``d_logprob``, ``d_lse``, ``d_entropy`` [rows] and
     ``d_top_logprob`` [rows][k] (with the ``top_token`` that the forward call wrote), in one launch."""
     rows, vocab, stride, code = _logit_matrix(logits, "logits")
-    dev, k = logits.device, 0
+    dev, k = logits.get_device(), 0
     if d_top_logprob is not None:
         if top_token is None or d_top_logprob.dim() != 2:
             raise ValueError("d_top_logprob [rows][k] goes with top_token")
@@ -534,7 +540,7 @@ def qn_distill(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_value:
     probabilities as ``qn_logprobs`` writes them (``QN_TEACHER_LOGPROBS``: the rest of the vocabulary is one more outcome)
     or logits (``QN_TEACHER_LOGITS``: normalised over the list).  ``weight`` float32 [rows], 0 for padding."""
     rows, vocab, stride, code = _logit_matrix(logits, "logits")
-    dev = logits.device
+    dev = logits.get_device()
     if teacher_token is None or teacher_value is None or loss is None or teacher_token.dim() != 2:
         raise ValueError("teacher_token and teacher_value [rows][k] and loss [rows] are required")
     k = teacher_token.shape[1]
