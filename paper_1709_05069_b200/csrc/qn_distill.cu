@@ -24,6 +24,7 @@ struct DistillParams {
 
 // Out of line: it is called for every entry of the list, and instruction cache is scarce in this kernel.
 __device__ __noinline__ double exp64(double x) { return exp(x); }
+__device__ __noinline__ double log64(double x) { return log(x); }
 
 struct Distill {
     using Params = DistillParams;
@@ -32,9 +33,11 @@ struct Distill {
     struct Shared {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
         float q[QN_TOP_MAX], z[QN_TOP_MAX];
-        float q_sum, q_log_q, q_rest, weight;
+        double q_total, q_log_q;  // of the q as rounded to 32 bits
+        float q_sum, q_rest, weight;
         Gradient g;
-        float rest, s, dot;  // of the row, relative to its maximum
+        float rest, s;  // of the row, relative to its maximum
+        double dot;     // sum of q_k (z_k - origin(its maximum))
     };
     __device__ static void without(const Params& p, int64_t r, float loss) { p.loss[r] = loss; }
     __device__ static __forceinline__ int entries(const Params& p) { return p.k; }
@@ -86,7 +89,8 @@ struct Distill {
         }
         named = __reduce_add_sync(0xffffffffu, named);
         wrong = __any_sync(0xffffffffu, wrong);
-        float top = 0.0f, log_norm = 0.0f, inv = 1.0f;
+        float top = 0.0f, inv = 1.0f;
+        double log_norm = 0.0;
         if (!p.logprobs) {
             top = -INFINITY;
 #pragma unroll
@@ -96,27 +100,30 @@ struct Distill {
             inv = p.inv_t;
             double norm = 0.0;
 #pragma unroll
-            for (int i = 0; i < kMine; ++i) norm += exp64(static_cast<double>((v[i] - top) * inv));
-            log_norm = static_cast<float>(log(warp_reduce<double, add_op>(norm)));
+            for (int i = 0; i < kMine; ++i) norm += exp64((static_cast<double>(v[i]) - top) * inv);
+            log_norm = log64(warp_reduce<double, add_op>(norm));
         }
         // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
         double q_sum = 0.0;
-        float q_log_q = 0.0f;
+        double q_total = 0.0, q_log_q = 0.0;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int j = lane + 32 * i;
             if (j >= p.k) continue;
-            const float log_q = (v[i] - top) * inv - log_norm;
-            const double q = exp64(static_cast<double>(log_q));
+            const double log_q = (static_cast<double>(v[i]) - top) * inv - log_norm, q = exp64(log_q);
             q_sum += q;
-            if (q != 0.0) q_log_q += static_cast<float>(q) * log_q;
-            sh.q[j] = static_cast<float>(q);
+            const float q32 = static_cast<float>(q);
+            if (q32 != 0.0f) q_log_q += q32 * log_q;
+            q_total += q32;
+            sh.q[j] = q32;
         }
         q_sum = warp_reduce<double, add_op>(q_sum);
-        q_log_q = warp_reduce<float, add_op>(q_log_q);
+        q_total = warp_reduce<double, add_op>(q_total);
+        q_log_q = warp_reduce<double, add_op>(q_log_q);
         if (lane == 0) {
             sh.weight = f.weight;
             sh.q_sum = wrong ? NAN : static_cast<float>(q_sum);
+            sh.q_total = q_total;
             sh.q_log_q = q_log_q;
             sh.q_rest = 0.0f;
             if (p.logprobs && named < p.vocab) sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
@@ -124,27 +131,36 @@ struct Distill {
         __syncwarp();
     }
 
-    // Of the list's entries in a warp's chunks: the largest logit; sums of e_k and q_k u_k relative to it; sum of q_k.
+    // Of the list's entries in a warp's chunks: the largest logit m; sum of e_k relative to it; sums of q_k and of
+    // q_k (z_k - origin(m)).  The loss is the small difference of sums over the list and ln S: what it is made of is kept in
+    // 64 bits.  (The origin is 0 for all ordinary logits, so that joining such sums adds no rounding.)
+    __device__ static __forceinline__ float origin(float m) {
+        return m == -INFINITY ? 0.0f : fabsf(m) < 0x1p30f ? 1024.0f * rintf(m * (1.0f / 1024.0f)) : m;
+    }
     struct Extra {
-        float m = -INFINITY, list = 0.0f, dot = 0.0f, q = 0.0f;
+        float m = -INFINITY, list = 0.0f;
+        double dot = 0.0, q = 0.0;
         __device__ __forceinline__ void down_to(const Params& p, float to) {
             if (!(to > m)) return;
-            const float d = m - to;  // -inf at first, with nothing in the sums
-            list *= exp2_approx(d * p.scale);
-            if (q > 0.0f) dot += q * (d * p.inv_t);
+            list *= exp2_approx((m - to) * p.scale);  // 0 at first, of nothing
+            const float from = origin(m), o = origin(to);
+            if (q > 0.0 && from != o) dot += q * (static_cast<double>(from) - o);
             m = to;
         }
         __device__ __forceinline__ void take(const Params& p, const Shared& sh, int k, float z) {
             down_to(p, z);
-            const float d = z - (m == -INFINITY ? 0.0f : m), qk = sh.q[k];
-            list += exp2_approx(d * p.scale);
-            if (qk > 0.0f) dot += qk * (d * p.inv_t);
-            q += qk;
+            list += exp2_approx((z - (m == -INFINITY ? 0.0f : m)) * p.scale);
+            const double qk = sh.q[k];
+            if (qk > 0.0) dot += qk * (static_cast<double>(z) - origin(m)), q += qk;
         }
-        __device__ __forceinline__ float4 message(const Params& p) {
+        // in two pieces: what the warp's other message has room for, and its own
+        __device__ __forceinline__ float4 message(const Params& p, float4& other) {
             down_to(p, warp_max_f32(m));
-            return make_float4(m, warp_reduce<float, add_op>(list), warp_reduce<float, add_op>(dot),
-                               warp_reduce<float, add_op>(q));
+            const double all = warp_reduce<double, add_op>(dot);
+            const float high = static_cast<float>(all);
+            other.z = static_cast<float>(warp_reduce<double, add_op>(q));
+            return make_float4(m, warp_reduce<float, add_op>(list), high,
+                               isfinite(high) ? static_cast<float>(all - high) : 0.0f);
         }
     };
 
@@ -156,7 +172,8 @@ struct Distill {
 #pragma unroll 1
         for (int i = lane; i < all; i += 32) m = fmaxf(m, in[i].x);
         m = warp_max_f32(m);
-        float rest = 0.0f, list = 0.0f, dot = 0.0f;
+        float rest = 0.0f, list = 0.0f;
+        double dot = 0.0;
 #pragma unroll 1
         for (int i = lane; i < all; i += 32) {
             const float4 v = in[i];
@@ -165,13 +182,14 @@ struct Distill {
                 rest += f * v.y;  // masked elements only: 0, or NaN where there is one
             } else {
                 list += f * v.y;
-                dot += v.z;
-                if (v.w > 0.0f && v.x != m) dot += v.w * ((v.x - m) * p.inv_t);
+                const float q = in[i - kWarps].z, from = origin(v.x), to = origin(m);
+                dot += static_cast<double>(v.z) + v.w;
+                if (q > 0.0f && from != to) dot += q * (static_cast<double>(from) - to);
             }
         }
         rest = warp_reduce<float, add_op>(rest);
         list = warp_reduce<float, add_op>(list);
-        dot = warp_reduce<float, add_op>(dot);
+        dot = warp_reduce<double, add_op>(dot);
         const float s = m == INFINITY ? NAN : rest + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
         Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (s != 0.0f) {
@@ -192,11 +210,14 @@ struct Distill {
                 if (s.holds(sh.pos[j]))
                     Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - g.m) * p.scale) - g.unit * sh.q[j]);
         if (first && (threadIdx.x & 31) == 0) {
-            // sum q (ln q - ln p) with ln p = u - m/T - ln S
-            const float log_s = logf(sh.s);
-            float loss = sh.s == 0.0f ? INFINITY : sh.q_log_q - sh.dot + sh.q_sum * log_s;
-            if (sh.s != 0.0f && sh.q_rest != 0.0f) loss += sh.q_rest * (logf(sh.q_rest) - (logf(sh.rest) - log_s));
-            p.loss[r] = sh.q_sum + sh.q_rest != sh.q_sum + sh.q_rest ? NAN : loss;
+            // sum q (ln q - ln p) with ln p = ln 2 s (z - m) - ln S
+            const double log_s = log64(static_cast<double>(sh.s));
+            double loss = INFINITY;
+            if (sh.s != 0.0f) {
+                loss = sh.q_log_q - 0.6931471805599453 * p.scale * (sh.dot + sh.q_total * (static_cast<double>(origin(g.m)) - g.m)) + sh.q_total * log_s;
+                if (sh.q_rest != 0.0f) loss += sh.q_rest * (logf(sh.q_rest) - logf(sh.rest) + log_s);
+            }
+            p.loss[r] = sh.q_sum + sh.q_rest != sh.q_sum + sh.q_rest ? NAN : static_cast<float>(loss);
         }
     }
 };

@@ -177,6 +177,11 @@ struct Lanes<float> {
         return make_uint4(__float_as_uint(max_nan(__uint_as_float(v.x), floor)), __float_as_uint(max_nan(__uint_as_float(v.y), floor)),
                           __float_as_uint(max_nan(__uint_as_float(v.z), floor)), __float_as_uint(max_nan(__uint_as_float(v.w), floor)));
     }
+    // the elements whose bit is set become -inf
+    __device__ static __forceinline__ uint4 without(const uint4& v, uint32_t bits) {
+        return make_uint4(bits & 1 ? 0xff800000u : v.x, bits & 2 ? 0xff800000u : v.y, bits & 4 ? 0xff800000u : v.z,
+                          bits & 8 ? 0xff800000u : v.w);
+    }
     __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     // running maximum of a thread, several elements side by side; NaN if there is one
     struct Max {
@@ -199,6 +204,14 @@ struct Lanes<__nv_bfloat16> {
         Max f;
         f.start(floor);
         return make_uint4(Max::max2(v.x, f.m), Max::max2(v.y, f.m), Max::max2(v.z, f.m), Max::max2(v.w, f.m));
+    }
+    __device__ static __forceinline__ uint32_t without2(uint32_t w, uint32_t bits) {
+        if (bits & 1) w = (w & 0xffff0000u) | 0xff80u;
+        if (bits & 2) w = (w & 0xffffu) | 0xff800000u;
+        return w;
+    }
+    __device__ static __forceinline__ uint4 without(const uint4& v, uint32_t bits) {
+        return make_uint4(without2(v.x, bits), without2(v.y, bits >> 2), without2(v.z, bits >> 4), without2(v.w, bits >> 6));
     }
     __device__ static __forceinline__ uint4 masked4() { return make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     struct Max {

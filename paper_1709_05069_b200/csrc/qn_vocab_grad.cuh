@@ -103,6 +103,23 @@ __device__ __noinline__ void write_constant(T* out, const Slice<T> s, int tid, f
     if (tail < hi && tid < kVec) Storage<T>::store1(out + tail, x);
 }
 
+// Loads of logits whose place the gradient may take.
+__device__ __forceinline__ uint4 load_stream(const void* p) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p)
+                 : "memory");
+    return v;
+}
+template <typename T>
+__device__ __noinline__ uint4 load_edge_rw(const T* row, int32_t origin, int32_t vocab) {
+    float x[Storage<T>::kVec];
+#pragma unroll
+    for (int e = 0; e < Storage<T>::kVec; ++e) x[e] = origin + e >= 0 && origin + e < vocab ? load_rw(row + origin + e) : -INFINITY;
+    return Storage<T>::pack(x);
+}
+
 // The elements of one vector that lie inside the row, one at a time.
 template <typename T>
 __device__ __noinline__ void write_edge(T* out, int32_t origin, int32_t vocab, uint4 w) {
@@ -291,9 +308,11 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                     msg.z = warp_reduce<float, add_op>(msg.z);
                 }
                 msg.y = warp_reduce<float, add_op>(msg.y);
+                float4 list;
+                if constexpr (Op::kListMessage) list = extra.message(p, msg);
                 if (!may_send(u)) return;
                 send(u, worker, msg);
-                if constexpr (Op::kListMessage) send(u, kSumWarps + worker, extra.message(p));
+                if constexpr (Op::kListMessage) send(u, kSumWarps + worker, list);
                 ++u;
             }
             __syncwarp();
@@ -533,15 +552,176 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
         for (int64_t r = row0 + static_cast<int64_t>(oldest) * row_step; r < p.rows; r += mine_step) Op::without(p, r, NAN);
 }
 
+// ---- small problems --------------------------------------------------------------------------------------------------
+
+// The same for problems whose time is latency: a CTA (of a cluster, where there are few rows or long ones) takes a slice of up
+// to 32 KB straight into registers, its first warp the special elements meanwhile; sums, exchange, gradient, end.
+constexpr int kSmallVectors = 8;  // of a thread
+
+template <typename T, int NT, typename Op, bool kAligned>
+__global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const typename Op::Params p, const int32_t per_cta) {
+    constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
+    constexpr int kWarps = NT / 32, kMessages = Op::kListMessage ? 2 : 1;
+    constexpr bool moments = Op::kMoments;
+    __shared__ typename Op::Shared sh;
+    __shared__ __align__(16) float4 inbox[kMaxCluster * kMessages];
+    __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWarps][32];
+    __shared__ float4 warp_sums[kWarps];
+    __shared__ float warp_max[kWarps];
+    __shared__ uint8_t special[Op::kMask ? NT * kSmallVectors : 1];  // which elements of a vector leave the sums
+    __shared__ bool want;
+    const uint32_t ctas = cluster_size(), rank = cluster_rank();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
+    const int64_t r = blockIdx.x / ctas;
+    const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
+    T* out = p.dlogits ? static_cast<T*>(p.dlogits) + r * p.dlogits_stride : nullptr;
+    const Slice<T> s(row, p.vocab, per_cta, rank);
+    const int32_t fb = s.full_begin(), fe = s.full_end();
+    uint4 v[kSmallVectors];
+#pragma unroll
+    for (int q = 0; q < kSmallVectors; ++q) {
+        const int32_t j = q * NT + tid;
+        v[q] = Lanes<T>::masked4();
+        if (j >= fb && j < fe) v[q] = load_stream(row + s.origin() + j * kVec);
+        else if (j < s.count) v[q] = load_edge_rw(row, s.origin() + j * kVec, s.vocab);
+    }
+    if (Op::kMask)
+        for (int i = tid; i < NT * kSmallVectors / 4; i += NT) reinterpret_cast<uint32_t*>(special)[i] = 0;
+    typename Op::Extra extra;
+    if (warp == 0) {
+        const typename Op::Fetched now = Op::fetch(p, r);
+        const bool wanted = Op::wanted(p, now);
+        if (wanted) {
+            Op::begin(p, sh, now);
+#pragma unroll 1
+            for (int k = lane; k < Op::entries(p); k += 32)
+                if (s.holds(sh.pos[k])) sh.z[k] = load_rw(row + sh.pos[k]);
+        }
+        if (lane == 0) want = wanted;
+    }
+    typename Lanes<T>::Max top;
+#pragma unroll
+    for (int q = 0; q < kSmallVectors; ++q) top.take(v[q]);
+    const float mine = top.get();  // NaN if there is one: then all of the row becomes NaN
+    {
+        const float wm = mine != mine ? INFINITY : mine;
+        const float x = warp_max_f32(wm);
+        if (lane == 0) warp_max[warp] = x;
+    }
+    __syncthreads();
+    if (!want) {
+        if (out) write_constant<T, NT>(out, s, tid, 0.0f);
+        if (rank == 0 && tid == 0) Op::without(p, r, 0.0f);
+        if (ctas > 1) cluster_wait();
+        return;
+    }
+    float m = warp_max[0];
+#pragma unroll
+    for (int w = 1; w < kWarps; ++w) m = fmaxf(m, warp_max[w]);
+    if (Op::kMask) {
+        if (warp == 0)
+#pragma unroll 1
+            for (int k = lane; k < Op::entries(p); k += 32)
+                if (s.holds(sh.pos[k])) {
+                    const int at = sh.pos[k] - s.origin(), bit = at / kVec * 8 + at % kVec;
+                    atomicOr(reinterpret_cast<uint32_t*>(special) + bit / 32, 1u << bit % 32);
+                    extra.take(p, sh, k, sh.z[k]);
+                }
+        __syncthreads();
+    }
+    const float ref = m == -INFINITY ? 0.0f : m;
+    const f32x2 minus = pack2(-ref, -ref), scale = pack2(p.scale, p.scale);
+    f32x2 sum = 0, moment = 0;
+#pragma unroll
+    for (int q = 0; q < kSmallVectors; ++q) {
+        if (q * NT >= s.count) break;
+        uint4 w = v[q];
+        if (Op::kMask) {
+            const uint32_t bits = special[q * NT + tid];
+            if (bits) w = Lanes<T>::without(w, bits);
+        }
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            const f32x2 d = mul2(add2(Lanes<T>::pair(w, i), minus), scale), e = exp2_pair(d);
+            sum = add2(sum, e);
+            if constexpr (moments) moment = fma2(e, finite_pair(d), moment);
+        }
+    }
+    float s0, s1, e0, e1;
+    unpack2(sum, s0, s1);
+    unpack2(moment, e0, e1);
+    float4 x = make_float4(m, s0 + s1, e0 + e1, 0.0f);
+    x.y = warp_reduce<float, add_op>(x.y);
+    if constexpr (moments) x.z = warp_reduce<float, add_op>(x.z);
+    if (lane == 0) warp_sums[warp] = x;
+    __syncthreads();
+    if (warp == 0) {
+        x = warp_sums[0];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) x.y += warp_sums[w].y, x.z += warp_sums[w].z;
+        float4 list = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        if constexpr (Op::kListMessage) list = extra.message(p, x);
+        if (ctas == 1) {
+            if (lane == 0) {
+                inbox[0] = x;
+                if (Op::kListMessage) inbox[1] = list;
+            }
+        } else {
+            cluster_wait();
+            if (lane < static_cast<int>(ctas)) {
+                store_remote(&inbox[rank * kMessages], lane, x);
+                if (Op::kListMessage) store_remote(&inbox[rank * kMessages + 1], lane, list);
+            }
+        }
+        __syncwarp();
+    }
+    if (ctas > 1) {
+        if (warp != 0) cluster_wait();
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 0) Op::template join<1>(p, sh, inbox, static_cast<int>(ctas));
+    __syncthreads();
+    if (out) {
+        const Gradient g = sh.g;
+        const f32x2 minus_m = pack2(-g.m, -g.m), c0 = pack2(g.c0, g.c0), c1 = pack2(g.c1, g.c1);
+#pragma unroll
+        for (int q = 0; q < kSmallVectors; ++q) {
+            if (q * NT >= s.count) break;
+            const int32_t j = q * NT + tid, at = s.origin() + j * kVec, j0 = j - lane;
+            float y[kVec];
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus_m), scale), e = exp2_pair(d);
+                unpack2(moments ? mul2(e, fma2(finite_pair(d), c1, c0)) : mul2(e, c0), y[2 * i], y[2 * i + 1]);
+            }
+            const uint4 w = Storage<T>::pack(y);
+            if (kAligned) {
+                if (j >= fb && j < fe) stg_stream16(out + at, w);
+                else if (j < s.count) write_edge(out, at, s.vocab, w);
+            } else if (j0 >= fb && j0 + 32 <= fe) {
+                __syncwarp();
+                stage[warp][lane] = w;
+                __syncwarp();
+                write_run(out, at - lane * kVec, stage[warp]);
+            } else if (j < s.count) {
+                write_edge(out, at, s.vocab, w);
+            }
+        }
+        __syncthreads();  // the special elements are written after the others
+    }
+    if (warp == 0) Op::template fix<T>(p, sh, s, out, r, rank == 0);
+}
+
 // ---- host ----------------------------------------------------------------------------------------------------------
 
 template <typename T, typename Op, bool kAligned>
-cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t st) {
+cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, cudaStream_t st) {
     auto kernel = row_gradient_kernel<T, Op, kAligned>;
     // CTAs a row: slices of up to 128 KB, of up to 192 KB where 8 of them are not enough; where there are few rows, more and
     // smaller ones, down to a chunk for every sum warp
-    constexpr int kVec = Storage<T>::kVec, kGood = 32 * kChunk;
-    const int64_t all = (static_cast<int64_t>(p.vocab) + 2 * kVec - 2) / kVec;  // vectors, whatever the alignment
+    constexpr int kGood = 32 * kChunk;
     int ctas = 1;
     while (ctas < kMaxCluster && (all + ctas - 1) / ctas > kGood) ++ctas;
     while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= qn_sm_count() && all / ctas > kSumWarps * kChunk) ctas *= 2;
@@ -574,6 +754,49 @@ cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t s
     }
     cfg.gridDim = dim3(static_cast<unsigned>((p.rows < clusters ? p.rows : clusters) * ctas));
     return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(per_cta));
+}
+
+// Vectors that a row may span, whatever its alignment.
+template <typename T, typename Params>
+int64_t row_vectors(const Params& p) {
+    constexpr int kVec = Storage<T>::kVec;
+    const bool aligned = reinterpret_cast<uintptr_t>(p.logits) % 16 == 0 && (p.rows == 1 || p.row_stride % kVec == 0);
+    return (static_cast<int64_t>(p.vocab) + (aligned ? kVec - 1 : 2 * kVec - 2)) / kVec;
+}
+
+template <typename T, int NT, typename Op, bool kAligned>
+cudaError_t launch_gradient_small(const typename Op::Params& p, int ctas, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.rows * ctas));
+    cfg.blockDim = dim3(NT);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = ctas;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    const int per_cta = static_cast<int>((row_vectors<T>(p) + ctas - 1) / ctas);
+    return cudaLaunchKernelEx(&cfg, row_gradient_small_kernel<T, NT, Op, kAligned>, p, static_cast<int32_t>(per_cta));
+}
+
+template <typename T, typename Op, bool kAligned>
+cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t st) {
+    const int64_t all = row_vectors<T>(p);
+    int ctas = 1;
+    while (ctas <= kMaxCluster && all > ctas * 256 * kSmallVectors) ++ctas;
+    // Rows in flight one by one against the pipeline.  Measured, us (rows x vocab, small kernel / pipeline; the list has 32
+    // tokens): bf16 128 x 131072 20 / 22, 1024 x 32000 36 / 36, 8192 x 32000 260 / 207, 1024 x 131072 134 / 115,
+    // 8192 x 8192 87 / 118; fp32 128 x 32000 9.7 / 14, 1024 x 32000 71 / 53, 1024 x 8192 17 / 21, 8192 x 8192 129 / 116;
+    // one row of 8192: 5 / 9.  So: all logits more than 64 MB, in rows of more than 32 KB.
+    const int64_t bytes = p.vocab * static_cast<int64_t>(sizeof(T));
+    if (ctas > kMaxCluster || (bytes > (32 << 10) && p.rows > (64 << 20) / bytes))
+        return launch_gradient_pipeline<T, Op, kAligned>(p, all, st);
+    // few rows: more CTAs, down to a vector a thread; many: no more threads than a row has work for
+    while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= 2 * qn_sm_count() && all > ctas * 256) ctas *= 2;
+    const bool many = p.rows * ctas > 4 * qn_sm_count();
+    if (all <= 64 || (many && all <= 64 * kSmallVectors)) return launch_gradient_small<T, 64, Op, kAligned>(p, ctas, st);
+    return launch_gradient_small<T, 256, Op, kAligned>(p, ctas, st);
 }
 
 template <typename T, typename Op>
