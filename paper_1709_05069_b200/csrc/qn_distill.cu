@@ -28,23 +28,23 @@ __device__ __noinline__ double log64(double x) { return log(x); }
 
 struct Distill {
     using Params = DistillParams;
-    static constexpr bool kMoments = false, kListMessage = true, kMask = true;
+    static constexpr bool kMoments = false, kMask = true;
     static constexpr int kMine = QN_TOP_MAX / 32;  // entries of the list a lane
     struct Shared {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
         float q[QN_TOP_MAX], z[QN_TOP_MAX];
         double q_total, q_log_q;  // of the q as rounded to 32 bits
         float q_sum, q_rest, weight;
+        float list_m, list_s;  // of the list's logits: the largest, sum of e_k relative to it
         Gradient g;
         float rest, s;  // of the row, relative to its maximum
-        double dot;     // sum of q_k (z_k - origin(its maximum))
     };
     __device__ static void without(const Params& p, int64_t r, float loss) { p.loss[r] = loss; }
     __device__ static __forceinline__ int entries(const Params& p) { return p.k; }
 
     struct Fetched {
         int64_t at[kMine];
-        float v[kMine], weight;
+        float v[kMine], z[kMine], weight;
     };
     __device__ static __forceinline__ Fetched fetch(const Params& p, int64_t r) {
         Fetched f;
@@ -62,6 +62,13 @@ struct Distill {
                                   : __ldg(static_cast<const float*>(p.value) + entry);
         }
         return f;
+    }
+
+    template <typename T>
+    __device__ static __forceinline__ void gather(const Params& p, int64_t r, Fetched& f) {
+        const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) f.z[i] = f.at[i] >= 0 && f.at[i] < p.vocab ? load_rw(row + f.at[i]) : -INFINITY;
     }
 
     // false: weight 0, or no teacher (no token at all, or of logits none that weighs anything)
@@ -117,11 +124,24 @@ struct Distill {
             q_total += q32;
             sh.q[j] = q32;
         }
+        float list_m = -INFINITY, list_s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) list_m = fmaxf(list_m, f.z[i]);
+        list_m = warp_max_f32(list_m);
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            if (f.at[i] < 0 || f.at[i] >= p.vocab) continue;
+            list_s += exp2_approx((f.z[i] - (list_m == -INFINITY ? 0.0f : list_m)) * p.scale);
+            sh.z[lane + 32 * i] = f.z[i];
+        }
+        list_s = warp_reduce<float, add_op>(list_s);
         q_sum = warp_reduce<double, add_op>(q_sum);
         q_total = warp_reduce<double, add_op>(q_total);
         q_log_q = warp_reduce<double, add_op>(q_log_q);
         if (lane == 0) {
             sh.weight = f.weight;
+            sh.list_m = list_m;
+            sh.list_s = list_s;
             sh.q_sum = wrong ? NAN : static_cast<float>(q_sum);
             sh.q_total = q_total;
             sh.q_log_q = q_log_q;
@@ -131,65 +151,23 @@ struct Distill {
         __syncwarp();
     }
 
-    // Of the list's entries in a warp's chunks: the largest logit m; sum of e_k relative to it; sums of q_k and of
-    // q_k (z_k - origin(m)).  The loss is the small difference of sums over the list and ln S: what it is made of is kept in
-    // 64 bits.  (The origin is 0 for all ordinary logits, so that joining such sums adds no rounding.)
-    __device__ static __forceinline__ float origin(float m) {
-        return m == -INFINITY ? 0.0f : fabsf(m) < 0x1p30f ? 1024.0f * rintf(m * (1.0f / 1024.0f)) : m;
-    }
-    struct Extra {
-        float m = -INFINITY, list = 0.0f;
-        double dot = 0.0, q = 0.0;
-        __device__ __forceinline__ void down_to(const Params& p, float to) {
-            if (!(to > m)) return;
-            list *= exp2_approx((m - to) * p.scale);  // 0 at first, of nothing
-            const float from = origin(m), o = origin(to);
-            if (q > 0.0 && from != o) dot += q * (static_cast<double>(from) - o);
-            m = to;
-        }
-        __device__ __forceinline__ void take(const Params& p, const Shared& sh, int k, float z) {
-            down_to(p, z);
-            list += exp2_approx((z - (m == -INFINITY ? 0.0f : m)) * p.scale);
-            const double qk = sh.q[k];
-            if (qk > 0.0) dot += qk * (static_cast<double>(z) - origin(m)), q += qk;
-        }
-        // in two pieces: what the warp's other message has room for, and its own
-        __device__ __forceinline__ float4 message(const Params& p, float4& other) {
-            down_to(p, warp_max_f32(m));
-            const double all = warp_reduce<double, add_op>(dot);
-            const float high = static_cast<float>(all);
-            other.z = static_cast<float>(warp_reduce<double, add_op>(q));
-            return make_float4(m, warp_reduce<float, add_op>(list), high,
-                               isfinite(high) ? static_cast<float>(all - high) : 0.0f);
-        }
-    };
-
-    // messages: of a CTA's warps, their maximum and sum of e_i; then of each what Extra has
+    // messages: a warp's maximum and sum of e_i off the list
     template <int kWarps>
     __device__ static __forceinline__ void join(const Params& p, Shared& sh, const float4* in, int ctas) {
-        const int lane = threadIdx.x & 31, all = ctas * (2 * kWarps);
-        float m = -INFINITY;
+        const int lane = threadIdx.x & 31, all = ctas * kWarps;
+        float m = sh.list_m;
 #pragma unroll 1
         for (int i = lane; i < all; i += 32) m = fmaxf(m, in[i].x);
         m = warp_max_f32(m);
-        float rest = 0.0f, list = 0.0f;
-        double dot = 0.0;
+        float rest = 0.0f;
 #pragma unroll 1
         for (int i = lane; i < all; i += 32) {
             const float4 v = in[i];
-            const float f = v.x == m || v.x == -INFINITY ? 1.0f : exp2_approx((v.x - m) * p.scale);
-            if (i % (2 * kWarps) < kWarps) {
-                rest += f * v.y;  // masked elements only: 0, or NaN where there is one
-            } else {
-                list += f * v.y;
-                const float q = in[i - kWarps].z, from = origin(v.x), to = origin(m);
-                dot += static_cast<double>(v.z) + v.w;
-                if (q > 0.0f && from != to) dot += q * (static_cast<double>(from) - to);
-            }
+            // of masked elements only: 0, or NaN where there is one
+            rest += v.y * (v.x == m || v.x == -INFINITY ? 1.0f : exp2_approx((v.x - m) * p.scale));
         }
         rest = warp_reduce<float, add_op>(rest);
-        list = warp_reduce<float, add_op>(list);
-        dot = warp_reduce<double, add_op>(dot);
+        const float list = sh.list_s * (sh.list_m == m || sh.list_m == -INFINITY ? 1.0f : exp2_approx((sh.list_m - m) * p.scale));
         const float s = m == INFINITY ? NAN : rest + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
         Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (s != 0.0f) {
@@ -198,7 +176,7 @@ struct Distill {
             g.on = g.unit * __fdividef(mass, s);
             g.c0 = q_rest > 0.0f && rest > 0.0f ? g.on - g.unit * __fdividef(q_rest, rest) : g.on;
         }
-        if (lane == 0) sh.g = g, sh.rest = rest, sh.s = s, sh.dot = dot;
+        if (lane == 0) sh.g = g, sh.rest = rest, sh.s = s;
     }
 
     template <typename T>
@@ -209,12 +187,17 @@ struct Distill {
             for (int j = threadIdx.x & 31; j < p.k; j += 32)
                 if (s.holds(sh.pos[j]))
                     Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - g.m) * p.scale) - g.unit * sh.q[j]);
-        if (first && (threadIdx.x & 31) == 0) {
-            // sum q (ln q - ln p) with ln p = ln 2 s (z - m) - ln S
+        if (!first) return;
+        // sum q (ln q - ln p) with ln p = ln 2 s (z - m) - ln S: the small difference of these sums, so in 64 bits
+        double dot = 0.0;
+        for (int j = threadIdx.x & 31; j < p.k; j += 32)
+            if (sh.pos[j] >= 0 && sh.q[j] > 0.0f) dot += sh.q[j] * (static_cast<double>(sh.z[j]) - g.m);
+        dot = warp_reduce<double, add_op>(dot);
+        if ((threadIdx.x & 31) == 0) {
             const double log_s = log64(static_cast<double>(sh.s));
             double loss = INFINITY;
             if (sh.s != 0.0f) {
-                loss = sh.q_log_q - 0.6931471805599453 * p.scale * (sh.dot + sh.q_total * (static_cast<double>(origin(g.m)) - g.m)) + sh.q_total * log_s;
+                loss = sh.q_log_q - 0.6931471805599453 * p.scale * dot + sh.q_total * log_s;
                 if (sh.q_rest != 0.0f) loss += sh.q_rest * (logf(sh.q_rest) - logf(sh.rest) + log_s);
             }
             p.loss[r] = sh.q_sum + sh.q_rest != sh.q_sum + sh.q_rest ? NAN : static_cast<float>(loss);

@@ -429,7 +429,7 @@ template <bool kEntropy>
 struct Backward {
     using Params = BackwardParams;
     static constexpr bool kMoments = kEntropy;
-    static constexpr bool kListMessage = false, kMask = false;
+    static constexpr bool kMask = false;
     struct Shared {
         int32_t pos[QN_TOP_MAX + 1];  // sparse terms: 0 the given token, 1..k the alternatives; -1 for none
         float add[QN_TOP_MAX + 1], z[QN_TOP_MAX + 1];
@@ -438,14 +438,11 @@ struct Backward {
     };
     __device__ static void without(const Params&, int64_t, float) {}
     __device__ static __forceinline__ int entries(const Params& p) { return p.k + 1; }
-    struct Extra {
-        __device__ __forceinline__ void take(const Params&, const Shared&, int, float) {}
-    };
 
     static constexpr int kMine = QN_TOP_MAX / 32 + 1;  // sparse terms a lane
     struct Fetched {
         int64_t at[kMine];
-        float x[kMine], d_lse, d_h;
+        float x[kMine], z[kMine], d_lse, d_h;
     };
     __device__ static __forceinline__ Fetched fetch(const Params& p, int64_t r) {
         Fetched f;
@@ -461,6 +458,12 @@ struct Backward {
             if (row && j >= 1 && j <= p.k) f.at[i] = p.top_token[r * p.k + j - 1], f.x[i] = p.d_top[r * p.k + j - 1];
         }
         return f;
+    }
+    template <typename T>
+    __device__ static __forceinline__ void gather(const Params& p, int64_t r, Fetched& f) {
+        const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) f.z[i] = f.at[i] >= 0 && f.at[i] < p.vocab ? load_rw(row + f.at[i]) : -INFINITY;
     }
     // a sparse term's gradient: none for an absent token, NaN for one that is not in the vocabulary
     __device__ static __forceinline__ float term(const Params& p, const Fetched& f, int i) {
@@ -482,6 +485,7 @@ struct Backward {
             if (j > p.k) continue;
             sh.pos[j] = f.at[i] >= 0 && f.at[i] < p.vocab ? static_cast<int32_t>(f.at[i]) : -1;
             sh.add[j] = term(p, f, i);
+            sh.z[j] = f.z[i];
             sum += sh.add[j];
         }
         sum = warp_reduce<float, add_op>(sum);

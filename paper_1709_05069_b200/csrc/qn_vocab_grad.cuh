@@ -7,11 +7,10 @@
 //
 // There is one CTA on an SM, it stays, and its warps are stages of a pipeline over chunks of 4 KB in a ring of 48:
 //   list warps     a row each: read the few elements of it that are special (a given token, alternatives, a teacher's list),
-//                  work out what depends on them alone, and sort them by chunk; when the row has been written, write their
-//                  gradients
+//                  work out what depends on them alone, and sort those by chunk that must not be added; when the row has been
+//                  written, write their gradients
 //   copy warp      brings the slices of the coming rows in
-//   sum warps      a chunk each: fetch the special elements' logits, take them out where they must not be added, and add
-//                  e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative to a running maximum m of each thread; at the end of a
+//   sum warps      a chunk each: take out what must not be added, and add e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative to a running maximum m of each thread; at the end of a
 //                  slice each sends its maximum and sums to every CTA of the cluster (asynchronous stores into shared
 //                  memory that count on a barrier there)
 //   join warp      from all messages, in the same order in every CTA, to the row's coefficients
@@ -23,11 +22,11 @@
 //
 // An operator Op brings:
 //   Params, Shared        arguments; what the warps tell one another of a row
-//   Fetched, fetch        a row's special elements as a lane of a list warp loads them, ahead of their use
+//   Fetched, fetch        a row's special elements as a lane of a list warp loads them, two rows ahead of their use
+//   gather                their logits (of the whole row, also outside the slice), a row ahead
 //   wanted                false if the row is padding: its gradient is 0 and it is not read
 //   begin                 list warp: what depends on the special elements alone, and their places (Shared::pos)
 //   kMask                 whether the special elements leave the sums
-//   Extra                 what a sum warp adds up over the special elements of its chunks (kListMessage: and sends)
 //   join                  from all messages to Shared::g
 //   fix                   list warp, at the end: the special elements' gradients, and the row's loss
 #pragma once
@@ -168,7 +167,7 @@ struct Gradient {
 template <typename T, typename Op, bool kAligned>
 __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
-    constexpr int kMessages = kSumWarps * (Op::kListMessage ? 2 : 1);
+    constexpr int kMessages = kSumWarps;
     constexpr bool moments = Op::kMoments;
     extern __shared__ __align__(128) uint4 ring[];
     __shared__ typename Op::Shared lists[kLists];
@@ -225,7 +224,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                 const int chunks = chunks_of(s);
                 const f32x2 scale = pack2(p.scale, p.scale);
                 typename Op::Shared& sh = lists[li];
-                typename Op::Extra extra;
                 float m = -INFINITY;
                 f32x2 sum = 0, moment = 0;
                 bool patched = false;  // a bulk copy may only write there again after a fence
@@ -235,23 +233,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                 for (int c = worker; c < chunks; c += kSumWarps) {
                     const uint32_t slot = (n + c) % kSlots;
                     if (!wait_item(full, n + c, kSlots)) return;
-                    const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
-                    if (begin < end) {
-                        T* first = reinterpret_cast<T*>(ring + slot * kChunk) - (s.origin() + c * (kChunk * kVec));
-#pragma unroll 1
-                        for (int i = begin + lane; i < end; i += 32) {
-                            const int k = order[li][i];
-                            const float z = load_rw(first + sh.pos[k]);
-                            sh.z[k] = z;
-                            extra.take(p, sh, k, z);
-                        }
-                        if constexpr (Op::kMask) {
-                            __syncwarp();
+                    if constexpr (Op::kMask) {
+                        const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
+                        if (begin < end) {
+                            T* first = reinterpret_cast<T*>(ring + slot * kChunk) - (s.origin() + c * (kChunk * kVec));
 #pragma unroll 1
                             for (int i = begin + lane; i < end; i += 32) first[sh.pos[order[li][i]]] = masked<T>();
                             patched = true;
+                            __syncwarp();
                         }
-                        __syncwarp();
                     }
                     const uint4* data = ring + slot * kChunk + lane;
                     const int count = min(kChunk, s.count - c * kChunk) - lane;
@@ -308,11 +298,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                     msg.z = warp_reduce<float, add_op>(msg.z);
                 }
                 msg.y = warp_reduce<float, add_op>(msg.y);
-                float4 list;
-                if constexpr (Op::kListMessage) list = extra.message(p, msg);
                 if (!may_send(u)) return;
                 send(u, worker, msg);
-                if constexpr (Op::kListMessage) send(u, kSumWarps + worker, list);
                 ++u;
             }
             __syncwarp();
@@ -494,7 +481,8 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
     const int64_t mine = row0 + static_cast<int64_t>(turn) * row_step, mine_step = kListWarps * row_step;
     uint32_t oldest = turn;  // not retired
     bool ok = true;
-    typename Op::Fetched next = Op::fetch(p, mine);
+    typename Op::Fetched next = Op::fetch(p, mine), later = Op::fetch(p, mine + mine_step);
+    Op::template gather<T>(p, mine, next);
 #pragma unroll 1
     for (int64_t r = mine; r < p.rows; r += mine_step, turn += kListWarps) {
         const int li = turn % kLists;
@@ -505,41 +493,45 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
             oldest += kListWarps;
         }
         const typename Op::Fetched now = next;
-        next = Op::fetch(p, r + mine_step);
+        next = later;
+        Op::template gather<T>(p, r + mine_step, next);
+        later = Op::fetch(p, r + 2 * mine_step);
         const bool want = Op::wanted(p, now);
         if (want) {
             Op::begin(p, sh, now);
-            // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
-            const Slice<T> s = slice_of(r);
-            chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
-            __syncwarp();
-            int in[Op::kMine], place[Op::kMine];
-#pragma unroll
-            for (int i = 0; i < Op::kMine; ++i) {
-                const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
-                in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
-                place[i] = 0;
-                if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
-                const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
-                if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
+            if constexpr (Op::kMask) {
+                // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
+                const Slice<T> s = slice_of(r);
+                chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
                 __syncwarp();
-                if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
+                int in[Op::kMine], place[Op::kMine];
+#pragma unroll
+                for (int i = 0; i < Op::kMine; ++i) {
+                    const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
+                    in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
+                    place[i] = 0;
+                    if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
+                    const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
+                    if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
+                    __syncwarp();
+                    if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
+                    __syncwarp();
+                }
+                int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
+#pragma unroll
+                for (int o = 1; o < 32; o *= 2) {
+                    const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
+                    if (lane >= o) a += up, b += up2;
+                }
+                b += __shfl_sync(0xffffffffu, a, 31);
                 __syncwarp();
-            }
-            int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
+                chunk_begin[li][lane] = static_cast<uint8_t>(a);
+                chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
+                __syncwarp();
 #pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
-                if (lane >= o) a += up, b += up2;
+                for (int i = 0; i < Op::kMine; ++i)
+                    if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
             }
-            b += __shfl_sync(0xffffffffu, a, 31);
-            __syncwarp();
-            chunk_begin[li][lane] = static_cast<uint8_t>(a);
-            chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < Op::kMine; ++i)
-                if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
         }
         if (lane == 0) wanted[li] = want;
         __syncwarp();
@@ -561,10 +553,10 @@ constexpr int kSmallVectors = 8;  // of a thread
 template <typename T, int NT, typename Op, bool kAligned>
 __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const typename Op::Params p, const int32_t per_cta) {
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
-    constexpr int kWarps = NT / 32, kMessages = Op::kListMessage ? 2 : 1;
+    constexpr int kWarps = NT / 32;
     constexpr bool moments = Op::kMoments;
     __shared__ typename Op::Shared sh;
-    __shared__ __align__(16) float4 inbox[kMaxCluster * kMessages];
+    __shared__ __align__(16) float4 inbox[kMaxCluster];
     __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWarps][32];
     __shared__ float4 warp_sums[kWarps];
     __shared__ float warp_max[kWarps];
@@ -588,17 +580,13 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
     }
     if (Op::kMask)
         for (int i = tid; i < NT * kSmallVectors / 4; i += NT) reinterpret_cast<uint32_t*>(special)[i] = 0;
-    typename Op::Extra extra;
     if (warp == 0) {
-        const typename Op::Fetched now = Op::fetch(p, r);
+        typename Op::Fetched now = Op::fetch(p, r);
+        Op::template gather<T>(p, r, now);
         const bool wanted = Op::wanted(p, now);
-        if (wanted) {
-            Op::begin(p, sh, now);
-#pragma unroll 1
-            for (int k = lane; k < Op::entries(p); k += 32)
-                if (s.holds(sh.pos[k])) sh.z[k] = load_rw(row + sh.pos[k]);
-        }
+        if (wanted) Op::begin(p, sh, now);
         if (lane == 0) want = wanted;
+        __syncwarp();
     }
     typename Lanes<T>::Max top;
 #pragma unroll
@@ -626,7 +614,6 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
                 if (s.holds(sh.pos[k])) {
                     const int at = sh.pos[k] - s.origin(), bit = at / kVec * 8 + at % kVec;
                     atomicOr(reinterpret_cast<uint32_t*>(special) + bit / 32, 1u << bit % 32);
-                    extra.take(p, sh, k, sh.z[k]);
                 }
         __syncthreads();
     }
@@ -660,19 +647,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
         x = warp_sums[0];
 #pragma unroll
         for (int w = 1; w < kWarps; ++w) x.y += warp_sums[w].y, x.z += warp_sums[w].z;
-        float4 list = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if constexpr (Op::kListMessage) list = extra.message(p, x);
         if (ctas == 1) {
-            if (lane == 0) {
-                inbox[0] = x;
-                if (Op::kListMessage) inbox[1] = list;
-            }
+            if (lane == 0) inbox[0] = x;
         } else {
             cluster_wait();
-            if (lane < static_cast<int>(ctas)) {
-                store_remote(&inbox[rank * kMessages], lane, x);
-                if (Op::kListMessage) store_remote(&inbox[rank * kMessages + 1], lane, list);
-            }
+            if (lane < static_cast<int>(ctas)) store_remote(&inbox[rank], lane, x);
         }
         __syncwarp();
     }
