@@ -28,7 +28,7 @@ __device__ __noinline__ double log64(double x) { return log(x); }
 
 struct Distill {
     using Params = DistillParams;
-    static constexpr bool kMoments = false, kMask = true;
+    static constexpr bool kMoments = false, kMask = true, kAlone = true;  // kAlone: it may be called without a gradient to write
     static constexpr int kMine = QN_TOP_MAX / 32;  // entries of the list a lane
     struct Shared {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token

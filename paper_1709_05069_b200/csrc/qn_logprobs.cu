@@ -429,7 +429,7 @@ template <bool kEntropy>
 struct Backward {
     using Params = BackwardParams;
     static constexpr bool kMoments = kEntropy;
-    static constexpr bool kMask = false;
+    static constexpr bool kMask = false, kAlone = false;  // kAlone: it may be called without a gradient to write
     struct Shared {
         int32_t pos[QN_TOP_MAX + 1];  // sparse terms: 0 the given token, 1..k the alternatives; -1 for none
         float add[QN_TOP_MAX + 1], z[QN_TOP_MAX + 1];

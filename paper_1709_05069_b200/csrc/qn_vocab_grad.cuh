@@ -38,10 +38,15 @@ namespace {
 constexpr int kMaxCluster = 8;
 constexpr int kChunk = 256;      // vectors in a chunk
 constexpr int kSlots = 48;       // chunks in the ring
-constexpr int kSumWarps = 11, kWriteWarps = 12;
 constexpr int kListWarps = 3;
 constexpr int kLists = 2 * kListWarps;  // rows between the list warps' beginning and end of them
-constexpr int kGradThreads = 32 * (kSumWarps + kWriteWarps + 2 + kListWarps);
+// Warps that sum and that write.  Measured for 4096 x 131072 bf16 with a list of 64
+// tokens, us: 8 / 8 468, 10 / 13 449, 11 / 12 440 (28 warps are the most that leave 72 registers for each).
+template <bool kWrite>
+struct Roles {
+    static constexpr int kSum = 11, kWriting = kWrite ? 12 : 0;  // the same sums, to the bit, with and without a gradient
+    static constexpr int kThreads = 32 * (kSum + kWriting + 2 + kListWarps);
+};
 
 // ---- clusters ------------------------------------------------------------------------------------------------------
 
@@ -163,16 +168,48 @@ struct Gradient {
     float on, unit;
 };
 
+// Elements [begin, end) of a row, as far as they are in [0, vocab), from 16-byte aligned shared memory to an output that is
+// not aligned as they are, by one warp: 16-byte stores, put together from 4-byte pieces.
+template <typename T>
+__device__ __forceinline__ void write_run(T* out, int32_t begin, int32_t end, int32_t vocab, const T* from) {
+    constexpr int kVec = Storage<T>::kVec;
+    const int lane = threadIdx.x & 31;
+    const int32_t lo = max(0, begin), hi = min(vocab, end);
+    const int32_t head = min(hi - lo, static_cast<int32_t>((16 - (reinterpret_cast<uintptr_t>(out + lo) & 15)) / sizeof(T)) % kVec);
+    const int32_t first = lo + head, vectors = (hi - first) / kVec;
+    const int32_t skip = first - begin;  // elements of `from` before the first vector
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(from) + (sizeof(T) == 4 ? skip : skip / 2);
+    const bool odd = sizeof(T) == 2 && skip % 2;
+    if (lane < head) out[lo + lane] = from[lo - begin + lane];
+#pragma unroll 2
+    for (int j = lane; j < vectors; j += 32) {
+        uint32_t w[5];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = words[4 * j + i];
+        if (odd) {
+            w[4] = words[4 * j + 4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+        }
+        stg_stream16(out + first + j * kVec, make_uint4(w[0], w[1], w[2], w[3]));
+    }
+    const int32_t tail = first + vectors * kVec + lane;
+    if (tail < hi) out[tail] = from[tail - begin];
+}
+
 // kAligned: every row of the gradient starts as far from a 16-byte boundary as its row of logits.
-template <typename T, typename Op, bool kAligned>
-__global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
+// kEdges: rows may start or end elsewhere than on 16 bytes.
+template <typename T, typename Op, bool kAligned, bool kEdges, bool kWrite>
+__global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
+    row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
+    constexpr int kSumWarps = Roles<kWrite>::kSum, kWriteWarps = Roles<kWrite>::kWriting;
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
     constexpr int kMessages = kSumWarps;
     constexpr bool moments = Op::kMoments;
     extern __shared__ __align__(128) uint4 ring[];
     __shared__ typename Op::Shared lists[kLists];
     __shared__ __align__(16) float4 inbox[kLists][kMaxCluster * kMessages];
-    __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWriteWarps][32];
+    __shared__ __align__(16) uint4 edges[kLists][2];  // a slice's first and last vector, where they reach past the row
     // a row's special elements in the order of their chunks, and where each chunk's begin
     __shared__ uint8_t order[kLists][QN_TOP_MAX + 32], chunk_begin[kLists][64];
     // full: a chunk has arrived; empty: it has been written.  By row: ready: begun; done: summed and written.  By row that is
@@ -223,6 +260,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                 const Slice<T> s = slice_of(r);
                 const int chunks = chunks_of(s);
                 const f32x2 scale = pack2(p.scale, p.scale);
+                const int32_t fb = s.full_begin(), fe = s.full_end();
                 typename Op::Shared& sh = lists[li];
                 float m = -INFINITY;
                 f32x2 sum = 0, moment = 0;
@@ -248,12 +286,15 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
 #pragma unroll 1
                     for (int j = 0; j < kChunk; j += 128, data += 128) {
                         uint4 v[4];
-                        if (count + lane == kChunk) {
+                        if (c * kChunk >= fb && (c + 1) * kChunk <= fe) {
 #pragma unroll
                             for (int q = 0; q < 4; ++q) v[q] = data[32 * q];
                         } else {
 #pragma unroll
-                            for (int q = 0; q < 4; ++q) v[q] = j + 32 * q < count ? data[32 * q] : Lanes<T>::masked4();
+                            for (int q = 0; q < 4; ++q) {
+                                const int k = c * kChunk + j + 32 * q + lane;
+                                v[q] = j + 32 * q >= count ? Lanes<T>::masked4() : kEdges && k < fb ? edges[li][0] : kEdges && k >= fe ? edges[li][1] : data[32 * q];
+                            }
                         }
                         typename Lanes<T>::Max top;
 #pragma unroll
@@ -277,7 +318,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                                 if constexpr (moments) moment = fma2(e, finite_pair(d), moment);
                             }
                     }
-                    if (!p.dlogits) {  // nobody else needs the chunk
+                    if (!kWrite) {  // nobody else needs the chunk
                         if (patched) fence_async();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(&empty[slot]);
@@ -307,7 +348,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
         }
         return;
     }
-    if (warp < kSumWarps + kWriteWarps) {
+    if constexpr (kWrite) if (warp < kSumWarps + kWriteWarps) {
         constexpr int NT = 32 * kWriteWarps;
         const int w = warp - kSumWarps, tid = threadIdx.x - 32 * kSumWarps;
 #pragma unroll 1
@@ -316,14 +357,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
             bool ok = wait_item(ready, turn, kLists);
             if (ok && wanted[li]) ok = wait_item(joined, u, kLists);
             if (!ok) {  // a wait ran out: what is left becomes NaN
-                if (p.dlogits)
 #pragma unroll 1
                     for (; r < p.rows; r += row_step) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
                 return;
             }
             const Slice<T> s = slice_of(r);
             if (!wanted[li]) {
-                if (p.dlogits) write_constant<T, NT>(out_of(r), s, tid, 0.0f);
+                write_constant<T, NT>(out_of(r), s, tid, 0.0f);
             } else {
                 ++u;
                 const int chunks = chunks_of(s);
@@ -355,23 +395,36 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
 #pragma unroll
                                 for (int h = 0; h < 4; ++h) stg_stream16(to + 32 * kVec * h, gradient(data[32 * h]));
                             }
+                        } else if (!kAligned) {
+                            // the gradient in place of the chunk, and the chunk, one run of the row, from there
+                            uint4* in_place = ring + slot * kChunk + lane;
+                            const int count = min(kChunk, s.count - c * kChunk);
+                            if (c * kChunk >= fb && (c + 1) * kChunk <= fe) {
+#pragma unroll 1
+                                for (int q = 0; q < kChunk / 32; q += 4, in_place += 128) {
+#pragma unroll
+                                    for (int h = 0; h < 4; ++h) in_place[32 * h] = gradient(in_place[32 * h]);
+                                }
+                            } else {
+#pragma unroll 1
+                                for (int j = lane; j < count; j += 32, in_place += 32) {
+                                    const int k = c * kChunk + j;
+                                    *in_place = gradient(k < fb ? edges[li][0] : k >= fe ? edges[li][1] : *in_place);
+                                }
+                            }
+                            __syncwarp();
+                            write_run(out, s.origin() + c * (kChunk * kVec), s.origin() + (c * kChunk + count) * kVec, s.vocab,
+                                      reinterpret_cast<const T*>(ring + slot * kChunk));
+                            fence_async();
                         } else {
                             const int count = min(kChunk, s.count - c * kChunk);
 #pragma unroll 1
                             for (int q = 0; 32 * q < count; ++q) {
                                 const int j = 32 * q + lane, k = c * kChunk + j;
-                                const uint4 x = gradient(j < count ? data[32 * q] : Lanes<T>::masked4());
-                                if (kAligned) {
-                                    if (k >= fb && k < fe) stg_stream16(out + at + 32 * q * kVec, x);
-                                    else if (j < count) write_edge(out, at + 32 * q * kVec, s.vocab, x);
-                                } else if (k - lane >= fb && k - lane + 32 <= fe) {
-                                    __syncwarp();
-                                    stage[w][lane] = x;
-                                    __syncwarp();
-                                    write_run(out, at + (32 * q - lane) * kVec, stage[w]);
-                                } else if (j < count) {
-                                    write_edge(out, at + 32 * q * kVec, s.vocab, x);
-                                }
+                                if (j >= count) break;
+                                const uint4 x = gradient(kEdges && k < fb ? edges[li][0] : kEdges && k >= fe ? edges[li][1] : data[32 * q]);
+                                if (k >= fb && k < fe) stg_stream16(out + at + 32 * q * kVec, x);
+                                else write_edge(out, at + 32 * q * kVec, s.vocab, x);
                             }
                         }
                         __syncwarp();
@@ -406,7 +459,6 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                 const uint32_t slot = (n + c) % kSlots, parity = ((n + c) / kSlots & 1) ^ 1;
                 uint4* to = ring + slot * kChunk;
                 const int32_t j0 = c * kChunk, j1 = min(j0 + kChunk, s.count), b0 = max(j0, fb), b1 = min(j1, fe);
-                const bool edge = c < chunks && (j0 < fb || j1 > max(fe, j0));
                 uint32_t pending = __ballot_sync(0xffffffffu, c < chunks);
                 while (pending) {
                     const uint32_t first = n + c0 + __ffs(pending) - 1;  // slots come free in about this order
@@ -418,26 +470,9 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
                             mbar_expect_tx(&full[slot], bytes);
                             bulk_load(to + (b0 - j0), base + static_cast<int64_t>(b0) * kVec, bytes, &full[slot]);
                         }
-                        if (!edge) mbar_arrive(&full[slot]);
+                        mbar_arrive(&full[slot]);
                     }
                     pending &= ~__ballot_sync(0xffffffffu, mine);
-                }
-                if (edge) {  // a row's first and last vector, where they reach past it
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        const int32_t j = h == 0 ? j0 : j1 - 1;
-                        if (j >= fb && j < fe) continue;
-                        T x[kVec];
-#pragma unroll
-                        for (int e = 0; e < kVec; ++e) {
-                            const int32_t i = s.origin() + j * kVec + e;
-                            x[e] = i >= 0 && i < s.vocab ? row[i] : masked<T>();
-                        }
-#pragma unroll
-                        for (int e = 0; e < kVec; ++e) reinterpret_cast<T*>(to + (j - j0))[e] = x[e];
-                    }
-                    fence_async();
-                    mbar_arrive(&full[slot]);
                 }
                 __syncwarp();
             }
@@ -472,7 +507,7 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
         const int64_t r = row0 + static_cast<int64_t>(t) * row_step;
         const int li = t % kLists;
         if (!wait_item(done, t, kLists)) return false;
-        if (wanted[li]) Op::template fix<T>(p, lists[li], slice_of(r), p.dlogits ? out_of(r) : nullptr, r, rank == 0);
+        if (wanted[li]) Op::template fix<T>(p, lists[li], slice_of(r), kWrite ? out_of(r) : nullptr, r, rank == 0);
         else if (rank == 0 && lane == 0) Op::without(p, r, 0.0f);
         __syncwarp();
         return true;
@@ -483,6 +518,14 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
     bool ok = true;
     typename Op::Fetched next = Op::fetch(p, mine), later = Op::fetch(p, mine + mine_step);
     Op::template gather<T>(p, mine, next);
+    // an element of the first or last vector of a slice, where that reaches past the row
+    auto edge_of = [&](int64_t r) {
+        if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
+        const Slice<T> s = slice_of(r);
+        const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
+        return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
+    };
+    T edge = edge_of(mine);
 #pragma unroll 1
     for (int64_t r = mine; r < p.rows; r += mine_step, turn += kListWarps) {
         const int li = turn % kLists;
@@ -496,9 +539,12 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
         next = later;
         Op::template gather<T>(p, r + mine_step, next);
         later = Op::fetch(p, r + 2 * mine_step);
+        const T edge_now = edge;
+        edge = edge_of(r + mine_step);
         const bool want = Op::wanted(p, now);
         if (want) {
             Op::begin(p, sh, now);
+            if (kEdges && lane < 2 * kVec) reinterpret_cast<T*>(edges[li])[lane] = edge_now;
             if constexpr (Op::kMask) {
                 // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
                 const Slice<T> s = slice_of(r);
@@ -531,6 +577,13 @@ __global__ void __launch_bounds__(kGradThreads, 1) row_gradient_kernel(const typ
 #pragma unroll
                 for (int i = 0; i < Op::kMine; ++i)
                     if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
+#pragma unroll
+                for (int i = 0; i < Op::kMine; ++i) {  // and in the edges
+                    if (!kEdges || in[i] < 0) continue;
+                    const int32_t at = sh.pos[lane + 32 * i] - s.origin(), last = at - (s.count - 1) * kVec;
+                    if (at < kVec) reinterpret_cast<T*>(edges[li])[at] = masked<T>();
+                    if (last >= 0) reinterpret_cast<T*>(edges[li])[kVec + last] = masked<T>();
+                }
             }
         }
         if (lane == 0) wanted[li] = want;
@@ -695,21 +748,21 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
 
 // ---- host ----------------------------------------------------------------------------------------------------------
 
-template <typename T, typename Op, bool kAligned>
+template <typename T, typename Op, bool kAligned, bool kEdges, bool kWrite>
 cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, cudaStream_t st) {
-    auto kernel = row_gradient_kernel<T, Op, kAligned>;
+    auto kernel = row_gradient_kernel<T, Op, kAligned, kEdges, kWrite>;
     // CTAs a row: slices of up to 128 KB, of up to 192 KB where 8 of them are not enough; where there are few rows, more and
     // smaller ones, down to a chunk for every sum warp
     constexpr int kGood = 32 * kChunk;
     int ctas = 1;
     while (ctas < kMaxCluster && (all + ctas - 1) / ctas > kGood) ++ctas;
-    while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= qn_sm_count() && all / ctas > kSumWarps * kChunk) ctas *= 2;
+    while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= qn_sm_count() && all / ctas > Roles<kWrite>::kSum * kChunk) ctas *= 2;
     const int per_cta = static_cast<int>((all + ctas - 1) / ctas);
     if (per_cta > kSlots * kChunk) return cudaErrorInvalidValue;
     constexpr int kBytes = kSlots * kChunk * 16;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(ctas);
-    cfg.blockDim = dim3(kGradThreads);
+    cfg.blockDim = dim3(Roles<kWrite>::kThreads);
     cfg.dynamicSmemBytes = kBytes;
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -735,12 +788,17 @@ cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, 
     return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(per_cta));
 }
 
+// Every row starts on 16 bytes.
+template <typename T, typename Params>
+bool rows_aligned(const Params& p) {
+    return reinterpret_cast<uintptr_t>(p.logits) % 16 == 0 && (p.rows == 1 || p.row_stride % Storage<T>::kVec == 0);
+}
+
 // Vectors that a row may span, whatever its alignment.
 template <typename T, typename Params>
 int64_t row_vectors(const Params& p) {
     constexpr int kVec = Storage<T>::kVec;
-    const bool aligned = reinterpret_cast<uintptr_t>(p.logits) % 16 == 0 && (p.rows == 1 || p.row_stride % kVec == 0);
-    return (static_cast<int64_t>(p.vocab) + (aligned ? kVec - 1 : 2 * kVec - 2)) / kVec;
+    return (static_cast<int64_t>(p.vocab) + (rows_aligned<T>(p) ? kVec - 1 : 2 * kVec - 2)) / kVec;
 }
 
 template <typename T, int NT, typename Op, bool kAligned>
@@ -770,7 +828,22 @@ cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t s
     // one row of 8192: 5 / 9.  So: all logits more than 64 MB, in rows of more than 32 KB.
     const int64_t bytes = p.vocab * static_cast<int64_t>(sizeof(T));
     if (ctas > kMaxCluster || (bytes > (32 << 10) && p.rows > (64 << 20) / bytes))
-        return launch_gradient_pipeline<T, Op, kAligned>(p, all, st);
+    {
+        // rows that start and end on 16 bytes have no vectors that reach past them
+        const bool edges = !rows_aligned<T>(p) || p.vocab % Storage<T>::kVec != 0;
+        if constexpr (!Op::kAlone) {
+            if (!kAligned) return launch_gradient_pipeline<T, Op, false, true, true>(p, all, st);
+            return edges ? launch_gradient_pipeline<T, Op, true, true, true>(p, all, st)
+                         : launch_gradient_pipeline<T, Op, true, false, true>(p, all, st);
+        } else {
+            if (!p.dlogits)
+                return edges ? launch_gradient_pipeline<T, Op, true, true, false>(p, all, st)
+                             : launch_gradient_pipeline<T, Op, true, false, false>(p, all, st);
+            if (!kAligned) return launch_gradient_pipeline<T, Op, false, true, true>(p, all, st);
+            return edges ? launch_gradient_pipeline<T, Op, true, true, true>(p, all, st)
+                         : launch_gradient_pipeline<T, Op, true, false, true>(p, all, st);
+        }
+    }
     // few rows: more CTAs, down to a vector a thread; many: no more threads than a row has work for
     while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= 2 * qn_sm_count() && all > ctas * 256) ctas *= 2;
     const bool many = p.rows * ctas > 4 * qn_sm_count();
