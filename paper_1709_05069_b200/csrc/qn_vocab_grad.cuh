@@ -7,14 +7,14 @@
 //
 // There is one CTA on an SM, it stays, and its warps are stages of a pipeline over chunks of 4 KB in a ring of 48:
 //   list warps     a row each: read the few elements of it that are special (a given token, alternatives, a teacher's list),
-//                  work out what depends on them alone, and sort those by chunk that must not be added; when the row has been
-//                  written, write their gradients
+//                  work out what depends on them alone, and sort those by chunk that must not be added
 //   copy warp      brings the slices of the coming rows in
 //   sum warps      a chunk each: take out what must not be added, and add e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative to a running maximum m of each thread; at the end of a
 //                  slice each sends its maximum and sums to every CTA of the cluster (asynchronous stores into shared
 //                  memory that count on a barrier there)
 //   join warp      from all messages, in the same order in every CTA, to the row's coefficients
 //   write warps    a chunk each: e_i times the coefficient; give the chunk back
+//   end warp       when a row has been written, its special elements' gradients, and the row's loss
 // So HBM is read and written at the same time, and the exchange of one row passes while others are summed and written.
 // Loops are short and rolled: a form that kept the slice in registers (unrolled over them) ran out of the instruction cache.
 // exp2 is taken twice for an element: at 16 a cycle and SM that is 73 % of the time in which bf16 logits come from HBM and
@@ -28,7 +28,7 @@
 //   begin                 list warp: what depends on the special elements alone, and their places (Shared::pos)
 //   kMask                 whether the special elements leave the sums
 //   join                  from all messages to Shared::g
-//   fix                   list warp, at the end: the special elements' gradients, and the row's loss
+//   fix                   end warp: the special elements' gradients, and the row's loss
 #pragma once
 
 #include "qn_vocab.cuh"
@@ -38,14 +38,14 @@ namespace {
 constexpr int kMaxCluster = 8;
 constexpr int kChunk = 256;      // vectors in a chunk
 constexpr int kSlots = 48;       // chunks in the ring
-constexpr int kListWarps = 3;
-constexpr int kLists = 2 * kListWarps;  // rows between the list warps' beginning and end of them
+constexpr int kListWarps = 2;
+constexpr int kLists = 6;  // rows between the list warps' beginning and the end warp's end of them
 // Warps that sum and that write.  Measured for 4096 x 131072 bf16 with a list of 64
 // tokens, us: 8 / 8 468, 10 / 13 449, 11 / 12 440 (28 warps are the most that leave 72 registers for each).
 template <bool kWrite>
 struct Roles {
     static constexpr int kSum = 11, kWriting = kWrite ? 12 : 0;  // the same sums, to the bit, with and without a gradient
-    static constexpr int kThreads = 32 * (kSum + kWriting + 2 + kListWarps);
+    static constexpr int kThreads = 32 * (kSum + kWriting + 3 + kListWarps);
 };
 
 // ---- clusters ------------------------------------------------------------------------------------------------------
@@ -197,11 +197,27 @@ __device__ __forceinline__ void write_run(T* out, int32_t begin, int32_t end, in
     if (tail < hi) out[tail] = from[tail - begin];
 }
 
+// The rows of a cluster.  In every turn the n clusters take the next n rows, moved on by `rotation` (< n) from the last turn,
+// so that one of them goes through the rows in a stride without small factors: padding at every s-th row then falls to all
+// clusters alike.
+struct Walk {
+    int64_t base;
+    uint32_t at, n, rotation;
+    __device__ __forceinline__ int64_t row() const { return base + at; }
+    __device__ __forceinline__ void next(int turns = 1) {
+        for (int t = 0; t < turns; ++t) {
+            base += n;
+            at += rotation;
+            if (at >= n) at -= n;
+        }
+    }
+};
+
 // kAligned: every row of the gradient starts as far from a 16-byte boundary as its row of logits.
 // kEdges: rows may start or end elsewhere than on 16 bytes.
 template <typename T, typename Op, bool kAligned, bool kEdges, bool kWrite>
 __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
-    row_gradient_kernel(const typename Op::Params p, const int32_t per_cta) {
+    row_gradient_kernel(const typename Op::Params p, const int32_t per_cta, const uint32_t rotation) {
     constexpr int kSumWarps = Roles<kWrite>::kSum, kWriteWarps = Roles<kWrite>::kWriting;
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
     constexpr int kMessages = kSumWarps;
@@ -212,9 +228,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     __shared__ __align__(16) uint4 edges[kLists][2];  // a slice's first and last vector, where they reach past the row
     // a row's special elements in the order of their chunks, and where each chunk's begin
     __shared__ uint8_t order[kLists][QN_TOP_MAX + 32], chunk_begin[kLists][64];
-    // full: a chunk has arrived; empty: it has been written.  By row: ready: begun; done: summed and written.  By row that is
-    // wanted: heard: all messages; joined: coefficients
-    __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists];
+    // full: a chunk has arrived; empty: it has been written.  By row: ready: begun; done: summed and written.  retired: its
+    // special elements too.  By row that is wanted: heard: all messages; joined: coefficients
+    __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists], retired[kLists];
     __shared__ bool wanted[kLists];
     __shared__ int abort;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
@@ -225,14 +241,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         for (int i = 0; i < kSlots; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
 #pragma unroll 1
         for (int i = 0; i < kLists; ++i) {
-            mbar_init(&ready[i], 1), mbar_init(&done[i], kSumWarps + kWriteWarps + 2);
+            mbar_init(&ready[i], 1), mbar_init(&done[i], kSumWarps + kWriteWarps + 2), mbar_init(&retired[i], 1);
             mbar_init(&heard[i], 1), mbar_init(&joined[i], 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     __syncthreads();
     if (ctas > 1) cluster_sync();  // every CTA's barriers are there before the first store into it
-    const int64_t row0 = blockIdx.x / ctas, row_step = gridDim.x / ctas;
+    const Walk walk{0, blockIdx.x / ctas, gridDim.x / ctas, rotation};
     auto row_of = [&](int64_t r) { return static_cast<const T*>(p.logits) + r * p.row_stride; };
     auto out_of = [&](int64_t r) { return static_cast<T*>(p.dlogits) + r * p.dlogits_stride; };
     auto slice_of = [&](int64_t r) { return Slice<T>(row_of(r), p.vocab, per_cta, rank); };
@@ -252,8 +268,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     uint32_t turn = 0;  // rows so far
     uint32_t u = 0;     // wanted rows so far
     if (warp < kSumWarps) {
+        Walk rows = walk;
 #pragma unroll 1
-        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+        for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
             if (!wait_item(ready, turn, kLists)) return;
             if (wanted[li]) {
@@ -351,14 +368,15 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     if constexpr (kWrite) if (warp < kSumWarps + kWriteWarps) {
         constexpr int NT = 32 * kWriteWarps;
         const int w = warp - kSumWarps, tid = threadIdx.x - 32 * kSumWarps;
+        Walk rows = walk;
 #pragma unroll 1
-        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+        for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
             bool ok = wait_item(ready, turn, kLists);
             if (ok && wanted[li]) ok = wait_item(joined, u, kLists);
             if (!ok) {  // a wait ran out: what is left becomes NaN
 #pragma unroll 1
-                    for (; r < p.rows; r += row_step) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
+                for (; (r = rows.row()) < p.rows; rows.next()) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
                 return;
             }
             const Slice<T> s = slice_of(r);
@@ -440,8 +458,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     }
     if (warp == kSumWarps + kWriteWarps) {
         // ---- copy warp
+        Walk rows = walk;
 #pragma unroll 1
-        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+        for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             if (!wait_item(ready, turn, kLists)) return;
             const bool want = wanted[turn % kLists];
             __syncwarp();
@@ -482,8 +501,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     }
     if (warp == kSumWarps + kWriteWarps + 1) {
         // ---- join warp
+        Walk rows = walk;
 #pragma unroll 1
-        for (int64_t r = row0; r < p.rows; r += row_step, ++turn) {
+        for (; rows.row() < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
             if (!wait_item(ready, turn, kLists)) return;
             if (wanted[li]) {
@@ -501,23 +521,31 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         }
         return;
     }
+    if (warp == kSumWarps + kWriteWarps + 2) {
+        // ---- end warp: what is left to do of a row once the others are through with it
+        Walk rows = walk;
+#pragma unroll 1
+        for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
+            const int li = turn % kLists;
+            if (!wait_item(done, turn, kLists)) break;
+            if (wanted[li]) Op::template fix<T>(p, lists[li], slice_of(r), kWrite ? out_of(r) : nullptr, r, rank == 0);
+            else if (rank == 0 && lane == 0) Op::without(p, r, 0.0f);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&retired[li]);
+        }
+        if (rank == 0 && lane == 0)  // a wait ran out, if any rows are left
+#pragma unroll 1
+            for (; rows.row() < p.rows; rows.next()) Op::without(p, rows.row(), NAN);
+        return;
+    }
     // ---- list warps
-    // what is left to do of a row once the others are through with it
-    auto retire = [&](uint32_t t) {
-        const int64_t r = row0 + static_cast<int64_t>(t) * row_step;
-        const int li = t % kLists;
-        if (!wait_item(done, t, kLists)) return false;
-        if (wanted[li]) Op::template fix<T>(p, lists[li], slice_of(r), kWrite ? out_of(r) : nullptr, r, rank == 0);
-        else if (rank == 0 && lane == 0) Op::without(p, r, 0.0f);
-        __syncwarp();
-        return true;
-    };
-    turn = warp - (kSumWarps + kWriteWarps + 2);
-    const int64_t mine = row0 + static_cast<int64_t>(turn) * row_step, mine_step = kListWarps * row_step;
-    uint32_t oldest = turn;  // not retired
-    bool ok = true;
-    typename Op::Fetched next = Op::fetch(p, mine), later = Op::fetch(p, mine + mine_step);
-    Op::template gather<T>(p, mine, next);
+    turn = warp - (kSumWarps + kWriteWarps + 3);
+    Walk rows = walk;
+    rows.next(turn);
+    Walk ahead = rows;
+    ahead.next(kListWarps);
+    typename Op::Fetched next = Op::fetch(p, rows.row()), later = Op::fetch(p, ahead.row());
+    Op::template gather<T>(p, rows.row(), next);
     // an element of the first or last vector of a slice, where that reaches past the row
     auto edge_of = [&](int64_t r) {
         if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
@@ -525,22 +553,20 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
         return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
     };
-    T edge = edge_of(mine);
+    T edge = edge_of(rows.row());
 #pragma unroll 1
-    for (int64_t r = mine; r < p.rows; r += mine_step, turn += kListWarps) {
+    for (int64_t r; (r = rows.row()) < p.rows; rows.next(kListWarps), turn += kListWarps) {
         const int li = turn % kLists;
         typename Op::Shared& sh = lists[li];
-        if (turn >= kLists) {
-            ok = retire(oldest);
-            if (!ok) break;
-            oldest += kListWarps;
-        }
+        if (turn >= kLists && !wait_item(retired, turn - kLists, kLists)) return;
         const typename Op::Fetched now = next;
         next = later;
-        Op::template gather<T>(p, r + mine_step, next);
-        later = Op::fetch(p, r + 2 * mine_step);
+        const int64_t following = ahead.row();
+        ahead.next(kListWarps);
+        Op::template gather<T>(p, following, next);
+        later = Op::fetch(p, ahead.row());
         const T edge_now = edge;
-        edge = edge_of(r + mine_step);
+        edge = edge_of(following);
         const bool want = Op::wanted(p, now);
         if (want) {
             Op::begin(p, sh, now);
@@ -590,11 +616,6 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&ready[li]);
     }
-#pragma unroll 1
-    for (; oldest < turn && ok; oldest += kListWarps) ok = retire(oldest);
-    if (!ok && rank == 0 && lane == 0)  // a wait ran out
-#pragma unroll 1
-        for (int64_t r = row0 + static_cast<int64_t>(oldest) * row_step; r < p.rows; r += mine_step) Op::without(p, r, NAN);
 }
 
 // ---- small problems --------------------------------------------------------------------------------------------------
@@ -751,9 +772,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
 template <typename T, typename Op, bool kAligned, bool kEdges, bool kWrite>
 cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, cudaStream_t st) {
     auto kernel = row_gradient_kernel<T, Op, kAligned, kEdges, kWrite>;
-    // CTAs a row: slices of up to 128 KB, of up to 192 KB where 8 of them are not enough; where there are few rows, more and
-    // smaller ones, down to a chunk for every sum warp
-    constexpr int kGood = 32 * kChunk;
+    // CTAs a row: slices of up to 128 KB (80 KB of rows that are not aligned), of up to 192 KB where 8 of them are not enough;
+    // where there are few rows, more and smaller ones, down to a chunk for every sum warp.  Measured with slices of up to 128,
+    // 96 and 72 KB, us: 4096 x 131072 bf16 386, 400, 417; 2047 x 100003 bf16 175, 160, 160 (156 with 80).
+    constexpr int kGood = (kEdges ? 20 : 32) * kChunk;
     int ctas = 1;
     while (ctas < kMaxCluster && (all + ctas - 1) / ctas > kGood) ++ctas;
     while (2 * ctas <= kMaxCluster && p.rows * 2 * ctas <= qn_sm_count() && all / ctas > Roles<kWrite>::kSum * kChunk) ctas *= 2;
@@ -785,7 +807,9 @@ cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, 
         clusters = found;
     }
     cfg.gridDim = dim3(static_cast<unsigned>((p.rows < clusters ? p.rows : clusters) * ctas));
-    return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(per_cta));
+    uint32_t stride = static_cast<uint32_t>(clusters);
+    while (stride % 2 == 0 || stride % 3 == 0 || stride % 5 == 0 || stride % 7 == 0) ++stride;
+    return cudaLaunchKernelEx(&cfg, kernel, p, static_cast<int32_t>(per_cta), (stride - static_cast<uint32_t>(clusters)) % static_cast<uint32_t>(clusters));
 }
 
 // Every row starts on 16 bytes.
