@@ -1,7 +1,8 @@
 // qn_logprobs and qn_logprobs_backward: log probabilities over a vocabulary and their gradient.
 //
 // Forward: one pass over the row by a CTA (or, where there are few rows, by a cluster of up to 8 whose results its first
-// CTA joins), 256 threads with 16-byte loads straight to registers, two batches of four ahead of their use.  Each thread
+// CTA joins), 256 threads with 16-byte loads straight to registers, a batch of four ahead of its use, and four CTAs on an SM
+// (8192 x 131072 bf16 with 64 alternatives: 461 us; two batches ahead and three CTAs 519, none and five 471).  Each thread
 // keeps a running maximum m, S = sum e_i and E = sum e_i d_i with d_i = (z_i - m) log2(e) / T and e_i = 2^d_i; z - m is
 // formed before the scale, so that large logits lose nothing to the product's rounding.  At the end
 // lse = m / T + ln S, H = ln S - ln 2 E / S.
@@ -73,18 +74,21 @@ __device__ __forceinline__ uint4 load_vector(const T* row, const Slice<T>& s, in
     return j < s.count ? load_edge(row, at, s.vocab) : Lanes<T>::masked4();
 }
 
-// Gives the k largest of n keys (0 is none; the others are distinct) to `put(place, key)`, and 0 for the places that are
-// left.  All threads, after a barrier.
+// Gives the k largest of n distinct keys to `put(place, key)`, and 0 for the places that are left.  All threads, after a
+// barrier.
 template <typename Put>
 __device__ __forceinline__ void rank_keys(const uint64_t* key, int n, int k, Put put) {
 #pragma unroll 1
     for (int i = threadIdx.x; i < n || i < k; i += kThreads) {
-        const uint64_t mine = i < n ? key[i] : 0;
-        int above = 0, any = 0;
+        if (i < n) {
+            const uint64_t mine = key[i];
+            int above = 0;
 #pragma unroll 4
-        for (int j = 0; j < n; ++j) above += key[j] > mine, any += key[j] != 0;
-        if (mine != 0 && above < k) put(above, mine);
-        if (i >= any && i < k) put(i, 0);
+            for (int j = 0; j < n; ++j) above += key[j] > mine;
+            if (above < k) put(above, mine);
+        } else {
+            put(i, 0);
+        }
     }
 }
 
@@ -148,7 +152,7 @@ __device__ __noinline__ uint32_t search_bound(uint32_t mine, int k) {
 }
 
 template <typename T, bool kTop>
-__global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobParams p) {
+__global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobParams p) {
     constexpr int kVec = Storage<T>::kVec, kPairs = kVec / 2;
     extern __shared__ __align__(16) unsigned char shared_bytes[];
     LogprobShared& sh = *reinterpret_cast<LogprobShared*>(shared_bytes);
@@ -220,19 +224,15 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
                     moment = fma2(e, d, moment);
                 }
         };
-        uint4 a[kBatch], b[kBatch], c[kBatch];
+        uint4 a[kBatch], b[kBatch];
         if (batches > 0) load(0, a);
-        if (batches > 1) load(1, b);
 #pragma unroll 1
-        for (int i = 0; i < batches; i += 3) {
-            if (i + 2 < batches) load(i + 2, c);
+        for (int i = 0; i < batches; i += 2) {
+            if (i + 1 < batches) load(i + 1, b);
             take(a);
             if (i + 1 >= batches) break;
-            if (i + 3 < batches) load(i + 3, a);
+            if (i + 2 < batches) load(i + 2, a);
             take(b);
-            if (i + 2 >= batches) break;
-            if (i + 4 < batches) load(i + 4, b);
-            take(c);
         }
         if (kTop && left != per_group) sh.group_max[group++][tid] = group_top;
         // elements outside the slice were counted at the floor: in a slice with anything above it they are 0
@@ -352,8 +352,23 @@ __global__ void __launch_bounds__(kThreads, 3) logprobs_kernel(const LogprobPara
                 part.y += f * x.y;
                 if (f != 0.0f) part.z += f * fmaf(x.y, d, x.z);
             }
-            found = sh.best;
-            n = ctas * p.k;
+            if (kTop) {
+                // a bound of the k-th largest of all: the largest of the CTAs' k-th; or, as together they have k that large,
+                // the smallest of their (k / CTAs)-th
+                const int share = (p.k + ctas - 1) / ctas;
+                uint64_t low = ~0ull, high = 1;
+                for (uint32_t q = 0; q < ctas; ++q) {
+                    low = min(low, sh.best[q * p.k + share - 1]);
+                    high = max(high, sh.best[q * p.k + p.k - 1]);
+                }
+                const uint64_t bound = max(low, high);
+                if (tid == 0) sh.count = 0;
+                __syncthreads();
+                for (int i = tid; i < p.k * static_cast<int>(ctas); i += kThreads)
+                    if (sh.best[i] >= bound) sh.candidate[atomicAdd(&sh.count, 1)] = sh.best[i];
+                __syncthreads();
+                n = sh.count;
+            }
         }
         const bool bad = part.x == INFINITY, empty = part.x == -INFINITY;
         const float top = empty ? 0.0f : part.x, log_s = bad ? NAN : logf(part.y);
@@ -383,7 +398,7 @@ cudaError_t launch_logprobs(LogprobParams& p, cudaStream_t st) {
     constexpr int kVec = Storage<T>::kVec;
     const int64_t all = (static_cast<int64_t>(p.vocab) + 2 * kVec - 2) / kVec;  // vectors, whatever the alignment
     int ctas = 1;
-    while (ctas < kTopCluster && p.rows * 2 * ctas <= 3 * qn_sm_count() && all / ctas > 2 * kThreads) ctas *= 2;
+    while (ctas < kTopCluster && p.rows * 2 * ctas <= 4 * qn_sm_count() && all / ctas > 2 * kThreads) ctas *= 2;
     p.per_cta = static_cast<int32_t>((all + ctas - 1) / ctas);
     int dev = 0;
     static bool raised[64];
