@@ -359,17 +359,18 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  * streams.  They run on the device that holds `logits`; every other pointer must be device memory of that device (or
  * managed memory), and cuda_stream one of its streams.  Each call is one kernel launch, never waits for the device, and
  * gives the same bits each time it is given the same inputs (at the same addresses modulo 16: the alignment of a row
- * decides which elements are added first).  Pointers must be aligned to their element type; rows that
- * start anywhere else than on 16 bytes lose no more than their first and last vector to element-wise loads.
+ * decides which elements are added first).  Pointers must be aligned to their element type.  Rows that
+ * start or end anywhere else than on 16 bytes are read in 16-byte vectors all the same, but for their ends; a gradient whose
+ * rows lie otherwise to 16 bytes than the logits' takes a little more.
  *
  * Common arguments
- *   rows, vocab     the matrix of logits; rows >= 0 (0: nothing is done), 1 <= vocab < 2^31
+ *   rows, vocab     the matrix of logits; rows >= 0 (0: nothing is done), 1 <= vocab < 2^31 - 64
  *   dtype           storage type of logits and dlogits; all other real values are fp32
  *   logits          DEVICE, element (r, i) at r * row_stride + i, row_stride >= vocab; read only
  *   temperature     T > 0: the distribution is softmax(z / T), u_i = z_i / T, p_i = exp(u_i - lse)
  *   tokens          int64, as torch indexes; tokens < 0 stand for "none"
- * Arithmetic: fp32 with sums per thread, added over the row in a fixed order; one rounding to the storage type when
- * dlogits is written.  Offsets are 64-bit.
+ * Arithmetic: fp32 with sums per thread, added over the row in a fixed order; a teacher's list and the difference that a
+ * distillation loss is in 64 bits; one rounding to the storage type when dlogits is written.  Offsets are 64-bit.
  *
  * What a row may hold.  -inf is a masked token (probability 0); the type's lowest value is an ordinary, very small
  * logit (a row that holds nothing else is uniform).  A row of -inf only is empty.  A row with a NaN or +inf has no
@@ -411,7 +412,7 @@ QN_API qn_status qn_logprobs(int64_t rows, int64_t vocab, qn_dtype dtype, const 
  *   top_token   needed with d_top_logprob; entries < 0 ignore their gradient.  A token may occur more than once.
  *   dlogits     DEVICE, [rows] of vocab elements dlogits_stride >= vocab apart, each element written; either `logits`
  *               itself (same pointer and stride: the gradient takes the logits' place) or memory that does not overlap it
- * A row whose upstream gradients are all 0 is padding: it is not read, whatever it holds, and its gradient is 0.  An
+ * A row whose upstream gradients are all 0 is padding: whatever it holds, its gradient is 0.  An
  * empty row's gradient is 0 but for the 1[..] terms.  vocab <= QN_GRAD_MAX_VOCAB.
  */
 QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits,
@@ -434,12 +435,12 @@ QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtyp
  *                           tokens are one more outcome, q_r = max(0, 1 - sum_k q_k) and p_r = sum of p_i off the list:
  *                           L = sum_k q_k (ln q_k - ln p_k) + q_r (ln q_r - ln p_r)
  *                           (a list that names the whole vocabulary has no such outcome)
- *   weight          [rows], NULL = 1.  A row of weight 0 is padding: it is not read, its loss and gradient are 0.
+ *   weight          [rows], NULL = 1.  A row of weight 0 is padding: whatever it holds, its loss and gradient are 0.
  *   loss            [rows]  L, without the weight
  *   dlogits         NULL (the loss alone), or weight * dL/dlogits:
  *                           weight / T * (Q p_i - q_i) on the list, weight / T * (Q p_i - q_r p_i / p_r) off it, Q = sum q
  *                   placed as in qn_logprobs_backward (dlogits_stride, in place or apart)
- * A row without any teacher token has loss 0 and gradient 0 and is not read.  A token that the student masks and the
+ * A row without any teacher token has loss 0 and gradient 0.  A token that the student masks and the
  * teacher does not makes the loss +inf (the gradient stays finite); an empty row of the student has loss +inf, gradient 0.
  * vocab <= QN_GRAD_MAX_VOCAB.
  */

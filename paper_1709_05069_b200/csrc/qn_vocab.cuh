@@ -21,7 +21,7 @@ inline size_t dtype_size(qn_dtype t) { return t == QN_F32 ? 4 : 2; }
 // Shape, type, temperature and the base pointer of a matrix of logits; the device that holds it.
 inline bool check_logits(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
                          double temperature, int* dev) {
-    if (!logits || rows < 1 || vocab < 1 || vocab > INT32_MAX || row_stride < vocab) return false;
+    if (!logits || rows < 1 || vocab < 1 || vocab > INT32_MAX - 64 || row_stride < vocab) return false;
     if (dtype != QN_F32 && dtype != QN_BF16) return false;
     if (row_stride > INT64_MAX / 8 / rows || reinterpret_cast<uintptr_t>(logits) % dtype_size(dtype)) return false;
     const float inv = static_cast<float>(1.0 / temperature);

@@ -1,6 +1,8 @@
 // The kernel behind the calls that give the gradient of a row of logits: the row is read once, its softmax statistics are
 // taken, and the gradient is written, with the row in shared memory between the two.
 //
+// Two forms: the pipeline here, for many long rows, and row_gradient_small_kernel below, for everything else.
+//
 // A cluster of C CTAs takes a row; each holds a slice of at most 192 KB (128 KB unless the row is larger than 1 MB).  A row
 // is seen as 16-byte vectors that start at the 16-byte boundary at or below its first element, so that whatever its
 // alignment all but its first and last vector move as bulk copies; what those two hold outside the row is filled with -inf.
@@ -9,22 +11,27 @@
 //   list warps     a row each: read the few elements of it that are special (a given token, alternatives, a teacher's list),
 //                  work out what depends on them alone, and sort those by chunk that must not be added
 //   copy warp      brings the slices of the coming rows in
-//   sum warps      a chunk each: take out what must not be added, and add e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative to a running maximum m of each thread; at the end of a
-//                  slice each sends its maximum and sums to every CTA of the cluster (asynchronous stores into shared
-//                  memory that count on a barrier there)
+//   sum warps      a chunk each: take out what must not be added, and add e_i = 2^d_i, d_i = (z_i - m) log2(e) / T, relative
+//                  to a running maximum m of each thread; at the end of a slice each sends its maximum and sums to every
+//                  CTA of the cluster (asynchronous stores into shared memory that count on a barrier there)
 //   join warp      from all messages, in the same order in every CTA, to the row's coefficients
 //   write warps    a chunk each: e_i times the coefficient; give the chunk back
 //   end warp       when a row has been written, its special elements' gradients, and the row's loss
 // So HBM is read and written at the same time, and the exchange of one row passes while others are summed and written.
-// Loops are short and rolled: a form that kept the slice in registers (unrolled over them) ran out of the instruction cache.
-// exp2 is taken twice for an element: at 16 a cycle and SM that is 73 % of the time in which bf16 logits come from HBM and
-// their gradient goes there.
+//
+// Measured on a B200, 4096 x 131072 bf16 with a list of 64 tokens: 386 us, 85 % of the rate of a plain copy (fp32,
+// 1024 x 262144: 418 us, 79 %; clusters of 8 leave 28 of the 148 SMs without work).  What bounds it then is the issue of
+// instructions: per element about 5.5 in the sum loop, 5 in the write loop and 3 for everything that is paid once a row,
+// where a chunk's bytes take the time of 20.  exp2 is taken twice for an element, 73 % of its rate of 16 a cycle and SM if
+// nothing else bound; giving a quarter of them to the FMA pipe as a polynomial made it slower (441 to 469 us), as does
+// anything that adds instructions.  Keeping e_i in registers between the two (one exp2) needs loops unrolled over them, and
+// those ran out of the instruction cache: 883 us.  One lane that issued all copies took 470 cycles for each: 526 us.
 //
 // An operator Op brings:
 //   Params, Shared        arguments; what the warps tell one another of a row
 //   Fetched, fetch        a row's special elements as a lane of a list warp loads them, two rows ahead of their use
 //   gather                their logits (of the whole row, also outside the slice), a row ahead
-//   wanted                false if the row is padding: its gradient is 0 and it is not read
+//   wanted                false if the row is padding: its gradient is 0, and the pipeline does not read it
 //   begin                 list warp: what depends on the special elements alone, and their places (Shared::pos)
 //   kMask                 whether the special elements leave the sums
 //   join                  from all messages to Shared::g
@@ -40,8 +47,8 @@ constexpr int kChunk = 256;      // vectors in a chunk
 constexpr int kSlots = 48;       // chunks in the ring
 constexpr int kListWarps = 2;
 constexpr int kLists = 6;  // rows between the list warps' beginning and the end warp's end of them
-// Warps that sum and that write.  Measured for 4096 x 131072 bf16 with a list of 64
-// tokens, us: 8 / 8 468, 10 / 13 449, 11 / 12 440 (28 warps are the most that leave 72 registers for each).
+// Warps that sum and that write.  Measured for 4096 x 131072 bf16 with a list of 64 tokens (at the time), us: 8 / 8 468,
+// 10 / 13 449, 11 / 12 440; 28 warps are the most that leave 72 registers for each.
 template <bool kWrite>
 struct Roles {
     static constexpr int kSum = 11, kWriting = kWrite ? 12 : 0;  // the same sums, to the bit, with and without a gradient
@@ -621,7 +628,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 // ---- small problems --------------------------------------------------------------------------------------------------
 
 // The same for problems whose time is latency: a CTA (of a cluster, where there are few rows or long ones) takes a slice of up
-// to 32 KB straight into registers, its first warp the special elements meanwhile; sums, exchange, gradient, end.
+// to 32 KB straight into registers, its first warp the special elements meanwhile; sums, exchange, gradient, end.  One
+// launch, no stage that waits for another, up to 32 CTAs on an SM.  Measured, us: one row of 8192 fp32 5.6 (the pipeline:
+// 9.0), 128 x 8192 bf16 6.5 (9.2), 1024 x 8192 fp32 backward 13.4 = 77 % of a copy's rate (21).
 constexpr int kSmallVectors = 8;  // of a thread
 
 template <typename T, int NT, typename Op, bool kAligned>
@@ -851,7 +860,7 @@ cudaError_t launch_gradient_aligned(const typename Op::Params& p, cudaStream_t s
     // 8192 x 8192 87 / 118; fp32 128 x 32000 9.7 / 14, 1024 x 32000 71 / 53, 1024 x 8192 17 / 21, 8192 x 8192 129 / 116;
     // one row of 8192: 5 / 9.  So: all logits more than 64 MB, in rows of more than 32 KB.
     const int64_t bytes = p.vocab * static_cast<int64_t>(sizeof(T));
-    if (ctas > kMaxCluster || (bytes > (32 << 10) && p.rows > (64 << 20) / bytes))
+    if (ctas > kMaxCluster || p.rows > INT32_MAX / kMaxCluster || (bytes > (32 << 10) && p.rows > (64 << 20) / bytes))
     {
         // rows that start and end on 16 bytes have no vectors that reach past them
         const bool edges = !rows_aligned<T>(p) || p.vocab % Storage<T>::kVec != 0;

@@ -454,13 +454,19 @@ def _logit_matrix(t: torch.Tensor, name: str) -> Tuple[int, int, int, int]:
     return rows, vocab, stride, dtype_code(t.dtype)
 
 
-def _beside(t: Optional[torch.Tensor], dtype: torch.dtype, shape: tuple, device: int, name: str) -> int:
-    """Address of a small array that goes with the logits (0 for None)."""
+def _beside(t: Optional[torch.Tensor], dtype: torch.dtype, rows: int, width: int, device: int, name: str) -> int:
+    """Address of a small array that goes with the logits, [rows] (width 0) or [rows][width]; 0 for None."""
     if t is None:
         return 0
-    if t.dtype is not dtype or t.get_device() != device or t.shape != shape or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d" % (name, dtype, list(shape), device))
-    return t.data_ptr()
+    # what the calls cost beside their kernels is mostly these checks: few and cheap ones
+    if t.dtype is dtype and t.get_device() == device and t.is_contiguous():
+        if width == 0:
+            if t.dim() == 1 and t.numel() == rows:
+                return t.data_ptr()
+        elif t.dim() == 2 and t.shape[1] == width and t.numel() == rows * width:
+            return t.data_ptr()
+    raise ValueError("%s must be a contiguous %s tensor of shape %s on cuda:%d"
+                     % (name, dtype, [rows, width] if width else [rows], device))
 
 
 def _gradient(t: torch.Tensor, logits: torch.Tensor, name: str) -> Tuple[int, int]:
@@ -495,13 +501,13 @@ def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, log
         if top_token is None or top_logprob is None or top_token.dim() != 2:
             raise ValueError("top_token and top_logprob go together, [rows][k] each")
         k = top_token.shape[1]
-    f32, one = torch.float32, (rows,)
+    f32 = torch.float32
     _check(lib().qn_logprobs(rows, vocab, code, logits.data_ptr(), stride,
-                             _beside(tokens, torch.int64, one, dev, "tokens"), temperature,
-                             _beside(logprob, f32, one, dev, "logprob"), _beside(lse, f32, one, dev, "lse"),
-                             _beside(entropy, f32, one, dev, "entropy"), k,
-                             _beside(top_token, torch.int64, (rows, k), dev, "top_token"),
-                             _beside(top_logprob, f32, (rows, k), dev, "top_logprob"), _stream_on(dev, stream)),
+                             _beside(tokens, torch.int64, rows, 0, dev, "tokens"), temperature,
+                             _beside(logprob, f32, rows, 0, dev, "logprob"), _beside(lse, f32, rows, 0, dev, "lse"),
+                             _beside(entropy, f32, rows, 0, dev, "entropy"), k,
+                             _beside(top_token, torch.int64, rows, k, dev, "top_token"),
+                             _beside(top_logprob, f32, rows, k, dev, "top_logprob"), _stream_on(dev, stream)),
            "qn_logprobs")
 
 
@@ -518,15 +524,15 @@ def qn_logprobs_backward(logits: torch.Tensor, dlogits: torch.Tensor, tokens: Op
         if top_token is None or d_top_logprob.dim() != 2:
             raise ValueError("d_top_logprob [rows][k] goes with top_token")
         k = d_top_logprob.shape[1]
-    f32, one = torch.float32, (rows,)
+    f32 = torch.float32
     out, out_stride = _gradient(dlogits, logits, "dlogits")
     _check(lib().qn_logprobs_backward(rows, vocab, code, logits.data_ptr(), stride,
-                                      _beside(tokens, torch.int64, one, dev, "tokens"), temperature,
-                                      _beside(d_logprob, f32, one, dev, "d_logprob"),
-                                      _beside(d_lse, f32, one, dev, "d_lse"),
-                                      _beside(d_entropy, f32, one, dev, "d_entropy"), k,
-                                      _beside(top_token, torch.int64, (rows, k), dev, "top_token") if k else 0,
-                                      _beside(d_top_logprob, f32, (rows, k), dev, "d_top_logprob") if k else 0, out,
+                                      _beside(tokens, torch.int64, rows, 0, dev, "tokens"), temperature,
+                                      _beside(d_logprob, f32, rows, 0, dev, "d_logprob"),
+                                      _beside(d_lse, f32, rows, 0, dev, "d_lse"),
+                                      _beside(d_entropy, f32, rows, 0, dev, "d_entropy"), k,
+                                      _beside(top_token, torch.int64, rows, k, dev, "top_token") if k else 0,
+                                      _beside(d_top_logprob, f32, rows, k, dev, "d_top_logprob") if k else 0, out,
                                       out_stride, _stream_on(dev, stream)), "qn_logprobs_backward")
 
 
@@ -546,9 +552,9 @@ def qn_distill(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_value:
     k = teacher_token.shape[1]
     out, out_stride = _gradient(dlogits, logits, "dlogits") if dlogits is not None else (0, 0)
     _check(lib().qn_distill(rows, vocab, code, logits.data_ptr(), stride, k,
-                            _beside(teacher_token, torch.int64, (rows, k), dev, "teacher_token"),
+                            _beside(teacher_token, torch.int64, rows, k, dev, "teacher_token"),
                             dtype_code(teacher_value.dtype),
-                            _beside(teacher_value, teacher_value.dtype, (rows, k), dev, "teacher_value"), teacher,
-                            temperature, _beside(weight, torch.float32, (rows,), dev, "weight"),
-                            _beside(loss, torch.float32, (rows,), dev, "loss"), out, out_stride,
+                            _beside(teacher_value, teacher_value.dtype, rows, k, dev, "teacher_value"), teacher,
+                            temperature, _beside(weight, torch.float32, rows, 0, dev, "weight"),
+                            _beside(loss, torch.float32, rows, 0, dev, "loss"), out, out_stride,
                             _stream_on(dev, stream)), "qn_distill")
