@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
     LogprobShared& sh = *reinterpret_cast<LogprobShared*>(shared_bytes);
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int tid = threadIdx.x;
+    start_after_last();
     if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
     for (int64_t r = blockIdx.x / ctas; r < p.rows; r += gridDim.x / ctas) {
         const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
@@ -234,6 +235,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
             if (i + 2 < batches) load(i + 2, a);
             take(b);
         }
+        let_next_start();
         if (kTop && left != per_group) sh.group_max[group++][tid] = group_top;
         // elements outside the slice were counted at the floor: in a slice with anything above it they are 0
 
@@ -410,18 +412,8 @@ cudaError_t launch_logprobs(LogprobParams& p, cudaStream_t st) {
         raised[dev] = true;
     }
     const int64_t most = INT32_MAX / kTopCluster;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((p.rows < most ? p.rows : most) * ctas));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = sizeof(LogprobShared);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, p);
+    const EarlyLaunch launch((p.rows < most ? p.rows : most) * ctas, kThreads, sizeof(LogprobShared), ctas, st);
+    return cudaLaunchKernelEx(&launch.cfg, kernel, p);
 }
 
 struct BackwardParams {

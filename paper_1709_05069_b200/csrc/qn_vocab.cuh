@@ -48,6 +48,25 @@ inline bool check_gradient(int64_t rows, int64_t vocab, qn_dtype dtype, const vo
                      matrix_bytes(rows, vocab, row_stride, dtype));
 }
 
+// A launch whose set-up may overlap the end of the stream's last kernel (see start_after_last), as clusters of `ctas`.
+struct EarlyLaunch {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    EarlyLaunch(int64_t grid, int threads, size_t shared, int ctas, cudaStream_t st) {
+        cfg.gridDim = dim3(static_cast<unsigned>(grid));
+        cfg.blockDim = dim3(threads);
+        cfg.dynamicSmemBytes = shared;
+        cfg.stream = st;
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        attr[1].id = cudaLaunchAttributeClusterDimension;
+        attr[1].val.clusterDim.x = ctas;
+        attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = ctas > 1 ? 2 : 1;
+    }
+};
+
 // ---- device --------------------------------------------------------------------------------------------------------
 
 __device__ __forceinline__ float exp2_approx(float x) {
@@ -277,6 +296,11 @@ __device__ __forceinline__ void store_remote(const float4* mine, uint32_t cta, f
 __device__ __forceinline__ void store_remote(const uint64_t* mine, uint32_t cta, uint64_t x) {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(map_remote(mine, cta)), "l"(x) : "memory");
 }
+
+// For kernels launched with EarlyLaunch: nothing is read or written before the stream's last kernel has ended; and from
+// `let_next_start` on the next such kernel may be set up beside this one (it too waits for this one's end).
+__device__ __forceinline__ void start_after_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void let_next_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 
 // ---- geometry ------------------------------------------------------------------------------------------------------
 

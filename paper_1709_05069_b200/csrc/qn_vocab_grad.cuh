@@ -647,6 +647,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
     __shared__ bool want;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    start_after_last();
     if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
     const int64_t r = blockIdx.x / ctas;
     const T* row = static_cast<const T*>(p.logits) + r * p.row_stride;
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
         if (lane == 0) want = wanted;
         __syncwarp();
     }
+    let_next_start();
     typename Lanes<T>::Max top;
 #pragma unroll
     for (int q = 0; q < kSmallVectors; ++q) top.take(v[q]);
@@ -836,18 +838,9 @@ int64_t row_vectors(const Params& p) {
 
 template <typename T, int NT, typename Op, bool kAligned>
 cudaError_t launch_gradient_small(const typename Op::Params& p, int ctas, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.rows * ctas));
-    cfg.blockDim = dim3(NT);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = ctas;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    const EarlyLaunch launch(p.rows * ctas, NT, 0, ctas, st);
     const int per_cta = static_cast<int>((row_vectors<T>(p) + ctas - 1) / ctas);
-    return cudaLaunchKernelEx(&cfg, row_gradient_small_kernel<T, NT, Op, kAligned>, p, static_cast<int32_t>(per_cta));
+    return cudaLaunchKernelEx(&launch.cfg, row_gradient_small_kernel<T, NT, Op, kAligned>, p, static_cast<int32_t>(per_cta));
 }
 
 template <typename T, typename Op, bool kAligned>
