@@ -1,7 +1,9 @@
 // qn_distill: a student's loss against a teacher's top logits, and its gradient.
 //
-// An operator of the row-gradient kernel.  With e_i = 2^((z_i - m) log2(e) / T) and the student's sums kept apart for the list (S_l) and the
-// rest (S_r), S = S_l + S_r: p_k = e_k / S, and the mass off the list p_r = S_r / S comes without a subtraction.
+// An operator of the row-gradient kernels.  With e_i = 2^((z_i - m) log2(e) / T) and the student's sums kept apart for the
+// list (S_l) and the rest (S_r), S = S_l + S_r: p_k = e_k / S, and the mass off the list p_r = S_r / S comes without a
+// subtraction (its relative error would be that of S times S / S_r).  The list's own sums, 1 - sum q and the loss are in 64 bits.
+// One launch gives the loss and the gradient; what bounds it and what it measured is in qn_vocab_grad.cuh.
 #include <nvtx3/nvToolsExt.h>
 
 #include "qn_vocab_grad.cuh"
@@ -28,7 +30,8 @@ __device__ __noinline__ double log64(double x) { return log(x); }
 
 struct Distill {
     using Params = DistillParams;
-    static constexpr bool kMoments = false, kMask = true, kAlone = true;  // kAlone: it may be called without a gradient to write
+    static constexpr bool kMoments = false, kMask = true;
+    static constexpr bool kAlone = true;  // it may be called without a gradient to write
     static constexpr int kMine = QN_TOP_MAX / 32;  // entries of the list a lane
     struct Shared {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
