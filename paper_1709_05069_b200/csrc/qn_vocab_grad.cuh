@@ -89,6 +89,27 @@ __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile in
     return mbar_try(bar, parity) || wait_slow(bar, parity, abort);
 }
 
+// A warp's wait for the copy of one item, where the last item in that slot may still be on its way.  A parity cannot tell the
+// phase before from the one after, so the slot also says which item it was last issued for.  That is read before the barrier:
+// once it is this item, the phase before has ended.
+__device__ __noinline__ bool wait_copy_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* issued, uint32_t item, volatile int* abort) {
+    const uint64_t began = global_timer_ns();
+    for (uint32_t it = 0; it < kWaitLimit; ++it) {
+        const bool known = *issued == item;
+        if (!wait_slow(bar, parity, abort)) return false;
+        if (known) return true;
+        __nanosleep(64);
+        if (*abort) return false;
+        if (global_timer_ns() - began > kWaitLimitNs) break;
+    }
+    *abort = 1;
+    return false;
+}
+__device__ __forceinline__ bool wait_copy(uint64_t* bar, uint32_t parity, volatile uint32_t* issued, uint32_t item, volatile int* abort) {
+    const uint32_t last = *issued;
+    const bool here = mbar_try(bar, parity) && last == item;
+    return here || wait_copy_slow(bar, parity, issued, item, abort);
+}
 
 // Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
@@ -238,10 +259,12 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     // full: a chunk has arrived; empty: it has been written.  By row: ready: begun; done: summed and written.  retired: its
     // special elements too.  By row that is wanted: heard: all messages; joined: coefficients
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists], retired[kLists];
+    __shared__ uint32_t issued[kWrite ? 1 : kSlots];  // the item that each slot's last copy is of (see wait_copy)
     __shared__ bool wanted[kLists];
     __shared__ int abort;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (!kWrite && threadIdx.x < kSlots) issued[threadIdx.x] = ~0u;
     if (threadIdx.x == 0) {
         abort = 0;
 #pragma unroll 1
@@ -275,6 +298,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     uint32_t turn = 0;  // rows so far
     uint32_t u = 0;     // wanted rows so far
     if (warp < kSumWarps) {
+        uint32_t one_before = 0, two_before = 0;  // the first item of the wanted row before, and of the one before that
         Walk rows = walk;
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
@@ -289,12 +313,28 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                 float m = -INFINITY;
                 f32x2 sum = 0, moment = 0;
                 bool patched = false;  // a bulk copy may only write there again after a fence
+                // Copies land in any order, and warps go at their own pace: at an item one may meet a slot whose last item, 48
+                // before, is still on its way, and take its arrival for the item's own (see wait_copy).  Not so once the row of
+                // that one has been joined; the sum warp knows it of all rows before `known`, that is, of items before
+                // `sure` - 48.  With a gradient a slot is given back after its row's join, so that to wait for that first
+                // costs nothing; without one the slot says what it holds.
+                uint32_t known = u < 2 ? 0 : u - 2, sure = two_before + kSlots;
                 // chunk c is for worker c % kSumWarps; which warp that is moves on from row to row
                 const int worker = (warp + kSumWarps - turn % kSumWarps) % kSumWarps;
 #pragma unroll 1
                 for (int c = worker; c < chunks; c += kSumWarps) {
                     const uint32_t slot = (n + c) % kSlots;
-                    if (!wait_item(full, n + c, kSlots)) return;
+                    if constexpr (kWrite) {
+                        while (n + c >= sure) {
+                            if (!wait_item(joined, known, kLists)) return;
+                            sure = (++known == u ? n : one_before) + kSlots;
+                        }
+                        if (!wait_item(full, n + c, kSlots)) return;
+                    } else if (n + c < sure) {
+                        if (!wait_item(full, n + c, kSlots)) return;
+                    } else {
+                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) return;
+                    }
                     if constexpr (Op::kMask) {
                         const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
                         if (begin < end) {
@@ -348,6 +388,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                         if (lane == 0) mbar_arrive(&empty[slot]);
                     }
                 }
+                two_before = one_before, one_before = n;
                 n += chunks;
                 if (patched) fence_async();
                 // the warp's message: its maximum, and sums relative to it
@@ -496,6 +537,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                             mbar_expect_tx(&full[slot], bytes);
                             bulk_load(to + (b0 - j0), base + static_cast<int64_t>(b0) * kVec, bytes, &full[slot]);
                         }
+                        if constexpr (!kWrite) *static_cast<volatile uint32_t*>(&issued[slot]) = n + c;
                         mbar_arrive(&full[slot]);
                     }
                     pending &= ~__ballot_sync(0xffffffffu, mine);
