@@ -102,6 +102,7 @@ template <typename T>
 __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, LogprobShared& sh, uint64_t* out) {
     const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
     uint64_t least = static_cast<uint64_t>(kOrderMasked) << 32 | 0xffffffffu;  // above every masked logit
+    __syncthreads();  // every thread has read the count that sent it here
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
 #pragma unroll 1
