@@ -73,9 +73,8 @@ __device__ __noinline__ uint4 load_edge(const T* row, int32_t origin, int32_t vo
 // Vector j of a slice (-inf outside of it).
 template <typename T>
 __device__ __forceinline__ uint4 load_vector(const T* row, const Slice<T>& s, int32_t fb, int32_t fe, int32_t j) {
-    const int32_t at = s.origin() + j * Slice<T>::kVec;
-    if (j >= fb && j < fe) return ldg_stream16(row + at);
-    return j < s.count ? load_edge(row, at, s.vocab) : Lanes<T>::masked4();
+    if (j >= fb && j < fe) return ldg_stream16(row + (s.origin() + j * Slice<T>::kVec));
+    return j < s.count ? load_edge(row, s.origin() + j * Slice<T>::kVec, s.vocab) : Lanes<T>::masked4();
 }
 
 // Gives the k largest of n distinct keys to `put(place, key)`, and 0 for the places that are left.  All threads, after a
@@ -97,7 +96,7 @@ __device__ __forceinline__ void rank_keys(const uint64_t* key, int n, int k, Put
 }
 
 // At most kCandidates logits of a slice, the k largest among them, whatever it holds: in steps of a logit for each thread,
-// those above the k-th of what there is.
+// those above the k-th of what there is.  A step past the end of the largest rows leaves 32 bits, here and in slice_slow.
 template <typename T>
 __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, LogprobShared& sh, uint64_t* out) {
     const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
@@ -106,9 +105,9 @@ __device__ __noinline__ void select_slow(const T* row, const Slice<T> s, int k, 
     if (threadIdx.x == 0) sh.count = 0;
     __syncthreads();
 #pragma unroll 1
-    for (int32_t i0 = lo; i0 < hi; i0 += kThreads) {
-        const int32_t i = i0 + threadIdx.x;
-        const uint64_t key = i < hi ? key_of(Storage<T>::load1(row + i), i) : 0;
+    for (int64_t i0 = lo; i0 < hi; i0 += kThreads) {
+        const int64_t i = i0 + threadIdx.x;
+        const uint64_t key = i < hi ? key_of(Storage<T>::load1(row + i), static_cast<uint32_t>(i)) : 0;
         if (key > least) sh.candidate[atomicAdd(&sh.count, 1)] = key;
         __syncthreads();
         if (sh.count > kCandidates - kThreads) {
@@ -129,12 +128,12 @@ __device__ __noinline__ float4 slice_slow(const T* row, const Slice<T> s, float 
     const int32_t lo = max(0, s.origin()), hi = min(s.vocab, s.origin() + s.count * Slice<T>::kVec);
     float m = -INFINITY;
 #pragma unroll 1
-    for (int32_t i = lo + threadIdx.x; i < hi; i += kThreads) m = fmaxf(m, Storage<T>::load1(row + i));
+    for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) m = fmaxf(m, Storage<T>::load1(row + i));
     m = block_reduce<float, max_op>(m, sh.max);
     const float ref = m == -INFINITY ? 0.0f : m;
     float sum = 0.0f, moment = 0.0f;
 #pragma unroll 1
-    for (int32_t i = lo + threadIdx.x; i < hi; i += kThreads) {
+    for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
         const float d = (Storage<T>::load1(row + i) - ref) * scale, e = exp2_approx(d);
         sum += e;
         if (e != 0.0f) moment += e * d;

@@ -40,3 +40,27 @@ def test_alternatives_among_more_ties_than_are_collected(qn, rows, vocab, dtype)
             again, again_lse = torch.zeros_like(top), torch.zeros_like(lse)
             qn.qn_logprobs(z, lse=again_lse, top_token=again, top_logprob=torch.empty((rows, k), device="cuda"))
             assert torch.equal(again, top) and torch.equal(again_lse, lse)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_largest_vocabulary_of_the_forward_call(qn, dtype):
+    """2^31 - 65 logits, the few that are not masked near the end, in a form that only the exhaustive paths take."""
+    vocab = (1 << 31) - 65
+    low = torch.finfo(dtype).min
+    z = torch.full((1, vocab), -INF, dtype=dtype, device="cuda")
+    z[0, -1] = low
+    tokens = torch.tensor([vocab - 1], device="cuda")
+    lp, lse, ent = (torch.zeros(1, device="cuda") for _ in range(3))
+    top, top_lp = torch.zeros((1, 3), dtype=torch.int64, device="cuda"), torch.zeros((1, 3), device="cuda")
+
+    def numbers():
+        qn.qn_logprobs(z, tokens, lp, lse=lse, entropy=ent, top_token=top, top_logprob=top_lp)
+        return float(lp), float(lse), float(ent), top[0].tolist(), top_lp[0].tolist()
+
+    assert numbers() == (0.0, float(torch.tensor(low, dtype=dtype).float()), 0.0, [vocab - 1, -1, -1], [0.0, -INF, -INF])
+    z[0, -2] = low
+    z[0, 5] = low
+    a, b, c, d, e = numbers()
+    assert d == [5, vocab - 2, vocab - 1] and all(abs(x + math.log(3)) < 1e-5 for x in e + [a]) and abs(c - math.log(3)) < 1e-5
+    z[0, vocab - 300] = 2.0
+    assert numbers()[3] == [vocab - 300, 5, vocab - 2] and float(lse) == 2.0 and float(lp) < -3e38
