@@ -685,7 +685,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
     __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWarps][32];
     __shared__ float4 warp_sums[kWarps];
     __shared__ float warp_max[kWarps];
-    __shared__ uint8_t special[Op::kMask ? NT * kSmallVectors : 1];  // which elements of a vector leave the sums
+    __shared__ __align__(4) uint8_t special[Op::kMask ? NT * kSmallVectors : 1];  // which elements of a vector leave the sums; set by words
     __shared__ bool want;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
