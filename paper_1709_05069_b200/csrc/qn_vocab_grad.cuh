@@ -67,8 +67,13 @@ __device__ __forceinline__ void store_async(const void* mine, const uint64_t* ba
 __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-// A bounded wait.  Its slow part is out of line (instruction cache), and leaves the warp suspended for up to 20 us at a time
-// instead of polling: with polls in their place half of the instructions that the SM issued were those of waiting warps.
+// Takes bytes off what a barrier still waits for.
+__device__ __forceinline__ void mbar_complete_tx(uint64_t* bar, uint32_t bytes) {
+    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
+// A bounded wait of a warp; all its lanes get the same answer, so that they leave together.  Its slow part is out of line
+// (instruction cache), and leaves the warp suspended for up to 20 us at a time instead of polling: with polls in their place
+// half of the instructions that the SM issued were those of waiting warps.
 __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort) {
     const uint64_t began = global_timer_ns();
     for (uint32_t it = 0; it < kWaitLimit; ++it) {
@@ -86,7 +91,7 @@ __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile 
     return false;
 }
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
-    return mbar_try(bar, parity) || wait_slow(bar, parity, abort);
+    return __all_sync(0xffffffffu, mbar_try(bar, parity)) || __all_sync(0xffffffffu, wait_slow(bar, parity, abort));
 }
 
 // A warp's wait for the copy of one item, where the last item in that slot may still be on its way.  A parity cannot tell the
@@ -108,11 +113,44 @@ __device__ __noinline__ bool wait_copy_slow(uint64_t* bar, uint32_t parity, vola
 __device__ __forceinline__ bool wait_copy(uint64_t* bar, uint32_t parity, volatile uint32_t* issued, uint32_t item, volatile int* abort) {
     const uint32_t last = *issued;
     const bool here = mbar_try(bar, parity) && last == item;
-    return here || wait_copy_slow(bar, parity, issued, item, abort);
+    return __all_sync(0xffffffffu, here) || __all_sync(0xffffffffu, wait_copy_slow(bar, parity, issued, item, abort));
 }
 
 // Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// ---- the way out of a kernel in which a wait ran out (kSlots and kLists are those of the ring and of the lists) ----------
+
+// Copy warp: waits for the last copy into each slot, of the items before `begun` and of the lanes of `mask` after it.
+__device__ __noinline__ void wait_copies(uint64_t* full, uint32_t begun, uint32_t mask, volatile int* late) {
+    const uint32_t lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (uint32_t i = lane; i < kSlots && i < begun; i += 32) {
+        const uint32_t item = begun - 1 - i;
+        if (i < kSlots - 32 || !(mask >> (kSlots - 1 - i) & 1)) wait_slow(&full[item % kSlots], item / kSlots & 1, late);
+    }
+    if (mask >> lane & 1) wait_slow(&full[(begun + lane) % kSlots], (begun + lane) / kSlots & 1, late);
+}
+
+// Join warp: waits for the messages of row u, if they are `expected` already, and of those after it, as many as were sent; the
+// `all` warps that send have sent those of rows below sent[i].
+__device__ __noinline__ void wait_messages(uint64_t* heard, const uint64_t* sent, uint32_t u, bool expected, int all, volatile int* late) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (;; ++u, expected = false) {
+        int count = 0;
+        for (int i = lane; i < all; i += 32) count += sent[i] > u;
+        count = __reduce_add_sync(0xffffffffu, count);
+        if (count == 0) return;
+        uint64_t* bar = &heard[u % kLists];
+        if (lane == 0) {
+            if (expected) mbar_complete_tx(bar, (all - count) * 16u);
+            else mbar_arrive_expect_tx(bar, count * 16u);
+        }
+        __syncwarp();
+        if (!wait(bar, u / kLists & 1, late)) return;
+    }
+}
 
 // ---- writing -------------------------------------------------------------------------------------------------------
 
@@ -261,12 +299,16 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists], retired[kLists];
     __shared__ uint32_t issued[kWrite ? 1 : kSlots];  // the item that each slot's last copy is of (see wait_copy)
     __shared__ bool wanted[kLists];
-    __shared__ int abort;
+    __shared__ int abort, late;  // a wait ran out; one on the way out did
+    // on the way out: how many wanted rows' messages each sum warp has sent, and the join warp has heard (x 2, + 1 if it has
+    // announced the next row's)
+    __shared__ uint64_t sent[kMaxCluster * kMessages];
+    __shared__ uint32_t heard_of;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!kWrite && threadIdx.x < kSlots) issued[threadIdx.x] = ~0u;
     if (threadIdx.x == 0) {
-        abort = 0;
+        abort = late = 0;
 #pragma unroll 1
         for (int i = 0; i < kSlots; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
 #pragma unroll 1
@@ -303,7 +345,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            if (!wait_item(ready, turn, kLists)) return;
+            if (!wait_item(ready, turn, kLists)) goto sent_last;
             if (wanted[li]) {
                 const Slice<T> s = slice_of(r);
                 const int chunks = chunks_of(s);
@@ -326,14 +368,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                     const uint32_t slot = (n + c) % kSlots;
                     if constexpr (kWrite) {
                         while (n + c >= sure) {
-                            if (!wait_item(joined, known, kLists)) return;
+                            if (!wait_item(joined, known, kLists)) goto sent_last;
                             sure = (++known == u ? n : one_before) + kSlots;
                         }
-                        if (!wait_item(full, n + c, kSlots)) return;
+                        if (!wait_item(full, n + c, kSlots)) goto sent_last;
                     } else if (n + c < sure) {
-                        if (!wait_item(full, n + c, kSlots)) return;
+                        if (!wait_item(full, n + c, kSlots)) goto sent_last;
                     } else {
-                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) return;
+                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) goto sent_last;
                     }
                     if constexpr (Op::kMask) {
                         const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
@@ -404,14 +446,16 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                     msg.z = warp_reduce<float, add_op>(msg.z);
                 }
                 msg.y = warp_reduce<float, add_op>(msg.y);
-                if (!may_send(u)) return;
+                if (!may_send(u)) goto sent_last;
                 send(u, worker, msg);
                 ++u;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-        return;
+    sent_last:
+        if (ctas > 1 && lane < static_cast<int>(ctas)) store_remote(&sent[rank * kMessages + warp], lane, u);
+        goto out;
     }
     if constexpr (kWrite) if (warp < kSumWarps + kWriteWarps) {
         constexpr int NT = 32 * kWriteWarps;
@@ -425,7 +469,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             if (!ok) {  // a wait ran out: what is left becomes NaN
 #pragma unroll 1
                 for (; (r = rows.row()) < p.rows; rows.next()) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
-                return;
+                goto out;
             }
             const Slice<T> s = slice_of(r);
             if (!wanted[li]) {
@@ -502,14 +546,17 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-        return;
+        goto out;
     }
     if (warp == kSumWarps + kWriteWarps) {
         // ---- copy warp
         Walk rows = walk;
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
-            if (!wait_item(ready, turn, kLists)) return;
+            if (!wait_item(ready, turn, kLists)) {
+                wait_copies(full, n, 0, &late);
+                goto out;
+            }
             const bool want = wanted[turn % kLists];
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[turn % kLists]);
@@ -526,10 +573,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                 const uint32_t slot = (n + c) % kSlots, parity = ((n + c) / kSlots & 1) ^ 1;
                 uint4* to = ring + slot * kChunk;
                 const int32_t j0 = c * kChunk, j1 = min(j0 + kChunk, s.count), b0 = max(j0, fb), b1 = min(j1, fe);
-                uint32_t pending = __ballot_sync(0xffffffffu, c < chunks);
+                const uint32_t group = __ballot_sync(0xffffffffu, c < chunks);
+                uint32_t pending = group;
                 while (pending) {
                     const uint32_t first = n + c0 + __ffs(pending) - 1;  // slots come free in about this order
-                    if (!wait_free(empty, first, kSlots)) return;
+                    if (!wait_free(empty, first, kSlots)) {
+                        wait_copies(full, n + c0, group & ~pending, &late);
+                        goto out;
+                    }
                     const bool mine = (pending >> lane & 1) && mbar_try(&empty[slot], parity);
                     if (mine) {
                         if (b1 > b0) {
@@ -546,20 +597,23 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             }
             n += chunks;
         }
-        return;
+        goto out;
     }
     if (warp == kSumWarps + kWriteWarps + 1) {
         // ---- join warp
+        bool expected = false;
         Walk rows = walk;
 #pragma unroll 1
         for (; rows.row() < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            if (!wait_item(ready, turn, kLists)) return;
+            if (!wait_item(ready, turn, kLists)) goto heard_last;
             if (wanted[li]) {
                 const int set = u % kLists;
                 if (lane == 0) mbar_arrive_expect_tx(&heard[set], ctas * (kMessages * 16u));
                 __syncwarp();
-                if (!wait_item(heard, u, kLists)) return;
+                expected = true;
+                if (!wait_item(heard, u, kLists)) goto heard_last;
+                expected = false;
                 Op::template join<kSumWarps>(p, lists[li], inbox[set], static_cast<int>(ctas));
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&joined[set]);
@@ -568,7 +622,9 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-        return;
+    heard_last:
+        if (lane == 0) heard_of = 2 * u + expected;
+        goto out;
     }
     if (warp == kSumWarps + kWriteWarps + 2) {
         // ---- end warp: what is left to do of a row once the others are through with it
@@ -585,85 +641,97 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         if (rank == 0 && lane == 0)  // a wait ran out, if any rows are left
 #pragma unroll 1
             for (; rows.row() < p.rows; rows.next()) Op::without(p, rows.row(), NAN);
-        return;
+        goto out;
     }
-    // ---- list warps
-    turn = warp - (kSumWarps + kWriteWarps + 3);
-    Walk rows = walk;
-    rows.next(turn);
-    Walk ahead = rows;
-    ahead.next(kListWarps);
-    typename Op::Fetched next = Op::fetch(p, rows.row()), later = Op::fetch(p, ahead.row());
-    Op::template gather<T>(p, rows.row(), next);
-    // an element of the first or last vector of a slice, where that reaches past the row
-    auto edge_of = [&](int64_t r) {
-        if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
-        const Slice<T> s = slice_of(r);
-        const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
-        return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
-    };
-    T edge = edge_of(rows.row());
-#pragma unroll 1
-    for (int64_t r; (r = rows.row()) < p.rows; rows.next(kListWarps), turn += kListWarps) {
-        const int li = turn % kLists;
-        typename Op::Shared& sh = lists[li];
-        if (turn >= kLists && !wait_item(retired, turn - kLists, kLists)) return;
-        const typename Op::Fetched now = next;
-        next = later;
-        const int64_t following = ahead.row();
+    {
+        // ---- list warps
+        turn = warp - (kSumWarps + kWriteWarps + 3);
+        Walk rows = walk;
+        rows.next(turn);
+        Walk ahead = rows;
         ahead.next(kListWarps);
-        Op::template gather<T>(p, following, next);
-        later = Op::fetch(p, ahead.row());
-        const T edge_now = edge;
-        edge = edge_of(following);
-        const bool want = Op::wanted(p, now);
-        if (want) {
-            Op::begin(p, sh, now);
-            if (kEdges && lane < 2 * kVec) reinterpret_cast<T*>(edges[li])[lane] = edge_now;
-            if constexpr (Op::kMask) {
-                // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
-                const Slice<T> s = slice_of(r);
-                chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
-                __syncwarp();
-                int in[Op::kMine], place[Op::kMine];
-#pragma unroll
-                for (int i = 0; i < Op::kMine; ++i) {
-                    const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
-                    in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
-                    place[i] = 0;
-                    if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
-                    const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
-                    if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
+        typename Op::Fetched next = Op::fetch(p, rows.row()), later = Op::fetch(p, ahead.row());
+        Op::template gather<T>(p, rows.row(), next);
+        // an element of the first or last vector of a slice, where that reaches past the row
+        auto edge_of = [&](int64_t r) {
+            if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
+            const Slice<T> s = slice_of(r);
+            const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
+            return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
+        };
+        T edge = edge_of(rows.row());
+#pragma unroll 1
+        for (int64_t r; (r = rows.row()) < p.rows; rows.next(kListWarps), turn += kListWarps) {
+            const int li = turn % kLists;
+            typename Op::Shared& sh = lists[li];
+            if (turn >= kLists && !wait_item(retired, turn - kLists, kLists)) goto out;
+            const typename Op::Fetched now = next;
+            next = later;
+            const int64_t following = ahead.row();
+            ahead.next(kListWarps);
+            Op::template gather<T>(p, following, next);
+            later = Op::fetch(p, ahead.row());
+            const T edge_now = edge;
+            edge = edge_of(following);
+            const bool want = Op::wanted(p, now);
+            if (want) {
+                Op::begin(p, sh, now);
+                if (kEdges && lane < 2 * kVec) reinterpret_cast<T*>(edges[li])[lane] = edge_now;
+                if constexpr (Op::kMask) {
+                    // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
+                    const Slice<T> s = slice_of(r);
+                    chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
                     __syncwarp();
-                    if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
+                    int in[Op::kMine], place[Op::kMine];
+#pragma unroll
+                    for (int i = 0; i < Op::kMine; ++i) {
+                        const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
+                        in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
+                        place[i] = 0;
+                        if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
+                        const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
+                        if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
+                        __syncwarp();
+                        if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
+                        __syncwarp();
+                    }
+                    int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
+#pragma unroll
+                    for (int o = 1; o < 32; o *= 2) {
+                        const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
+                        if (lane >= o) a += up, b += up2;
+                    }
+                    b += __shfl_sync(0xffffffffu, a, 31);
                     __syncwarp();
-                }
-                int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
+                    chunk_begin[li][lane] = static_cast<uint8_t>(a);
+                    chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
+                    __syncwarp();
 #pragma unroll
-                for (int o = 1; o < 32; o *= 2) {
-                    const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
-                    if (lane >= o) a += up, b += up2;
-                }
-                b += __shfl_sync(0xffffffffu, a, 31);
-                __syncwarp();
-                chunk_begin[li][lane] = static_cast<uint8_t>(a);
-                chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
-                __syncwarp();
+                    for (int i = 0; i < Op::kMine; ++i)
+                        if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
 #pragma unroll
-                for (int i = 0; i < Op::kMine; ++i)
-                    if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
-#pragma unroll
-                for (int i = 0; i < Op::kMine; ++i) {  // and in the edges
-                    if (!kEdges || in[i] < 0) continue;
-                    const int32_t at = sh.pos[lane + 32 * i] - s.origin(), last = at - (s.count - 1) * kVec;
-                    if (at < kVec) reinterpret_cast<T*>(edges[li])[at] = masked<T>();
-                    if (last >= 0) reinterpret_cast<T*>(edges[li])[kVec + last] = masked<T>();
+                    for (int i = 0; i < Op::kMine; ++i) {  // and in the edges
+                        if (!kEdges || in[i] < 0) continue;
+                        const int32_t at = sh.pos[lane + 32 * i] - s.origin(), last = at - (s.count - 1) * kVec;
+                        if (at < kVec) reinterpret_cast<T*>(edges[li])[at] = masked<T>();
+                        if (last >= 0) reinterpret_cast<T*>(edges[li])[kVec + last] = masked<T>();
+                    }
                 }
             }
+            if (lane == 0) wanted[li] = want;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&ready[li]);
         }
-        if (lane == 0) wanted[li] = want;
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&ready[li]);
+    }
+out:
+    // The way out of every warp, also of one whose wait ran out: no CTA leaves while another one may still send into it, nor
+    // while a copy or a message into it is on its way (those that were waited for have arrived).  Every wait so far is
+    // bounded, so all warps of the cluster come here.
+    __syncwarp();
+    if (ctas > 1) {
+        cluster_sync();
+        if (warp == kSumWarps + kWriteWarps + 1 && abort)
+            wait_messages(heard, sent, heard_of / 2, heard_of % 2, static_cast<int>(ctas) * kMessages, &late);
     }
 }
 
