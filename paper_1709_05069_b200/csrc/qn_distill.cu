@@ -2,7 +2,10 @@
 //
 // An operator of the row-gradient kernels.  With e_i = 2^((z_i - m) log2(e) / T) and the student's sums kept apart for the
 // list (S_l) and the rest (S_r), S = S_l + S_r: p_k = e_k / S, and the mass off the list p_r = S_r / S comes without a
-// subtraction (its relative error would be that of S times S / S_r).  The list's own sums, 1 - sum q and the loss are in 64 bits.
+// subtraction (its relative error would be that of S times S / S_r).  S_r is kept relative to the largest logit off the list,
+// m_r, and so is the gradient there: in a row whose list leads by more than 87 T, S_r relative to m would be 0, where
+// ln p_r = (m_r - m) / T + ln S_r - ln S and the softmax over the rest, e_i / S_r, are ordinary numbers.
+// The list's own sums, 1 - sum q and the loss are in 64 bits.
 // One launch gives the loss and the gradient; what bounds it and what it measured is in qn_vocab_grad.cuh.
 #include <nvtx3/nvToolsExt.h>
 
@@ -39,8 +42,9 @@ struct Distill {
         double q_total, q_log_q;  // of the q as rounded to 32 bits
         float q_sum, q_rest, weight;
         float list_m, list_s;  // of the list's logits: the largest, sum of e_k relative to it
-        Gradient g;
-        float rest, s;  // of the row, relative to its maximum
+        Gradient g;             // off the list: relative to m_rest
+        float m, m_rest;        // the largest of the row (0 if it is empty), and of what is off the list
+        float rest, s;          // the sums relative to these
     };
     __device__ static void without(const Params& p, int64_t r, float loss) { p.loss[r] = loss; }
     __device__ static __forceinline__ int entries(const Params& p) { return p.k; }
@@ -158,28 +162,31 @@ struct Distill {
     template <int kWarps>
     __device__ static __forceinline__ void join(const Params& p, Shared& sh, const float4* in, int ctas) {
         const int lane = threadIdx.x & 31, all = ctas * kWarps;
-        float m = sh.list_m;
+        float m_rest = -INFINITY;
 #pragma unroll 1
-        for (int i = lane; i < all; i += 32) m = fmaxf(m, in[i].x);
-        m = warp_max_f32(m);
+        for (int i = lane; i < all; i += 32) m_rest = fmaxf(m_rest, in[i].x);
+        m_rest = warp_max_f32(m_rest);
+        const float m = fmaxf(m_rest, sh.list_m);
         float rest = 0.0f;
 #pragma unroll 1
         for (int i = lane; i < all; i += 32) {
             const float4 v = in[i];
             // of masked elements only: 0, or NaN where there is one
-            rest += v.y * (v.x == m || v.x == -INFINITY ? 1.0f : exp2_approx((v.x - m) * p.scale));
+            rest += v.y * (v.x == m_rest || v.x == -INFINITY ? 1.0f : exp2_approx((v.x - m_rest) * p.scale));
         }
         rest = warp_reduce<float, add_op>(rest);
+        const float rest_at = m_rest == m || m_rest == -INFINITY ? 1.0f : exp2_approx((m_rest - m) * p.scale);
         const float list = sh.list_s * (sh.list_m == m || sh.list_m == -INFINITY ? 1.0f : exp2_approx((sh.list_m - m) * p.scale));
-        const float s = m == INFINITY ? NAN : rest + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
+        const float s = m == INFINITY ? NAN : rest * rest_at + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
         Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (s != 0.0f) {
-            g.m = m == -INFINITY ? 0.0f : m;
+            g.m = m_rest == -INFINITY ? 0.0f : m_rest;
             g.unit = sh.weight * p.inv_t;
             g.on = g.unit * __fdividef(mass, s);
-            g.c0 = q_rest > 0.0f && rest > 0.0f ? g.on - g.unit * __fdividef(q_rest, rest) : g.on;
+            g.c0 = g.on * rest_at;
+            if (q_rest > 0.0f && rest > 0.0f) g.c0 -= g.unit * __fdividef(q_rest, rest);
         }
-        if (lane == 0) sh.g = g, sh.rest = rest, sh.s = s;
+        if (lane == 0) sh.g = g, sh.m = m == -INFINITY ? 0.0f : m, sh.m_rest = m_rest, sh.rest = rest, sh.s = s;
     }
 
     template <typename T>
@@ -189,19 +196,23 @@ struct Distill {
 #pragma unroll 1
             for (int j = threadIdx.x & 31; j < p.k; j += 32)
                 if (s.holds(sh.pos[j]))
-                    Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - g.m) * p.scale) - g.unit * sh.q[j]);
+                    Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - sh.m) * p.scale) - g.unit * sh.q[j]);
         if (!first) return;
         // sum q (ln q - ln p) with ln p = ln 2 s (z - m) - ln S: the small difference of these sums, so in 64 bits
         double dot = 0.0;
         for (int j = threadIdx.x & 31; j < p.k; j += 32)
-            if (sh.pos[j] >= 0 && sh.q[j] > 0.0f) dot += sh.q[j] * (static_cast<double>(sh.z[j]) - g.m);
+            if (sh.pos[j] >= 0 && sh.q[j] > 0.0f) dot += sh.q[j] * (static_cast<double>(sh.z[j]) - sh.m);
         dot = warp_reduce<double, add_op>(dot);
         if ((threadIdx.x & 31) == 0) {
             const double log_s = log64(static_cast<double>(sh.s));
             double loss = INFINITY;
             if (sh.s != 0.0f) {
                 loss = sh.q_log_q - 0.6931471805599453 * p.scale * dot + sh.q_total * log_s;
-                if (sh.q_rest != 0.0f) loss += sh.q_rest * (logf(sh.q_rest) - logf(sh.rest) + log_s);
+                if (sh.q_rest != 0.0f) {
+                    const double log_rest = log64(static_cast<double>(sh.rest)) +
+                                            0.6931471805599453 * p.scale * (static_cast<double>(sh.m_rest) - sh.m);
+                    loss += sh.q_rest * (logf(sh.q_rest) - log_rest + log_s);
+                }
             }
             p.loss[r] = sh.q_sum + sh.q_rest != sh.q_sum + sh.q_rest ? NAN : static_cast<float>(loss);
         }

@@ -33,7 +33,7 @@
 //   gather                their logits (of the whole row, also outside the slice), a row ahead
 //   wanted                false if the row is padding: its gradient is 0, and the pipeline does not read it
 //   begin                 list warp: what depends on the special elements alone, and their places (Shared::pos)
-//   kMask                 whether the special elements leave the sums
+//   kMask                 whether the special elements leave the sums and the maximum
 //   join                  from all messages to Shared::g
 //   fix                   end warp: the special elements' gradients, and the row's loss
 #pragma once
@@ -753,7 +753,7 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
     __shared__ __align__(16) uint4 stage[kAligned ? 1 : kWarps][32];
     __shared__ float4 warp_sums[kWarps];
     __shared__ float warp_max[kWarps];
-    __shared__ __align__(4) uint8_t special[Op::kMask ? NT * kSmallVectors : 1];  // which elements of a vector leave the sums; set by words
+    __shared__ __align__(4) uint8_t special[Op::kMask ? NT * kSmallVectors : 1];  // which elements of a vector leave them; set by words
     __shared__ bool want;
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -772,8 +772,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
         if (j >= fb && j < fe) v[q] = load_stream(row + s.origin() + j * kVec);
         else if (j < s.count) v[q] = load_edge_rw(row, s.origin() + j * kVec, s.vocab);
     }
-    if (Op::kMask)
+    if (Op::kMask) {
         for (int i = tid; i < NT * kSmallVectors / 4; i += NT) reinterpret_cast<uint32_t*>(special)[i] = 0;
+        __syncthreads();
+    }
     if (warp == 0) {
         typename Op::Fetched now = Op::fetch(p, r);
         Op::template gather<T>(p, r, now);
@@ -781,8 +783,23 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
         if (wanted) Op::begin(p, sh, now);
         if (lane == 0) want = wanted;
         __syncwarp();
+        if (Op::kMask && wanted)
+#pragma unroll 1
+            for (int k = lane; k < Op::entries(p); k += 32)
+                if (s.holds(sh.pos[k])) {
+                    const int at = sh.pos[k] - s.origin(), bit = at / kVec * 8 + at % kVec;
+                    atomicOr(reinterpret_cast<uint32_t*>(special) + bit / 32, 1u << bit % 32);
+                }
     }
     let_next_start();
+    if (Op::kMask) {
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < kSmallVectors; ++q) {
+            const uint32_t bits = special[q * NT + tid];
+            if (bits) v[q] = Lanes<T>::without(v[q], bits);
+        }
+    }
     typename Lanes<T>::Max top;
 #pragma unroll
     for (int q = 0; q < kSmallVectors; ++q) top.take(v[q]);
@@ -802,30 +819,15 @@ __global__ void __launch_bounds__(NT, 1024 / NT) row_gradient_small_kernel(const
     float m = warp_max[0];
 #pragma unroll
     for (int w = 1; w < kWarps; ++w) m = fmaxf(m, warp_max[w]);
-    if (Op::kMask) {
-        if (warp == 0)
-#pragma unroll 1
-            for (int k = lane; k < Op::entries(p); k += 32)
-                if (s.holds(sh.pos[k])) {
-                    const int at = sh.pos[k] - s.origin(), bit = at / kVec * 8 + at % kVec;
-                    atomicOr(reinterpret_cast<uint32_t*>(special) + bit / 32, 1u << bit % 32);
-                }
-        __syncthreads();
-    }
     const float ref = m == -INFINITY ? 0.0f : m;
     const f32x2 minus = pack2(-ref, -ref), scale = pack2(p.scale, p.scale);
     f32x2 sum = 0, moment = 0;
 #pragma unroll
     for (int q = 0; q < kSmallVectors; ++q) {
         if (q * NT >= s.count) break;
-        uint4 w = v[q];
-        if (Op::kMask) {
-            const uint32_t bits = special[q * NT + tid];
-            if (bits) w = Lanes<T>::without(w, bits);
-        }
 #pragma unroll
         for (int i = 0; i < kPairs; ++i) {
-            const f32x2 d = mul2(add2(Lanes<T>::pair(w, i), minus), scale), e = exp2_pair(d);
+            const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus), scale), e = exp2_pair(d);
             sum = add2(sum, e);
             if constexpr (moments) moment = fma2(e, finite_pair(d), moment);
         }

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import vocab_reference as ref
-from test_gpu_vocab import DTYPES, check_logprobs, some_tokens
+from test_gpu_vocab import DTYPES, check_distill, check_logprobs, some_tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +64,46 @@ def test_largest_vocabulary_of_the_forward_call(qn, dtype):
     assert d == [5, vocab - 2, vocab - 1] and all(abs(x + math.log(3)) < 1e-5 for x in e + [a]) and abs(c - math.log(3)) < 1e-5
     z[0, vocab - 300] = 2.0
     assert numbers()[3] == [vocab - 300, 5, vocab - 2] and float(lse) == 2.0 and float(lp) < -3e38
+
+
+# ---- distillation: a list far above or below the rest of the vocabulary ---------------------------------------------
+
+# the first four sizes go to the kernel for small problems, the others (rows beyond 256 KB) to the pipeline
+GAP_SHAPES = [(5, 40), (5, 1000), (300, 5003), (4, 40001), (4, 140001), (3, 300001)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", GAP_SHAPES)
+@pytest.mark.parametrize("gap,temperature", [(80.0, 1.0), (100.0, 1.0), (300.0, 1.0), (30.0, 0.1), (600.0, 1.5)])
+def test_distill_list_far_above_or_below_the_rest(qn, rows, vocab, gap, temperature, dtype):
+    """What is left to the rest of the vocabulary, or to the list, is far below the smallest float: neither the loss nor
+    the gradient may lose it."""
+    k = 4
+    z = ref.make_logits(rows, vocab, dtype, vocab)
+    token = ref.make_logits(rows, vocab, torch.float32, 3).topk(k, 1).indices
+    value = torch.tensor([-0.1, -4.0, -5.0, -5.0], device="cuda").expand(rows, k).contiguous()
+    on = torch.zeros((rows, vocab), dtype=torch.bool, device="cuda").scatter_(1, token, True)
+    above = on.clone()
+    above[1::4] = False
+    above[1::4].scatter_(1, token[1::4, 2:3], True)  # one of the list alone
+    above[2::4] = ~on[2::4]  # the rest
+    above[3::4] = ~on[3::4] & (torch.arange(vocab, device="cuda") % 16 == 5)  # some of the rest
+    z = torch.where(above, z.float() + gap, z.float()).to(dtype)
+    weight = torch.rand(rows, device="cuda") + 0.5
+    for logprobs in (True, False):
+        loss, out = check_distill(qn, z, token, value, logprobs, temperature, weight)
+        assert bool(torch.isfinite(loss).all()) and bool(torch.isfinite(out).all())
+
+
+@pytest.mark.parametrize("vocab", [1000, 140001])
+def test_distill_one_listed_token_leads(qn, vocab):
+    """One listed logit of 100 above zeros, ln q = -0.1: by hand, p_r = (vocab - 1) e^-100 and every other gradient is
+    -q_r / (vocab - 1)."""
+    z = torch.zeros((1, vocab), device="cuda")
+    z[0, 7] = 100.0
+    token, value = torch.full((1, 1), 7, device="cuda"), torch.full((1, 1), -0.1, device="cuda")
+    loss, out = check_distill(qn, z, token, value, True)
+    q = math.exp(float(value))
+    want = q * math.log(q) + (1 - q) * (math.log(1 - q) + 100 - math.log(vocab - 1))
+    assert abs(float(loss) - want) < 5e-5
+    assert abs(float(out[0, 3]) * (vocab - 1) + 1 - q) < 1e-6 and abs(float(out.double().sum())) < 1e-6
