@@ -40,7 +40,7 @@ struct Distill {
         int32_t pos[QN_TOP_MAX];  // the teacher's list; -1 for an absent token
         float q[QN_TOP_MAX], z[QN_TOP_MAX];
         double q_total, q_log_q;  // of the q as rounded to 32 bits
-        float q_sum, q_rest, weight;
+        float q_sum, q_rest, q_noise, weight;  // q_noise: what rounding of the values may leave of 1 - sum q
         float list_m, list_s;  // of the list's logits: the largest, sum of e_k relative to it
         Gradient g;             // off the list: relative to m_rest
         float m, m_rest;        // the largest of the row (0 if it is empty), and of what is off the list
@@ -120,6 +120,7 @@ struct Distill {
         // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
         double q_sum = 0.0;
         double q_total = 0.0, q_log_q = 0.0;
+        float noise = 0.0f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int j = lane + 32 * i;
@@ -127,7 +128,7 @@ struct Distill {
             const double log_q = (static_cast<double>(v[i]) - top) * inv - log_norm, q = exp64(log_q);
             q_sum += q;
             const float q32 = static_cast<float>(q);
-            if (q32 != 0.0f) q_log_q += q32 * log_q;
+            if (q32 != 0.0f) q_log_q += q32 * log_q, noise += q32 * (1.0f + fabsf(v[i]));
             q_total += q32;
             sh.q[j] = q32;
         }
@@ -145,6 +146,7 @@ struct Distill {
         q_sum = warp_reduce<double, add_op>(q_sum);
         q_total = warp_reduce<double, add_op>(q_total);
         q_log_q = warp_reduce<double, add_op>(q_log_q);
+        noise = warp_reduce<float, add_op>(noise);
         if (lane == 0) {
             sh.weight = f.weight;
             sh.list_m = list_m;
@@ -153,6 +155,7 @@ struct Distill {
             sh.q_total = q_total;
             sh.q_log_q = q_log_q;
             sh.q_rest = 0.0f;
+            sh.q_noise = noise * (p.value_bf16 ? 0x1p-9f : 0x1p-18f);
             if (p.logprobs && named < p.vocab) sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
         }
         __syncwarp();
@@ -177,7 +180,9 @@ struct Distill {
         rest = warp_reduce<float, add_op>(rest);
         const float rest_at = m_rest == m || m_rest == -INFINITY ? 1.0f : exp2_approx((m_rest - m) * p.scale);
         const float list = sh.list_s * (sh.list_m == m || sh.list_m == -INFINITY ? 1.0f : exp2_approx((sh.list_m - m) * p.scale));
-        const float s = m == INFINITY ? NAN : rest * rest_at + list, q_rest = sh.q_rest, mass = sh.q_sum + q_rest;
+        const float s = m == INFINITY ? NAN : rest * rest_at + list;
+        // nothing is left off the list: then the teacher's rest is what its values' rounding left, if it is no more than that
+        const float q_rest = rest == 0.0f && sh.q_rest <= sh.q_noise ? 0.0f : sh.q_rest, mass = sh.q_sum + q_rest;
         Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (s != 0.0f) {
             g.m = m_rest == -INFINITY ? 0.0f : m_rest;
@@ -186,7 +191,8 @@ struct Distill {
             g.c0 = g.on * rest_at;
             if (q_rest > 0.0f && rest > 0.0f) g.c0 -= g.unit * __fdividef(q_rest, rest);
         }
-        if (lane == 0) sh.g = g, sh.m = m == -INFINITY ? 0.0f : m, sh.m_rest = m_rest, sh.rest = rest, sh.s = s;
+        __syncwarp();
+        if (lane == 0) sh.g = g, sh.q_rest = q_rest, sh.m = m == -INFINITY ? 0.0f : m, sh.m_rest = m_rest, sh.rest = rest, sh.s = s;
     }
 
     template <typename T>

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import vocab_reference as ref
-from test_gpu_vocab import DTYPES, check_distill, check_logprobs, some_tokens
+from test_gpu_vocab import DTYPES, check_distill, check_logprobs, close, some_tokens
 
 pytestmark = pytest.mark.gpu
 
@@ -107,3 +107,57 @@ def test_distill_one_listed_token_leads(qn, vocab):
     want = q * math.log(q) + (1 - q) * (math.log(1 - q) + 100 - math.log(vocab - 1))
     assert abs(float(loss) - want) < 5e-5
     assert abs(float(out[0, 3]) * (vocab - 1) + 1 - q) < 1e-6 and abs(float(out.double().sum())) < 1e-6
+
+
+# ---- distillation: teacher and student masked alike -------------------------------------------------------------------
+
+
+def distill_list_alone64(z, token, value, temperature):
+    """Loss, gradient and sizes of their terms for a student that masks all but listed tokens, q_r = 0."""
+    here = token >= 0
+    logp = torch.log_softmax(z.double() / temperature, 1)
+    v = torch.where(here, value.double(), -INF)
+    q = v.exp()
+    at = token.clamp(min=0)
+    terms = torch.where(here, q * (v - logp.gather(1, at)), 0.0)
+    q_all = torch.zeros_like(logp).scatter_add_(1, at, q)
+    p, mass = logp.exp(), q.sum(1, keepdim=True)
+    return terms.sum(1), (mass * p - q_all) / temperature, (mass * p + q_all) / temperature
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(2000, 512), (600, 9001), (7, 140001), (3, 300001)])
+@pytest.mark.parametrize("temperature", [1.0, 2.0])
+def test_distill_teacher_and_student_masked_alike(qn, rows, vocab, temperature, dtype):
+    """Fewer allowed tokens than alternatives: the list names all of them, and 1 - sum q is what rounding left of it."""
+    k, allowed = 20, 10
+    z = ref.make_logits(rows, vocab, dtype, 12)
+    keep = ref.make_logits(rows, vocab, torch.float32, 13).topk(allowed, 1).indices
+    z = torch.full_like(z, -INF).scatter_(1, keep, z.gather(1, keep))
+    top, top_lp = torch.empty((rows, k), dtype=torch.int64, device="cuda"), torch.empty((rows, k), device="cuda")
+    qn.qn_logprobs(z, top_token=top, top_logprob=top_lp, temperature=temperature)
+    assert bool((top[:, :allowed] >= 0).all()) and bool((top[:, allowed:] == -1).all())
+    for value in (top_lp, top_lp.bfloat16()):
+        loss, out, again = torch.empty(rows, device="cuda"), torch.empty_like(z), torch.empty(rows, device="cuda")
+        qn.qn_distill(z, top, value, loss, dlogits=out, temperature=temperature)
+        qn.qn_distill(z, top, value, again, temperature=temperature)
+        want, grad, size = distill_list_alone64(z, top, value, temperature)
+        close(loss, want, torch.full_like(want, 5e-6 * 20), "loss")
+        assert torch.equal(loss, again)
+        bound = 1e-5 * size + 1e-30 + (2.0 ** -8 * grad.abs() + 2.0 ** -133 if dtype == torch.bfloat16 else 0.0)
+        close(out, grad, bound, "dlogits")
+        if value is top_lp:
+            assert float(loss.abs().max()) < 1e-5 and float(out.float().abs().max()) < 1e-5
+
+
+def test_distill_what_the_student_masks_and_the_teacher_does_not_is_infinite(qn):
+    """More left for the rest than rounding leaves: the loss stays +inf."""
+    for value_dtype, left in ((torch.float32, 1e-3), (torch.bfloat16, 0.2)):
+        for vocab in (600, 300001):
+            z = torch.full((3, vocab), -INF, device="cuda")
+            z[:, 5:9] = 1.0
+            token = torch.tensor([[5, 6, 7, 8, -1]], device="cuda").expand(3, 5).contiguous()
+            value = torch.full((3, 5), math.log((1 - left) / 4), device="cuda").to(value_dtype)
+            loss, out = torch.empty(3, device="cuda"), torch.empty_like(z)
+            qn.qn_distill(z, token, value, loss, dlogits=out)
+            assert bool((loss == INF).all()) and bool(torch.isfinite(out).all())
