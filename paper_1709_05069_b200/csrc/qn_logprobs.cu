@@ -549,7 +549,7 @@ struct Backward {
                 extra += sh.add[i];
             }
             const float d = (sh.z[j] - g.m) * p.scale;
-            if (first) Storage<T>::store1(out + at, exp2_approx(d) * (g.c0 + g.c1 * fmaxf(d, -1e30f)) + extra * p.inv_t);
+            if (first) Storage<T>::store1(out + at, exp2_approx(d) * (g.c0 + g.c1 * fmaxf(d, kFarBelow)) + extra * p.inv_t);
         }
     }
 };

@@ -171,11 +171,13 @@ __device__ __forceinline__ f32x2 exp2_pair(f32x2 d) {
     unpack2(d, lo, hi);
     return pack2(exp2_approx(lo), exp2_approx(hi));
 }
-// -inf becomes a number that a zero can be multiplied with; NaN does too, but e_i keeps it.
+// d_i where e_i d_i is wanted: below kFarBelow, -inf included, e_i is 0 already, and a number that is no larger than needed
+// takes the place of d_i, so that its product with an upstream gradient stays finite.  NaN does not stay, but e_i keeps it.
+constexpr float kFarBelow = -256.0f;
 __device__ __forceinline__ f32x2 finite_pair(f32x2 d) {
     float lo, hi;
     unpack2(d, lo, hi);
-    return pack2(fmaxf(lo, -1e30f), fmaxf(hi, -1e30f));
+    return pack2(fmaxf(lo, kFarBelow), fmaxf(hi, kFarBelow));
 }
 
 __device__ __forceinline__ float max_nan(float a, float b) {

@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import vocab_reference as ref
-from test_gpu_vocab import DTYPES, check_distill, check_logprobs, close, some_tokens
+from test_gpu_vocab import DTYPES, check_backward, check_distill, check_logprobs, close, some_tokens, upstream
 
 pytestmark = pytest.mark.gpu
 
@@ -161,3 +161,20 @@ def test_distill_what_the_student_masks_and_the_teacher_does_not_is_infinite(qn)
             loss, out = torch.empty(3, device="cuda"), torch.empty_like(z)
             qn.qn_distill(z, token, value, loss, dlogits=out)
             assert bool((loss == INF).all()) and bool(torch.isfinite(out).all())
+
+
+# ---- backward: the size of the upstream gradients ----------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(6, 50), (6, 9001), (3, 150001)])
+def test_backward_of_large_upstream_gradients_and_masked_tokens(qn, rows, vocab, dtype):
+    """A scaled loss: a masked token's gradient is its sparse terms alone, however large the entropy's factor is."""
+    z = ref.make_logits(rows, vocab, dtype, 4)
+    z[:, ::3] = -INF
+    t = torch.full((rows,), 7, device="cuda")
+    top = torch.tensor([3, 4], device="cuda").expand(rows, 2).contiguous()  # token 3 is masked
+    for size in (1e6, 1e10, 1e15):
+        out = check_backward(qn, z, t, 1.0, size * upstream(rows, 1), None, size * upstream(rows, 2), top,
+                             size * upstream(rows, 3, 2))
+        assert bool(torch.isfinite(out).all())
