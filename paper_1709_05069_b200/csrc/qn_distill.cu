@@ -192,6 +192,7 @@ struct Distill {
             if (q_rest > 0.0f && rest > 0.0f) g.c0 -= g.unit * __fdividef(q_rest, rest);
         }
         __syncwarp();
+        if (sh.q_sum != sh.q_sum) g.on = g.c0 = NAN;  // also in an empty row
         if (lane == 0) sh.g = g, sh.q_rest = q_rest, sh.m = m == -INFINITY ? 0.0f : m, sh.m_rest = m_rest, sh.rest = rest, sh.s = s;
     }
 

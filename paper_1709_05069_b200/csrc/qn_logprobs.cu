@@ -444,7 +444,8 @@ struct Backward {
     struct Shared {
         int32_t pos[QN_TOP_MAX + 1];  // sparse terms: 0 the given token, 1..k the alternatives; -1 for none
         float add[QN_TOP_MAX + 1], z[QN_TOP_MAX + 1];
-        float total, d_lse, d_h;
+        float total, d_lse, d_h;  // total: NaN if a token is not in the vocabulary
+        bool wrong;               // one is
         Gradient g;
     };
     __device__ static void without(const Params&, int64_t, float) {}
@@ -490,9 +491,11 @@ struct Backward {
 
     __device__ static __forceinline__ void begin(const Params& p, Shared& sh, const Fetched& f) {
         float sum = 0.0f;
+        bool wrong = false;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int j = (threadIdx.x & 31) + 32 * i;
+            wrong = wrong || f.at[i] >= p.vocab;
             if (j > p.k) continue;
             sh.pos[j] = f.at[i] >= 0 && f.at[i] < p.vocab ? static_cast<int32_t>(f.at[i]) : -1;
             sh.add[j] = term(p, f, i);
@@ -500,7 +503,8 @@ struct Backward {
             sum += sh.add[j];
         }
         sum = warp_reduce<float, add_op>(sum);
-        if ((threadIdx.x & 31) == 0) sh.total = sum, sh.d_lse = f.d_lse, sh.d_h = f.d_h;
+        wrong = __any_sync(0xffffffffu, wrong);
+        if ((threadIdx.x & 31) == 0) sh.total = sum, sh.d_lse = f.d_lse, sh.d_h = f.d_h, sh.wrong = wrong;
         __syncwarp();
     }
 
@@ -530,6 +534,7 @@ struct Backward {
             g.c0 = unit * (sh.d_lse - sh.total + sh.d_h * (kLn2 * e / s));
             g.c1 = -unit * sh.d_h * kLn2;
         }
+        if (sh.wrong) g.c0 = NAN;  // also in an empty row
         if (lane == 0) sh.g = g;
     }
 

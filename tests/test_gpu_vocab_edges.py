@@ -178,3 +178,30 @@ def test_backward_of_large_upstream_gradients_and_masked_tokens(qn, rows, vocab,
         out = check_backward(qn, z, t, 1.0, size * upstream(rows, 1), None, size * upstream(rows, 2), top,
                              size * upstream(rows, 3, 2))
         assert bool(torch.isfinite(out).all())
+
+
+# ---- tokens that are not in the vocabulary -------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("vocab", [60, 9001, 150001])
+def test_gradients_of_a_token_that_is_not_in_the_vocabulary(qn, vocab, dtype):
+    """NaN in its whole row, also where every token is masked; its neighbours keep theirs."""
+    z = ref.make_logits(4, vocab, dtype, 9)
+    z[1] = -INF
+    z[2] = -INF
+    t = torch.tensor([3, vocab, 3, vocab + 5], device="cuda")
+    g = torch.ones(4, device="cuda")
+    out, loss = torch.zeros_like(z), torch.zeros(4, device="cuda")
+    for entropy in (None, g):
+        out.zero_()
+        qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g, d_entropy=entropy)
+        assert out.isnan().all(1).tolist() == [False, True, False, True] and bool(torch.isfinite(out[::2]).all())
+    qn.qn_logprobs_backward(z, out, top_token=t[:, None].contiguous(), d_top_logprob=g[:, None].contiguous())
+    assert out.isnan().all(1).tolist() == [False, True, False, True]
+    for teacher in (qn.QN_TEACHER_LOGITS, qn.QN_TEACHER_LOGPROBS):
+        out.zero_()
+        qn.qn_distill(z, torch.stack([t, t * 0 + 1], 1), torch.full((4, 2), -1.0, device="cuda"), loss, dlogits=out,
+                      teacher=teacher)
+        assert out.isnan().all(1).tolist() == [False, True, False, True] and bool(torch.isfinite(out[::2]).all())
+        assert loss.isnan().tolist() == [False, True, False, True] and loss[2] == INF
