@@ -485,7 +485,7 @@ struct Backward {
     __device__ static __forceinline__ bool wanted(const Params& p, const Fetched& f) {
         bool any = f.d_lse != 0.0f || f.d_h != 0.0f;
 #pragma unroll
-        for (int i = 0; i < kMine; ++i) any = any || term(p, f, i) != 0.0f;
+        for (int i = 0; i < kMine; ++i) any = any || (f.at[i] >= 0 && f.x[i] != 0.0f);
         return __any_sync(0xffffffffu, any);
     }
 

@@ -205,3 +205,15 @@ def test_gradients_of_a_token_that_is_not_in_the_vocabulary(qn, vocab, dtype):
                       teacher=teacher)
         assert out.isnan().all(1).tolist() == [False, True, False, True] and bool(torch.isfinite(out[::2]).all())
         assert loss.isnan().tolist() == [False, True, False, True] and loss[2] == INF
+
+
+@pytest.mark.parametrize("vocab", [60, 150001])
+def test_padding_may_name_any_token(qn, vocab):
+    """Rows whose upstream gradients are all 0 are padding whatever they hold, tokens outside the vocabulary included."""
+    z = ref.make_logits(3, vocab, torch.float32, 9)
+    t = torch.tensor([3, vocab, vocab + 7], device="cuda")
+    g = torch.tensor([1.0, 0.0, 0.0], device="cuda")
+    out = torch.ones_like(z)
+    qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g, d_entropy=g, top_token=t[:, None].contiguous(),
+                            d_top_logprob=g[:, None].contiguous())
+    assert bool((out[1:] == 0).all()) and bool(torch.isfinite(out[0]).all()) and float(out[0].abs().max()) > 0
