@@ -411,7 +411,8 @@ QN_API qn_status qn_logprobs(int64_t rows, int64_t vocab, qn_dtype dtype, const 
  *   tokens      needed with d_logprob; rows whose token is < 0 ignore their d_logprob
  *   top_token   needed with d_top_logprob; entries < 0 ignore their gradient.  A token may occur more than once.
  *   dlogits     DEVICE, [rows] of vocab elements dlogits_stride >= vocab apart, each element written; either `logits`
- *               itself (same pointer and stride: the gradient takes the logits' place) or memory that does not overlap it
+ *               itself (same pointer and stride: the gradient takes the logits' place), or memory apart from it, or, with
+ *               the same stride, rows that lie between those of the logits (two halves of one buffer's rows)
  * A row whose upstream gradients are all 0 is padding: whatever it holds, and whatever its tokens are, its gradient is 0.
  * An empty row's gradient is 0 but for the 1[..] terms.  vocab <= QN_GRAD_MAX_VOCAB.
  */

@@ -38,14 +38,22 @@ inline size_t matrix_bytes(int64_t rows, int64_t vocab, int64_t row_stride, qn_d
     return static_cast<size_t>((rows - 1) * row_stride + vocab) * dtype_size(dtype);
 }
 
-// dlogits takes the place of the logits (same pointer and stride) or does not touch them.
+// dlogits takes the place of the logits (same pointer and stride) or does not touch them: the two lie apart, or their rows
+// lie between one another's (same stride).
 inline bool check_gradient(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
                            const void* dlogits, int64_t dlogits_stride, int dev) {
     if (dlogits_stride < vocab || dlogits_stride > INT64_MAX / 8 / rows) return false;
     if (!check_array(dlogits, dtype_size(dtype), dev)) return false;
     if (dlogits == logits && (dlogits_stride == row_stride || rows == 1)) return true;
-    return !overlaps(dlogits, matrix_bytes(rows, vocab, dlogits_stride, dtype), logits,
-                     matrix_bytes(rows, vocab, row_stride, dtype));
+    if (!overlaps(dlogits, matrix_bytes(rows, vocab, dlogits_stride, dtype), logits,
+                  matrix_bytes(rows, vocab, row_stride, dtype)))
+        return true;
+    if (dlogits_stride != row_stride) return false;
+    // elements from some row of the logits to the next row of dlogits
+    const int64_t apart = (reinterpret_cast<intptr_t>(dlogits) - reinterpret_cast<intptr_t>(logits)) /
+                          static_cast<int64_t>(dtype_size(dtype));
+    const int64_t next = (apart % row_stride + row_stride) % row_stride;
+    return next >= vocab && next <= row_stride - vocab;
 }
 
 // A launch whose set-up may overlap the end of the stream's last kernel (see start_after_last), as clusters of `ctas`.

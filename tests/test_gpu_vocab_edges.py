@@ -9,7 +9,8 @@ import pytest
 import torch
 
 import vocab_reference as ref
-from test_gpu_vocab import DTYPES, check_backward, check_distill, check_logprobs, close, some_tokens, upstream
+from test_gpu_vocab import (DTYPES, check_backward, check_distill, check_logprobs, close, make_teacher,
+                            some_tokens, upstream)
 
 pytestmark = pytest.mark.gpu
 
@@ -217,3 +218,48 @@ def test_padding_may_name_any_token(qn, vocab):
     qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g, d_entropy=g, top_token=t[:, None].contiguous(),
                             d_top_logprob=g[:, None].contiguous())
     assert bool((out[1:] == 0).all()) and bool(torch.isfinite(out[0]).all()) and float(out[0].abs().max()) > 0
+
+
+# ---- arguments -----------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(5, 33), (3, 8192), (4, 150001), (3, 160000)])
+def test_gradient_interleaved_with_the_logits(qn, rows, vocab, dtype):
+    """Logits and gradient as the two halves of one buffer's rows, whichever comes first."""
+    near = ref.make_logits(rows, vocab, dtype, 2)
+    t, g = some_tokens(rows, vocab, 1), upstream(rows, 1)
+    token, value = make_teacher(near, 5, 1.0, True, 1)
+    loss, want_loss = torch.zeros(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    for swap in (0, 1):
+        store = torch.zeros((rows, 2 * vocab), dtype=dtype, device="cuda")
+        halves = (store[:, :vocab], store[:, vocab:])
+        z, out = halves[swap], halves[1 - swap]
+        z.copy_(near)
+        qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g, d_entropy=g)
+        apart = torch.zeros((rows, 2 * vocab), dtype=dtype, device="cuda")[:, :vocab]
+        qn.qn_logprobs_backward(z, apart, tokens=t, d_logprob=g, d_entropy=g)
+        assert torch.equal(out, apart) and torch.equal(z, near)
+        qn.qn_distill(z, token, value, loss, dlogits=out)
+        qn.qn_distill(z, token, value, want_loss, dlogits=apart)
+        assert torch.equal(out, apart) and torch.equal(z, near) and torch.equal(loss, want_loss)
+
+
+def test_gradient_that_shares_elements_with_the_logits_is_refused(qn):
+    rows, vocab = 3, 10
+    store = torch.zeros(200, device="cuda")
+    t, g, loss = torch.zeros(rows, dtype=torch.int64, device="cuda"), torch.ones(rows, device="cuda"), torch.zeros(rows, device="cuda")
+    z = store.as_strided((rows, vocab), (25, 1), 30)
+    token, value = torch.zeros((rows, 1), dtype=torch.int64, device="cuda"), torch.zeros((rows, 1), device="cuda")
+
+    def calls(out):
+        yield lambda: qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g)
+        yield lambda: qn.qn_distill(z, token, value, loss, dlogits=out)
+
+    for stride, offset in ((25, 21), (25, 39), (25, 46), (25, 14), (24, 40), (30, 0)):
+        for call in calls(store.as_strided((rows, vocab), (stride, 1), offset)):
+            with pytest.raises(qn.QNError):
+                call()
+    for stride, offset in ((25, 20), (25, 40), (25, 45), (25, 15), (25, 110), (10, 0)):
+        for call in calls(store.as_strided((rows, vocab), (stride, 1), offset)):
+            call()
