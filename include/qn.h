@@ -367,7 +367,8 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  *   rows, vocab     the matrix of logits; rows >= 0 (0: nothing is done), 1 <= vocab < 2^31 - 64
  *   dtype           storage type of logits and dlogits; all other real values are fp32
  *   logits          DEVICE, element (r, i) at r * row_stride + i, row_stride >= vocab; read only
- *   temperature     T > 0: the distribution is softmax(z / T), u_i = z_i / T, p_i = exp(u_i - lse)
+ *   temperature     T > 0: the distribution is softmax(z / T), u_i = z_i / T, p_i = exp(u_i - lse); 1 / T and log2(e) / T
+ *                   must be numbers in fp32 (T from 4.3e-39 to 7e44)
  *   tokens          int64, as torch indexes; tokens < 0 stand for "none"
  * Arithmetic: fp32 with sums per thread, added over the row in a fixed order; a teacher's list and the difference that a
  * distillation loss is in 64 bits; one rounding to the storage type when dlogits is written.  Offsets are 64-bit.

@@ -24,8 +24,9 @@ inline bool check_logits(int64_t rows, int64_t vocab, qn_dtype dtype, const void
     if (!logits || rows < 1 || vocab < 1 || vocab > INT32_MAX - 64 || row_stride < vocab) return false;
     if (dtype != QN_F32 && dtype != QN_BF16) return false;
     if (row_stride > INT64_MAX / 8 / rows || reinterpret_cast<uintptr_t>(logits) % dtype_size(dtype)) return false;
-    const float inv = static_cast<float>(1.0 / temperature);
-    if (!(temperature > 0.0) || !isfinite(inv) || !(inv > 0.0f)) return false;
+    // 1 / T and log2(e) / T, which the kernels get in 32 bits
+    const float inv = static_cast<float>(1.0 / temperature), scale = static_cast<float>(1.4426950408889634 / temperature);
+    if (!(temperature > 0.0) || !(inv > 0.0f) || !isfinite(scale)) return false;
     return device_of(logits, dev);
 }
 

@@ -263,3 +263,20 @@ def test_gradient_that_shares_elements_with_the_logits_is_refused(qn):
     for stride, offset in ((25, 20), (25, 40), (25, 45), (25, 15), (25, 110), (10, 0)):
         for call in calls(store.as_strided((rows, vocab), (stride, 1), offset)):
             call()
+
+
+def test_temperatures_whose_inverse_does_not_fit_are_refused(qn):
+    """1 / T still fits in 32 bits for these, log2(e) / T does not; the smallest that fit give numbers."""
+    z = ref.make_logits(2, 50, torch.float32, 1)
+    z[:, 7] = 100.0
+    t, v = torch.full((2,), 7, device="cuda"), torch.zeros(2, device="cuda")
+    token, value = t[:, None].contiguous(), torch.zeros((2, 1), device="cuda")
+    out = torch.zeros_like(z)
+    for temperature in (3e-39, 4e-39):
+        for call in (lambda x: qn.qn_logprobs(z, t, v, temperature=x),
+                     lambda x: qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=v, temperature=x),
+                     lambda x: qn.qn_distill(z, token, value, v, dlogits=out, temperature=x)):
+            with pytest.raises(qn.QNError):
+                call(temperature)
+    qn.qn_logprobs(z, t, v, temperature=5e-39)
+    assert v.tolist() == [0.0, 0.0]
