@@ -498,7 +498,7 @@ def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, log
     rows, vocab, stride, code = _logit_matrix(logits, "logits")
     dev, k = logits.get_device(), 0
     if top_token is not None or top_logprob is not None:
-        if top_token is None or top_logprob is None or top_token.dim() != 2:
+        if top_token is None or top_logprob is None or top_token.dim() != 2 or top_token.shape != top_logprob.shape:
             raise ValueError("top_token and top_logprob go together, [rows][k] each")
         k = top_token.shape[1]
     f32 = torch.float32
@@ -506,8 +506,8 @@ def qn_logprobs(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, log
                              _beside(tokens, torch.int64, rows, 0, dev, "tokens"), temperature,
                              _beside(logprob, f32, rows, 0, dev, "logprob"), _beside(lse, f32, rows, 0, dev, "lse"),
                              _beside(entropy, f32, rows, 0, dev, "entropy"), k,
-                             _beside(top_token, torch.int64, rows, k, dev, "top_token"),
-                             _beside(top_logprob, f32, rows, k, dev, "top_logprob"), _stream_on(dev, stream)),
+                             _beside(top_token, torch.int64, rows, k, dev, "top_token") if k else 0,
+                             _beside(top_logprob, f32, rows, k, dev, "top_logprob") if k else 0, _stream_on(dev, stream)),
            "qn_logprobs")
 
 

@@ -280,3 +280,20 @@ def test_temperatures_whose_inverse_does_not_fit_are_refused(qn):
                 call(temperature)
     qn.qn_logprobs(z, t, v, temperature=5e-39)
     assert v.tolist() == [0.0, 0.0]
+
+
+def test_no_alternatives_of_width_zero(qn):
+    """top_token [rows][0] is k = 0, as d_top_logprob [rows][0] is."""
+    z = ref.make_logits(4, 100, torch.float32, 1)
+    t, g = some_tokens(4, 100, 1), upstream(4, 1)
+    none, none_lp = torch.empty((4, 0), dtype=torch.int64, device="cuda"), torch.empty((4, 0), device="cuda")
+    lp, want = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda")
+    qn.qn_logprobs(z, t, want)
+    qn.qn_logprobs(z, t, lp, top_token=none, top_logprob=none_lp)
+    assert torch.equal(lp, want)
+    out, same = torch.zeros_like(z), torch.zeros_like(z)
+    qn.qn_logprobs_backward(z, out, tokens=t, d_logprob=g)
+    qn.qn_logprobs_backward(z, same, tokens=t, d_logprob=g, top_token=none, d_top_logprob=none_lp)
+    assert torch.equal(out, same)
+    with pytest.raises(ValueError, match="top_logprob"):
+        qn.qn_logprobs(z, t, lp, top_token=none, top_logprob=torch.empty((4, 1), device="cuda"))
