@@ -71,9 +71,8 @@ __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
 __device__ __forceinline__ void mbar_complete_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-// A bounded wait of a warp; all its lanes get the same answer, so that they leave together.  Its slow part is out of line
-// (instruction cache), and leaves the warp suspended for up to 20 us at a time instead of polling: with polls in their place
-// half of the instructions that the SM issued were those of waiting warps.
+// A bounded wait.  Its slow part is out of line (instruction cache), and leaves the warp suspended for up to 20 us at a time
+// instead of polling: with polls in their place half of the instructions that the SM issued were those of waiting warps.
 __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort) {
     const uint64_t began = global_timer_ns();
     for (uint32_t it = 0; it < kWaitLimit; ++it) {
@@ -90,11 +89,15 @@ __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile 
     *abort = 1;
     return false;
 }
+__device__ __forceinline__ bool wait_lane(uint64_t* bar, uint32_t parity, volatile int* abort) {
+    return mbar_try(bar, parity) || wait_slow(bar, parity, abort);
+}
+// With one answer for all lanes of the warp, so that they leave together.
 __device__ __forceinline__ bool wait(uint64_t* bar, uint32_t parity, volatile int* abort) {
     return __all_sync(0xffffffffu, mbar_try(bar, parity)) || __all_sync(0xffffffffu, wait_slow(bar, parity, abort));
 }
 
-// A warp's wait for the copy of one item, where the last item in that slot may still be on its way.  A parity cannot tell the
+// A lane's wait for the copy of one item, where the last item in that slot may still be on its way.  A parity cannot tell the
 // phase before from the one after, so the slot also says which item it was last issued for.  That is read before the barrier:
 // once it is this item, the phase before has ended.
 __device__ __noinline__ bool wait_copy_slow(uint64_t* bar, uint32_t parity, volatile uint32_t* issued, uint32_t item, volatile int* abort) {
@@ -113,13 +116,26 @@ __device__ __noinline__ bool wait_copy_slow(uint64_t* bar, uint32_t parity, vola
 __device__ __forceinline__ bool wait_copy(uint64_t* bar, uint32_t parity, volatile uint32_t* issued, uint32_t item, volatile int* abort) {
     const uint32_t last = *issued;
     const bool here = mbar_try(bar, parity) && last == item;
-    return __all_sync(0xffffffffu, here) || __all_sync(0xffffffffu, wait_copy_slow(bar, parity, issued, item, abort));
+    return here || wait_copy_slow(bar, parity, issued, item, abort);
 }
 
 // Before an arrival after which a bulk copy may write what this thread wrote.
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
-// ---- the way out of a kernel in which a wait ran out (kSlots and kLists are those of the ring and of the lists) ----------
+// ---- when a wait ran out (kSlots and kLists are those of the ring and of the lists) ---------------------------------------
+//
+// No CTA may leave while another one may still send into its shared memory, nor while a copy or a message into it is on its way.
+// Those that were waited for have arrived, and once its warps are through with all rows, all have.  So every warp simply ends,
+// but for the join warp: it keeps the CTA until all other threads of the cluster have ended or have come to the same barrier
+// (every wait is bounded, so that they do).  If a wait ran out, the copy warp first waits for its copies, and the join warp after
+// the barrier for the messages that were sent; a sum warp that ends early tells how many those are.
+
+// Sum warp, once it has sent the messages of `u` wanted rows and will send no more.
+__device__ __noinline__ void tell_sent(const uint64_t* sent, uint32_t ctas, uint32_t u) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (lane < ctas) store_remote(sent, lane, u);
+    asm volatile("fence.acq_rel.cluster;" ::: "memory");
+}
 
 // Copy warp: waits for the last copy into each slot, of the items before `begun` and of the lanes of `mask` after it.
 __device__ __noinline__ void wait_copies(uint64_t* full, uint32_t begun, uint32_t mask, volatile int* late) {
@@ -132,8 +148,8 @@ __device__ __noinline__ void wait_copies(uint64_t* full, uint32_t begun, uint32_
     if (mask >> lane & 1) wait_slow(&full[(begun + lane) % kSlots], (begun + lane) / kSlots & 1, late);
 }
 
-// Join warp: waits for the messages of row u, if they are `expected` already, and of those after it, as many as were sent; the
-// `all` warps that send have sent those of rows below sent[i].
+// Join warp: waits for the messages of row u, if they are `expected` already, and of those after it, as many as were sent: the
+// `all` warps that send have sent those of rows below sent[i], or of all rows.
 __device__ __noinline__ void wait_messages(uint64_t* heard, const uint64_t* sent, uint32_t u, bool expected, int all, volatile int* late) {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
@@ -299,14 +315,12 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists], retired[kLists];
     __shared__ uint32_t issued[kWrite ? 1 : kSlots];  // the item that each slot's last copy is of (see wait_copy)
     __shared__ bool wanted[kLists];
-    __shared__ int abort, late;  // a wait ran out; one on the way out did
-    // on the way out: how many wanted rows' messages each sum warp has sent, and the join warp has heard (x 2, + 1 if it has
-    // announced the next row's)
-    __shared__ uint64_t sent[kMaxCluster * kMessages];
-    __shared__ uint32_t heard_of;
+    __shared__ int abort, late;  // a wait ran out; one after that did
+    __shared__ uint64_t sent[kMaxCluster * kMessages];  // of how many wanted rows each sum warp sent its message, if not of all
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!kWrite && threadIdx.x < kSlots) issued[threadIdx.x] = ~0u;
+    if (threadIdx.x < kMaxCluster * kMessages) sent[threadIdx.x] = ~0ull;
     if (threadIdx.x == 0) {
         abort = late = 0;
 #pragma unroll 1
@@ -327,10 +341,12 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     auto chunks_of = [](const Slice<T>& s) { return (s.count + kChunk - 1) / kChunk; };
     // rounds of a ring: item n is in slot n % size, and is the (n / size)-th there
     auto wait_item = [&](uint64_t* bars, uint32_t n, uint32_t size) { return wait(&bars[n % size], n / size & 1, &abort); };
-    auto wait_free = [&](uint64_t* bars, uint32_t n, uint32_t size) { return wait(&bars[n % size], (n / size & 1) ^ 1, &abort); };
+    // by each lane for itself, where a vote is dear: for every chunk, and on the way to a row's coefficients (votes for these took
+    // 2 to 4 %)
+    auto wait_alone = [&](uint64_t* bars, uint32_t n, uint32_t size) { return wait_lane(&bars[n % size], n / size & 1, &abort); };
     // A CTA sends a row's messages once it has joined the row before the last.  So whoever has heard all of row u knows that
     // every CTA has joined u - 2, and may send u + 2: four sets of messages never meet
-    auto may_send = [&](uint32_t u) { return u < 2 || wait_item(joined, u - 2, kLists); };
+    auto may_send = [&](uint32_t u) { return u < 2 || wait_alone(joined, u - 2, kLists); };
     auto send = [&](uint32_t u, int index, float4 msg) {
         if (lane < static_cast<int>(ctas))
             store_async(&inbox[u % kLists][rank * kMessages + index], &heard[u % kLists], lane, msg);
@@ -345,7 +361,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            if (!wait_item(ready, turn, kLists)) goto sent_last;
+            if (!wait_alone(ready, turn, kLists)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
             if (wanted[li]) {
                 const Slice<T> s = slice_of(r);
                 const int chunks = chunks_of(s);
@@ -368,14 +384,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                     const uint32_t slot = (n + c) % kSlots;
                     if constexpr (kWrite) {
                         while (n + c >= sure) {
-                            if (!wait_item(joined, known, kLists)) goto sent_last;
+                            if (!wait_alone(joined, known, kLists)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
                             sure = (++known == u ? n : one_before) + kSlots;
                         }
-                        if (!wait_item(full, n + c, kSlots)) goto sent_last;
+                        if (!wait_alone(full, n + c, kSlots)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
                     } else if (n + c < sure) {
-                        if (!wait_item(full, n + c, kSlots)) goto sent_last;
+                        if (!wait_alone(full, n + c, kSlots)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
                     } else {
-                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) goto sent_last;
+                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
                     }
                     if constexpr (Op::kMask) {
                         const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
@@ -430,6 +446,8 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                         if (lane == 0) mbar_arrive(&empty[slot]);
                     }
                 }
+                // a lane that left alone has set `abort`: then the sums are not those of the row, and the message says NaN
+                const int left_alone = *static_cast<volatile int*>(&abort);
                 two_before = one_before, one_before = n;
                 n += chunks;
                 if (patched) fence_async();
@@ -446,16 +464,15 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                     msg.z = warp_reduce<float, add_op>(msg.z);
                 }
                 msg.y = warp_reduce<float, add_op>(msg.y);
-                if (!may_send(u)) goto sent_last;
+                msg.y = left_alone ? NAN : msg.y;
+                if (!may_send(u)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
                 send(u, worker, msg);
                 ++u;
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-    sent_last:
-        if (ctas > 1 && lane < static_cast<int>(ctas)) store_remote(&sent[rank * kMessages + warp], lane, u);
-        goto out;
+        return;
     }
     if constexpr (kWrite) if (warp < kSumWarps + kWriteWarps) {
         constexpr int NT = 32 * kWriteWarps;
@@ -464,12 +481,11 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            bool ok = wait_item(ready, turn, kLists);
-            if (ok && wanted[li]) ok = wait_item(joined, u, kLists);
-            if (!ok) {  // a wait ran out: what is left becomes NaN
+            const bool ok = wait_alone(ready, turn, kLists) && (!wanted[li] || wait_alone(joined, u, kLists));
+            if (!__all_sync(0xffffffffu, ok)) {  // a wait ran out: what is left becomes NaN
 #pragma unroll 1
                 for (; (r = rows.row()) < p.rows; rows.next()) write_constant<T, NT>(out_of(r), slice_of(r), tid, NAN);
-                goto out;
+                return;
             }
             const Slice<T> s = slice_of(r);
             if (!wanted[li]) {
@@ -486,7 +502,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
                     for (int c = (w + kWriteWarps - turn % kWriteWarps) % kWriteWarps; c < chunks; c += kWriteWarps) {
                         const uint32_t slot = (n + c) % kSlots;
-                        wait_item(full, n + c, kSlots);  // it has been: this thread sees the chunk too
+                        wait_alone(full, n + c, kSlots);  // it has been: this thread sees the chunk too
                         const uint4* data = ring + slot * kChunk + lane;
                         auto gradient = [&](const uint4& v) {
                             float y[kVec];
@@ -546,17 +562,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-        goto out;
+        return;
     }
     if (warp == kSumWarps + kWriteWarps) {
         // ---- copy warp
         Walk rows = walk;
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
-            if (!wait_item(ready, turn, kLists)) {
-                wait_copies(full, n, 0, &late);
-                goto out;
-            }
+            if (!wait_item(ready, turn, kLists)) return wait_copies(full, n, 0, &late);
             const bool want = wanted[turn % kLists];
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[turn % kLists]);
@@ -577,10 +590,8 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                 uint32_t pending = group;
                 while (pending) {
                     const uint32_t first = n + c0 + __ffs(pending) - 1;  // slots come free in about this order
-                    if (!wait_free(empty, first, kSlots)) {
-                        wait_copies(full, n + c0, group & ~pending, &late);
-                        goto out;
-                    }
+                    if (!wait(&empty[first % kSlots], (first / kSlots & 1) ^ 1, &abort))
+                        return wait_copies(full, n + c0, group & ~pending, &late);
                     const bool mine = (pending >> lane & 1) && mbar_try(&empty[slot], parity);
                     if (mine) {
                         if (b1 > b0) {
@@ -597,7 +608,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             }
             n += chunks;
         }
-        goto out;
+        return;
     }
     if (warp == kSumWarps + kWriteWarps + 1) {
         // ---- join warp
@@ -606,13 +617,13 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
         for (; rows.row() < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            if (!wait_item(ready, turn, kLists)) goto heard_last;
+            if (!wait_item(ready, turn, kLists)) break;
             if (wanted[li]) {
                 const int set = u % kLists;
                 if (lane == 0) mbar_arrive_expect_tx(&heard[set], ctas * (kMessages * 16u));
                 __syncwarp();
                 expected = true;
-                if (!wait_item(heard, u, kLists)) goto heard_last;
+                if (!wait_item(heard, u, kLists)) break;
                 expected = false;
                 Op::template join<kSumWarps>(p, lists[li], inbox[set], static_cast<int>(ctas));
                 __syncwarp();
@@ -622,9 +633,12 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[li]);
         }
-    heard_last:
-        if (lane == 0) heard_of = 2 * u + expected;
-        goto out;
+        __syncwarp();
+        if (ctas > 1) {
+            cluster_sync();
+            if (abort) wait_messages(heard, sent, u, expected, static_cast<int>(ctas) * kMessages, &late);
+        }
+        return;
     }
     if (warp == kSumWarps + kWriteWarps + 2) {
         // ---- end warp: what is left to do of a row once the others are through with it
@@ -641,97 +655,85 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         if (rank == 0 && lane == 0)  // a wait ran out, if any rows are left
 #pragma unroll 1
             for (; rows.row() < p.rows; rows.next()) Op::without(p, rows.row(), NAN);
-        goto out;
+        return;
     }
-    {
-        // ---- list warps
-        turn = warp - (kSumWarps + kWriteWarps + 3);
-        Walk rows = walk;
-        rows.next(turn);
-        Walk ahead = rows;
-        ahead.next(kListWarps);
-        typename Op::Fetched next = Op::fetch(p, rows.row()), later = Op::fetch(p, ahead.row());
-        Op::template gather<T>(p, rows.row(), next);
-        // an element of the first or last vector of a slice, where that reaches past the row
-        auto edge_of = [&](int64_t r) {
-            if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
-            const Slice<T> s = slice_of(r);
-            const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
-            return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
-        };
-        T edge = edge_of(rows.row());
+    // ---- list warps
+    turn = warp - (kSumWarps + kWriteWarps + 3);
+    Walk rows = walk;
+    rows.next(turn);
+    Walk ahead = rows;
+    ahead.next(kListWarps);
+    typename Op::Fetched next = Op::fetch(p, rows.row()), later = Op::fetch(p, ahead.row());
+    Op::template gather<T>(p, rows.row(), next);
+    // an element of the first or last vector of a slice, where that reaches past the row
+    auto edge_of = [&](int64_t r) {
+        if (!kEdges || r >= p.rows || lane >= 2 * kVec) return masked<T>();
+        const Slice<T> s = slice_of(r);
+        const int32_t i = s.origin() + (lane < kVec ? lane : (s.count - 2) * kVec + lane);
+        return s.count > 0 && i >= 0 && i < s.vocab ? row_of(r)[i] : masked<T>();
+    };
+    T edge = edge_of(rows.row());
 #pragma unroll 1
-        for (int64_t r; (r = rows.row()) < p.rows; rows.next(kListWarps), turn += kListWarps) {
-            const int li = turn % kLists;
-            typename Op::Shared& sh = lists[li];
-            if (turn >= kLists && !wait_item(retired, turn - kLists, kLists)) goto out;
-            const typename Op::Fetched now = next;
-            next = later;
-            const int64_t following = ahead.row();
-            ahead.next(kListWarps);
-            Op::template gather<T>(p, following, next);
-            later = Op::fetch(p, ahead.row());
-            const T edge_now = edge;
-            edge = edge_of(following);
-            const bool want = Op::wanted(p, now);
-            if (want) {
-                Op::begin(p, sh, now);
-                if (kEdges && lane < 2 * kVec) reinterpret_cast<T*>(edges[li])[lane] = edge_now;
-                if constexpr (Op::kMask) {
-                    // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
-                    const Slice<T> s = slice_of(r);
-                    chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
+    for (int64_t r; (r = rows.row()) < p.rows; rows.next(kListWarps), turn += kListWarps) {
+        const int li = turn % kLists;
+        typename Op::Shared& sh = lists[li];
+        if (turn >= kLists && !wait_item(retired, turn - kLists, kLists)) return;
+        const typename Op::Fetched now = next;
+        next = later;
+        const int64_t following = ahead.row();
+        ahead.next(kListWarps);
+        Op::template gather<T>(p, following, next);
+        later = Op::fetch(p, ahead.row());
+        const T edge_now = edge;
+        edge = edge_of(following);
+        const bool want = Op::wanted(p, now);
+        if (want) {
+            Op::begin(p, sh, now);
+            if (kEdges && lane < 2 * kVec) reinterpret_cast<T*>(edges[li])[lane] = edge_now;
+            if constexpr (Op::kMask) {
+                // the special elements in this slice by chunk: how many each has, where it begins, and each element's place
+                const Slice<T> s = slice_of(r);
+                chunk_begin[li][lane] = chunk_begin[li][lane + 32] = 0;
+                __syncwarp();
+                int in[Op::kMine], place[Op::kMine];
+#pragma unroll
+                for (int i = 0; i < Op::kMine; ++i) {
+                    const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
+                    in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
+                    place[i] = 0;
+                    if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
+                    const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
+                    if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
                     __syncwarp();
-                    int in[Op::kMine], place[Op::kMine];
-#pragma unroll
-                    for (int i = 0; i < Op::kMine; ++i) {
-                        const int k = lane + 32 * i, pos = k < Op::entries(p) ? sh.pos[k] : -1;
-                        in[i] = s.holds(pos) ? (pos - s.origin()) / (kChunk * kVec) : -1;
-                        place[i] = 0;
-                        if (!__any_sync(0xffffffffu, in[i] >= 0)) continue;
-                        const uint32_t same = __match_any_sync(0xffffffffu, in[i]);
-                        if (in[i] >= 0) place[i] = chunk_begin[li][in[i] + 1] + __popc(same & ((1u << lane) - 1));
-                        __syncwarp();
-                        if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
-                        __syncwarp();
-                    }
-                    int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
-#pragma unroll
-                    for (int o = 1; o < 32; o *= 2) {
-                        const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
-                        if (lane >= o) a += up, b += up2;
-                    }
-                    b += __shfl_sync(0xffffffffu, a, 31);
+                    if (in[i] >= 0 && (same >> lane) == 1) chunk_begin[li][in[i] + 1] += __popc(same);  // the last of its chunk
                     __syncwarp();
-                    chunk_begin[li][lane] = static_cast<uint8_t>(a);
-                    chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
-                    __syncwarp();
+                }
+                int a = chunk_begin[li][lane], b = chunk_begin[li][lane + 32];
 #pragma unroll
-                    for (int i = 0; i < Op::kMine; ++i)
-                        if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
+                for (int o = 1; o < 32; o *= 2) {
+                    const int up = __shfl_up_sync(0xffffffffu, a, o), up2 = __shfl_up_sync(0xffffffffu, b, o);
+                    if (lane >= o) a += up, b += up2;
+                }
+                b += __shfl_sync(0xffffffffu, a, 31);
+                __syncwarp();
+                chunk_begin[li][lane] = static_cast<uint8_t>(a);
+                chunk_begin[li][lane + 32] = static_cast<uint8_t>(b);
+                __syncwarp();
 #pragma unroll
-                    for (int i = 0; i < Op::kMine; ++i) {  // and in the edges
-                        if (!kEdges || in[i] < 0) continue;
-                        const int32_t at = sh.pos[lane + 32 * i] - s.origin(), last = at - (s.count - 1) * kVec;
-                        if (at < kVec) reinterpret_cast<T*>(edges[li])[at] = masked<T>();
-                        if (last >= 0) reinterpret_cast<T*>(edges[li])[kVec + last] = masked<T>();
-                    }
+                for (int i = 0; i < Op::kMine; ++i)
+                    if (in[i] >= 0) order[li][chunk_begin[li][in[i]] + place[i]] = static_cast<uint8_t>(lane + 32 * i);
+#pragma unroll
+                for (int i = 0; i < Op::kMine; ++i) {  // and in the edges
+                    if (!kEdges || in[i] < 0) continue;
+                    const int32_t at = sh.pos[lane + 32 * i] - s.origin(), last = at - (s.count - 1) * kVec;
+                    if (at < kVec) reinterpret_cast<T*>(edges[li])[at] = masked<T>();
+                    if (last >= 0) reinterpret_cast<T*>(edges[li])[kVec + last] = masked<T>();
                 }
             }
-            if (lane == 0) wanted[li] = want;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&ready[li]);
         }
-    }
-out:
-    // The way out of every warp, also of one whose wait ran out: no CTA leaves while another one may still send into it, nor
-    // while a copy or a message into it is on its way (those that were waited for have arrived).  Every wait so far is
-    // bounded, so all warps of the cluster come here.
-    __syncwarp();
-    if (ctas > 1) {
-        cluster_sync();
-        if (warp == kSumWarps + kWriteWarps + 1 && abort)
-            wait_messages(heard, sent, heard_of / 2, heard_of % 2, static_cast<int>(ctas) * kMessages, &late);
+        if (lane == 0) wanted[li] = want;
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&ready[li]);
     }
 }
 
