@@ -120,7 +120,6 @@ struct Distill {
         // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
         double q_sum = 0.0;
         double q_total = 0.0, q_log_q = 0.0;
-        float noise = 0.0f;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int j = lane + 32 * i;
@@ -128,7 +127,7 @@ struct Distill {
             const double log_q = (static_cast<double>(v[i]) - top) * inv - log_norm, q = exp64(log_q);
             q_sum += q;
             const float q32 = static_cast<float>(q);
-            if (q32 != 0.0f) q_log_q += q32 * log_q, noise += q32 * (1.0f + fabsf(v[i]));
+            if (q32 != 0.0f) q_log_q += q32 * log_q;
             q_total += q32;
             sh.q[j] = q32;
         }
@@ -146,7 +145,6 @@ struct Distill {
         q_sum = warp_reduce<double, add_op>(q_sum);
         q_total = warp_reduce<double, add_op>(q_total);
         q_log_q = warp_reduce<double, add_op>(q_log_q);
-        noise = warp_reduce<float, add_op>(noise);
         if (lane == 0) {
             sh.weight = f.weight;
             sh.list_m = list_m;
@@ -155,7 +153,7 @@ struct Distill {
             sh.q_total = q_total;
             sh.q_log_q = q_log_q;
             sh.q_rest = 0.0f;
-            sh.q_noise = noise * (p.value_bf16 ? 0x1p-9f : 0x1p-18f);
+            sh.q_noise = static_cast<float>(q_total - q_log_q) * (p.value_bf16 ? 0x1p-9f : 0x1p-18f);
             if (p.logprobs && named < p.vocab) sh.q_rest = q_sum != q_sum ? NAN : static_cast<float>(fmax(0.0, 1.0 - q_sum));
         }
         __syncwarp();
@@ -199,16 +197,17 @@ struct Distill {
     template <typename T>
     __device__ static void fix(const Params& p, const Shared& sh, const Slice<T>& s, T* out, int64_t r, bool first) {
         const Gradient g = sh.g;
+        const float m = sh.m;
         if (out)
 #pragma unroll 1
             for (int j = threadIdx.x & 31; j < p.k; j += 32)
                 if (s.holds(sh.pos[j]))
-                    Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - sh.m) * p.scale) - g.unit * sh.q[j]);
+                    Storage<T>::store1(out + sh.pos[j], g.on * exp2_approx((sh.z[j] - m) * p.scale) - g.unit * sh.q[j]);
         if (!first) return;
         // sum q (ln q - ln p) with ln p = ln 2 s (z - m) - ln S: the small difference of these sums, so in 64 bits
         double dot = 0.0;
         for (int j = threadIdx.x & 31; j < p.k; j += 32)
-            if (sh.pos[j] >= 0 && sh.q[j] > 0.0f) dot += sh.q[j] * (static_cast<double>(sh.z[j]) - sh.m);
+            if (sh.pos[j] >= 0 && sh.q[j] > 0.0f) dot += sh.q[j] * (static_cast<double>(sh.z[j]) - m);
         dot = warp_reduce<double, add_op>(dot);
         if ((threadIdx.x & 31) == 0) {
             const double log_s = log64(static_cast<double>(sh.s));
@@ -217,7 +216,7 @@ struct Distill {
                 loss = sh.q_log_q - 0.6931471805599453 * p.scale * dot + sh.q_total * log_s;
                 if (sh.q_rest != 0.0f) {
                     const double log_rest = log64(static_cast<double>(sh.rest)) +
-                                            0.6931471805599453 * p.scale * (static_cast<double>(sh.m_rest) - sh.m);
+                                            0.6931471805599453 * p.scale * (static_cast<double>(sh.m_rest) - m);
                     loss += sh.q_rest * (logf(sh.q_rest) - log_rest + log_s);
                 }
             }
