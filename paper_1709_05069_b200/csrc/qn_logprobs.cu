@@ -48,7 +48,7 @@ struct LogprobParams {
 };
 
 struct LogprobShared {
-    float4 sums[kThreads / 32];
+    float2 sums[kThreads / 32];
     float max[kThreads / 32];
     float4 part[kTopCluster];  // of the cluster's CTAs: maximum, S, E
     int32_t count, hot_count;
@@ -138,7 +138,7 @@ __device__ __noinline__ float4 slice_slow(const T* row, const Slice<T> s, float 
         sum += e;
         if (e != 0.0f) moment += e * d;
     }
-    const float4 x = block_sum4<kThreads>(make_float4(sum, moment, 0.0f, 0.0f), sh.sums);
+    const float2 x = block_sum2<kThreads>(make_float2(sum, moment), sh.sums);
     return make_float4(m, x.x, x.y, 0.0f);
 }
 
@@ -255,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
             float s0, s1, e0, e1;
             unpack2(sum, s0, s1);
             unpack2(moment, e0, e1);
-            float4 x = make_float4(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f, 0.0f, 0.0f);
+            float2 x = make_float2(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f);
             x.x = warp_reduce<float, add_op>(x.x);
             x.y = warp_reduce<float, add_op>(x.y);
             if (lane == 0) sh.sums[warp] = x;

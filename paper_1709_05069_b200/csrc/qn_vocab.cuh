@@ -11,7 +11,6 @@ namespace {
 
 using namespace qn;
 
-constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 // ---- host ----------------------------------------------------------------------------------------------------------
@@ -108,7 +107,6 @@ __device__ __forceinline__ float key_value(uint64_t key) {
 __device__ __forceinline__ float add_op(float a, float b) { return a + b; }
 __device__ __forceinline__ double add_op(double a, double b) { return a + b; }
 __device__ __forceinline__ float max_op(float a, float b) { return fmaxf(a, b); }
-__device__ __forceinline__ uint64_t max_op(uint64_t a, uint64_t b) { return a > b ? a : b; }
 
 template <typename V, V (*op)(V, V)>
 __device__ __forceinline__ V warp_reduce(V x) {
@@ -117,22 +115,19 @@ __device__ __forceinline__ V warp_reduce(V x) {
     return x;
 }
 
-// Sums of four values over the CTA, in a fixed order, with one pair of barriers.
+// Sums of two values over a CTA of NT threads, in a fixed order, with one pair of barriers.
 template <int NT>
-__device__ __forceinline__ float4 block_sum4(float4 x, float4* scratch) {
+__device__ __forceinline__ float2 block_sum2(float2 x, float2* scratch) {
     x.x = warp_reduce<float, add_op>(x.x);
     x.y = warp_reduce<float, add_op>(x.y);
-    x.z = warp_reduce<float, add_op>(x.z);
-    x.w = warp_reduce<float, add_op>(x.w);
-    if constexpr (NT == 32) return x;
     __syncthreads();  // scratch may still be read from the last use
     if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = x;
     __syncthreads();
     x = scratch[0];
 #pragma unroll
     for (int w = 1; w < NT / 32; ++w) {
-        const float4 y = scratch[w];
-        x.x += y.x, x.y += y.y, x.z += y.z, x.w += y.w;
+        const float2 y = scratch[w];
+        x.x += y.x, x.y += y.y;
     }
     return x;
 }

@@ -493,69 +493,67 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
             } else {
                 ++u;
                 const int chunks = chunks_of(s);
-                if (p.dlogits) {
-                    T* out = out_of(r);
-                    const Gradient g = lists[li].g;
-                    const f32x2 minus = pack2(-g.m, -g.m), scale = pack2(p.scale, p.scale);
-                    const f32x2 c0 = pack2(g.c0, g.c0), c1 = pack2(g.c1, g.c1);
-                    const int32_t fb = s.full_begin(), fe = s.full_end();
+                T* out = out_of(r);
+                const Gradient g = lists[li].g;
+                const f32x2 minus = pack2(-g.m, -g.m), scale = pack2(p.scale, p.scale);
+                const f32x2 c0 = pack2(g.c0, g.c0), c1 = pack2(g.c1, g.c1);
+                const int32_t fb = s.full_begin(), fe = s.full_end();
 #pragma unroll 1
-                    for (int c = (w + kWriteWarps - turn % kWriteWarps) % kWriteWarps; c < chunks; c += kWriteWarps) {
-                        const uint32_t slot = (n + c) % kSlots;
-                        wait_alone(full, n + c, kSlots);  // it has been: this thread sees the chunk too
-                        const uint4* data = ring + slot * kChunk + lane;
-                        auto gradient = [&](const uint4& v) {
-                            float y[kVec];
+                for (int c = (w + kWriteWarps - turn % kWriteWarps) % kWriteWarps; c < chunks; c += kWriteWarps) {
+                    const uint32_t slot = (n + c) % kSlots;
+                    wait_alone(full, n + c, kSlots);  // it has been: this thread sees the chunk too
+                    const uint4* data = ring + slot * kChunk + lane;
+                    auto gradient = [&](const uint4& v) {
+                        float y[kVec];
 #pragma unroll
-                            for (int i = 0; i < kPairs; ++i) {
-                                const f32x2 d = mul2(add2(Lanes<T>::pair(v, i), minus), scale), e = exp2_pair(d);
-                                unpack2(moments ? mul2(e, fma2(finite_pair(d), c1, c0)) : mul2(e, c0), y[2 * i], y[2 * i + 1]);
-                            }
-                            return Storage<T>::pack(y);
-                        };
-                        const int32_t at = s.origin() + (c * kChunk + lane) * kVec;
-                        if (kAligned && c * kChunk >= fb && (c + 1) * kChunk <= fe) {
-                            T* to = out + at;
+                        for (int i = 0; i < kPairs; ++i) {
+                            const f32x2 d = mul2(add2(Lanes<T>::pair(v, i), minus), scale), e = exp2_pair(d);
+                            unpack2(moments ? mul2(e, fma2(finite_pair(d), c1, c0)) : mul2(e, c0), y[2 * i], y[2 * i + 1]);
+                        }
+                        return Storage<T>::pack(y);
+                    };
+                    const int32_t at = s.origin() + (c * kChunk + lane) * kVec;
+                    if (kAligned && c * kChunk >= fb && (c + 1) * kChunk <= fe) {
+                        T* to = out + at;
 #pragma unroll 1
-                            for (int q = 0; q < kChunk / 32; q += 4, data += 128, to += 128 * kVec) {
+                        for (int q = 0; q < kChunk / 32; q += 4, data += 128, to += 128 * kVec) {
 #pragma unroll
-                                for (int h = 0; h < 4; ++h) stg_stream16(to + 32 * kVec * h, gradient(data[32 * h]));
-                            }
-                        } else if (!kAligned) {
-                            // the gradient in place of the chunk, and the chunk, one run of the row, from there
-                            uint4* in_place = ring + slot * kChunk + lane;
-                            const int count = min(kChunk, s.count - c * kChunk);
-                            if (c * kChunk >= fb && (c + 1) * kChunk <= fe) {
+                            for (int h = 0; h < 4; ++h) stg_stream16(to + 32 * kVec * h, gradient(data[32 * h]));
+                        }
+                    } else if (!kAligned) {
+                        // the gradient in place of the chunk, and the chunk, one run of the row, from there
+                        uint4* in_place = ring + slot * kChunk + lane;
+                        const int count = min(kChunk, s.count - c * kChunk);
+                        if (c * kChunk >= fb && (c + 1) * kChunk <= fe) {
 #pragma unroll 1
-                                for (int q = 0; q < kChunk / 32; q += 4, in_place += 128) {
+                            for (int q = 0; q < kChunk / 32; q += 4, in_place += 128) {
 #pragma unroll
-                                    for (int h = 0; h < 4; ++h) in_place[32 * h] = gradient(in_place[32 * h]);
-                                }
-                            } else {
-#pragma unroll 1
-                                for (int j = lane; j < count; j += 32, in_place += 32) {
-                                    const int k = c * kChunk + j;
-                                    *in_place = gradient(k < fb ? edges[li][0] : k >= fe ? edges[li][1] : *in_place);
-                                }
+                                for (int h = 0; h < 4; ++h) in_place[32 * h] = gradient(in_place[32 * h]);
                             }
-                            __syncwarp();
-                            write_run(out, s.origin() + c * (kChunk * kVec), s.origin() + (c * kChunk + count) * kVec, s.vocab,
-                                      reinterpret_cast<const T*>(ring + slot * kChunk));
-                            fence_async();
                         } else {
-                            const int count = min(kChunk, s.count - c * kChunk);
 #pragma unroll 1
-                            for (int q = 0; 32 * q < count; ++q) {
-                                const int j = 32 * q + lane, k = c * kChunk + j;
-                                if (j >= count) break;
-                                const uint4 x = gradient(kEdges && k < fb ? edges[li][0] : kEdges && k >= fe ? edges[li][1] : data[32 * q]);
-                                if (k >= fb && k < fe) stg_stream16(out + at + 32 * q * kVec, x);
-                                else write_edge(out, at + 32 * q * kVec, s.vocab, x);
+                            for (int j = lane; j < count; j += 32, in_place += 32) {
+                                const int k = c * kChunk + j;
+                                *in_place = gradient(k < fb ? edges[li][0] : k >= fe ? edges[li][1] : *in_place);
                             }
                         }
                         __syncwarp();
-                        if (lane == 0) mbar_arrive(&empty[slot]);
+                        write_run(out, s.origin() + c * (kChunk * kVec), s.origin() + (c * kChunk + count) * kVec, s.vocab,
+                                  reinterpret_cast<const T*>(ring + slot * kChunk));
+                        fence_async();
+                    } else {
+                        const int count = min(kChunk, s.count - c * kChunk);
+#pragma unroll 1
+                        for (int q = 0; 32 * q < count; ++q) {
+                            const int j = 32 * q + lane, k = c * kChunk + j;
+                            if (j >= count) break;
+                            const uint4 x = gradient(kEdges && k < fb ? edges[li][0] : kEdges && k >= fe ? edges[li][1] : data[32 * q]);
+                            if (k >= fb && k < fe) stg_stream16(out + at + 32 * q * kVec, x);
+                            else write_edge(out, at + 32 * q * kVec, s.vocab, x);
+                        }
                     }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&empty[slot]);
                 }
                 n += chunks;
             }
