@@ -67,10 +67,6 @@ __device__ __forceinline__ void store_async(const void* mine, const uint64_t* ba
 __device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
     asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
 }
-// Takes bytes off what a barrier still waits for.
-__device__ __forceinline__ void mbar_complete_tx(uint64_t* bar, uint32_t bytes) {
-    asm volatile("mbarrier.complete_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
-}
 // A bounded wait.  Its slow part is out of line (instruction cache), and leaves the warp suspended for up to 20 us at a time
 // instead of polling: with polls in their place half of the instructions that the SM issued were those of waiting warps.
 __device__ __noinline__ bool wait_slow(uint64_t* bar, uint32_t parity, volatile int* abort) {
@@ -128,14 +124,7 @@ __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.
 // Those that were waited for have arrived, and once its warps are through with all rows, all have.  So every warp simply ends,
 // but for the join warp: it keeps the CTA until all other threads of the cluster have ended or have come to the same barrier
 // (every wait is bounded, so that they do).  If a wait ran out, the copy warp first waits for its copies, and the join warp after
-// the barrier for the messages that were sent; a sum warp that ends early tells how many those are.
-
-// Sum warp, once it has sent the messages of `u` wanted rows and will send no more.
-__device__ __noinline__ void tell_sent(const uint64_t* sent, uint32_t ctas, uint32_t u) {
-    const uint32_t lane = threadIdx.x & 31;
-    if (lane < ctas) store_remote(sent, lane, u);
-    asm volatile("fence.acq_rel.cluster;" ::: "memory");
-}
+// the barrier for the messages that were sent: one after the other, until none has come within the limit.
 
 // Copy warp: waits for the last copy into each slot, of the items before `begun` and of the lanes of `mask` after it.
 __device__ __noinline__ void wait_copies(uint64_t* full, uint32_t begun, uint32_t mask, volatile int* late) {
@@ -148,24 +137,13 @@ __device__ __noinline__ void wait_copies(uint64_t* full, uint32_t begun, uint32_
     if (mask >> lane & 1) wait_slow(&full[(begun + lane) % kSlots], (begun + lane) / kSlots & 1, late);
 }
 
-// Join warp: waits for the messages of row u, if they are `expected` already, and of those after it, as many as were sent: the
-// `all` warps that send have sent those of rows below sent[i], or of all rows.
-__device__ __noinline__ void wait_messages(uint64_t* heard, const uint64_t* sent, uint32_t u, bool expected, int all, volatile int* late) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll 1
-    for (;; ++u, expected = false) {
-        int count = 0;
-        for (int i = lane; i < all; i += 32) count += sent[i] > u;
-        count = __reduce_add_sync(0xffffffffu, count);
-        if (count == 0) return;
-        uint64_t* bar = &heard[u % kLists];
-        if (lane == 0) {
-            if (expected) mbar_complete_tx(bar, (all - count) * 16u);
-            else mbar_arrive_expect_tx(bar, count * 16u);
-        }
+// Join warp: waits for the messages of row u (`bytes`, if `expected` announced already), and of those after it.
+__device__ __noinline__ void wait_messages(uint64_t* heard, uint32_t u, bool expected, uint32_t bytes, volatile int* late) {
+    do {
+        if (!expected && (threadIdx.x & 31) == 0) mbar_arrive_expect_tx(&heard[u % kLists], bytes);
         __syncwarp();
-        if (!wait(bar, u / kLists & 1, late)) return;
-    }
+        expected = false;
+    } while (wait(&heard[u % kLists], u / kLists & 1, late) && ++u);
 }
 
 // ---- writing -------------------------------------------------------------------------------------------------------
@@ -315,14 +293,12 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
     __shared__ uint64_t full[kSlots], empty[kSlots], ready[kLists], done[kLists], heard[kLists], joined[kLists], retired[kLists];
     __shared__ uint32_t issued[kWrite ? 1 : kSlots];  // the item that each slot's last copy is of (see wait_copy)
     __shared__ bool wanted[kLists];
-    __shared__ int abort, late;  // a wait ran out; one after that did
-    __shared__ uint64_t sent[kMaxCluster * kMessages];  // of how many wanted rows each sum warp sent its message, if not of all
+    __shared__ int abort, late[2];  // a wait ran out; one after that did, of the copy warp or of the join warp
     const uint32_t ctas = cluster_size(), rank = cluster_rank();
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     if (!kWrite && threadIdx.x < kSlots) issued[threadIdx.x] = ~0u;
-    if (threadIdx.x < kMaxCluster * kMessages) sent[threadIdx.x] = ~0ull;
     if (threadIdx.x == 0) {
-        abort = late = 0;
+        abort = late[0] = late[1] = 0;
 #pragma unroll 1
         for (int i = 0; i < kSlots; ++i) mbar_init(&full[i], 1), mbar_init(&empty[i], 1);
 #pragma unroll 1
@@ -361,7 +337,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
             const int li = turn % kLists;
-            if (!wait_alone(ready, turn, kLists)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+            if (!wait_alone(ready, turn, kLists)) return;
             if (wanted[li]) {
                 const Slice<T> s = slice_of(r);
                 const int chunks = chunks_of(s);
@@ -384,14 +360,14 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                     const uint32_t slot = (n + c) % kSlots;
                     if constexpr (kWrite) {
                         while (n + c >= sure) {
-                            if (!wait_alone(joined, known, kLists)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+                            if (!wait_alone(joined, known, kLists)) return;
                             sure = (++known == u ? n : one_before) + kSlots;
                         }
-                        if (!wait_alone(full, n + c, kSlots)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+                        if (!wait_alone(full, n + c, kSlots)) return;
                     } else if (n + c < sure) {
-                        if (!wait_alone(full, n + c, kSlots)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+                        if (!wait_alone(full, n + c, kSlots)) return;
                     } else {
-                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+                        if (!wait_copy(&full[slot], (n + c) / kSlots & 1, &issued[slot], n + c, &abort)) return;
                     }
                     if constexpr (Op::kMask) {
                         const int begin = chunk_begin[li][c], end = chunk_begin[li][c + 1];
@@ -465,7 +441,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                 }
                 msg.y = warp_reduce<float, add_op>(msg.y);
                 msg.y = left_alone ? NAN : msg.y;
-                if (!may_send(u)) return tell_sent(&sent[rank * kMessages + warp], ctas, u);
+                if (!may_send(u)) return;
                 send(u, worker, msg);
                 ++u;
             }
@@ -567,7 +543,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         Walk rows = walk;
 #pragma unroll 1
         for (int64_t r; (r = rows.row()) < p.rows; rows.next(), ++turn) {
-            if (!wait_item(ready, turn, kLists)) return wait_copies(full, n, 0, &late);
+            if (!wait_item(ready, turn, kLists)) return wait_copies(full, n, 0, &late[0]);
             const bool want = wanted[turn % kLists];
             __syncwarp();
             if (lane == 0) mbar_arrive(&done[turn % kLists]);
@@ -589,7 +565,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                 while (pending) {
                     const uint32_t first = n + c0 + __ffs(pending) - 1;  // slots come free in about this order
                     if (!wait(&empty[first % kSlots], (first / kSlots & 1) ^ 1, &abort))
-                        return wait_copies(full, n + c0, group & ~pending, &late);
+                        return wait_copies(full, n + c0, group & ~pending, &late[0]);
                     const bool mine = (pending >> lane & 1) && mbar_try(&empty[slot], parity);
                     if (mine) {
                         if (b1 > b0) {
@@ -634,7 +610,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
         __syncwarp();
         if (ctas > 1) {
             cluster_sync();
-            if (abort) wait_messages(heard, sent, u, expected, static_cast<int>(ctas) * kMessages, &late);
+            if (abort) wait_messages(heard, u, expected, ctas * (kMessages * 16u), &late[1]);
         }
         return;
     }
