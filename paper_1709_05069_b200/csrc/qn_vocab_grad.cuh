@@ -401,7 +401,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                         if (!(most <= m)) {  // a new maximum, or NaN (then m and all sums become NaN)
                             const float d = (m - most) * p.scale, f = exp2_approx(d);
                             const f32x2 f2 = pack2(f, f);
-                            if (moments && f != 0.0f) moment = mul2(f2, fma2(sum, pack2(d, d), moment));
+                            if (moments) moment = f != 0.0f ? mul2(f2, fma2(sum, pack2(d, d), moment)) : 0;
                             sum = mul2(sum, f2);
                             m = most;
                         }

@@ -297,3 +297,21 @@ def test_no_alternatives_of_width_zero(qn):
     assert torch.equal(out, same)
     with pytest.raises(ValueError, match="top_logprob"):
         qn.qn_logprobs(z, t, lp, top_token=none, top_logprob=torch.empty((4, 1), device="cuda"))
+
+
+# ---- backward: rows whose maximum is far above what comes before it --------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(6, 1000), (5, 30000), (300, 140001), (4, 150000), (40, 300001)])
+@pytest.mark.parametrize("temperature,step", [(1.0, 60.0), (1.0, 200.0), (0.05, 3.0)])
+def test_backward_of_the_entropy_where_the_maximum_rises_in_steps(qn, rows, vocab, temperature, step, dtype):
+    """Each tenth of a row is a step above the one before it (and the other way round in every other row): what was
+    summed before a step weighs nothing after it."""
+    z = ref.make_logits(rows, vocab, dtype, vocab)
+    rise = step * torch.div(10 * torch.arange(vocab, device="cuda"), vocab, rounding_mode="floor")
+    z = (z.float() + torch.where(torch.arange(rows, device="cuda")[:, None] % 2 == 0, rise, rise.flip(0))).to(dtype)
+    t = torch.full((rows,), vocab - 1, device="cuda")
+    check_backward(qn, z, t, temperature, None, None, upstream(rows, 1), None, None)
+    check_backward(qn, z, t, temperature, upstream(rows, 2), upstream(rows, 3), upstream(rows, 4), None, None)
+    check_logprobs(qn, z, t, 3, temperature)
