@@ -436,9 +436,10 @@ QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtyp
  *     QN_TEACHER_LOGPROBS   log probabilities at this temperature, as qn_logprobs writes them: q_k = exp(v_k); all other
  *                           tokens are one more outcome, q_r = max(0, 1 - sum_k q_k) and p_r = sum of p_i off the list:
  *                           L = sum_k q_k (ln q_k - ln p_k) + q_r (ln q_r - ln p_r)
- *                           (a list that names the whole vocabulary has no such outcome; and where the student masks
- *                           everything off the list, a q_r within the rounding of the values, 2^-18 sum_k q_k (1 - v_k)
- *                           or 2^-9 of that sum for bf16 values, counts as 0: teacher and student are masked alike)
+ *                           (a list that names the whole vocabulary has no such outcome; and where the student leaves
+ *                           nothing off the list, p_r = 0 or below e^-1000 as by masks, a q_r within the rounding of the
+ *                           values, 2^-18 sum_k q_k (1 - v_k) or 2^-9 of that sum for bf16 values, counts as 0: teacher
+ *                           and student are masked alike)
  *   weight          [rows], NULL = 1.  A row of weight 0 is padding: whatever it holds, its loss and gradient are 0.
  *   loss            [rows]  L, without the weight
  *   dlogits         NULL (the loss alone), or weight * dL/dlogits:

@@ -31,6 +31,8 @@ struct DistillParams {
 __device__ __noinline__ double exp64(double x) { return exp(x); }
 __device__ __noinline__ double log64(double x) { return log(x); }
 
+constexpr float kNothing = 1442.695f;  // log2(e) * 1000
+
 struct Distill {
     using Params = DistillParams;
     static constexpr bool kMoments = false, kMask = true;
@@ -179,8 +181,10 @@ struct Distill {
         const float rest_at = m_rest == m || m_rest == -INFINITY ? 1.0f : exp2_approx((m_rest - m) * p.scale);
         const float list = sh.list_s * (sh.list_m == m || sh.list_m == -INFINITY ? 1.0f : exp2_approx((sh.list_m - m) * p.scale));
         const float s = m == INFINITY ? NAN : rest * rest_at + list;
-        // nothing is left off the list: then the teacher's rest is what its values' rounding left, if it is no more than that
-        const float q_rest = rest == 0.0f && sh.q_rest <= sh.q_noise ? 0.0f : sh.q_rest, mass = sh.q_sum + q_rest;
+        // (as good as) nothing is left off the list, by masks of -inf or of a very low number: then the teacher's rest is what its
+        // values' rounding left, if it is no more than that
+        const bool nothing = rest == 0.0f || (m_rest - m) * p.scale < -kNothing;
+        const float q_rest = nothing && sh.q_rest <= sh.q_noise ? 0.0f : sh.q_rest, mass = sh.q_sum + q_rest;
         Gradient g = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
         if (s != 0.0f) {
             g.m = m_rest == -INFINITY ? 0.0f : m_rest;

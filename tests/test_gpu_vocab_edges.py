@@ -120,7 +120,7 @@ def distill_list_alone64(z, token, value, temperature):
     v = torch.where(here, value.double(), -INF)
     q = v.exp()
     at = token.clamp(min=0)
-    terms = torch.where(here, q * (v - logp.gather(1, at)), 0.0)
+    terms = torch.where(q > 0, q * (v - logp.gather(1, at)), 0.0)
     q_all = torch.zeros_like(logp).scatter_add_(1, at, q)
     p, mass = logp.exp(), q.sum(1, keepdim=True)
     return terms.sum(1), (mass * p - q_all) / temperature, (mass * p + q_all) / temperature
@@ -315,3 +315,27 @@ def test_backward_of_the_entropy_where_the_maximum_rises_in_steps(qn, rows, voca
     check_backward(qn, z, t, temperature, None, None, upstream(rows, 1), None, None)
     check_backward(qn, z, t, temperature, upstream(rows, 2), upstream(rows, 3), upstream(rows, 4), None, None)
     check_logprobs(qn, z, t, 3, temperature)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fill", ["lowest", -10000.0])
+@pytest.mark.parametrize("rows,vocab", [(500, 600), (40, 9001), (7, 140001), (3, 300001)])
+def test_distill_teacher_and_student_masked_alike_by_a_very_low_number(qn, rows, vocab, fill, dtype):
+    """The same where the mask is the type's lowest value, or -10000: all allowed tokens are listed, some of the others too, and the
+    student gives the rest e^-9000 or less."""
+    k, allowed = 20, 10
+    z = ref.make_logits(rows, vocab, dtype, 12)
+    keep = ref.make_logits(rows, vocab, torch.float32, 13).topk(allowed, 1).indices
+    z = torch.full_like(z, torch.finfo(dtype).min if fill == "lowest" else fill).scatter_(1, keep, z.gather(1, keep))
+    top, top_lp = torch.empty((rows, k), dtype=torch.int64, device="cuda"), torch.empty((rows, k), device="cuda")
+    qn.qn_logprobs(z, top_token=top, top_logprob=top_lp)
+    assert bool((top >= 0).all())
+    for value in (top_lp, top_lp.bfloat16()):
+        loss, out, again = torch.empty(rows, device="cuda"), torch.empty_like(z), torch.empty(rows, device="cuda")
+        qn.qn_distill(z, top, value, loss, dlogits=out)
+        qn.qn_distill(z, top, value, again)
+        want, grad, size = distill_list_alone64(z, top, value, 1.0)
+        close(loss, want, torch.full_like(want, 5e-6 * 20), "loss")
+        assert torch.equal(loss, again)
+        bound = 1e-5 * size + 1e-30 + (2.0 ** -8 * grad.abs() + 2.0 ** -133 if dtype == torch.bfloat16 else 0.0)
+        close(out, grad, bound, "dlogits")
