@@ -360,8 +360,9 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  * managed memory), and cuda_stream one of its streams.  Each call is one kernel launch, never waits for the device, and
  * gives the same bits each time it is given the same inputs (at the same addresses modulo 16: the alignment of a row
  * decides which elements are added first).  Pointers must be aligned to their element type.  Rows that
- * start or end anywhere else than on 16 bytes are read in 16-byte vectors all the same, but for their ends; a gradient whose
- * rows lie otherwise to 16 bytes than the logits' takes a little more.
+ * start or end anywhere else than on 16 bytes are read in 16-byte vectors all the same, but for their ends.  Many long rows
+ * are fastest on 16 bytes, and slowest where the gradient's rows lie otherwise to 16 bytes than the logits' (half of a copy's
+ * rate, where aligned ones have three quarters and more).
  *
  * Common arguments
  *   rows, vocab     the matrix of logits; rows >= 0 (0: nothing is done), 1 <= vocab < 2^31 - 64
@@ -440,6 +441,7 @@ QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtyp
  *                           nothing off the list, p_r = 0 or below e^-1000 as by masks, a q_r within the rounding of the
  *                           values, 2^-18 sum_k q_k (1 - v_k) or 2^-9 of that sum for bf16 values, counts as 0: teacher
  *                           and student are masked alike)
+ *                   q_k are numbers of 32 bits: one below 1e-45 is 0.
  *   weight          [rows], NULL = 1.  A row of weight 0 is padding: whatever it holds, its loss and gradient are 0.
  *   loss            [rows]  L, without the weight
  *   dlogits         NULL (the loss alone), or weight * dL/dlogits:

@@ -3,8 +3,8 @@
 //
 // Two forms: the pipeline here, for many long rows, and row_gradient_small_kernel below, for everything else.
 //
-// A cluster of C CTAs takes a row; each holds a slice of at most 192 KB (128 KB unless the row is larger than 1 MB).  A row
-// is seen as 16-byte vectors that start at the 16-byte boundary at or below its first element, so that whatever its
+// A cluster of C CTAs takes a row; each holds a slice of up to 128 KB (80 KB where rows do not start and end on 16 bytes), and
+// of up to 192 KB where eight of those are not enough.  A row is seen as 16-byte vectors that start at the 16-byte boundary at or below its first element, so that whatever its
 // alignment all but its first and last vector move as bulk copies; what those two hold outside the row is filled with -inf.
 //
 // There is one CTA on an SM, it stays, and its warps are stages of a pipeline over chunks of 4 KB in a ring of 48:
@@ -19,13 +19,15 @@
 //   end warp       when a row has been written, its special elements' gradients, and the row's loss
 // So HBM is read and written at the same time, and the exchange of one row passes while others are summed and written.
 //
-// Measured on a B200, 4096 x 131072 bf16 with a list of 64 tokens: 386 us, 85 % of the rate of a plain copy (fp32,
-// 1024 x 262144: 418 us, 79 %; clusters of 8 leave 28 of the 148 SMs without work).  What bounds it then is the issue of
-// instructions: per element about 5.5 in the sum loop, 5 in the write loop and 3 for everything that is paid once a row,
-// where a chunk's bytes take the time of 20.  exp2 is taken twice for an element, 73 % of its rate of 16 a cycle and SM if
-// nothing else bound; giving a quarter of them to the FMA pipe as a polynomial made it slower (441 to 469 us), as does
-// anything that adds instructions.  Keeping e_i in registers between the two (one exp2) needs loops unrolled over them, and
-// those ran out of the instruction cache: 883 us.  One lane that issued all copies took 470 cycles for each: 526 us.
+// Measured on a B200, 4096 x 131072 bf16 with a list of 64 tokens: 417 us at an SM clock of 1.82 GHz under the power cap, 79 %
+// of the rate of a plain copy (fp32, 1024 x 262144: 426 us at 1.94 GHz, 77 %; clusters of 8 leave 28 of the 148 SMs without
+// work).  The time follows the SM clock, but no unit is full: 14.5 instructions an element (17 with an entropy gradient) keep
+// the issue slots 51 to 58 % busy, the two exp2 of an element their unit 53 %, and DRAM is active in half of its cycles (1024
+// rows; the stages wait for one another).  Whatever adds instructions adds time: a quarter of the exp2 as a polynomial on the
+// FMA pipe made 469 us of 441, a vote for every chunk's wait 1.5 %.  Keeping e_i in registers between the two (one exp2) needs
+// loops unrolled over them, and those ran out of the instruction cache: 883 us.  One lane that issued all copies took 470
+// cycles for each: 526 us.  28 warps of seven roles share 72 registers a thread: with a gradient, 24 to 144 bytes of a thread
+// are spilled, most where an entropy gradient meets rows that do not lie on 16 bytes.
 //
 // An operator Op brings:
 //   Params, Shared        arguments; what the warps tell one another of a row
@@ -51,7 +53,7 @@ constexpr int kLists = 6;  // rows between the list warps' beginning and the end
 // 10 / 13 449, 11 / 12 440; 28 warps are the most that leave 72 registers for each.
 template <bool kWrite>
 struct Roles {
-    static constexpr int kSum = 11, kWriting = kWrite ? 12 : 0;  // the same sums, to the bit, with and without a gradient
+    static constexpr int kSum = 11, kWriting = kWrite ? 12 : 0;  // the same sums with and without a gradient
     static constexpr int kThreads = 32 * (kSum + kWriting + 3 + kListWarps);
 };
 
@@ -715,7 +717,7 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
 
 // The same for problems whose time is latency: a CTA (of a cluster, where there are few rows or long ones) takes a slice of up
 // to 32 KB straight into registers, its first warp the special elements meanwhile; sums, exchange, gradient, end.  One
-// launch, no stage that waits for another, up to 32 CTAs on an SM.  Measured, us: one row of 8192 fp32 5.6 (the pipeline:
+// launch, no stage that waits for another, up to 32 CTAs on an SM.  Measured (when it was built), us: one row of 8192 fp32 5.6 (the pipeline:
 // 9.0), 128 x 8192 bf16 6.5 (9.2), 1024 x 8192 fp32 backward 13.4 = 77 % of a copy's rate (21).
 constexpr int kSmallVectors = 8;  // of a thread
 
@@ -873,7 +875,7 @@ cudaError_t launch_gradient_pipeline(const typename Op::Params& p, int64_t all, 
     auto kernel = row_gradient_kernel<T, Op, kAligned, kEdges, kWrite>;
     // CTAs a row: slices of up to 128 KB (80 KB of rows that are not aligned), of up to 192 KB where 8 of them are not enough;
     // where there are few rows, more and smaller ones, down to a chunk for every sum warp.  Measured with slices of up to 128,
-    // 96 and 72 KB, us: 4096 x 131072 bf16 386, 400, 417; 2047 x 100003 bf16 175, 160, 160 (156 with 80).
+    // 96 and 72 KB, us (when this was chosen): 4096 x 131072 bf16 386, 400, 417; 2047 x 100003 bf16 175, 160, 160 (156 with 80).
     constexpr int kGood = (kEdges ? 20 : 32) * kChunk;
     int ctas = 1;
     while (ctas < kMaxCluster && (all + ctas - 1) / ctas > kGood) ++ctas;
