@@ -441,7 +441,6 @@ QN_API qn_status qn_logprobs_backward(int64_t rows, int64_t vocab, qn_dtype dtyp
  *                           nothing off the list, p_r = 0 or below e^-1000 as by masks, a q_r within the rounding of the
  *                           values, 2^-18 sum_k q_k (1 - v_k) or 2^-9 of that sum for bf16 values, counts as 0: teacher
  *                           and student are masked alike)
- *                   q_k are numbers of 32 bits: one below 1e-45 is 0.
  *   weight          [rows], NULL = 1.  A row of weight 0 is padding: whatever it holds, its loss and gradient are 0.
  *   loss            [rows]  L, without the weight
  *   dlogits         NULL (the loss alone), or weight * dL/dlogits:

@@ -44,6 +44,7 @@ struct Distill {
         double q_total, q_log_q;  // of the q as rounded to 32 bits
         float q_sum, q_rest, q_noise, weight;  // q_noise: what rounding of the values may leave of 1 - sum q
         float list_m, list_s;  // of the list's logits: the largest, sum of e_k relative to it
+        bool lost;             // the student masks a token that the teacher does not, however little it weighs
         Gradient g;             // off the list: relative to m_rest
         float m, m_rest;        // the largest of the row (0 if it is empty), and of what is off the list
         float rest, s;          // the sums relative to these
@@ -122,12 +123,14 @@ struct Distill {
         // what is left of 1 may be far smaller than 1: the list is added up in 64 bits
         double q_sum = 0.0;
         double q_total = 0.0, q_log_q = 0.0;
+        bool lost = false;
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
             const int j = lane + 32 * i;
             if (j >= p.k) continue;
             const double log_q = (static_cast<double>(v[i]) - top) * inv - log_norm, q = exp64(log_q);
             q_sum += q;
+            lost = lost || (q > 0.0 && f.z[i] == -INFINITY);
             const float q32 = static_cast<float>(q);
             if (q32 != 0.0f) q_log_q += q32 * log_q;
             q_total += q32;
@@ -147,8 +150,10 @@ struct Distill {
         q_sum = warp_reduce<double, add_op>(q_sum);
         q_total = warp_reduce<double, add_op>(q_total);
         q_log_q = warp_reduce<double, add_op>(q_log_q);
+        lost = __any_sync(0xffffffffu, lost);
         if (lane == 0) {
             sh.weight = f.weight;
+            sh.lost = lost;
             sh.list_m = list_m;
             sh.list_s = list_s;
             sh.q_sum = wrong ? NAN : static_cast<float>(q_sum);
@@ -216,7 +221,7 @@ struct Distill {
         if ((threadIdx.x & 31) == 0) {
             const double log_s = log64(static_cast<double>(sh.s));
             double loss = INFINITY;
-            if (sh.s != 0.0f) {
+            if (sh.s != 0.0f && !sh.lost) {
                 loss = sh.q_log_q - 0.6931471805599453 * p.scale * dot + sh.q_total * log_s;
                 if (sh.q_rest != 0.0f) {
                     const double log_rest = log64(static_cast<double>(sh.rest)) +

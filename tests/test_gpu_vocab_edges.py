@@ -339,3 +339,18 @@ def test_distill_teacher_and_student_masked_alike_by_a_very_low_number(qn, rows,
         assert torch.equal(loss, again)
         bound = 1e-5 * size + 1e-30 + (2.0 ** -8 * grad.abs() + 2.0 ** -133 if dtype == torch.bfloat16 else 0.0)
         close(out, grad, bound, "dlogits")
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("logprobs", [False, True])
+@pytest.mark.parametrize("vocab", [300, 150001])
+def test_distill_of_a_masked_token_that_the_teacher_weighs_less_than_the_smallest_float(qn, vocab, logprobs, dtype):
+    """q = e^-200 is 0 in 32 bits and the student masks it: +inf all the same; not so where the teacher masks it too, with
+    -inf or the lowest value."""
+    z = ref.make_logits(4, vocab, dtype, 3)
+    token = torch.tensor([3, 8, 9], device="cuda").expand(4, 3).contiguous()
+    z[:3, 8] = -INF
+    value = torch.tensor([-0.5, -200.0, -2.0], device="cuda").repeat(4, 1)
+    value[1, 1], value[2, 1] = -INF, torch.finfo(torch.float32).min
+    loss, out = check_distill(qn, z, token, value, logprobs)
+    assert loss[0] == INF and bool(torch.isfinite(loss[1:]).all()) and bool(torch.isfinite(out).all())
