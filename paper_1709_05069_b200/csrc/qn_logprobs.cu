@@ -136,14 +136,14 @@ __device__ __noinline__ float4 slice_slow(const T* row, const Slice<T> s, float 
     for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) m = fmaxf(m, Storage<T>::load1(row + i));
     m = block_reduce<float, max_op>(m, sh.max);
     const float ref = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f, moment = 0.0f;
+    double sum = 0.0, moment = 0.0;
 #pragma unroll 1
     for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
         const float d = (Storage<T>::load1(row + i) - ref) * scale, e = exp2_approx(d);
         sum += e;
         if (e != 0.0f) moment += e * d;
     }
-    const float2 x = block_sum2<kThreads>(make_float2(sum, moment), sh.sums);
+    const float2 x = block_sum2<kThreads>(make_float2(static_cast<float>(sum), static_cast<float>(moment)), sh.sums);
     return make_float4(m, x.x, x.y, 0.0f);
 }
 
@@ -198,7 +198,8 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
             for (int i = tid; i < kBins; i += kThreads) sh.bins[i] = 0;
         }
         float m = kFloor, group_top = kFloor;
-        f32x2 sum = 0, moment = 0;
+        float sum = 0.0f;
+        f32x2 moment = 0;
         const f32x2 scale = pack2(p.scale, p.scale);
         int left = per_group, group = 0;
         auto take = [&](uint4* v) {
@@ -212,9 +213,8 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
             const float most = top.get();
             if (!(most <= m)) {  // a new maximum, or NaN (then m and all sums become NaN)
                 const float d = (m - most) * p.scale, f = exp2_approx(d);
-                const f32x2 f2 = pack2(f, f);
-                moment = f != 0.0f ? mul2(f2, fma2(sum, pack2(d, d), moment)) : 0;
-                sum = mul2(sum, f2);
+                moment = f != 0.0f ? mul2(pack2(f, f), add2(moment, pack2(sum * d, 0.0f))) : 0;
+                sum *= f;
                 m = most;
             }
             if (kTop) {
@@ -224,15 +224,21 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
                     left = per_group, group_top = kFloor;
                 }
             }
+            // a batch by itself first: beside a term of 1, one below 2^-24 would be lost, and a thousand of them add up (the
+            // moment has no such term: d is 0 there)
             const f32x2 minus = pack2(-m, -m);
+            f32x2 part;
 #pragma unroll
             for (int q = 0; q < kBatch; ++q)
 #pragma unroll
                 for (int i = 0; i < kPairs; ++i) {
                     const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus), scale), e = exp2_pair(d);
-                    sum = add2(sum, e);
+                    part = q + i == 0 ? e : add2(part, e);
                     moment = fma2(e, d, moment);
                 }
+            float lo, hi;
+            unpack2(part, lo, hi);
+            sum += lo + hi;
         };
         uint4 a[kBatch], b[kBatch];
         if (batches > 0) load(0, a);
@@ -257,10 +263,9 @@ __global__ void __launch_bounds__(kThreads, 4) logprobs_kernel(const LogprobPara
         for (int w = 0; w < kThreads / 32; ++w) part.x = fmaxf(part.x, sh.max[w]);
         {
             const float d = (m - part.x) * p.scale, f = exp2_approx(d);
-            float s0, s1, e0, e1;
-            unpack2(sum, s0, s1);
+            float e0, e1;
             unpack2(moment, e0, e1);
-            float2 x = make_float2(f * (s0 + s1), f != 0.0f ? f * fmaf(s0 + s1, d, e0 + e1) : 0.0f);
+            float2 x = make_float2(f * sum, f != 0.0f ? f * fmaf(sum, d, e0 + e1) : 0.0f);
             x.x = warp_reduce<float, add_op>(x.x);
             x.y = warp_reduce<float, add_op>(x.y);
             if (lane == 0) sh.sums[warp] = x;

@@ -407,16 +407,20 @@ __global__ void __launch_bounds__(Roles<kWrite>::kThreads, 1)
                             sum = mul2(sum, f2);
                             m = most;
                         }
+                        // four vectors by themselves first: beside a term of 1, one below 2^-24 would be lost, and a thousand
+                        // of them add up (the moment has no such term: d is 0 there)
                         const float ref = m == -INFINITY ? 0.0f : m;
                         const f32x2 minus = pack2(-ref, -ref);
+                        f32x2 part;
 #pragma unroll
                         for (int q = 0; q < 4; ++q)
 #pragma unroll
                             for (int i = 0; i < kPairs; ++i) {
                                 const f32x2 d = mul2(add2(Lanes<T>::pair(v[q], i), minus), scale), e = exp2_pair(d);
-                                sum = add2(sum, e);
+                                part = q + i == 0 ? e : add2(part, e);
                                 if constexpr (moments) moment = fma2(e, finite_pair(d), moment);
                             }
+                        sum = add2(sum, part);
                     }
                     if (!kWrite) {  // nobody else needs the chunk
                         if (patched) fence_async();

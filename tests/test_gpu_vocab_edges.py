@@ -354,3 +354,22 @@ def test_distill_of_a_masked_token_that_the_teacher_weighs_less_than_the_smalles
     value[1, 1], value[2, 1] = -INF, torch.finfo(torch.float32).min
     loss, out = check_distill(qn, z, token, value, logprobs)
     assert loss[0] == INF and bool(torch.isfinite(loss[1:]).all()) and bool(torch.isfinite(out).all())
+
+
+# ---- many small terms beside a large one -----------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("rows,vocab", [(400, 30000), (700, 131072), (300, 262144), (2, 393000)])
+def test_small_terms_beside_the_peak_are_not_lost(qn, rows, vocab, dtype):
+    """One token at 0 and all others near -16: each of them is below half of the last bit of the peak's term, together they
+    are a few per cent of the sum."""
+    z = (ref.make_logits(rows, vocab, torch.float32, 2, spread=0.05) - 16.5).to(dtype)
+    at = torch.arange(rows, device="cuda") * 7 % 64
+    z[torch.arange(rows, device="cuda"), at] = 0.0
+    check_logprobs(qn, z, at, 3)
+    g = upstream(rows, 1)
+    check_backward(qn, z, at + 100, 1.0, g, None, g, None, None)
+    token, value = make_teacher(z, 2, 1.0, True, 1)
+    token[:, 0] = at + 500  # the peak is off the list
+    check_distill(qn, z, token, value, True)
