@@ -17,10 +17,10 @@
 // bit instead (33 counts over the CTA).  With logits as a language model gives them that is no row for k up to 20, 28 to 99 % of
 // rows for k = 64 (131072 to 8192 tokens), and every row for k = 128.
 //
-// Measured on a B200: 8192 x 131072 bf16 with 64 alternatives 492 us a call at an SM clock of 1.79 GHz (67 % of a copy's rate):
+// Measured on a B200: 8192 x 131072 bf16 with 64 alternatives 492 to 505 us a call at SM clocks of 1.79 to 1.76 GHz (66 % of a copy's rate):
 // 9.7 instructions an element keep the issue slots 56 % busy, and behind the pass come the barriers of the alternatives.  One
 // token of 32768 with 8 alternatives 8.3 us in a graph, 3.0 without alternatives.  More CTAs a row than fit at once (96 x
-// 131072 in clusters of 8): 29 us against 17.  At 64 registers the forms with alternatives spill 32 (bf16) and 60 bytes.
+// 131072 in clusters of 8): 29 us against 17.  At 64 registers the forms with alternatives spill 36 (bf16) and 60 bytes.
 //
 // Backward: an operator of the row-gradient kernel.
 #include <nvtx3/nvToolsExt.h>

@@ -19,14 +19,14 @@
 //   end warp       when a row has been written, its special elements' gradients, and the row's loss
 // So HBM is read and written at the same time, and the exchange of one row passes while others are summed and written.
 //
-// Measured on a B200, 4096 x 131072 bf16 with a list of 64 tokens: 417 us at an SM clock of 1.82 GHz under the power cap, 79 %
-// of the rate of a plain copy (fp32, 1024 x 262144: 426 us at 1.94 GHz, 77 %; clusters of 8 leave 28 of the 148 SMs without
+// Measured on a B200, 4096 x 131072 bf16 with a list of 64 tokens: 417 to 423 us at SM clocks of 1.82 to 1.79 GHz under the power
+// cap, 78 % of the rate of a plain copy (fp32, 1024 x 262144: 426 to 432 us near 1.95 GHz, 76 %; clusters of 8 leave 28 of the 148 SMs without
 // work).  The time follows the SM clock, but no unit is full: 14.5 instructions an element (17 with an entropy gradient) keep
 // the issue slots 51 to 58 % busy, the two exp2 of an element their unit 53 %, and DRAM is active in half of its cycles (1024
 // rows; the stages wait for one another).  Whatever adds instructions adds time: a quarter of the exp2 as a polynomial on the
 // FMA pipe made 469 us of 441, a vote for every chunk's wait 1.5 %.  Keeping e_i in registers between the two (one exp2) needs
 // loops unrolled over them, and those ran out of the instruction cache: 883 us.  One lane that issued all copies took 470
-// cycles for each: 526 us.  28 warps of seven roles share 72 registers a thread: with a gradient, 24 to 144 bytes of a thread
+// cycles for each: 526 us.  28 warps of seven roles share 72 registers a thread: with a gradient, 32 to 144 bytes of a thread
 // are spilled, most where an entropy gradient meets rows that do not lie on 16 bytes.
 //
 // An operator Op brings:
