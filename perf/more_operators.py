@@ -517,7 +517,8 @@ def _own_adam(s):
         qn.qn_adam_norm(s["plan"], s["sumsq"])
         out["sumsq"] = s["sumsq"]
     qn.qn_adam_step(s["plan"], s["step"], lr=_LR, beta1=_BETA1, beta2=_BETA2, eps=_EPS,
-                    sumsq=s["sumsq"] if case["clip"] else None, max_norm=_MAX_NORM, stochastic=True, seed=_SEED)
+                    sumsq=s["sumsq"] if case["clip"] else None, max_norm=_MAX_NORM if case["clip"] else 0.0,
+                    stochastic=True, seed=_SEED)
     if case["master"]:
         out["master"] = s["master"]
     if case["bits"] == 8:
