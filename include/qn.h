@@ -458,6 +458,99 @@ QN_API qn_status qn_distill(int64_t rows, int64_t vocab, qn_dtype dtype, const v
                             int64_t dlogits_stride, void* cuda_stream);
 
 /*
+ * The Worker's step: AdamW over the tensors of its parameter vector, many at once (the paper's Workers compute gradients and
+ * leave the step to the Server; a Worker that steps by itself between two Writes, or a Server that is compared with the
+ * usual optimiser, needs this one).
+ *
+ * For each element, with g~ = c g and t the number of this step (*step before it, plus 1):
+ *     m' = beta1 m + (1 - beta1) g~               v' = beta2 v + (1 - beta2) g~^2
+ *     theta' = theta (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m' / (sqrt(v' / (1 - beta2^t)) + eps),   lr' = lr lr_scale
+ *     c = grad_scale * min(1, max_norm / (|grad_scale| norm)),   norm^2 = *sumsq
+ * Arithmetic: fp32, each product and sum that leads to m' and v' rounded by itself; what is the same for all elements of a tensor
+ * is in fp64.
+ *
+ * A plan holds the tensors' addresses and sizes on the device that has them (and a small workspace): it is made once, outside
+ * stream capture, for tensors that stay where they are.  Gradients that move are named again with qn_adam_grads.  Calls
+ * on one plan share its workspace and must be ordered, as those on a qn_handle; so must replays of graphs that
+ * captured them.  A call is one kernel launch that waits for nothing (qn_adam_grads: one for each 256 tensors), and can
+ * be captured: step, lr_device and sumsq are read when the kernel runs.  The same inputs give the same bits.
+ */
+#define QN_ADAM_BLOCK 32   /* elements that share a scale, where states are held in 8 bits */
+#define QN_STATE_F32 0     /* m and v in fp32 */
+#define QN_STATE_8BIT 1    /* m and sqrt(v) in 8 bits each, and 8 bits of scale a block for each */
+#define QN_ROUND_NEAREST 0
+#define QN_ROUND_STOCHASTIC 1
+
+typedef struct qn_adam_plan* qn_adam_handle;
+
+/*
+ * One tensor: contiguous arrays of numel elements, each aligned to its element type.  Arrays at multiples of 8 elements'
+ * size (32 bytes of fp32, 16 of bf16, 8 of codes) are moved in vectors, others element by element.
+ *   param       theta, of the plan's parameter type; read and written
+ *   grad        g, of the plan's gradient type; read only.  NULL: the tensor has none, and is left alone with its states
+ *   master      NULL, or (for all tensors of a plan, whose parameters are bf16) theta in fp32: the step is taken from it and
+ *               param becomes its copy, rounded to nearest
+ *   m, v        QN_STATE_F32: fp32; QN_STATE_8BIT: codes of 8 bits.  Zeros to begin with
+ *   m_scale, v_scale   QN_STATE_8BIT: 8 bits for each QN_ADAM_BLOCK elements (the last block may be short); else NULL
+ * Codes: a block's scale s stands for 2^(s - 127), and puts the block's largest finite magnitude in [128, 256) (s = 0: all of
+ * the block is 0; otherwise s >= 1).  m is E4M3, as torch.float8_e4m3fn.  The code b of the root r = sqrt(v) has no sign: exponent
+ * b / 16, fraction b % 16 / 16, r = 2^(s - 127) (1 + fraction) 2^(exponent - 7), or fraction 2^-6 for exponent 0.
+ * Codes are rounded up or down by chance (seed), so that they keep the mean of the moving averages; a root that
+ * is not 0 does not become 0.  An m that is not finite is held as NaN, such a root as the largest code, and neither counts for the
+ * scale.
+ */
+typedef struct {
+    int64_t numel; /* 0: nothing, its pointers are not looked at */
+    void* param;
+    const void* grad;
+    float* master;
+    void* m;
+    void* v;
+    uint8_t* m_scale;
+    uint8_t* v_scale;
+    double weight_decay, lr_scale; /* >= 0 */
+} qn_adam_tensor;
+
+/*
+ * A plan for `count` tensors (HOST array), all on one device: no two arrays that a step writes may overlap, and no gradient may
+ * overlap one of them.  Waits for the device.
+ */
+QN_API qn_status qn_adam_create(int32_t count, const qn_adam_tensor* tensors, qn_dtype param, qn_dtype grad, int32_t state,
+                                qn_adam_handle* out);
+QN_API qn_status qn_adam_destroy(qn_adam_handle h);
+
+/* New addresses of the gradients: `count` pointers (HOST array, read before the call returns), NULL for a tensor without one. */
+QN_API qn_status qn_adam_grads(qn_adam_handle h, const void* const* grads, void* cuda_stream);
+
+/* sumsq (DEVICE): the sum of g^2 over all tensors, in fp64.  A plan of one rank's tensors may add it up with the others'. */
+QN_API qn_status qn_adam_norm(qn_adam_handle h, double* sumsq, void* cuda_stream);
+
+/*
+ * One step.
+ *   step        DEVICE int64: steps taken so far; counted up by one
+ *   lr          learning rate >= 0; lr_device (DEVICE fp32, may be NULL) takes its place
+ *   beta1, beta2 in [0, 1);  eps > 0 in fp32
+ *   sumsq       DEVICE, may be NULL: the norm's square (qn_adam_norm).  If it is not finite nothing is changed, *step neither
+ *   max_norm    > 0: gradients whose norm (times |grad_scale|) is larger are scaled down to it; needs sumsq.  Otherwise no bound
+ *   grad_scale  gradients are multiplied by it first (1 / a loss scale)
+ *   rounding    of bf16 parameters without a master copy: to nearest, or up or down by chance, which keeps the mean of steps that
+ *               are smaller than their last bit
+ *   seed        of all chances, with the step's number and the element's place: the same seed and step round the same way
+ * Without sumsq, gradients that are not finite reach the parameters.
+ */
+QN_API qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, const float* lr_device, double beta1, double beta2,
+                              double eps, const double* sumsq, double max_norm, double grad_scale, int32_t rounding,
+                              uint64_t seed, void* cuda_stream);
+
+/*
+ * What the states stand for: m and the root sqrt(v), each a vector of qn_adam_places elements of `dtype` (bf16 holds what 8
+ * bits stand for exactly), either may be NULL.  Tensors follow one another in whole blocks: each begins at a multiple of
+ * QN_ADAM_BLOCK, and the rest of its last block is 0.
+ */
+QN_API int64_t qn_adam_places(qn_adam_handle h);
+QN_API qn_status qn_adam_state(qn_adam_handle h, qn_dtype dtype, void* m, void* root, void* cuda_stream);
+
+/*
  * Per-kernel timing, for benchmarks.  Between qn_timing_begin and qn_timing_end every kernel the
  * handle launches (up to max_kernels of them) is bracketed by two CUDA events recorded on the
  * stream of the call.  qn_timing_end waits for those events and returns, per kind of kernel,

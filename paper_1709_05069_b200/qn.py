@@ -7,7 +7,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -21,6 +21,11 @@ QN_TOP_MAX = 128
 QN_TEACHER_LOGITS = 0
 QN_TEACHER_LOGPROBS = 1
 QN_GRAD_MAX_VOCAB = 393208
+QN_ADAM_BLOCK = 32
+QN_STATE_F32 = 0
+QN_STATE_8BIT = 1
+QN_ROUND_NEAREST = 0
+QN_ROUND_STOCHASTIC = 1
 
 (QN_OK, QN_ERR_INVALID, QN_ERR_ALLOC, QN_ERR_CUDA, QN_ERR_STATE, QN_ERR_NOT_CONVERGED, QN_ERR_NONFINITE,
  QN_ERR_DEVICE_TIMEOUT) = range(8)
@@ -38,6 +43,7 @@ EXPORTS = (
     "qn_timing_end",
     "qn_gram_static", "qn_selftest_bounded_wait",
     "qn_logprobs", "qn_logprobs_backward", "qn_distill",
+    "qn_adam_create", "qn_adam_destroy", "qn_adam_grads", "qn_adam_norm", "qn_adam_step", "qn_adam_places", "qn_adam_state",
 )
 TIME_KINDS = ("gram", "solve", "combine", "row")
 KERNEL_NAMES = {
@@ -100,6 +106,15 @@ def lib() -> ctypes.CDLL:
         L.qn_logprobs_backward.argtypes = [i64, i64, i32, vp, i64, vp, dbl, vp, vp, vp, i32, vp, vp, vp, i64, vp]
         L.qn_distill.argtypes = [i64, i64, i32, vp, i64, i32, vp, i32, vp, i32, dbl, vp, vp, vp, i64, vp]
         L.qn_logprobs.restype = L.qn_logprobs_backward.restype = L.qn_distill.restype = i32
+        L.qn_adam_create.argtypes = [i32, vp, i32, i32, i32, ctypes.POINTER(vp)]
+        L.qn_adam_destroy.argtypes = [vp]
+        L.qn_adam_grads.argtypes = [vp, vp, vp]
+        L.qn_adam_norm.argtypes = [vp, vp, vp]
+        L.qn_adam_step.argtypes = [vp, vp, dbl, vp, dbl, dbl, dbl, vp, dbl, dbl, i32, ctypes.c_uint64, vp]
+        L.qn_adam_state.argtypes = [vp, i32, vp, vp, vp]
+        for name in ("create", "destroy", "grads", "norm", "step", "state"):
+            getattr(L, "qn_adam_" + name).restype = i32
+        L.qn_adam_places.argtypes, L.qn_adam_places.restype = [vp], i64
         _lib = L
     return _lib
 
@@ -558,3 +573,140 @@ def qn_distill(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_value:
                             temperature, _beside(weight, torch.float32, rows, 0, dev, "weight"),
                             _beside(loss, torch.float32, rows, 0, dev, "loss"), out, out_stride,
                             _stream_on(dev, stream)), "qn_distill")
+
+
+# ---- AdamW over many tensors ------------------------------------------------------------------------------------------
+
+
+class _AdamTensor(ctypes.Structure):
+    _fields_ = [("numel", ctypes.c_int64), ("param", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("master", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("m_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("weight_decay", ctypes.c_double),
+                ("lr_scale", ctypes.c_double)]
+
+
+class Adam:
+    """Owner of a ``qn_adam_handle`` and of references to the tensors whose addresses it holds."""
+
+    def __init__(self, ptr: int, tensors: Sequence, grads: Sequence, sizes: Sequence[int], grad_dtype: torch.dtype, device: int):
+        self.ptr, self.tensors, self.grads, self.sizes = ptr, tensors, grads, sizes
+        self.grad_dtype, self.device = grad_dtype, device
+
+    def close(self):
+        if self.ptr:
+            lib().qn_adam_destroy(self.ptr)
+            self.ptr = 0
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    @property
+    def places(self) -> int:
+        """Elements of the vectors that ``qn_adam_state`` writes."""
+        return lib().qn_adam_places(self.ptr)
+
+
+def _of_tensor(t: Optional[torch.Tensor], dtype: torch.dtype, numel: int, device: int, name: str) -> int:
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != device or t.numel() != numel or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of %d elements on cuda:%d" % (name, dtype, numel, device))
+    return t.data_ptr()
+
+
+def _one_each(given, count: int, name: str) -> Sequence:
+    if given is None:
+        return [None] * count
+    if isinstance(given, torch.Tensor) or len(given) != count:
+        raise ValueError("%s must be a list with an entry for each of the %d tensors" % (name, count))
+    return list(given)
+
+
+def _number_each(given, count: int, name: str) -> Sequence[float]:
+    return [float(given)] * count if isinstance(given, (int, float)) else [float(x) for x in _one_each(given, count, name)]
+
+
+def qn_adam_create(params: Sequence[torch.Tensor], grads: Sequence[Optional[torch.Tensor]], m: Sequence[torch.Tensor],
+                   v: Sequence[torch.Tensor], master: Optional[Sequence[torch.Tensor]] = None,
+                   m_scale: Optional[Sequence[torch.Tensor]] = None, v_scale: Optional[Sequence[torch.Tensor]] = None,
+                   weight_decay=0.0, lr_scale=1.0) -> Adam:
+    """A plan for AdamW steps on ``params`` (float32 or bfloat16), whose gradients are ``grads`` (None: left alone).
+
+    ``m`` and ``v`` are float32, or uint8 with ``m_scale`` and ``v_scale`` (uint8, one for each ``QN_ADAM_BLOCK`` elements)
+    for states in 8 bits; all begin as zeros.  ``master``: float32 copies of bfloat16 parameters.  ``weight_decay`` and
+    ``lr_scale``: a number, or one for each tensor.  The tensors must stay where they are; the plan keeps them alive."""
+    params = list(params)
+    count = len(params)
+    if not count or not params[0].is_cuda:
+        raise ValueError("params must be CUDA tensors, one at least")
+    lists = [params] + [_one_each(x, count, name) for x, name in ((grads, "grads"), (m, "m"), (v, "v"), (master, "master"),
+                                                                  (m_scale, "m_scale"), (v_scale, "v_scale"))]
+    decay, scale = _number_each(weight_decay, count, "weight_decay"), _number_each(lr_scale, count, "lr_scale")
+    device, eight = params[0].get_device(), m_scale is not None or v_scale is not None
+    grad_dtype = next((g.dtype for g in lists[1] if g is not None), params[0].dtype)
+    state = torch.uint8 if eight else torch.float32
+    names, sizes = ("params", "grads", "m", "v", "master", "m_scale", "v_scale"), [p.numel() for p in params]
+    dtypes = (params[0].dtype, grad_dtype, state, state, torch.float32, torch.uint8, torch.uint8)
+    table = (_AdamTensor * count)()
+    for i, size in enumerate(sizes):
+        blocks = (size + QN_ADAM_BLOCK - 1) // QN_ADAM_BLOCK
+        at = [_of_tensor(x[i], dtype, blocks if "scale" in name else size, device, name)
+              for x, dtype, name in zip(lists, dtypes, names)]
+        table[i] = _AdamTensor(size, at[0], at[1], at[4], at[2], at[3], at[5], at[6], decay[i], scale[i])
+    out = ctypes.c_void_p(0)
+    with torch.cuda.device(device):
+        _check(lib().qn_adam_create(count, ctypes.addressof(table), dtype_code(params[0].dtype), dtype_code(grad_dtype),
+                                    QN_STATE_8BIT if eight else QN_STATE_F32, ctypes.byref(out)), "qn_adam_create")
+    return Adam(out.value, lists[:1] + lists[2:], lists[1], sizes, grad_dtype, device)
+
+
+def qn_adam_destroy(h: Adam) -> None:
+    h.close()
+
+
+def qn_adam_grads(h: Adam, grads: Sequence[Optional[torch.Tensor]], stream=None) -> None:
+    """Gradients that have moved (None: the tensor has none, and is left alone from now on)."""
+    grads = _one_each(grads, len(h.sizes), "grads")
+    at = (ctypes.c_void_p * len(grads))(*[_of_tensor(g, h.grad_dtype, size, h.device, "grads") or None
+                                          for g, size in zip(grads, h.sizes)])
+    _check(lib().qn_adam_grads(h.ptr, ctypes.addressof(at), _stream_on(h.device, stream)), "qn_adam_grads")
+    h.grads = grads
+
+
+def qn_adam_norm(h: Adam, sumsq: torch.Tensor, stream=None) -> None:
+    """The sum of the squares of all gradients into ``sumsq`` (float64, one element)."""
+    _check(lib().qn_adam_norm(h.ptr, _of_tensor(sumsq, torch.float64, 1, h.device, "sumsq"), _stream_on(h.device, stream)),
+           "qn_adam_norm")
+
+
+def qn_adam_step(h: Adam, step: torch.Tensor, lr=1e-3, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                 sumsq: Optional[torch.Tensor] = None, max_norm: float = 0.0, grad_scale: float = 1.0,
+                 stochastic: bool = False, seed: int = 0, stream=None) -> None:
+    """One AdamW step on all tensors of the plan, in one launch that waits for nothing.
+
+    ``step`` (int64, one element, on the device): steps so far, counted up.  ``lr``: a number, or a float32 CUDA tensor of one
+    element.  ``sumsq``: what ``qn_adam_norm`` wrote; with ``max_norm`` > 0 the gradients are clipped to that norm, and nothing
+    changes if it is not finite.  ``stochastic``: bfloat16 parameters without a master copy are rounded by chance."""
+    on_device = isinstance(lr, torch.Tensor)
+    _check(lib().qn_adam_step(h.ptr, _of_tensor(step, torch.int64, 1, h.device, "step"), 0.0 if on_device else lr,
+                              _of_tensor(lr, torch.float32, 1, h.device, "lr") if on_device else 0, beta1, beta2, eps,
+                              _of_tensor(sumsq, torch.float64, 1, h.device, "sumsq"), max_norm, grad_scale,
+                              QN_ROUND_STOCHASTIC if stochastic else QN_ROUND_NEAREST, seed & 0xFFFFFFFFFFFFFFFF,
+                              _stream_on(h.device, stream)), "qn_adam_step")
+
+
+def qn_adam_state(h: Adam, m: Optional[torch.Tensor], root: Optional[torch.Tensor], stream=None) -> None:
+    """What the states stand for: the moving average and the root of that of squares, into vectors of ``h.places`` elements
+    (float32 or bfloat16), where tensors follow one another in whole blocks of ``QN_ADAM_BLOCK``."""
+    dtype = next((x.dtype for x in (m, root) if x is not None), torch.float32)
+    _check(lib().qn_adam_state(h.ptr, dtype_code(dtype), _of_tensor(m, dtype, h.places, h.device, "m"),
+                               _of_tensor(root, dtype, h.places, h.device, "root"), _stream_on(h.device, stream)), "qn_adam_state")
