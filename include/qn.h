@@ -355,7 +355,7 @@ QN_API qn_status qn_gram_static(int64_t n, int32_t m, qn_dtype dtype, const void
  * language model it starts at the logits).  A Worker whose J is a token loss turns the dlogits of one of the calls below
  * into its g_k with its model's own backward pass.
  *
- * Three calls without a handle: they need no workspace, keep nothing between calls and may overlap on different
+ * Calls without a handle: they need no workspace, keep nothing between calls and may overlap on different
  * streams.  They run on the device that holds `logits`; every other pointer must be device memory of that device (or
  * managed memory), and cuda_stream one of its streams.  Each call is one kernel launch, never waits for the device, and
  * gives the same bits each time it is given the same inputs (at the same addresses modulo 16: the alignment of a row
@@ -456,6 +456,64 @@ QN_API qn_status qn_distill(int64_t rows, int64_t vocab, qn_dtype dtype, const v
                             int32_t k, const int64_t* teacher_token, qn_dtype teacher_dtype, const void* teacher_value,
                             int32_t teacher, double temperature, const float* weight, float* loss, void* dlogits,
                             int64_t dlogits_stride, void* cuda_stream);
+
+/*
+ * Clipped policy loss of given tokens (an answer that the Worker's own model, or an older one, has sampled), with a KL term to a
+ * reference and an entropy bonus, and its gradient, in one launch that reads a row once.  With l = u_t - lse:
+ *     r = exp(l - old);   s = max(-A r, -A clip(r, 1 - clip_low, 1 + clip_high));   if dual > 0 and A < 0: s = min(s, -A dual)
+ *     L = s + kl (exp(ref - l) - (ref - l) - 1) - entropy_bonus H
+ *     dlogits = weight dL/dlogits = weight / T [ f' (1[i = t] - p_i) + entropy_bonus p_i (ln p_i + H) ],
+ *     f' = (-A r where s is -A r, else 0) + kl (1 - exp(ref - l))
+ *   tokens        int64[rows]; a row whose token is < 0, or whose weight is 0, is padding: whatever else it holds, its
+ *                 numbers and its gradient are 0
+ *   old_logprob   [rows]  the token's log probability when it was sampled, at this temperature
+ *   ref_logprob   [rows]  that of the reference; may be NULL with kl = 0
+ *   advantage     [rows]  A
+ *   weight        [rows], NULL = 1
+ *   clip_low      in [0, 1];  clip_high >= 0 (INFINITY: no upper bound);  dual 0 (none) or > 1;  kl >= 0;  entropy_bonus finite
+ *   loss          [rows]  L, without the weight
+ *   logprob, entropy  [rows]  l and H, each may be NULL
+ *   dlogits       NULL (the loss alone), or placed as in qn_logprobs_backward
+ * A token that the policy masks (and an empty row) has r = 0, and no gradient passes through its l; its KL term is +inf
+ * unless the reference masks it too, which makes it 0.  An empty row's gradient is 0.  Inputs that are not numbers make their row's
+ * outputs NaN.  No output but dlogits may overlap an input or another output.  vocab <= QN_GRAD_MAX_VOCAB.
+ */
+QN_API qn_status qn_policy(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
+                           const int64_t* tokens, double temperature, const float* old_logprob, const float* ref_logprob,
+                           const float* advantage, const float* weight, double clip_low, double clip_high, double dual,
+                           double kl, double entropy_bonus, float* loss, float* logprob, float* entropy, void* dlogits,
+                           int64_t dlogits_stride, void* cuda_stream);
+
+/*
+ * Preference loss of pairs of answers, from the log probabilities of their tokens (as qn_logprobs writes them), and its gradient with
+ * respect to these (as qn_logprobs_backward takes it), in one launch.  Sequences are packed one after the other.
+ *     S = sum_t w_t (l_t - ref_t), divided by sum_t w_t with `normalise`;   R = beta S;   h = R_chosen - R_rejected - margin
+ *     QN_PREFERENCE_LOGISTIC  L = (1 - smoothing) ln(1 + e^-h) + smoothing ln(1 + e^h)
+ *     QN_PREFERENCE_HINGE     L = max(0, 1 - h)
+ *     QN_PREFERENCE_SQUARED   L = ((h - 1/2) / beta)^2
+ *   logprob       [tokens]  l
+ *   ref_logprob   [tokens] of ref_dtype, NULL = 0 (a loss without reference)
+ *   weight        [tokens], NULL = 1.  Tokens of weight 0 (prompts) count for nothing whatever they hold; their gradient is 0
+ *   offsets       int64[2 pairs + 1], ascending: sequence s has the tokens from offsets[s] to offsets[s + 1].  A pair with an offset
+ *                 outside [0, tokens] or a sequence of negative length has NaN for its loss, rewards and gradients, and
+ *                 touches nothing outside its other sequence.  Sequences must not overlap (not checked)
+ *   split         0: sequences 2 k and 2 k + 1 are the chosen and the rejected one of pair k;  1: sequences k and pairs + k
+ *   pair_weight   [pairs], NULL = 1.  A pair of weight 0 is padding: its loss, rewards and gradients are 0 whatever it holds
+ *   beta          > 0;  margin finite;  0 <= smoothing <= 1
+ *   loss          [pairs]  L, without the weight
+ *   reward        [2 pairs]  R in the order of the sequences; may be NULL
+ *   d_logprob     [tokens]  pair_weight dL/dl_t; may be NULL.  Tokens of no sequence are left as they were
+ * A sequence without tokens that count has R = 0.  A token that both sides mask (-inf) counts for nothing; a token that
+ * one side masks makes R infinite.  Sums are in fp64.  The call runs on the device that holds `loss`.  No output may overlap an
+ * input or another output.  tokens = 0 is allowed, pairs = 0 does nothing; pairs <= 2^28 - 1.
+ */
+#define QN_PREFERENCE_LOGISTIC 0
+#define QN_PREFERENCE_HINGE 1
+#define QN_PREFERENCE_SQUARED 2
+QN_API qn_status qn_preference(int64_t pairs, int64_t tokens, const float* logprob, qn_dtype ref_dtype,
+                               const void* ref_logprob, const float* weight, const int64_t* offsets, int32_t split,
+                               const float* pair_weight, int32_t kind, double beta, double margin, double smoothing,
+                               int32_t normalise, float* loss, float* reward, float* d_logprob, void* cuda_stream);
 
 /*
  * The Worker's step: AdamW over the tensors of its parameter vector, many at once (the paper's Workers compute gradients and

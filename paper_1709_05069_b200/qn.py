@@ -21,6 +21,9 @@ QN_TOP_MAX = 128
 QN_TEACHER_LOGITS = 0
 QN_TEACHER_LOGPROBS = 1
 QN_GRAD_MAX_VOCAB = 393208
+QN_PREFERENCE_LOGISTIC = 0
+QN_PREFERENCE_HINGE = 1
+QN_PREFERENCE_SQUARED = 2
 QN_ADAM_BLOCK = 32
 QN_STATE_F32 = 0
 QN_STATE_8BIT = 1
@@ -42,7 +45,7 @@ EXPORTS = (
     "qn_timing_begin",
     "qn_timing_end",
     "qn_gram_static", "qn_selftest_bounded_wait",
-    "qn_logprobs", "qn_logprobs_backward", "qn_distill",
+    "qn_logprobs", "qn_logprobs_backward", "qn_distill", "qn_policy", "qn_preference",
     "qn_adam_create", "qn_adam_destroy", "qn_adam_grads", "qn_adam_norm", "qn_adam_step", "qn_adam_places", "qn_adam_state",
 )
 TIME_KINDS = ("gram", "solve", "combine", "row")
@@ -106,6 +109,9 @@ def lib() -> ctypes.CDLL:
         L.qn_logprobs_backward.argtypes = [i64, i64, i32, vp, i64, vp, dbl, vp, vp, vp, i32, vp, vp, vp, i64, vp]
         L.qn_distill.argtypes = [i64, i64, i32, vp, i64, i32, vp, i32, vp, i32, dbl, vp, vp, vp, i64, vp]
         L.qn_logprobs.restype = L.qn_logprobs_backward.restype = L.qn_distill.restype = i32
+        L.qn_policy.argtypes = [i64, i64, i32, vp, i64, vp, dbl, vp, vp, vp, vp, dbl, dbl, dbl, dbl, dbl, vp, vp, vp, vp, i64, vp]
+        L.qn_preference.argtypes = [i64, i64, vp, i32, vp, vp, vp, i32, vp, i32, dbl, dbl, dbl, i32, vp, vp, vp, vp]
+        L.qn_policy.restype = L.qn_preference.restype = i32
         L.qn_adam_create.argtypes = [i32, vp, i32, i32, i32, ctypes.POINTER(vp)]
         L.qn_adam_destroy.argtypes = [vp]
         L.qn_adam_grads.argtypes = [vp, vp, vp]
@@ -573,6 +579,57 @@ def qn_distill(logits: torch.Tensor, teacher_token: torch.Tensor, teacher_value:
                             temperature, _beside(weight, torch.float32, rows, 0, dev, "weight"),
                             _beside(loss, torch.float32, rows, 0, dev, "loss"), out, out_stride,
                             _stream_on(dev, stream)), "qn_distill")
+
+
+def qn_policy(logits: torch.Tensor, tokens: torch.Tensor, old_logprob: torch.Tensor, advantage: torch.Tensor,
+              loss: torch.Tensor, dlogits: Optional[torch.Tensor] = None, ref_logprob: Optional[torch.Tensor] = None,
+              weight: Optional[torch.Tensor] = None, logprob: Optional[torch.Tensor] = None,
+              entropy: Optional[torch.Tensor] = None, clip_low: float = 0.2, clip_high: float = 0.2, dual: float = 0.0,
+              kl: float = 0.0, entropy_bonus: float = 0.0, temperature: float = 1.0, stream=None) -> None:
+    """Clipped policy loss of the given ``tokens`` int64 [rows] (into ``loss`` float32 [rows]) and, if ``dlogits`` is given (it
+    may be ``logits`` itself), the gradient of sum(weight * loss), in one launch.
+
+    ``old_logprob``, ``advantage``, ``ref_logprob`` (needed with ``kl`` > 0) and ``weight`` are float32 [rows]; a row whose
+    token is negative or whose weight is 0 is padding.  ``logprob`` and ``entropy`` float32 [rows] are written if given."""
+    rows, vocab, stride, code = _logit_matrix(logits, "logits")
+    dev, f32 = logits.get_device(), torch.float32
+    if tokens is None or old_logprob is None or advantage is None or loss is None:
+        raise ValueError("tokens, old_logprob, advantage and loss [rows] are required")
+    out, out_stride = _gradient(dlogits, logits, "dlogits") if dlogits is not None else (0, 0)
+    _check(lib().qn_policy(rows, vocab, code, logits.data_ptr(), stride, _beside(tokens, torch.int64, rows, 0, dev, "tokens"),
+                           temperature, _beside(old_logprob, f32, rows, 0, dev, "old_logprob"),
+                           _beside(ref_logprob, f32, rows, 0, dev, "ref_logprob"),
+                           _beside(advantage, f32, rows, 0, dev, "advantage"), _beside(weight, f32, rows, 0, dev, "weight"),
+                           clip_low, clip_high, dual, kl, entropy_bonus, _beside(loss, f32, rows, 0, dev, "loss"),
+                           _beside(logprob, f32, rows, 0, dev, "logprob"), _beside(entropy, f32, rows, 0, dev, "entropy"), out,
+                           out_stride, _stream_on(dev, stream)), "qn_policy")
+
+
+def qn_preference(logprob: torch.Tensor, offsets: torch.Tensor, loss: torch.Tensor, d_logprob: Optional[torch.Tensor] = None,
+                  ref_logprob: Optional[torch.Tensor] = None, weight: Optional[torch.Tensor] = None,
+                  pair_weight: Optional[torch.Tensor] = None, reward: Optional[torch.Tensor] = None,
+                  kind: int = QN_PREFERENCE_LOGISTIC, beta: float = 0.1, margin: float = 0.0, smoothing: float = 0.0,
+                  normalise: bool = False, split: bool = False, stream=None) -> None:
+    """Preference loss of pairs of packed sequences (into ``loss`` float32 [pairs]) and, if ``d_logprob`` is given, the gradient
+    of sum(pair_weight * loss) with respect to ``logprob``, in one launch.
+
+    ``logprob`` float32 [tokens], ``ref_logprob`` float32 or bfloat16 [tokens], ``weight`` float32 [tokens] (0: does not count),
+    ``offsets`` int64 [2 * pairs + 1]; ``reward`` float32 [2 * pairs] is written if given.  Sequences 2 k and 2 k + 1 are pair
+    k's chosen and rejected one, or k and pairs + k with ``split``."""
+    if loss is None or not loss.is_cuda or loss.dim() != 1:
+        raise ValueError("loss must be a CUDA tensor [pairs]")
+    if logprob is None or offsets is None or logprob.dim() != 1:
+        raise ValueError("logprob [tokens] and offsets [2 * pairs + 1] are required")
+    dev, f32, pairs, tokens = loss.get_device(), torch.float32, loss.numel(), logprob.numel()
+    ref_dtype = f32 if ref_logprob is None else ref_logprob.dtype
+    _check(lib().qn_preference(pairs, tokens, _beside(logprob, f32, tokens, 0, dev, "logprob"), dtype_code(ref_dtype),
+                               _beside(ref_logprob, ref_dtype, tokens, 0, dev, "ref_logprob"),
+                               _beside(weight, f32, tokens, 0, dev, "weight"),
+                               _beside(offsets, torch.int64, 2 * pairs + 1, 0, dev, "offsets"), bool(split),
+                               _beside(pair_weight, f32, pairs, 0, dev, "pair_weight"), kind, beta, margin, smoothing,
+                               bool(normalise), _beside(loss, f32, pairs, 0, dev, "loss"),
+                               _beside(reward, f32, 2 * pairs, 0, dev, "reward"),
+                               _beside(d_logprob, f32, tokens, 0, dev, "d_logprob"), _stream_on(dev, stream)), "qn_preference")
 
 
 # ---- AdamW over many tensors ------------------------------------------------------------------------------------------
