@@ -14,6 +14,7 @@
 // nearest it would stand still, so codes are rounded up or down with the probabilities that keep the mean.  A root that is not 0
 // is never rounded to 0, which would leave m' / eps as the next step.  The arithmetic that leads to a code is in 32
 // bits, each operation rounded by itself (no fused ones), so that the codes are the same wherever they are computed.
+#include <cuda_fp16.h>
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>
@@ -46,7 +47,7 @@ struct Chunk {
 
 struct Hyper {
     double lr, log_beta1, log_beta2, max_norm, grad_scale;
-    float beta1, rest1, beta2, rest2, eps;
+    float beta1, rest1, beta2, rest2, eps, minus_zero;
     uint32_t seed_low, seed_high;
     int32_t stochastic;
 };
@@ -172,9 +173,129 @@ __device__ __forceinline__ Element stepped(const Hyper& h, const Common& c, cons
 
 __device__ __forceinline__ void store_param(float* p, float x, uint32_t, bool) { *p = x; }
 // Rounded to nearest, or up or down with the probabilities that keep the mean.
+__device__ __forceinline__ uint32_t chance_bits(float x, uint32_t word) {  // the upper 16 bits are the result's
+    const uint32_t bits = __float_as_uint(x);
+    return x == x ? bits + ((word * kMix2) >> 16) : 0x7fff0000u;
+}
 __device__ __forceinline__ void store_param(__nv_bfloat16* p, float x, uint32_t word, bool stochastic) {
-    if (stochastic && x == x) *p = __ushort_as_bfloat16(static_cast<unsigned short>((__float_as_uint(x) + ((word * kMix2) >> 16)) >> 16));
-    else *p = __float2bfloat16_rn(x);
+    *p = stochastic ? __ushort_as_bfloat16(static_cast<unsigned short>(chance_bits(x, word) >> 16)) : __float2bfloat16_rn(x);
+}
+
+// ---- eight elements of a thread ----------------------------------------------------------------------------------------
+
+// In place arrays are read with ordinary loads: the same thread writes them back.
+__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
+    asm volatile("ld.global.L1::no_allocate.v8.f32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3]), "=f"(x[4]), "=f"(x[5]), "=f"(x[6]), "=f"(x[7])
+                 : "l"(p)
+                 : "memory");
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&x)[8]) {
+    uint4 v;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = Storage<__nv_bfloat16>::get(v, e);
+}
+__device__ __forceinline__ uint2 load8(const uint8_t* p) {
+    uint2 v;
+    asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");
+    return v;
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]),
+                 "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7])
+                 : "memory");
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+    *reinterpret_cast<uint4*>(p) = Storage<__nv_bfloat16>::pack(x);
+}
+
+// Eight codes of m, or of a root, and back.
+__device__ __forceinline__ void m_values(uint2 codes, uint32_t scale, float (&m)[8]) {
+    const float unit = power_of(scale);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t two = (q < 2 ? codes.x : codes.y) >> (16 * (q & 1));
+        uint32_t halves;
+        asm("{\n .reg .b16 lo;\n cvt.u16.u32 lo, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}" : "=r"(halves) : "r"(two));
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&halves));
+        m[2 * q] = x.x * unit;
+        m[2 * q + 1] = x.y * unit;
+    }
+}
+// A half has the same kind of fraction with five bits of exponent: a code moved up by 6 is one, 2^8 too small.
+__device__ __forceinline__ void root_values(uint2 codes, uint32_t scale, float (&r)[8]) {
+    const float unit = scale ? power_of(min(scale + 8u, 254u)) : 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t word = q < 2 ? codes.x : codes.y;
+        const uint32_t halves = __byte_perm(word, 0, q & 1 ? 0x3424 : 0x1404) >> 2;
+        const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&halves));
+        r[2 * q] = x.x * unit;
+        r[2 * q + 1] = x.y * unit;
+    }
+}
+
+template <bool k8>
+struct Octet {
+    float theta[8], m[8], v[8];  // v: r with states in 8 bits
+};
+
+__device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
+// A product that is rounded before it is added to anything: the compiler makes one fused operation of a packed product and a
+// packed sum (seen where the two cancel).  This one adds -0, which changes nothing, from an argument, so that the compiler does not know it.
+__device__ __forceinline__ f32x2 product(f32x2 a, f32x2 b, f32x2 minus_zero) { return fma2(a, b, minus_zero); }
+
+template <bool k8>
+__device__ __forceinline__ void step_octet(const Hyper& h, const Common& c, const Rates& rates, Octet<k8>& o, const float (&grad)[8]) {
+    const f32x2 coefficient = both(c.coefficient), beta1 = both(h.beta1), rest1 = both(h.rest1), beta2 = both(h.beta2),
+                rest2 = both(h.rest2), keep = both(rates.keep), speed = both(-rates.speed), spread = both(c.spread), eps = both(h.eps);
+    const f32x2 none = both(h.minus_zero);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f32x2 g = mul2(pack2(grad[2 * q], grad[2 * q + 1]), coefficient);
+        const f32x2 m = add2(product(pack2(o.m[2 * q], o.m[2 * q + 1]), beta1, none), product(g, rest1, none));
+        f32x2 v = pack2(o.v[2 * q], o.v[2 * q + 1]);
+        if (k8) v = mul2(v, v);
+        v = add2(product(v, beta2, none), product(mul2(g, g), rest2, none));
+        float v0, v1, r0, r1, i0, i1;
+        unpack2(v, v0, v1);
+        if (k8) {
+            r0 = __fsqrt_rn(v0), r1 = __fsqrt_rn(v1);
+            o.v[2 * q] = r0, o.v[2 * q + 1] = r1;
+        } else {
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(r0) : "f"(v0));
+            asm("sqrt.approx.f32 %0, %1;" : "=f"(r1) : "f"(v1));
+            o.v[2 * q] = v0, o.v[2 * q + 1] = v1;
+        }
+        unpack2(fma2(pack2(r0, r1), spread, eps), i0, i1);
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(i0) : "f"(i0));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(i1) : "f"(i1));
+        const f32x2 theta = fma2(mul2(m, speed), pack2(i0, i1), mul2(pack2(o.theta[2 * q], o.theta[2 * q + 1]), keep));
+        unpack2(m, o.m[2 * q], o.m[2 * q + 1]);
+        unpack2(theta, o.theta[2 * q], o.theta[2 * q + 1]);
+    }
+}
+
+// The largest magnitude of eight; NaN if there is one.
+__device__ __forceinline__ float largest(const float (&x)[8]) {
+    float a = fabsf(x[0]);
+#pragma unroll
+    for (int e = 1; e < 8; ++e) a = max_nan(a, fabsf(x[e]));
+    return a;
+}
+__device__ __noinline__ float largest_finite(float a, float b) {
+    return fmaxf(__uint_as_float(finite_bits(a)), __uint_as_float(finite_bits(b)));
+}
+// Of a block: four threads with eight elements each.
+__device__ __forceinline__ uint32_t block_scale(float mine) {
+    uint32_t bits = __float_as_uint(mine);
+    bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 1));
+    bits = max(bits, __shfl_xor_sync(0xffffffffu, bits, 2));
+    return scale_of(bits);
+}
+__device__ __forceinline__ uint32_t pack_bytes(const uint32_t* x) {
+    return __byte_perm(__byte_perm(x[0], x[1], 0x0040), __byte_perm(x[2], x[3], 0x0040), 0x5410);
 }
 
 // The last CTA to come here counts the step and leaves the ticket as it was.
@@ -186,6 +307,125 @@ __device__ __forceinline__ void count_step(int64_t* step, unsigned* ticket) {
             *ticket = 0;
             *step += 1;
         }
+    }
+}
+
+// Every array of the tensor lies at a multiple of eight of its elements.
+template <typename P, typename G, bool kMaster, bool k8>
+__device__ __forceinline__ bool whole_vectors(const Record& r) {
+    const auto off = [](const void* p, uint32_t size) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & (8u * size - 1u); };
+    return (off(r.param, sizeof(P)) | off(r.grad, sizeof(G)) | (kMaster ? off(r.master, 4) : 0u) | off(r.m, k8 ? 1 : 4) | off(r.v, k8 ? 1 : 4)) == 0;
+}
+
+// Eight elements from i on (fewer where the tensor ends), of a tensor whose arrays are aligned; all threads of a warp.
+template <typename P, typename G, bool kMaster, bool k8>
+__device__ __forceinline__ void step_vector(const Hyper& h, const Common& c, const Rates& rates, const Record& r, int64_t i, bool stochastic) {
+    const int here = static_cast<int>(max(min(r.numel - i, static_cast<int64_t>(kOctet)), static_cast<int64_t>(0)));
+    Octet<k8> o;
+    float g[8];
+    uint2 mc = {0, 0}, vc = {0, 0};
+    uint32_t ms = 0, vs = 0;
+    if (here == kOctet) {
+        load8(static_cast<const G*>(r.grad) + i, g);
+        if constexpr (kMaster) load8(r.master + i, o.theta);
+        else load8(static_cast<const P*>(r.param) + i, o.theta);
+        if constexpr (k8) {
+            mc = load8(static_cast<const uint8_t*>(r.m) + i), vc = load8(static_cast<const uint8_t*>(r.v) + i);
+        } else {
+            load8(static_cast<const float*>(r.m) + i, o.m);
+            load8(static_cast<const float*>(r.v) + i, o.v);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < kOctet; ++e) {
+            g[e] = o.theta[e] = 0.0f;
+            if constexpr (!k8) o.m[e] = o.v[e] = 0.0f;
+            if (e >= here) continue;
+            g[e] = Storage<G>::load1(static_cast<const G*>(r.grad) + i + e);
+            o.theta[e] = kMaster ? r.master[i + e] : load_rw(static_cast<const P*>(r.param) + i + e);
+            if constexpr (k8) {
+                const uint32_t a = static_cast<const uint8_t*>(r.m)[i + e], b = static_cast<const uint8_t*>(r.v)[i + e];
+                (e < 4 ? mc.x : mc.y) |= a << (8 * (e & 3));
+                (e < 4 ? vc.x : vc.y) |= b << (8 * (e & 3));
+            } else {
+                o.m[e] = static_cast<const float*>(r.m)[i + e];
+                o.v[e] = static_cast<const float*>(r.v)[i + e];
+            }
+        }
+    }
+    if constexpr (k8) {
+        if (here) ms = r.m_scale[i / QN_ADAM_BLOCK], vs = r.v_scale[i / QN_ADAM_BLOCK];
+        m_values(mc, ms, o.m);
+        root_values(vc, vs, o.v);
+    }
+    step_octet<k8>(h, c, rates, o, g);
+    const uint32_t word = k8 || stochastic ? octet_word(c.key, r.octet + i / kOctet) : 0;
+    if constexpr (k8) {
+        float top_m = largest(o.m), top_r = largest(o.v);
+        const bool odd = !(top_m < INFINITY) || !(top_r < INFINITY);  // something is not finite
+        if (odd) {
+            top_m = top_r = 0.0f;
+#pragma unroll
+            for (int e = 0; e < kOctet; ++e) top_m = largest_finite(top_m, o.m[e]), top_r = largest_finite(top_r, o.v[e]);
+        }
+        ms = block_scale(top_m);
+        vs = block_scale(top_r);
+        const float up_m = up_by(ms), up_r = up_by(vs);
+        uint32_t a[8], b[8];
+#pragma unroll
+        for (int e = 0; e < kOctet; ++e) {
+            const uint32_t w = element_word(word, e);
+            a[e] = ((magnitude_bits(o.m[e], up_m) + (((w >> 12) & 0xffff0u) | 8u)) >> 20) | (o.m[e] < 0.0f ? 0x80u : 0u);
+            b[e] = max((magnitude_bits(o.v[e], up_r) + (((w << 3) & 0x7fff8u) | 4u)) >> 19, min(__float_as_uint(o.v[e]), 1u));
+        }
+        if (odd) {
+#pragma unroll
+            for (int e = 0; e < kOctet; ++e) {
+                const uint32_t w = element_word(word, e);
+                a[e] = m_code(o.m[e], up_m, w), b[e] = root_code(o.v[e], up_r, w);
+            }
+        }
+        mc = make_uint2(pack_bytes(a), pack_bytes(a + 4));
+        vc = make_uint2(pack_bytes(b), pack_bytes(b + 4));
+        if (here && (i / kOctet) % 4 == 0) {
+            r.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(ms);
+            r.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(vs);
+        }
+    }
+    if (here == kOctet) {
+        if constexpr (k8) {
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(r.m) + i) = mc;
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(r.v) + i) = vc;
+        } else {
+            store8(static_cast<float*>(r.m) + i, o.m);
+            store8(static_cast<float*>(r.v) + i, o.v);
+        }
+        if constexpr (kMaster) store8(r.master + i, o.theta);
+        if constexpr (sizeof(P) == 2) {
+            if (stochastic) {
+                uint32_t x[8];
+#pragma unroll
+                for (int e = 0; e < kOctet; ++e) x[e] = chance_bits(o.theta[e], element_word(word, e));
+                *reinterpret_cast<uint4*>(static_cast<P*>(r.param) + i) =
+                    make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632), __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
+                return;
+            }
+        }
+        store8(static_cast<P*>(r.param) + i, o.theta);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < kOctet; ++e) {
+        if (e >= here) continue;
+        if constexpr (k8) {
+            static_cast<uint8_t*>(r.m)[i + e] = static_cast<uint8_t>((e < 4 ? mc.x : mc.y) >> (8 * (e & 3)));
+            static_cast<uint8_t*>(r.v)[i + e] = static_cast<uint8_t>((e < 4 ? vc.x : vc.y) >> (8 * (e & 3)));
+        } else {
+            static_cast<float*>(r.m)[i + e] = o.m[e];
+            static_cast<float*>(r.v)[i + e] = o.v[e];
+        }
+        if constexpr (kMaster) r.master[i + e] = o.theta[e];
+        store_param(static_cast<P*>(r.param) + i + e, o.theta[e], element_word(word, e), stochastic);
     }
 }
 
@@ -206,6 +446,13 @@ __global__ void __launch_bounds__(kThreads) adam_step_kernel(const Record* recor
         const Rates rates(c, r);
         const int64_t begin = static_cast<int64_t>(chunk.first) * kPiece;
         const int64_t end = min(r.numel, begin + static_cast<int64_t>(pieces) * kPiece);
+        if (whole_vectors<P, G, kMaster, k8>(r)) {  // eight elements a thread
+            for (int64_t base = begin; base < end; base += kPiece) {
+                const int64_t i = base + threadIdx.x * kOctet;
+                step_vector<P, G, kMaster, k8>(h, c, rates, r, i, stochastic);
+            }
+            continue;
+        }
         // an element a lane: a warp has one block of 32
         for (int64_t base = begin + (threadIdx.x & ~31u); base < end; base += kThreads) {
             const int64_t i = base + (threadIdx.x & 31);
@@ -265,7 +512,19 @@ __global__ void __launch_bounds__(kThreads) adam_norm_kernel(const Record* recor
         if (!grad) continue;
         const int64_t begin = static_cast<int64_t>(chunk.first) * kPiece;
         const int64_t end = min(numel, begin + static_cast<int64_t>(pieces) * kPiece);
-        for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
+        int64_t i = begin + threadIdx.x;
+        if (reinterpret_cast<uintptr_t>(grad) % (kOctet * sizeof(G)) == 0) {  // eight elements a thread
+#pragma unroll 4
+            for (int64_t at8 = begin + threadIdx.x * kOctet; at8 + kOctet <= end; at8 += kPiece) {
+                float g[kOctet];
+                load8(grad + at8, g);
+#pragma unroll
+                for (int e = 0; e < kOctet; ++e) sum += static_cast<double>(g[e]) * g[e];
+            }
+            i = end - (end - begin) % kOctet + threadIdx.x;
+        }
+#pragma unroll 1
+        for (; i < end; i += kThreads) {
             const double g = Storage<G>::load1(grad + i);
             sum += g * g;
         }
@@ -301,7 +560,30 @@ __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Record* reco
         const int64_t begin = static_cast<int64_t>(chunk.first) * kPiece;
         const int64_t whole = (r.numel + QN_ADAM_BLOCK - 1) / QN_ADAM_BLOCK * QN_ADAM_BLOCK;
         const int64_t end = min(whole, begin + static_cast<int64_t>(pieces) * kPiece);
-        for (int64_t i = begin + threadIdx.x; i < end; i += kThreads) {
+        int64_t i = begin + threadIdx.x;
+        T *m_to = m_out ? m_out + r.octet * kOctet : nullptr, *root_to = root_out ? root_out + r.octet * kOctet : nullptr;
+        const uintptr_t places = (reinterpret_cast<uintptr_t>(m_out) | reinterpret_cast<uintptr_t>(root_out)) % (kOctet * sizeof(T));
+        if (places == 0 && (reinterpret_cast<uintptr_t>(r.m) | reinterpret_cast<uintptr_t>(r.v)) % (kOctet * (k8 ? 1 : 4)) == 0) {
+            const int64_t full = min(end, r.numel / kOctet * kOctet);
+#pragma unroll 2
+            for (int64_t a = begin + threadIdx.x * kOctet; a < full; a += kPiece) {
+                float m[8], root[8];
+                if constexpr (k8) {
+                    m_values(load8(static_cast<const uint8_t*>(r.m) + a), r.m_scale[a / QN_ADAM_BLOCK], m);
+                    root_values(load8(static_cast<const uint8_t*>(r.v) + a), r.v_scale[a / QN_ADAM_BLOCK], root);
+                } else {
+                    load8(static_cast<const float*>(r.m) + a, m);
+                    load8(static_cast<const float*>(r.v) + a, root);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) root[e] = __fsqrt_rn(root[e]);
+                }
+                if (m_to) store8(m_to + a, m);
+                if (root_to) store8(root_to + a, root);
+            }
+            i = max(begin, full) + threadIdx.x;
+        }
+#pragma unroll 1
+        for (; i < end; i += kThreads) {
             float m = 0.0f, root = 0.0f;
             if (i < r.numel) {
                 if constexpr (k8) {
@@ -312,8 +594,8 @@ __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Record* reco
                     root = __fsqrt_rn(static_cast<const float*>(r.v)[i]);
                 }
             }
-            if (m_out) store_value(m_out + r.octet * kOctet + i, m);
-            if (root_out) store_value(root_out + r.octet * kOctet + i, root);
+            if (m_to) store_value(m_to + i, m);
+            if (root_to) store_value(root_to + i, root);
         }
     }
 }
@@ -368,9 +650,16 @@ bool check_grad(const qn_adam_plan& h, const void* p, int64_t numel) {
     return next == h.written.begin() || (next - 1)->second <= lo;
 }
 
-template <typename K, typename... A>
-cudaError_t launch(K kernel, int ctas, cudaStream_t st, A... args) {
-    kernel<<<ctas, kThreads, 0, st>>>(args...);
+// As many CTAs as are on the device at once (asked for once), or one for each chunk.
+template <typename... P, typename... A>
+cudaError_t launch(void (*kernel)(P...), int& resident, const qn_adam_plan& h, cudaStream_t st, A... args) {
+    if (resident == 0) {
+        int found = 0;
+        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&found, kernel, kThreads, 0);
+        if (e != cudaSuccess) return e;
+        resident = std::max(1, std::min(found, kMostCtas));
+    }
+    kernel<<<std::max(1, std::min(h.chunks, resident * qn_sm_count())), kThreads, 0, st>>>(args...);
     return cudaGetLastError();
 }
 
@@ -457,14 +746,13 @@ qn_status create(int32_t count, const qn_adam_tensor* tensors, qn_dtype param, q
     return QN_OK;
 }
 
-int ctas_of(const qn_adam_plan& h) { return std::max(1, std::min(h.chunks, h.most_ctas)); }
-
 template <typename P, typename G, bool kMaster>
 cudaError_t launch_step(const qn_adam_plan& h, const Hyper& hyper, int64_t* step, const float* lr, const double* sumsq, cudaStream_t st) {
-    const auto run = [&](auto kernel) {
-        return launch(kernel, ctas_of(h), st, static_cast<const Record*>(h.records), static_cast<const Chunk*>(h.chunk), h.chunks, h.pieces, hyper, step, lr, sumsq, h.tickets);
+    static int resident[2];
+    const auto run = [&](auto kernel, int& r) {
+        return launch(kernel, r, h, st, static_cast<const Record*>(h.records), static_cast<const Chunk*>(h.chunk), h.chunks, h.pieces, hyper, step, lr, sumsq, h.tickets);
     };
-    return h.eight ? run(adam_step_kernel<P, G, kMaster, true>) : run(adam_step_kernel<P, G, kMaster, false>);
+    return h.eight ? run(adam_step_kernel<P, G, kMaster, true>, resident[1]) : run(adam_step_kernel<P, G, kMaster, false>, resident[0]);
 }
 
 }  // namespace
@@ -518,10 +806,11 @@ extern "C" qn_status qn_adam_norm(qn_adam_handle h, double* sumsq, void* cuda_st
     if (!guard.ok) return QN_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:adam_norm");
-    const auto run = [&](auto kernel) {
-        return launch(kernel, ctas_of(*h), st, static_cast<const Record*>(h->records), static_cast<const Chunk*>(h->chunk), h->chunks, h->pieces, h->partials, h->tickets + 1, sumsq);
+    static int resident[2];
+    const auto run = [&](auto kernel, int& r) {
+        return launch(kernel, r, *h, st, static_cast<const Record*>(h->records), static_cast<const Chunk*>(h->chunk), h->chunks, h->pieces, h->partials, h->tickets + 1, sumsq);
     };
-    const cudaError_t e = h->grad == QN_F32 ? run(adam_norm_kernel<float>) : run(adam_norm_kernel<__nv_bfloat16>);
+    const cudaError_t e = h->grad == QN_F32 ? run(adam_norm_kernel<float>, resident[0]) : run(adam_norm_kernel<__nv_bfloat16>, resident[1]);
     nvtxRangePop();
     return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }
@@ -532,7 +821,7 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     if (!h || !step || !check_array(step, 8, h->device) || !check_array(lr_device, 4, h->device) || !check_array(sumsq, 8, h->device))
         return QN_ERR_INVALID;
     if (!lr_device && !(lr >= 0.0 && isfinite(lr))) return QN_ERR_INVALID;
-    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(static_cast<float>(eps) > 0.0f) || !isfinite(static_cast<float>(eps)))
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0) || !(static_cast<float>(eps) >= 0x1p-126f) || !isfinite(static_cast<float>(eps)))
         return QN_ERR_INVALID;
     if (max_norm != max_norm || (max_norm > 0.0 && !sumsq) || !isfinite(grad_scale)) return QN_ERR_INVALID;
     if (rounding != QN_ROUND_NEAREST && rounding != QN_ROUND_STOCHASTIC) return QN_ERR_INVALID;
@@ -540,7 +829,7 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     if (!guard.ok) return QN_ERR_CUDA;
     const Hyper hyper{lr, log(beta1), log(beta2), max_norm, grad_scale,
                       static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                      static_cast<float>(eps), static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32), rounding == QN_ROUND_STOCHASTIC};
+                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32), rounding == QN_ROUND_STOCHASTIC};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:adam_step");
     const auto by_grad = [&](auto grad) {
@@ -569,10 +858,11 @@ extern "C" qn_status qn_adam_state(qn_adam_handle h, qn_dtype dtype, void* m, vo
     nvtxRangePushA("qn:adam_state");
     const auto by_type = [&](auto t) {
         using T = decltype(t);
-        const auto run = [&](auto kernel) {
-            return launch(kernel, ctas_of(*h), st, static_cast<const Record*>(h->records), static_cast<const Chunk*>(h->chunk), h->chunks, h->pieces, static_cast<T*>(m), static_cast<T*>(root));
+        static int resident[2];
+        const auto run = [&](auto kernel, int& r) {
+            return launch(kernel, r, *h, st, static_cast<const Record*>(h->records), static_cast<const Chunk*>(h->chunk), h->chunks, h->pieces, static_cast<T*>(m), static_cast<T*>(root));
         };
-        return h->eight ? run(adam_state_kernel<T, true>) : run(adam_state_kernel<T, false>);
+        return h->eight ? run(adam_state_kernel<T, true>, resident[1]) : run(adam_state_kernel<T, false>, resident[0]);
     };
     const cudaError_t e = dtype == QN_F32 ? by_type(float()) : by_type(__nv_bfloat16());
     nvtxRangePop();
