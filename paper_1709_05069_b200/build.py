@@ -11,10 +11,10 @@ _INCLUDE = os.path.join(os.path.dirname(_PKG), "include")
 LIB_PATH = os.path.join(_PKG, "libqn.so")
 
 SOURCES = ["qn_api.cu", "qn_gram.cu", "qn_solve.cu", "qn_combine.cu", "qn_row.cu", "qn_static.cu", "qn_gram_tc.cu",
-           "qn_logprobs.cu", "qn_distill.cu", "qn_adam.cu",
+           "qn_logprobs.cu", "qn_distill.cu", "qn_adam.cu", "qn_adam_step.cu",
            "qn_policy.cu", "qn_preference.cu"]
 HEADERS = ["qn_internal.h", "qn_device.cuh", "qn_host.h", "qn_vocab.cuh",
-           "qn_vocab_grad.cuh"]
+           "qn_vocab_grad.cuh", "qn_adam.cuh"]
 
 NVCC_FLAGS = [
     "-gencode", "arch=compute_100a,code=sm_100a",

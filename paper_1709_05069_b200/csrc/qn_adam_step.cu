@@ -1,0 +1,613 @@
+// qn_adam_step: AdamW over the tensors of one parameter vector, with states in 32 bits or in 8.
+//
+// Per element, with g~ = c g (c: the clip coefficient times grad_scale) and t the number of this step:
+//     m' = b1 m + (1 - b1) g~        v' = b2 v + (1 - b2) g~^2        r' = sqrt(v')
+//     theta' = theta (1 - lr wd) - lr / (1 - b1^t) m' / (r' / sqrt(1 - b2^t) + eps)
+// Nothing is reused, so the floor is the bytes: each array once in and once out.
+//
+// CTAs stay, and each goes through a run of the pieces backwards: the last gradients that qn_adam_norm has read are the first
+// to be read again, from L2.  A thread has eight elements, in vectors of 8 to 32 bytes.  Tensors that do not lie on such
+// vectors go an element a lane, eight of them at a time, so that their loads are whole lines too.
+#include <nvtx3/nvToolsExt.h>
+
+#include "qn_adam.cuh"
+
+namespace {
+
+struct Hyper {
+    double lr, log_beta1, log_beta2, max_norm, grad_scale;
+    float beta1, rest1, beta2, rest2, eps, minus_zero;
+    uint32_t seed_low, seed_high;
+    int32_t stochastic;
+};
+
+// What is the same for all elements of a step.
+struct Common {
+    double lr, speed;           // learning rate, and lr / (1 - b1^t)
+    float coefficient, spread;  // spread: 1 / sqrt(1 - b2^t)
+    uint32_t key;
+    bool skip;  // the gradients' norm is not finite
+};
+struct Setting {
+    Hyper h;
+    Common c;
+};
+
+__device__ __forceinline__ Common common_of(const Hyper& h, const int64_t* step, const float* lr, const double* sumsq) {
+    Common c;
+    const int64_t t = *step + 1;
+    c.lr = lr ? static_cast<double>(*lr) : h.lr;
+    c.speed = c.lr / -expm1(static_cast<double>(t) * h.log_beta1);
+    c.spread = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(t) * h.log_beta2)));
+    double coefficient = h.grad_scale;
+    c.skip = false;
+    if (sumsq) {
+        const double norm = sqrt(*sumsq) * fabs(h.grad_scale);
+        c.skip = !isfinite(norm);
+        if (h.max_norm > 0.0 && norm > h.max_norm) coefficient *= h.max_norm / norm;
+    }
+    c.coefficient = static_cast<float>(coefficient);
+    c.key = step_key(h.seed_low, h.seed_high, t);
+    return c;
+}
+
+// The same for all elements of a tensor.
+struct Rates {
+    float keep, speed;  // 1 - lr wd, lr / (1 - b1^t)
+    __device__ __forceinline__ Rates(const Common& c, const Record& r)
+        : keep(static_cast<float>(1.0 - c.lr * r.lr_scale * r.decay)), speed(static_cast<float>(c.speed * r.lr_scale)) {}
+};
+
+// Where a run of a tensor's elements begins, and how many there are.  S: float, or uint8_t for codes.
+template <typename P, typename G, bool kMaster, typename S>
+struct Part {
+    P* param;
+    const G* grad;
+    float* master;
+    S *m, *v;
+    uint8_t *m_scale, *v_scale;
+    uint32_t octet;  // the first one's place (its low half: the hash takes no more)
+    int32_t count;
+    __device__ __forceinline__ Part(const Record& r, int64_t begin, int64_t count_)
+        : param(static_cast<P*>(r.param) + begin), grad(static_cast<const G*>(r.grad) + begin),
+          master(kMaster ? r.master + begin : nullptr), m(static_cast<S*>(r.m) + begin), v(static_cast<S*>(r.v) + begin),
+          m_scale(r.m_scale + begin / QN_ADAM_BLOCK), v_scale(r.v_scale + begin / QN_ADAM_BLOCK),
+          octet(static_cast<uint32_t>(r.octet + begin / kOctet)), count(static_cast<int32_t>(count_)) {}
+    __device__ __forceinline__ float theta(int i) const { return kMaster ? master[i] : load_rw(param + i); }
+    // every array at a multiple of eight of its elements
+    __device__ __forceinline__ bool whole_vectors() const {
+        const auto off = [](const void* p, uint32_t size) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) & (8u * size - 1u); };
+        return (off(param, sizeof(P)) | off(grad, sizeof(G)) | (kMaster ? off(master, 4) : 0u) | off(m, sizeof(S)) | off(v, sizeof(S))) == 0;
+    }
+};
+
+// ---- one element -------------------------------------------------------------------------------------------------------
+
+struct Element {
+    float theta, m, v, root;
+};
+// m and v: before the step.
+__device__ __forceinline__ Element stepped(const Hyper& h, const Common& c, const Rates& rates, float theta, float g, float m, float v) {
+    Element e;
+    g = __fmul_rn(g, c.coefficient);
+    e.m = __fadd_rn(__fmul_rn(m, h.beta1), __fmul_rn(g, h.rest1));
+    e.v = __fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2));
+    e.root = __fsqrt_rn(e.v);
+    // 2 ulp of the step are far below the rounding of theta
+    e.theta = theta * rates.keep - __fdividef(e.m * rates.speed, e.root * c.spread + h.eps);
+    return e;
+}
+
+__device__ __forceinline__ uint32_t chance_bits(float x, uint32_t word) {  // the upper 16 bits are the result's
+    const uint32_t bits = __float_as_uint(x);
+    return x == x ? bits + ((word * kMix2) >> 16) : 0x7fff0000u;
+}
+__device__ __forceinline__ void store_param(float* p, float x, uint32_t, bool) { *p = x; }
+// Rounded to nearest, or up or down with the probabilities that keep the mean.
+__device__ __forceinline__ void store_param(__nv_bfloat16* p, float x, uint32_t word, bool stochastic) {
+    *p = stochastic ? __ushort_as_bfloat16(static_cast<unsigned short>(chance_bits(x, word) >> 16)) : __float2bfloat16_rn(x);
+}
+
+// Element i from memory, with states in 32 bits; and with those in 8, whose block had the scales m_scale and v_scale.
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ Element element_at(const Setting& set, const Rates& rates, const Part<P, G, kMaster, float>& p, int i) {
+    return stepped(set.h, set.c, rates, p.theta(i), Storage<G>::load1(p.grad + i), p.m[i], p.v[i]);
+}
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ Element element_at(const Setting& set, const Rates& rates, const Part<P, G, kMaster, uint8_t>& p, int i,
+                                              uint32_t m_scale, uint32_t v_scale) {
+    const float root = root_value(p.v[i], v_scale);
+    return stepped(set.h, set.c, rates, p.theta(i), Storage<G>::load1(p.grad + i), m_value(p.m[i], m_scale), __fmul_rn(root, root));
+}
+
+// ---- eight elements, packed ----------------------------------------------------------------------------------------------
+
+// A product that is rounded before it is added to anything: the compiler makes one fused operation of a packed product and a
+// packed sum (seen where the two cancel).  This one adds -0, which changes nothing, from an argument, so that the compiler does
+// not know it.
+__device__ __forceinline__ f32x2 product(f32x2 a, f32x2 b, f32x2 minus_zero) { return fma2(a, b, minus_zero); }
+
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// theta' from m' and -r', two elements.
+__device__ __forceinline__ f32x2 moved(const Hyper& h, const Common& c, const Rates& rates, f32x2 theta, f32x2 m, f32x2 minus_r) {
+    float d0, d1;
+    unpack2(fma2(minus_r, both(c.spread), both(-h.eps)), d0, d1);
+    return fma2(mul2(m, both(rates.speed)), pack2(rcp_approx(d0), rcp_approx(d1)), mul2(theta, both(rates.keep)));
+}
+
+// States in 32 bits: theta, m and v before and after.
+__device__ __forceinline__ void step_pairs(const Hyper& h, const Common& c, const Rates& rates, f32x2 (&theta)[4], f32x2 (&m)[4],
+                                           f32x2 (&v)[4], const f32x2 (&grad)[4]) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f32x2 g = mul2(grad[q], both(c.coefficient));
+        m[q] = fma2(m[q], both(h.beta1), mul2(g, both(h.rest1)));
+        v[q] = fma2(v[q], both(h.beta2), mul2(mul2(g, g), both(h.rest2)));
+        float v0, v1, r0, r1;
+        unpack2(v[q], v0, v1);
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(r0) : "f"(v0));
+        asm("sqrt.approx.f32 %0, %1;" : "=f"(r1) : "f"(v1));
+        theta[q] = moved(h, c, rates, theta[q], m[q], pack2(-r0, -r1));
+    }
+}
+
+// max(a, |b|, |c|), NaN if there is one; min(a, |b|, |c|)
+__device__ __forceinline__ float largest(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float least(float a, float b, float c) {
+    float r;
+    asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// The root of a number in [2^-100, 2^100] rounded to nearest: s + e / (2 sqrt(v)) with the exact remainder e = v - s^2 (Markstein's
+// correction of a root), which was compared with the library's root at every one of these numbers.  Numbers come and go
+// with their signs changed, which spares the negations.
+constexpr float kRootLow = 0x1p-100f, kRootHigh = 0x1p100f;
+__device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
+    float v0, v1, y0, y1;
+    unpack2(minus_v, v0, v1);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y0) : "f"(-v0));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y1) : "f"(-v1));
+    const f32x2 y = pack2(y0, y1), s = mul2(minus_v, y);
+    return fma2(fma2(s, s, minus_v), mul2(y, both(0.5f)), s);
+}
+
+// States in 8 bits: m and r before the step become m' and -r'.  top_m: the largest m'; top_v: the largest v'.  False where this way is
+// not the right one: a second moment is 0, or very small or large, or something is not finite.
+__device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (&m)[4], f32x2 (&r)[4], const f32x2 (&grad)[4],
+                                        float& top_m, float& top_v) {
+    const f32x2 none = both(h.minus_zero);
+    float low_v = INFINITY;
+    top_m = top_v = 0.0f;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const f32x2 g = mul2(grad[q], both(c.coefficient));
+        m[q] = add2(product(m[q], both(h.beta1), none), product(g, both(h.rest1), none));
+        const f32x2 minus_v = add2(product(mul2(r[q], r[q]), both(-h.beta2), none), product(mul2(g, g), both(-h.rest2), none));
+        float m0, m1, v0, v1;
+        unpack2(m[q], m0, m1);
+        unpack2(minus_v, v0, v1);
+        top_m = largest(top_m, m0, m1);
+        top_v = largest(top_v, v0, v1);
+        low_v = least(low_v, v0, v1);
+        r[q] = minus_roots(minus_v);
+    }
+    return low_v >= kRootLow && top_v <= kRootHigh && top_m < INFINITY;
+}
+
+// What a block's elements are multiplied by, from the bits of its largest finite magnitude, which is not 0 (m: may be 0).
+__device__ __forceinline__ float up_root(uint32_t most) { return __uint_as_float((261u << 23) - (most & kInfinity)); }
+__device__ __forceinline__ float up_m(uint32_t most) { return up_root(max(most, 8u << 23)); }
+
+// Codes of two elements in the upper bytes: (bits + chance) moved up, a half of the chance's step added on the way; m's sign from m.
+// `word`: element_word, `upper` its upper half (which its last step does not change).
+__device__ __forceinline__ uint32_t m_byte(float z, float m, uint32_t upper) {
+    return (((__float_as_uint(z) + upper * 16u) * 16u + 128u) & 0x7fffffffu) | (__float_as_uint(m) & 0x80000000u);
+}
+__device__ __forceinline__ uint32_t root_byte(float z, uint32_t word) {
+    return max(__float_as_uint(z) + (word & 0xffffu) * 8u, (1u << 19) - 4u) * 32u + 128u;
+}
+__device__ __forceinline__ uint32_t upper_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
+// theta', codes, and theta' rounded by chance (in the upper halves), of two elements.
+template <bool kChance>
+struct Coded {
+    uint32_t m[2], r[2], theta[2];
+    f32x2 theta2;
+    // ups: what m and -r are multiplied by
+    __device__ __forceinline__ Coded(const Hyper& h, const Common& c, const Rates& rates, f32x2 theta_, f32x2 m_, f32x2 minus_r, f32x2 ups_m,
+                                     f32x2 ups_r, const uint32_t (&octets)[2], const uint32_t (&places)[2], bool stochastic) {
+        const f32x2 down = both(0x1p-120f);
+        float zm[2], zr[2], m1[2], t[2];
+        theta2 = moved(h, c, rates, theta_, m_, minus_r);
+        unpack2(mul2(mul2(m_, ups_m), down), zm[0], zm[1]);
+        unpack2(mul2(mul2(minus_r, ups_r), down), zr[0], zr[1]);
+        unpack2(m_, m1[0], m1[1]);
+        unpack2(theta2, t[0], t[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            uint32_t y = octets[k] + places[k];
+            y = (y ^ (y >> 15)) * kMix3;
+            const uint32_t upper = y >> 16;
+            y ^= upper;
+            m[k] = m_byte(zm[k], m1[k], upper);
+            r[k] = root_byte(zr[k], y);
+            theta[k] = __float_as_uint(t[k]) + (kChance && stochastic ? (y * kMix2) >> 16 : 0u);
+        }
+    }
+};
+
+// ---- tensors on vectors ----------------------------------------------------------------------------------------------------
+
+// Eight elements from i on, with states in 32 bits; element by element where there are fewer.
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
+                                           const Part<P, G, kMaster, float>& p, int i, bool stochastic) {
+    const uint32_t word = stochastic ? octet_word(c.key, p.octet + i / kOctet) : 0;
+    if (i + kOctet > p.count) {
+#pragma unroll 1
+        for (int e = i; e < p.count; ++e) {
+            const Element x = element_at(*set, rates, p, e);
+            p.m[e] = x.m, p.v[e] = x.v;
+            if constexpr (kMaster) p.master[e] = x.theta;
+            store_param(p.param + e, x.theta, element_word(word, e - i), stochastic);
+        }
+        return;
+    }
+    uint32_t graw[sizeof(G) == 4 ? 8 : 4], traw[kMaster || sizeof(P) == 4 ? 8 : 4], mraw[8], vraw[8];
+    load8(p.grad + i, graw);
+    if constexpr (kMaster) load8(p.master + i, traw);
+    else load8(p.param + i, traw);
+    load8(p.m + i, mraw);
+    load8(p.v + i, vraw);
+    f32x2 theta[4], m[4], v[4], g[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) theta[q] = two_of(traw, q), m[q] = two_of(mraw, q), v[q] = two_of(vraw, q), g[q] = two_of(graw, q);
+    step_pairs(h, c, rates, theta, m, v, g);
+    float t1[8], m1[8], v1[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) unpack2(theta[q], t1[2 * q], t1[2 * q + 1]), unpack2(m[q], m1[2 * q], m1[2 * q + 1]), unpack2(v[q], v1[2 * q], v1[2 * q + 1]);
+    store8(p.m + i, m1);
+    store8(p.v + i, v1);
+    if constexpr (kMaster) store8(p.master + i, t1);
+    if (sizeof(P) == 2 && stochastic) {
+        uint32_t x[8];
+#pragma unroll
+        for (int e = 0; e < kOctet; ++e) x[e] = chance_bits(t1[e], element_word(word, e));
+        *reinterpret_cast<uint4*>(p.param + i) = make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
+                                                            __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
+    } else {
+        store8(p.param + i, t1);
+    }
+}
+
+// Eight elements with states in 8 bits, as they lie in memory.
+template <typename P, typename G, bool kMaster>
+struct Raw {
+    uint32_t theta[kMaster || sizeof(P) == 4 ? 8 : 4], grad[sizeof(G) == 4 ? 8 : 4], m[2], v[2];
+    uint32_t m_scale, v_scale;
+    // From element i on; zeros if there are not eight.
+    __device__ __forceinline__ Raw(const Part<P, G, kMaster, uint8_t>& p, int i) {
+#pragma unroll
+        for (uint32_t& x : theta) x = 0;
+#pragma unroll
+        for (uint32_t& x : grad) x = 0;
+        m[0] = m[1] = v[0] = v[1] = m_scale = v_scale = 0;
+        if (i >= 0 && i + kOctet <= p.count) {
+            load8(p.grad + i, grad);
+            if constexpr (kMaster) load8(p.master + i, theta);
+            else load8(p.param + i, theta);
+            load8(p.m + i, m);
+            load8(p.v + i, v);
+        }
+        if (i >= 0 && i < p.count) m_scale = p.m_scale[i / QN_ADAM_BLOCK], v_scale = p.v_scale[i / QN_ADAM_BLOCK];
+    }
+};
+
+// For eight elements that are out of the ordinary, or fewer, from memory again: the largest finite magnitudes of m' and r'; and the step.
+template <typename P, typename G, bool kMaster>
+__device__ __noinline__ float2 largest_of_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
+                                              uint32_t v_scale) {
+    float2 top = {0.0f, 0.0f};
+#pragma unroll 1
+    for (int e = i; e < min(i + kOctet, p.count); ++e) {
+        const Element x = element_at(*set, rates, p, e, m_scale, v_scale);
+        top.x = fmaxf(top.x, __uint_as_float(finite_bits(x.m)));
+        top.y = fmaxf(top.y, __uint_as_float(finite_bits(x.root)));
+    }
+    return top;
+}
+template <typename P, typename G, bool kMaster>
+__device__ __noinline__ void step_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
+                                      uint32_t v_scale, uint32_t ms, uint32_t vs, bool stochastic) {
+    const uint32_t word = octet_word(set->c.key, p.octet + i / kOctet);
+#pragma unroll 1
+    for (int e = i; e < min(i + kOctet, p.count); ++e) {
+        const uint32_t w = element_word(word, e - i);
+        const Element x = element_at(*set, rates, p, e, m_scale, v_scale);
+        p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), w));
+        p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), w));
+        if constexpr (kMaster) p.master[e] = x.theta;
+        store_param(p.param + e, x.theta, w, stochastic);
+    }
+}
+
+// Eight elements from i on, or what there is of them; all threads of a warp, four of which have a block.
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
+                                           const Part<P, G, kMaster, uint8_t>& p, int i, bool stochastic, const Raw<P, G, kMaster>& raw) {
+    constexpr bool kChance = sizeof(P) == 2 && !kMaster;  // theta may be rounded by chance
+    f32x2 m[4], r[4], g[4];
+    float top_m, top_v;
+    m_values(raw.m, raw.m_scale, m);
+    root_values(raw.v, raw.v_scale, r);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
+    bool odd = !moments(h, c, m, r, g, top_m, top_v);
+    float top_r = __fsqrt_rn(top_v);  // the root of the largest is the largest root
+    if (odd) {
+        const float2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
+        top_m = top.x, top_r = top.y;
+    }
+#pragma unroll
+    for (int o = 1; o < 4; o *= 2) {
+        top_m = fmaxf(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
+        top_r = fmaxf(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
+    }
+    const uint32_t most_m = __float_as_uint(top_m), most_r = __float_as_uint(top_r);
+    if (i < p.count && (i / kOctet) % 4 == 0) {  // all four have read the old ones
+        p.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(scale_of(most_m));
+        p.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(scale_of(most_r));
+    }
+    const f32x2 ups_m = both(up_m(most_m)), ups_r = both(-up_root(most_r));
+    const uint32_t word = octet_word(c.key, p.octet + i / kOctet), octets[2] = {word, word};
+    uint32_t a[8], b[8], x[8];
+    f32x2 not_finite = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const uint32_t places[2] = {2 * q * kGolden, (2 * q + 1) * kGolden};
+        const Coded<kChance> two(h, c, rates, two_of(raw.theta, q), m[q], r[q], ups_m, ups_r, octets, places, stochastic);
+        if (kChance) not_finite = fma2(two.theta2, 0, not_finite);  // 0, or NaN
+#pragma unroll
+        for (int k = 0; k < 2; ++k) a[2 * q + k] = two.m[k], b[2 * q + k] = two.r[k], x[2 * q + k] = two.theta[k];
+    }
+    if (kChance) {
+        float n0, n1;
+        unpack2(not_finite, n0, n1);
+        odd = odd || n0 + n1 != 0.0f;
+    }
+    if (odd) return step_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale, scale_of(most_m), scale_of(most_r), stochastic);
+    *reinterpret_cast<uint2*>(p.m + i) = make_uint2(upper_bytes(a[0], a[1], a[2], a[3]), upper_bytes(a[4], a[5], a[6], a[7]));
+    *reinterpret_cast<uint2*>(p.v + i) = make_uint2(upper_bytes(b[0], b[1], b[2], b[3]), upper_bytes(b[4], b[5], b[6], b[7]));
+    if (kChance && stochastic) {
+        *reinterpret_cast<uint4*>(p.param + i) = make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
+                                                            __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
+    } else {
+        float t1[8];
+#pragma unroll
+        for (int e = 0; e < kOctet; ++e) t1[e] = __uint_as_float(x[e]);
+        if constexpr (kMaster) store8(p.master + i, t1);
+        store8(p.param + i, t1);
+    }
+}
+
+// ---- other tensors -----------------------------------------------------------------------------------------------------------
+
+// 256 elements of a warp, from i on: element i + 32 j + lane is lane's j-th.  States in 32 bits.
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
+                                           const Part<P, G, kMaster, float>& p, int i, bool stochastic) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t octet = stochastic ? octet_word(c.key, p.octet + i / kOctet + lane) : 0;  // of the warp's lane-th eight
+    float t[8], m[8], v[8], g[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int e = i + 32 * j + lane;
+        t[j] = m[j] = v[j] = g[j] = 0.0f;
+        if (e < p.count) t[j] = p.theta(e), m[j] = p.m[e], v[j] = p.v[e], g[j] = Storage<G>::load1(p.grad + e);
+    }
+    f32x2 t2[4], m2[4], v2[4], g2[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        t2[q] = pack2(t[2 * q], t[2 * q + 1]), m2[q] = pack2(m[2 * q], m[2 * q + 1]), v2[q] = pack2(v[2 * q], v[2 * q + 1]), g2[q] = pack2(g[2 * q], g[2 * q + 1]);
+    step_pairs(h, c, rates, t2, m2, v2, g2);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) unpack2(t2[q], t[2 * q], t[2 * q + 1]), unpack2(m2[q], m[2 * q], m[2 * q + 1]), unpack2(v2[q], v[2 * q], v[2 * q + 1]);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int e = i + 32 * j + lane;
+        const uint32_t word = stochastic ? element_word(__shfl_sync(0xffffffffu, octet, 4 * j + lane / 8), lane % 8) : 0;
+        if (e >= p.count) continue;
+        p.m[e] = m[j], p.v[e] = v[j];
+        if constexpr (kMaster) p.master[e] = t[j];
+        store_param(p.param + e, t[j], word, stochastic);
+    }
+    (void)set;
+}
+
+// The same for elements that are out of the ordinary, or fewer than 256, with states in 8 bits: a block at a time.
+template <typename P, typename G, bool kMaster>
+__device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, bool stochastic) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int base = i; base < min(i + 256, p.count); base += 32) {
+        const int e = base + lane, block = base / QN_ADAM_BLOCK;
+        Element x = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (e < p.count) x = element_at(*set, rates, p, e, p.m_scale[block], p.v_scale[block]);
+        const uint32_t ms = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.m)));
+        const uint32_t vs = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.root)));
+        const uint32_t word = element_word(octet_word(set->c.key, p.octet + e / kOctet), e % kOctet);
+        if (e < p.count) {
+            p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), word));
+            p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), word));
+            if constexpr (kMaster) p.master[e] = x.theta;
+            store_param(p.param + e, x.theta, word, stochastic);
+        }
+        if (lane == 0) p.m_scale[block] = static_cast<uint8_t>(ms), p.v_scale[block] = static_cast<uint8_t>(vs);
+    }
+}
+
+template <typename P, typename G, bool kMaster>
+__device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
+                                           const Part<P, G, kMaster, uint8_t>& p, int i, bool stochastic) {
+    constexpr bool kChance = sizeof(P) == 2 && !kMaster;
+    if (i >= p.count) return;
+    if (i + 256 > p.count) return step_lanes_any<P, G, kMaster>(set, rates, p, i, stochastic);
+    const int lane = threadIdx.x & 31, at = i + lane, block = i / QN_ADAM_BLOCK;
+    f32x2 m[4], r[4], g[4];
+    float t[8];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int e = at + 64 * q;
+        const uint32_t m0 = p.m[e], m1 = p.m[e + 32], r0 = p.v[e], r1 = p.v[e + 32];
+        m[q] = m_values(m0 + m1 * 256u, pack2(power_of(p.m_scale[block + 2 * q]), power_of(p.m_scale[block + 2 * q + 1])));
+        r[q] = root_values(r0 + r1 * 65536u, pack2(root_unit(p.v_scale[block + 2 * q]), root_unit(p.v_scale[block + 2 * q + 1])));
+        g[q] = pack2(Storage<G>::load1(p.grad + e), Storage<G>::load1(p.grad + e + 32));
+        t[2 * q] = p.theta(e), t[2 * q + 1] = p.theta(e + 32);
+    }
+    float top_m, top_v;
+    const bool odd = !moments(h, c, m, r, g, top_m, top_v);
+    if (__any_sync(0xffffffffu, odd)) return step_lanes_any<P, G, kMaster>(set, rates, p, i, stochastic);
+    const uint32_t octet = octet_word(c.key, p.octet + i / kOctet + lane);  // of the warp's lane-th eight
+    const uint32_t place = (lane % 8) * kGolden, places[2] = {place, place};
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        float m1[2], r1[2], t1[2];
+        uint32_t most_m[2], most_r[2], octets[2];
+        unpack2(m[q], m1[0], m1[1]);
+        unpack2(r[q], r1[0], r1[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            most_m[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(m1[k]) & 0x7fffffffu);
+            most_r[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(r1[k]) & 0x7fffffffu);
+            octets[k] = __shfl_sync(0xffffffffu, octet, 4 * (2 * q + k) + lane / 8);
+        }
+        const Coded<kChance> two(h, c, rates, pack2(t[2 * q], t[2 * q + 1]), m[q], r[q], pack2(up_m(most_m[0]), up_m(most_m[1])),
+                                 pack2(-up_root(most_r[0]), -up_root(most_r[1])), octets, places, stochastic);
+        unpack2(two.theta2, t1[0], t1[1]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int e = at + 64 * q + 32 * k;
+            p.m[e] = static_cast<uint8_t>(two.m[k] >> 24);
+            p.v[e] = static_cast<uint8_t>(two.r[k] >> 24);
+            if constexpr (kMaster) p.master[e] = t1[k];
+            if (kChance && stochastic) {
+                const uint32_t x = t1[k] == t1[k] ? two.theta[k] : 0x7fff0000u;
+                p.param[e] = P(__ushort_as_bfloat16(static_cast<unsigned short>(x >> 16)));
+            } else {
+                store_param(p.param + e, t1[k], 0, false);
+            }
+            if (lane == 0) {
+                p.m_scale[block + 2 * q + k] = static_cast<uint8_t>(scale_of(most_m[k]));
+                p.v_scale[block + 2 * q + k] = static_cast<uint8_t>(scale_of(most_r[k]));
+            }
+        }
+    }
+}
+
+// ---- the kernel ----------------------------------------------------------------------------------------------------------------
+
+// The last CTA to come here counts the step and leaves the ticket as it was.
+__device__ __forceinline__ void count_step(int64_t* step, unsigned* ticket) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
+            *ticket = 0;
+            *step += 1;
+        }
+    }
+}
+
+constexpr int64_t kMostPieces = 1 << 19;  // of a run: its elements are counted in 32 bits
+
+template <typename P, typename G, bool kMaster, typename S>
+__global__ void __launch_bounds__(kThreads) adam_step_kernel(const Tensors all, const Hyper h, int64_t* step, const float* lr,
+                                                             const double* sumsq, unsigned* ticket) {
+    __shared__ Setting set;
+    __shared__ int found;
+    const Share share(all.pieces);
+    if (share.hi > share.lo) find_tensor(all, share.hi - 1, &found);
+    if (threadIdx.x == 0) set.h = h, set.c = common_of(h, step, lr, sumsq);
+    __syncthreads();
+    const Common c = set.c;
+    if (c.skip) return;
+    const bool stochastic = h.stochastic && !kMaster && sizeof(P) == 2;
+    int tensor = found;
+#pragma unroll 1
+    for (int64_t piece = share.hi; piece > share.lo;) {
+        const Record r = all.records[tensor];
+        const int64_t first = all.first[tensor], from = max(max(share.lo, first), piece - kMostPieces), to = piece;
+        piece = from;
+        if (piece == first) --tensor;
+        if (to == from || !r.grad) continue;
+        const Rates rates(c, r);
+        const int64_t begin = (from - first) * kPiece;
+        const Part<P, G, kMaster, S> p(r, begin, min(r.numel - begin, (to - from) * kPiece));
+        const int last = static_cast<int>(to - from - 1) * kPiece;
+        if (!p.whole_vectors()) {
+#pragma unroll 1
+            for (int base = last; base >= 0; base -= kPiece) step_lanes(&set, h, c, rates, p, base + static_cast<int>(threadIdx.x / 32) * 256, stochastic);
+        } else if constexpr (sizeof(S) == 1) {
+            int i = last + threadIdx.x * kOctet;
+            Raw<P, G, kMaster> now(p, i);
+#pragma unroll 1
+            for (int base = last; base >= 0; base -= kPiece, i -= kPiece) {
+                const Raw<P, G, kMaster> next(p, i - kPiece);  // on its way meanwhile
+                step_octet(&set, h, c, rates, p, i, stochastic, now);
+                now = next;
+            }
+        } else {
+#pragma unroll 1
+            for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet(&set, h, c, rates, p, i, stochastic);
+        }
+    }
+    count_step(step, ticket);
+}
+
+template <typename P, typename G, bool kMaster>
+cudaError_t launch_step(const qn_adam_plan& h, const Hyper& hyper, int64_t* step, const float* lr, const double* sumsq, cudaStream_t st) {
+    static int resident[2];
+    return h.eight ? launch_over(adam_step_kernel<P, G, kMaster, uint8_t>, resident[1], h, st, hyper, step, lr, sumsq, h.tickets)
+                   : launch_over(adam_step_kernel<P, G, kMaster, float>, resident[0], h, st, hyper, step, lr, sumsq, h.tickets);
+}
+
+}  // namespace
+
+extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, const float* lr_device, double beta1, double beta2,
+                                  double eps, const double* sumsq, double max_norm, double grad_scale, int32_t rounding,
+                                  uint64_t seed, void* cuda_stream) {
+    if (!h || !step || !check_array(step, 8, h->device) || !check_array(lr_device, 4, h->device) || !check_array(sumsq, 8, h->device))
+        return QN_ERR_INVALID;
+    if (!lr_device && !(lr >= 0.0 && isfinite(lr))) return QN_ERR_INVALID;
+    if (!(beta1 >= 0.0 && beta1 < 1.0) || !(beta2 >= 0.0 && beta2 < 1.0)) return QN_ERR_INVALID;
+    if (!(static_cast<float>(eps) >= 0x1p-126f) || !isfinite(static_cast<float>(eps))) return QN_ERR_INVALID;
+    if (max_norm != max_norm || (max_norm > 0.0 && !sumsq) || !isfinite(grad_scale)) return QN_ERR_INVALID;
+    if (rounding != QN_ROUND_NEAREST && rounding != QN_ROUND_STOCHASTIC) return QN_ERR_INVALID;
+    DeviceGuard guard(h->device);
+    if (!guard.ok) return QN_ERR_CUDA;
+    const Hyper hyper{lr, log(beta1), log(beta2), max_norm, grad_scale,
+                      static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
+                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32), rounding == QN_ROUND_STOCHASTIC};
+    cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
+    nvtxRangePushA("qn:adam_step");
+    const auto by_grad = [&](auto grad) {
+        using G = decltype(grad);
+        if (h->param == QN_F32) return launch_step<float, G, false>(*h, hyper, step, lr_device, sumsq, st);
+        if (h->master) return launch_step<__nv_bfloat16, G, true>(*h, hyper, step, lr_device, sumsq, st);
+        return launch_step<__nv_bfloat16, G, false>(*h, hyper, step, lr_device, sumsq, st);
+    };
+    const cudaError_t e = h->grad == QN_F32 ? by_grad(float()) : by_grad(__nv_bfloat16());
+    nvtxRangePop();
+    return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
+}
