@@ -289,10 +289,10 @@ extern "C" qn_status qn_adam_norm(qn_adam_handle h, double* sumsq, void* cuda_st
     DeviceGuard guard(h->device);
     if (!guard.ok) return QN_ERR_CUDA;
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
-    static int resident[2];
+    static Resident resident[2];
     nvtxRangePushA("qn:adam_norm");
-    const cudaError_t e = h->grad == QN_F32 ? launch_over(adam_norm_kernel<float>, resident[0], *h, st, h->partials, h->tickets + 1, sumsq)
-                                            : launch_over(adam_norm_kernel<__nv_bfloat16>, resident[1], *h, st, h->partials, h->tickets + 1, sumsq);
+    const cudaError_t e = h->grad == QN_F32 ? launch_over(adam_norm_kernel<float>, resident[0], 0, *h, st, h->partials, h->tickets + 1, sumsq)
+                                            : launch_over(adam_norm_kernel<__nv_bfloat16>, resident[1], 0, *h, st, h->partials, h->tickets + 1, sumsq);
     nvtxRangePop();
     return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }
@@ -312,10 +312,10 @@ extern "C" qn_status qn_adam_state(qn_adam_handle h, qn_dtype dtype, void* m, vo
     nvtxRangePushA("qn:adam_state");
     const auto by_type = [&](auto t) {
         using T = decltype(t);
-        static int resident[2];
+        static Resident resident[2];
         T *m_out = static_cast<T*>(m), *root_out = static_cast<T*>(root);
-        return h->eight ? launch_over(adam_state_kernel<T, uint8_t>, resident[1], *h, st, m_out, root_out)
-                        : launch_over(adam_state_kernel<T, float>, resident[0], *h, st, m_out, root_out);
+        return h->eight ? launch_over(adam_state_kernel<T, uint8_t>, resident[1], 0, *h, st, m_out, root_out)
+                        : launch_over(adam_state_kernel<T, float>, resident[0], 0, *h, st, m_out, root_out);
     };
     const cudaError_t e = dtype == QN_F32 ? by_type(float()) : by_type(__nv_bfloat16());
     nvtxRangePop();

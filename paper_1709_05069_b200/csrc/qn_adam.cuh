@@ -207,17 +207,23 @@ struct qn_adam_plan {
 
 namespace {
 
-// As many CTAs as are on the device at once (asked for once), or one for each piece.
+// As many CTAs as are on the device at once (asked for once on each), or one for each piece.
+struct Resident {
+    int on[64];
+};
 template <typename... P, typename... A>
-cudaError_t launch_over(void (*kernel)(P...), int& resident, const qn_adam_plan& h, cudaStream_t st, A... args) {
+cudaError_t launch_over(void (*kernel)(P...), Resident& known, size_t shared, const qn_adam_plan& h, cudaStream_t st, A... args) {
+    if (h.device < 0 || h.device >= 64) return cudaErrorInvalidDevice;
+    int& resident = known.on[h.device];
     if (resident == 0) {
         int found = 0;
-        const cudaError_t e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&found, kernel, kThreads, 0);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(shared));
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&found, kernel, kThreads, shared);
         if (e != cudaSuccess) return e;
         resident = found < 1 ? 1 : found > kMostCtas ? kMostCtas : found;
     }
     const int64_t most = static_cast<int64_t>(resident) * qn_sm_count(), ctas = h.pieces < most ? h.pieces : most;
-    kernel<<<static_cast<unsigned>(ctas < 1 ? 1 : ctas), kThreads, 0, st>>>(h.tensors(), args...);
+    kernel<<<static_cast<unsigned>(ctas < 1 ? 1 : ctas), kThreads, shared, st>>>(h.tensors(), args...);
     return cudaGetLastError();
 }
 

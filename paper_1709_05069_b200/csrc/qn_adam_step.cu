@@ -18,7 +18,6 @@ struct Hyper {
     double lr, log_beta1, log_beta2, max_norm, grad_scale;
     float beta1, rest1, beta2, rest2, eps, minus_zero;
     uint32_t seed_low, seed_high;
-    int32_t stochastic;
 };
 
 // What is the same for all elements of a step.
@@ -102,10 +101,12 @@ __device__ __forceinline__ uint32_t chance_bits(float x, uint32_t word) {  // th
     const uint32_t bits = __float_as_uint(x);
     return x == x ? bits + ((word * kMix2) >> 16) : 0x7fff0000u;
 }
-__device__ __forceinline__ void store_param(float* p, float x, uint32_t, bool) { *p = x; }
-// Rounded to nearest, or up or down with the probabilities that keep the mean.
-__device__ __forceinline__ void store_param(__nv_bfloat16* p, float x, uint32_t word, bool stochastic) {
-    *p = stochastic ? __ushort_as_bfloat16(static_cast<unsigned short>(chance_bits(x, word) >> 16)) : __float2bfloat16_rn(x);
+// Rounded to nearest, or (kChance) up or down with the probabilities that keep the mean.
+template <bool kChance>
+__device__ __forceinline__ void store_param(float* p, float x, uint32_t) { *p = x; }
+template <bool kChance>
+__device__ __forceinline__ void store_param(__nv_bfloat16* p, float x, uint32_t word) {
+    *p = kChance ? __ushort_as_bfloat16(static_cast<unsigned short>(chance_bits(x, word) >> 16)) : __float2bfloat16_rn(x);
 }
 
 // Element i from memory, with states in 32 bits; and with those in 8, whose block had the scales m_scale and v_scale.
@@ -167,10 +168,10 @@ __device__ __forceinline__ float least(float a, float b, float c) {
     return r;
 }
 
-// The root of a number in [2^-100, 2^100] rounded to nearest: s + e / (2 sqrt(v)) with the exact remainder e = v - s^2 (Markstein's
+// The root of a number in [kLow, kHigh] rounded to nearest: s + e / (2 sqrt(v)) with the exact remainder e = v - s^2 (Markstein's
 // correction of a root), which was compared with the library's root at every one of these numbers.  Numbers come and go
 // with their signs changed, which spares the negations.
-constexpr float kRootLow = 0x1p-100f, kRootHigh = 0x1p100f;
+constexpr float kLow = 0x1p-100f, kHigh = 0x1p30f;
 __device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
     float v0, v1, y0, y1;
     unpack2(minus_v, v0, v1);
@@ -181,7 +182,7 @@ __device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
 }
 
 // States in 8 bits: m and r before the step become m' and -r'.  top_m: the largest m'; top_v: the largest v'.  False where this way is
-// not the right one: a second moment is 0, or very small or large, or something is not finite.
+// not the right one: a second moment is 0, or very small, or something is very large or not a number.
 __device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (&m)[4], f32x2 (&r)[4], const f32x2 (&grad)[4],
                                         float& top_m, float& top_v) {
     const f32x2 none = both(h.minus_zero);
@@ -200,12 +201,15 @@ __device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (
         low_v = least(low_v, v0, v1);
         r[q] = minus_roots(minus_v);
     }
-    return low_v >= kRootLow && top_v <= kRootHigh && top_m < INFINITY;
+    return low_v >= kLow && top_v <= kHigh && top_m <= kHigh;
 }
 
-// What a block's elements are multiplied by, from the bits of its largest finite magnitude, which is not 0 (m: may be 0).
-__device__ __forceinline__ float up_root(uint32_t most) { return __uint_as_float((261u << 23) - (most & kInfinity)); }
-__device__ __forceinline__ float up_m(uint32_t most) { return up_root(max(most, 8u << 23)); }
+// 2^-e / 2^120 (see magnitude_bits; below kHigh this is a number, and one product does for the two there) from the exponent
+// field of a block's largest finite magnitude, which is not 0 (m: may be 0).
+__device__ __forceinline__ float up_root(uint32_t field) { return power_of(261u - field) * 0x1p-120f; }
+__device__ __forceinline__ float up_m(uint32_t field) { return up_root(max(field, 8u)); }
+// Of the root, from v.  (The root of the largest v is the largest root, and does not round up to a power of two.)
+__device__ __forceinline__ uint32_t root_field(float v) { return ((__float_as_uint(v) >> 23) + 127u) >> 1; }
 
 // Codes of two elements in the upper bytes: (bits + chance) moved up, a half of the chance's step added on the way; m's sign from m.
 // `word`: element_word, `upper` its upper half (which its last step does not change).
@@ -226,12 +230,11 @@ struct Coded {
     f32x2 theta2;
     // ups: what m and -r are multiplied by
     __device__ __forceinline__ Coded(const Hyper& h, const Common& c, const Rates& rates, f32x2 theta_, f32x2 m_, f32x2 minus_r, f32x2 ups_m,
-                                     f32x2 ups_r, const uint32_t (&octets)[2], const uint32_t (&places)[2], bool stochastic) {
-        const f32x2 down = both(0x1p-120f);
+                                     f32x2 ups_r, const uint32_t (&octets)[2], const uint32_t (&places)[2]) {
         float zm[2], zr[2], m1[2], t[2];
         theta2 = moved(h, c, rates, theta_, m_, minus_r);
-        unpack2(mul2(mul2(m_, ups_m), down), zm[0], zm[1]);
-        unpack2(mul2(mul2(minus_r, ups_r), down), zr[0], zr[1]);
+        unpack2(mul2(m_, ups_m), zm[0], zm[1]);
+        unpack2(mul2(minus_r, ups_r), zr[0], zr[1]);
         unpack2(m_, m1[0], m1[1]);
         unpack2(theta2, t[0], t[1]);
 #pragma unroll
@@ -242,7 +245,7 @@ struct Coded {
             y ^= upper;
             m[k] = m_byte(zm[k], m1[k], upper);
             r[k] = root_byte(zr[k], y);
-            theta[k] = __float_as_uint(t[k]) + (kChance && stochastic ? (y * kMix2) >> 16 : 0u);
+            theta[k] = __float_as_uint(t[k]) + (kChance ? (y * kMix2) >> 16 : 0u);
         }
     }
 };
@@ -250,17 +253,17 @@ struct Coded {
 // ---- tensors on vectors ----------------------------------------------------------------------------------------------------
 
 // Eight elements from i on, with states in 32 bits; element by element where there are fewer.
-template <typename P, typename G, bool kMaster>
+template <bool kChance, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, float>& p, int i, bool stochastic) {
-    const uint32_t word = stochastic ? octet_word(c.key, p.octet + i / kOctet) : 0;
+                                           const Part<P, G, kMaster, float>& p, int i) {
+    const uint32_t word = kChance ? octet_word(c.key, p.octet + i / kOctet) : 0;
     if (i + kOctet > p.count) {
 #pragma unroll 1
         for (int e = i; e < p.count; ++e) {
             const Element x = element_at(*set, rates, p, e);
             p.m[e] = x.m, p.v[e] = x.v;
             if constexpr (kMaster) p.master[e] = x.theta;
-            store_param(p.param + e, x.theta, element_word(word, e - i), stochastic);
+            store_param<kChance>(p.param + e, x.theta, element_word(word, e - i));
         }
         return;
     }
@@ -280,7 +283,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     store8(p.m + i, m1);
     store8(p.v + i, v1);
     if constexpr (kMaster) store8(p.master + i, t1);
-    if (sizeof(P) == 2 && stochastic) {
+    if constexpr (kChance) {
         uint32_t x[8];
 #pragma unroll
         for (int e = 0; e < kOctet; ++e) x[e] = chance_bits(t1[e], element_word(word, e));
@@ -296,40 +299,74 @@ template <typename P, typename G, bool kMaster>
 struct Raw {
     uint32_t theta[kMaster || sizeof(P) == 4 ? 8 : 4], grad[sizeof(G) == 4 ? 8 : 4], m[2], v[2];
     uint32_t m_scale, v_scale;
-    // From element i on; zeros if there are not eight.
-    __device__ __forceinline__ Raw(const Part<P, G, kMaster, uint8_t>& p, int i) {
+};
+
+// The way of these elements through shared memory.  What a thread has under way in registers (some 40 bytes of an octet) is a
+// third of what it takes to cover the latency of a loaded memory, 2.5 us, so each thread copies its own eight elements of
+// the next pieces into slots of its own: asynchronously, and with nobody to wait for but itself.
+constexpr int kSlots = 4;
+template <typename P, typename G, bool kMaster>
+struct Slots {
+    static constexpr int kTheta = kMaster || sizeof(P) == 4 ? 2 : 1, kGrad = sizeof(G) == 4 ? 2 : 1;  // units of 16 bytes
+    uint4 theta[kSlots][kTheta][kThreads], grad[kSlots][kGrad][kThreads];
+    uint2 m[kSlots][kThreads], v[kSlots][kThreads];
+
+    __device__ static __forceinline__ void copy(uint4* to, const void* from) {
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+    }
+    __device__ static __forceinline__ void copy(uint2* to, const void* from) {
+        asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+    }
+    // Each call is a group, also if there is nothing to copy.
+    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int slot, int i, bool whole) {
+        const int tid = threadIdx.x;
+        if (whole) {
+            const char* at = kMaster ? reinterpret_cast<const char*>(p.master + i) : reinterpret_cast<const char*>(p.param + i);
 #pragma unroll
-        for (uint32_t& x : theta) x = 0;
+            for (int k = 0; k < kTheta; ++k) copy(&theta[slot][k][tid], at + 16 * k);
 #pragma unroll
-        for (uint32_t& x : grad) x = 0;
-        m[0] = m[1] = v[0] = v[1] = m_scale = v_scale = 0;
-        if (i >= 0 && i + kOctet <= p.count) {
-            load8(p.grad + i, grad);
-            if constexpr (kMaster) load8(p.master + i, theta);
-            else load8(p.param + i, theta);
-            load8(p.m + i, m);
-            load8(p.v + i, v);
+            for (int k = 0; k < kGrad; ++k) copy(&grad[slot][k][tid], reinterpret_cast<const char*>(p.grad + i) + 16 * k);
+            copy(&m[slot][tid], p.m + i);
+            copy(&v[slot][tid], p.v + i);
         }
-        if (i >= 0 && i < p.count) m_scale = p.m_scale[i / QN_ADAM_BLOCK], v_scale = p.v_scale[i / QN_ADAM_BLOCK];
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    // All groups but the last kSlots - 2 have arrived.
+    __device__ static __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
+    __device__ __forceinline__ void take(int slot, Raw<P, G, kMaster>& raw) const {
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kTheta; ++k) {
+            const uint4 x = theta[slot][k][tid];
+            raw.theta[4 * k] = x.x, raw.theta[4 * k + 1] = x.y, raw.theta[4 * k + 2] = x.z, raw.theta[4 * k + 3] = x.w;
+        }
+#pragma unroll
+        for (int k = 0; k < kGrad; ++k) {
+            const uint4 x = grad[slot][k][tid];
+            raw.grad[4 * k] = x.x, raw.grad[4 * k + 1] = x.y, raw.grad[4 * k + 2] = x.z, raw.grad[4 * k + 3] = x.w;
+        }
+        const uint2 a = m[slot][tid], b = v[slot][tid];
+        raw.m[0] = a.x, raw.m[1] = a.y, raw.v[0] = b.x, raw.v[1] = b.y;
     }
 };
 
-// For eight elements that are out of the ordinary, or fewer, from memory again: the largest finite magnitudes of m' and r'; and the step.
+// For eight elements that are out of the ordinary, or fewer, from memory again: the bits of the largest finite m' and the exponent field
+// of the largest finite r'; and the step.
 template <typename P, typename G, bool kMaster>
-__device__ __noinline__ float2 largest_of_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
+__device__ __noinline__ uint2 largest_of_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
                                               uint32_t v_scale) {
-    float2 top = {0.0f, 0.0f};
+    uint2 top = {0, 0};
 #pragma unroll 1
     for (int e = i; e < min(i + kOctet, p.count); ++e) {
         const Element x = element_at(*set, rates, p, e, m_scale, v_scale);
-        top.x = fmaxf(top.x, __uint_as_float(finite_bits(x.m)));
-        top.y = fmaxf(top.y, __uint_as_float(finite_bits(x.root)));
+        top.x = max(top.x, finite_bits(x.m));
+        top.y = max(top.y, finite_bits(x.root) >> 23);
     }
     return top;
 }
-template <typename P, typename G, bool kMaster>
+template <bool kChance, typename P, typename G, bool kMaster>
 __device__ __noinline__ void step_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
-                                      uint32_t v_scale, uint32_t ms, uint32_t vs, bool stochastic) {
+                                      uint32_t v_scale, uint32_t ms, uint32_t vs) {
     const uint32_t word = octet_word(set->c.key, p.octet + i / kOctet);
 #pragma unroll 1
     for (int e = i; e < min(i + kOctet, p.count); ++e) {
@@ -338,45 +375,46 @@ __device__ __noinline__ void step_any(const Setting* set, const Rates rates, con
         p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), w));
         p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), w));
         if constexpr (kMaster) p.master[e] = x.theta;
-        store_param(p.param + e, x.theta, w, stochastic);
+        store_param<kChance>(p.param + e, x.theta, w);
     }
 }
 
-// Eight elements from i on, or what there is of them; all threads of a warp, four of which have a block.
-template <typename P, typename G, bool kMaster>
+// Eight elements from i on (unless kWhole: or what there is of them); all threads of a warp, four of which have a block.
+template <bool kChance, bool kWhole, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, uint8_t>& p, int i, bool stochastic, const Raw<P, G, kMaster>& raw) {
-    constexpr bool kChance = sizeof(P) == 2 && !kMaster;  // theta may be rounded by chance
+                                           const Part<P, G, kMaster, uint8_t>& p, int i, const Raw<P, G, kMaster>& raw) {
     f32x2 m[4], r[4], g[4];
     float top_m, top_v;
     m_values(raw.m, raw.m_scale, m);
     root_values(raw.v, raw.v_scale, r);
 #pragma unroll
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
-    bool odd = !moments(h, c, m, r, g, top_m, top_v);
-    float top_r = __fsqrt_rn(top_v);  // the root of the largest is the largest root
+    bool odd = !moments(h, c, m, r, g, top_m, top_v) || (!kWhole && i + kOctet > p.count);
+    uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
     if (odd) {
-        const float2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
-        top_m = top.x, top_r = top.y;
+        const uint2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
+        most_m = top.x, field_r = top.y;
     }
 #pragma unroll
     for (int o = 1; o < 4; o *= 2) {
-        top_m = fmaxf(top_m, __shfl_xor_sync(0xffffffffu, top_m, o));
-        top_r = fmaxf(top_r, __shfl_xor_sync(0xffffffffu, top_r, o));
+        most_m = max(most_m, __shfl_xor_sync(0xffffffffu, most_m, o));
+        field_r = max(field_r, __shfl_xor_sync(0xffffffffu, field_r, o));
     }
-    const uint32_t most_m = __float_as_uint(top_m), most_r = __float_as_uint(top_r);
-    if (i < p.count && (i / kOctet) % 4 == 0) {  // all four have read the old ones
-        p.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(scale_of(most_m));
-        p.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(scale_of(most_r));
+    // another one's element may be too large for this one's way
+    odd = odd || most_m > __float_as_uint(kHigh) || field_r > (__float_as_uint(kHigh) >> 23);
+    const uint32_t ms = scale_of(most_m), vs = scale_of(field_r << 23);
+    if ((kWhole || i < p.count) && (i / kOctet) % 4 == 0) {  // all four have read the old ones
+        p.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(ms);
+        p.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(vs);
     }
-    const f32x2 ups_m = both(up_m(most_m)), ups_r = both(-up_root(most_r));
+    const f32x2 ups_m = both(up_m(most_m >> 23)), ups_r = both(-up_root(field_r));
     const uint32_t word = octet_word(c.key, p.octet + i / kOctet), octets[2] = {word, word};
     uint32_t a[8], b[8], x[8];
     f32x2 not_finite = 0;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const uint32_t places[2] = {2 * q * kGolden, (2 * q + 1) * kGolden};
-        const Coded<kChance> two(h, c, rates, two_of(raw.theta, q), m[q], r[q], ups_m, ups_r, octets, places, stochastic);
+        const Coded<kChance> two(h, c, rates, two_of(raw.theta, q), m[q], r[q], ups_m, ups_r, octets, places);
         if (kChance) not_finite = fma2(two.theta2, 0, not_finite);  // 0, or NaN
 #pragma unroll
         for (int k = 0; k < 2; ++k) a[2 * q + k] = two.m[k], b[2 * q + k] = two.r[k], x[2 * q + k] = two.theta[k];
@@ -386,10 +424,10 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
         unpack2(not_finite, n0, n1);
         odd = odd || n0 + n1 != 0.0f;
     }
-    if (odd) return step_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale, scale_of(most_m), scale_of(most_r), stochastic);
+    if (odd) return step_any<kChance, P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale, ms, vs);
     *reinterpret_cast<uint2*>(p.m + i) = make_uint2(upper_bytes(a[0], a[1], a[2], a[3]), upper_bytes(a[4], a[5], a[6], a[7]));
     *reinterpret_cast<uint2*>(p.v + i) = make_uint2(upper_bytes(b[0], b[1], b[2], b[3]), upper_bytes(b[4], b[5], b[6], b[7]));
-    if (kChance && stochastic) {
+    if constexpr (kChance) {
         *reinterpret_cast<uint4*>(p.param + i) = make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
                                                             __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
     } else {
@@ -404,11 +442,11 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
 // ---- other tensors -----------------------------------------------------------------------------------------------------------
 
 // 256 elements of a warp, from i on: element i + 32 j + lane is lane's j-th.  States in 32 bits.
-template <typename P, typename G, bool kMaster>
+template <bool kChance, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, float>& p, int i, bool stochastic) {
+                                           const Part<P, G, kMaster, float>& p, int i) {
     const int lane = threadIdx.x & 31;
-    const uint32_t octet = stochastic ? octet_word(c.key, p.octet + i / kOctet + lane) : 0;  // of the warp's lane-th eight
+    const uint32_t octet = kChance ? octet_word(c.key, p.octet + i / kOctet + lane) : 0;  // of the warp's lane-th eight
     float t[8], m[8], v[8], g[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -426,18 +464,18 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = i + 32 * j + lane;
-        const uint32_t word = stochastic ? element_word(__shfl_sync(0xffffffffu, octet, 4 * j + lane / 8), lane % 8) : 0;
+        const uint32_t word = kChance ? element_word(__shfl_sync(0xffffffffu, octet, 4 * j + lane / 8), lane % 8) : 0;
         if (e >= p.count) continue;
         p.m[e] = m[j], p.v[e] = v[j];
         if constexpr (kMaster) p.master[e] = t[j];
-        store_param(p.param + e, t[j], word, stochastic);
+        store_param<kChance>(p.param + e, t[j], word);
     }
     (void)set;
 }
 
 // The same for elements that are out of the ordinary, or fewer than 256, with states in 8 bits: a block at a time.
-template <typename P, typename G, bool kMaster>
-__device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, bool stochastic) {
+template <bool kChance, typename P, typename G, bool kMaster>
+__device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i) {
     const int lane = threadIdx.x & 31;
 #pragma unroll 1
     for (int base = i; base < min(i + 256, p.count); base += 32) {
@@ -451,18 +489,17 @@ __device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rate
             p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), word));
             p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), word));
             if constexpr (kMaster) p.master[e] = x.theta;
-            store_param(p.param + e, x.theta, word, stochastic);
+            store_param<kChance>(p.param + e, x.theta, word);
         }
         if (lane == 0) p.m_scale[block] = static_cast<uint8_t>(ms), p.v_scale[block] = static_cast<uint8_t>(vs);
     }
 }
 
-template <typename P, typename G, bool kMaster>
+template <bool kChance, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, uint8_t>& p, int i, bool stochastic) {
-    constexpr bool kChance = sizeof(P) == 2 && !kMaster;
+                                           const Part<P, G, kMaster, uint8_t>& p, int i) {
     if (i >= p.count) return;
-    if (i + 256 > p.count) return step_lanes_any<P, G, kMaster>(set, rates, p, i, stochastic);
+    if (i + 256 > p.count) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, i);
     const int lane = threadIdx.x & 31, at = i + lane, block = i / QN_ADAM_BLOCK;
     f32x2 m[4], r[4], g[4];
     float t[8];
@@ -477,7 +514,7 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
     }
     float top_m, top_v;
     const bool odd = !moments(h, c, m, r, g, top_m, top_v);
-    if (__any_sync(0xffffffffu, odd)) return step_lanes_any<P, G, kMaster>(set, rates, p, i, stochastic);
+    if (__any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, i);
     const uint32_t octet = octet_word(c.key, p.octet + i / kOctet + lane);  // of the warp's lane-th eight
     const uint32_t place = (lane % 8) * kGolden, places[2] = {place, place};
 #pragma unroll
@@ -492,8 +529,8 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
             most_r[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(r1[k]) & 0x7fffffffu);
             octets[k] = __shfl_sync(0xffffffffu, octet, 4 * (2 * q + k) + lane / 8);
         }
-        const Coded<kChance> two(h, c, rates, pack2(t[2 * q], t[2 * q + 1]), m[q], r[q], pack2(up_m(most_m[0]), up_m(most_m[1])),
-                                 pack2(-up_root(most_r[0]), -up_root(most_r[1])), octets, places, stochastic);
+        const Coded<kChance> two(h, c, rates, pack2(t[2 * q], t[2 * q + 1]), m[q], r[q], pack2(up_m(most_m[0] >> 23), up_m(most_m[1] >> 23)),
+                                 pack2(-up_root(most_r[0] >> 23), -up_root(most_r[1] >> 23)), octets, places);
         unpack2(two.theta2, t1[0], t1[1]);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -501,11 +538,11 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
             p.m[e] = static_cast<uint8_t>(two.m[k] >> 24);
             p.v[e] = static_cast<uint8_t>(two.r[k] >> 24);
             if constexpr (kMaster) p.master[e] = t1[k];
-            if (kChance && stochastic) {
+            if constexpr (kChance) {
                 const uint32_t x = t1[k] == t1[k] ? two.theta[k] : 0x7fff0000u;
                 p.param[e] = P(__ushort_as_bfloat16(static_cast<unsigned short>(x >> 16)));
             } else {
-                store_param(p.param + e, t1[k], 0, false);
+                store_param<false>(p.param + e, t1[k], 0);
             }
             if (lane == 0) {
                 p.m_scale[block + 2 * q + k] = static_cast<uint8_t>(scale_of(most_m[k]));
@@ -531,9 +568,10 @@ __device__ __forceinline__ void count_step(int64_t* step, unsigned* ticket) {
 
 constexpr int64_t kMostPieces = 1 << 19;  // of a run: its elements are counted in 32 bits
 
-template <typename P, typename G, bool kMaster, typename S>
-__global__ void __launch_bounds__(kThreads) adam_step_kernel(const Tensors all, const Hyper h, int64_t* step, const float* lr,
+template <typename P, typename G, bool kMaster, typename S, bool kChance>
+__global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors all, const Hyper h, int64_t* step, const float* lr,
                                                              const double* sumsq, unsigned* ticket) {
+    extern __shared__ __align__(16) unsigned char shared[];
     __shared__ Setting set;
     __shared__ int found;
     const Share share(all.pieces);
@@ -542,7 +580,6 @@ __global__ void __launch_bounds__(kThreads) adam_step_kernel(const Tensors all, 
     __syncthreads();
     const Common c = set.c;
     if (c.skip) return;
-    const bool stochastic = h.stochastic && !kMaster && sizeof(P) == 2;
     int tensor = found;
 #pragma unroll 1
     for (int64_t piece = share.hi; piece > share.lo;) {
@@ -557,29 +594,50 @@ __global__ void __launch_bounds__(kThreads) adam_step_kernel(const Tensors all, 
         const int last = static_cast<int>(to - from - 1) * kPiece;
         if (!p.whole_vectors()) {
 #pragma unroll 1
-            for (int base = last; base >= 0; base -= kPiece) step_lanes(&set, h, c, rates, p, base + static_cast<int>(threadIdx.x / 32) * 256, stochastic);
+            for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + static_cast<int>(threadIdx.x / 32) * 256);
         } else if constexpr (sizeof(S) == 1) {
-            int i = last + threadIdx.x * kOctet;
-            Raw<P, G, kMaster> now(p, i);
+            Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
+            int i = last + threadIdx.x * kOctet, slot = 0;
+            // scales are bytes at any address, and come through registers
+            uint32_t m_scale[kSlots], v_scale[kSlots];
+            const auto fetch = [&](int k, int ahead) {
+                const int at = i - k * kPiece;
+                slots.fetch(p, ahead, at, at >= 0 && at + kOctet <= p.count);
+                const int block = at >= 0 && at < p.count ? at / QN_ADAM_BLOCK : 0;
+                m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
+            };
+#pragma unroll
+            for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
+            bool first_one = true;
 #pragma unroll 1
             for (int base = last; base >= 0; base -= kPiece, i -= kPiece) {
-                const Raw<P, G, kMaster> next(p, i - kPiece);  // on its way meanwhile
-                step_octet(&set, h, c, rates, p, i, stochastic, now);
-                now = next;
+                Raw<P, G, kMaster> raw;
+                slots.wait();
+                slots.take(slot, raw);
+                raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
+#pragma unroll
+                for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
+                fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
+                m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
+                slot = slot == kSlots - 1 ? 0 : slot + 1;
+                if (first_one) step_octet<kChance, false>(&set, h, c, rates, p, i, raw);  // the piece at the run's end may not be whole
+                else step_octet<kChance, true>(&set, h, c, rates, p, i, raw);
+                first_one = false;
             }
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
         } else {
 #pragma unroll 1
-            for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet(&set, h, c, rates, p, i, stochastic);
+            for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(&set, h, c, rates, p, i);
         }
     }
     count_step(step, ticket);
 }
 
-template <typename P, typename G, bool kMaster>
+template <typename P, typename G, bool kMaster, bool kChance>
 cudaError_t launch_step(const qn_adam_plan& h, const Hyper& hyper, int64_t* step, const float* lr, const double* sumsq, cudaStream_t st) {
-    static int resident[2];
-    return h.eight ? launch_over(adam_step_kernel<P, G, kMaster, uint8_t>, resident[1], h, st, hyper, step, lr, sumsq, h.tickets)
-                   : launch_over(adam_step_kernel<P, G, kMaster, float>, resident[0], h, st, hyper, step, lr, sumsq, h.tickets);
+    static Resident resident[2];
+    return h.eight ? launch_over(adam_step_kernel<P, G, kMaster, uint8_t, kChance>, resident[1], sizeof(Slots<P, G, kMaster>), h, st, hyper, step, lr, sumsq, h.tickets)
+                   : launch_over(adam_step_kernel<P, G, kMaster, float, kChance>, resident[0], 0, h, st, hyper, step, lr, sumsq, h.tickets);
 }
 
 }  // namespace
@@ -598,14 +656,15 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     if (!guard.ok) return QN_ERR_CUDA;
     const Hyper hyper{lr, log(beta1), log(beta2), max_norm, grad_scale,
                       static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32), rounding == QN_ROUND_STOCHASTIC};
+                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:adam_step");
     const auto by_grad = [&](auto grad) {
         using G = decltype(grad);
-        if (h->param == QN_F32) return launch_step<float, G, false>(*h, hyper, step, lr_device, sumsq, st);
-        if (h->master) return launch_step<__nv_bfloat16, G, true>(*h, hyper, step, lr_device, sumsq, st);
-        return launch_step<__nv_bfloat16, G, false>(*h, hyper, step, lr_device, sumsq, st);
+        if (h->param == QN_F32) return launch_step<float, G, false, false>(*h, hyper, step, lr_device, sumsq, st);
+        if (h->master) return launch_step<__nv_bfloat16, G, true, false>(*h, hyper, step, lr_device, sumsq, st);
+        if (rounding == QN_ROUND_NEAREST) return launch_step<__nv_bfloat16, G, false, false>(*h, hyper, step, lr_device, sumsq, st);
+        return launch_step<__nv_bfloat16, G, false, true>(*h, hyper, step, lr_device, sumsq, st);
     };
     const cudaError_t e = h->grad == QN_F32 ? by_grad(float()) : by_grad(__nv_bfloat16());
     nvtxRangePop();
