@@ -12,8 +12,9 @@
 
 namespace {
 
-constexpr int kMaxCluster = 8;
-constexpr int kKept = 8;  // tokens whose weights a thread keeps; it reads those of longer pairs again (from L2, mostly)
+constexpr int kMaxCluster = 16;
+constexpr int kEach = 8;  // tokens of a tile a thread
+constexpr int kKept = 2;  // tiles whose weights a thread keeps; it reads those of longer pairs again (from L2, mostly)
 
 struct PreferenceParams {
     int64_t pairs, tokens;
@@ -27,41 +28,82 @@ struct PreferenceParams {
     float *loss, *reward, *d_logprob;
 };
 
-// What counts of a token: its weight, and its weighted log ratio.  A token of weight 0 counts for nothing whatever it
-// holds; nor does one that both sides mask.
-struct Token {
-    float weight;
-    double ratio;
+// A tile of a sequence: NT * kEach tokens from l, ref and weight on (`count` of them there), NT apart for a thread.  Its weights, and
+// what it adds to the sums.  A token of weight 0 counts for nothing whatever it holds; nor does one that both sides mask.
+template <typename R>
+struct Sequence {
+    const float *l, *weight;
+    const R* ref;
+    float* d;
+    int64_t length;
 };
-template <typename R, bool kRef>
-__device__ __forceinline__ Token token_at(const PreferenceParams& p, int64_t i) {
-    Token t;
-    t.weight = p.weight ? __ldg(p.weight + i) : 1.0f;
-    const float l = __ldg(p.logprob + i), ref = kRef ? Storage<R>::load1(static_cast<const R*>(p.ref) + i) : 0.0f;
-    if (kRef && l == -INFINITY && ref == -INFINITY) t.weight = 0.0f;
-    t.ratio = t.weight == 0.0f ? 0.0 : t.weight * (static_cast<double>(l) - static_cast<double>(ref));
-    return t;
-}
-
-__device__ __noinline__ double softplus(double x) { return log1p(exp(-fabs(x))) + fmax(x, 0.0); }
-__device__ __noinline__ double sigmoid(double x) { return 1.0 / (1.0 + exp(-x)); }
-
-// Loss and slope at h.
-__device__ __forceinline__ double2 preference(const PreferenceParams& p, double h) {
-    if (h != h) return make_double2(h, h);
-    if (p.kind == QN_PREFERENCE_HINGE) return make_double2(fmax(0.0, 1.0 - h), h < 1.0 ? -1.0 : 0.0);
-    if (p.kind == QN_PREFERENCE_SQUARED) {
-        const double x = (h - 0.5) / p.beta;
-        return make_double2(x * x, 2.0 * x / p.beta);
+template <int NT, typename R, bool kRef>
+struct Tile {
+    float l[kEach], ref[kEach], weight[kEach];
+    // Loads without conditions, so that all are under way together: in a part of a tile, of its last token for those that are not there.
+    template <bool kWhole>
+    __device__ __forceinline__ void load(const Sequence<R>& s, int64_t at, int count) {
+        const float *l_at = s.l + at, *weight_at = s.weight + at;
+        const R* ref_at = s.ref + at;
+        const int tid = threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const int i = kWhole ? k * NT + tid : min(k * NT + tid, count - 1);
+            l[k] = __ldg(l_at + i);
+            ref[k] = kRef ? Storage<R>::load1(ref_at + i) : 0.0f;
+            weight[k] = s.weight ? __ldg(weight_at + i) : 1.0f;
+        }
+        if (!kWhole)
+#pragma unroll
+            for (int k = 0; k < kEach; ++k)
+                if (k * NT + tid >= count) weight[k] = 0.0f;
     }
-    const double keep = 1.0 - p.smoothing;
-    double2 r = make_double2(keep * softplus(-h), -keep * sigmoid(-h));
-    if (p.smoothing != 0.0) r.x += p.smoothing * softplus(h), r.y += p.smoothing * sigmoid(h);
-    return r;
+    __device__ __forceinline__ Tile(const Sequence<R>& s, int64_t at, int count) {
+        if (count == NT * kEach) load<true>(s, at, count);
+        else load<false>(s, at, count);
+    }
+    __device__ __forceinline__ void add(double& ratios, double& weights) {
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            if (kRef && l[k] == -INFINITY && ref[k] == -INFINITY) weight[k] = 0.0f;
+            // products of numbers in 32 bits are exact in 64
+            const double w = weight[k];
+            ratios += w * static_cast<double>(weight[k] == 0.0f ? 0.0f : l[k]);
+            if (kRef) ratios -= w * static_cast<double>(weight[k] == 0.0f ? 0.0f : ref[k]);
+            weights += w;
+        }
+    }
+    __device__ static __forceinline__ void write(const Sequence<R>& s, int64_t at, int count, const float (&w)[kEach], float coefficient) {
+        float* d = s.d + at + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k)
+            if (k * NT + static_cast<int>(threadIdx.x) < count) d[k * NT] = w[k] == 0.0f ? 0.0f : w[k] * coefficient;
+    }
+};
+
+// Loss and slope at h; the slope is needed first (the gradients wait for it), so that the two come apart.  e = exp(-|h|).
+__device__ __forceinline__ double slope_at(const PreferenceParams& p, double h, double& e) {
+    e = 0.0;
+    if (h != h) return h;
+    if (p.kind == QN_PREFERENCE_HINGE) return h < 1.0 ? -1.0 : 0.0;
+    if (p.kind == QN_PREFERENCE_SQUARED) return 2.0 * ((h - 0.5) / p.beta) / p.beta;
+    e = exp(-fabs(h));
+    const double large = 1.0 / (1.0 + e), small = e * large;  // sigmoid(|h|), sigmoid(-|h|)
+    const double up = h > 0.0 ? large : small, down = h > 0.0 ? small : large;
+    return p.smoothing * up - (1.0 - p.smoothing) * down;
+}
+__device__ __forceinline__ double loss_at(const PreferenceParams& p, double h, double e) {
+    if (h != h) return h;
+    if (p.kind == QN_PREFERENCE_HINGE) return fmax(0.0, 1.0 - h);
+    if (p.kind == QN_PREFERENCE_SQUARED) return ((h - 0.5) / p.beta) * ((h - 0.5) / p.beta);
+    const double low = log1p(e), keep = 1.0 - p.smoothing;
+    double loss = keep != 0.0 ? keep * (low + fmax(-h, 0.0)) : 0.0;
+    if (p.smoothing != 0.0) loss += p.smoothing * (low + fmax(h, 0.0));
+    return loss;
 }
 
 template <int NT, typename R, bool kRef>
-__global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams p) {
+__global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const PreferenceParams p) {
     __shared__ double warp_sums[NT / 32][4];
     __shared__ uint64_t inbox[kMaxCluster][4];
     __shared__ float coefficient[2];
@@ -73,21 +115,41 @@ __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams p
     const int64_t pair = blockIdx.x / ctas;
     const int64_t chosen = p.split ? pair : 2 * pair, rejected = p.split ? p.pairs + pair : 2 * pair + 1;
     const float unit = p.pair_weight ? p.pair_weight[pair] : 1.0f;
-    int64_t begin[2], length[2];
+    Sequence<R> sequence[2];
     bool wrong = false;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
         const int64_t a = p.offsets[s ? rejected : chosen], b = p.offsets[(s ? rejected : chosen) + 1];
         const bool good = a >= 0 && a <= b && b <= p.tokens;
-        begin[s] = good ? a : 0;
-        length[s] = good ? b - a : 0;
+        const int64_t begin = good ? a : 0;
+        sequence[s] = Sequence<R>{p.logprob + begin, p.weight ? p.weight + begin : nullptr, kRef ? static_cast<const R*>(p.ref) + begin : nullptr,
+                                  p.d_logprob + (p.d_logprob ? begin : 0), good ? b - a : 0};
         wrong = wrong || !good;
     }
-    const int64_t all = length[0] + length[1], stride = static_cast<int64_t>(ctas) * NT, first = rank * NT + tid;
-    const auto place = [&](int64_t j) { return j < length[0] ? begin[0] + j : begin[1] + (j - length[0]); };
+    // tiles of the chosen sequence, then those of the rejected one, in turn for the CTAs
+    constexpr int kTile = NT * kEach;
+    const int64_t tiles0 = (sequence[0].length + kTile - 1) / kTile, tiles = tiles0 + (sequence[1].length + kTile - 1) / kTile;
+    const auto each_tile = [&](auto&& with, int64_t from) {
+#pragma unroll 1
+        for (int64_t t = from; t < tiles; t += ctas) with(t);
+    };
+    struct Place {
+        int s;
+        int64_t at;
+        int count;
+    };
+    const auto place = [&](int64_t t) {
+        const int s = t >= tiles0;
+        const int64_t at = (s ? t - tiles0 : t) * kTile;
+        return Place{s, at, static_cast<int>(min((s ? sequence[1].length : sequence[0].length) - at, static_cast<int64_t>(kTile)))};
+    };
     if (unit == 0.0f) {  // padding
         if (p.d_logprob)
-            for (int64_t j = first; j < all; j += stride) p.d_logprob[place(j)] = 0.0f;
+            each_tile([&](int64_t t) {
+                const Place x = place(t);
+                const float none[kEach] = {};
+                Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, none, 0.0f);
+            }, rank);
         if (rank == 0 && tid == 0) {
             p.loss[pair] = 0.0f;
             if (p.reward) p.reward[chosen] = p.reward[rejected] = 0.0f;
@@ -97,46 +159,51 @@ __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams p
         return;
     }
     double sums[4] = {0.0, 0.0, 0.0, 0.0};  // weighted ratios of the chosen and of the rejected, weights of both
-    float kept[kKept];
-    const auto add = [&](int64_t j, const Token& t) {
-        const bool second = j >= length[0];
-        sums[0] += second ? 0.0 : t.ratio, sums[1] += second ? t.ratio : 0.0;
-        if (p.normalise) sums[2] += second ? 0.0 : t.weight, sums[3] += second ? t.weight : 0.0;
+    float kept[kKept][kEach];
+    const auto add = [&](const Place& x, Tile<NT, R, kRef>& tile) {
+        double ratios = 0.0, weights = 0.0;
+        tile.add(ratios, weights);
+        if (x.s) sums[1] += ratios, sums[3] += weights;
+        else sums[0] += ratios, sums[2] += weights;
     };
-    {
-        Token t[kKept];
 #pragma unroll
-        for (int k = 0; k < kKept; ++k) {
-            const int64_t j = first + k * stride;
-            t[k] = Token{0.0f, 0.0};
-            if (j < all) t[k] = token_at<R, kRef>(p, place(j));
-        }
+    for (int k = 0; k < kKept; ++k) {
+        const int64_t t = rank + k * ctas;
+        if (t >= tiles) break;
+        const Place x = place(t);
+        Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
+        add(x, tile);
 #pragma unroll
-        for (int k = 0; k < kKept; ++k) {
-            add(first + k * stride, t[k]);
-            kept[k] = t[k].weight;
-        }
+        for (int e = 0; e < kEach; ++e) kept[k][e] = tile.weight[e];
     }
-#pragma unroll 4
-    for (int64_t j = first + kKept * stride; j < all; j += stride) add(j, token_at<R, kRef>(p, place(j)));
+    each_tile([&](int64_t t) {
+        const Place x = place(t);
+        Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
+        add(x, tile);
+    }, rank + kKept * ctas);
+    const int count = p.normalise ? 4 : 2;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
+        if (q >= count) break;
         const double x = warp_reduce<double, add_op>(sums[q]);
         if (lane == 0) warp_sums[warp][q] = x;
     }
     __syncthreads();
     if (warp == 0) {
-        double x = 0.0;
-        if (lane < 4)
-#pragma unroll 1
-            for (int w = 0; w < NT / 32; ++w) x += warp_sums[w][lane];
+        double mine = 0.0;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (q >= count) break;
+            const double x = warp_reduce<double, add_op>(lane < NT / 32 ? warp_sums[lane][q] : 0.0);
+            if (lane == q) mine = x;
+        }
         __syncwarp();
         if (ctas == 1) {
-            if (lane < 4) inbox[0][lane] = __double_as_longlong(x);
+            if (lane < 4) inbox[0][lane] = __double_as_longlong(mine);
         } else {
             cluster_wait();
             if (lane < 4)
-                for (uint32_t c = 0; c < ctas; ++c) store_remote(&inbox[rank][lane], c, __double_as_longlong(x));
+                for (uint32_t c = 0; c < ctas; ++c) store_remote(&inbox[rank][lane], c, __double_as_longlong(mine));
         }
         __syncwarp();
     }
@@ -145,6 +212,7 @@ __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams p
         cluster_arrive();
         cluster_wait();
     }
+    double h = 0.0, e = 0.0;
     if (tid == 0) {
         double total[4] = {0.0, 0.0, 0.0, 0.0};
         for (uint32_t c = 0; c < ctas; ++c)
@@ -154,26 +222,52 @@ __global__ void __launch_bounds__(NT) preference_kernel(const PreferenceParams p
             each[s] = !p.normalise ? p.beta : total[2 + s] != 0.0 ? p.beta / total[2 + s] : 0.0;
             reward[s] = each[s] == 0.0 ? 0.0 : each[s] * total[s];
         }
-        const double2 l = preference(p, wrong ? NAN : reward[0] - reward[1] - p.margin);
-        coefficient[0] = static_cast<float>(unit * l.y * each[0]);
-        coefficient[1] = static_cast<float>(-unit * l.y * each[1]);
-        if (rank == 0) {
-            p.loss[pair] = static_cast<float>(l.x);
-            if (p.reward) {
-                p.reward[chosen] = wrong ? NAN : static_cast<float>(reward[0]);
-                p.reward[rejected] = wrong ? NAN : static_cast<float>(reward[1]);
-            }
+        h = wrong ? NAN : reward[0] - reward[1] - p.margin;
+        const double slope = unit * slope_at(p, h, e);
+        coefficient[0] = static_cast<float>(slope * each[0]);
+        coefficient[1] = static_cast<float>(-slope * each[1]);
+        if (rank == 0 && p.reward) {
+            p.reward[chosen] = wrong ? NAN : static_cast<float>(reward[0]);
+            p.reward[rejected] = wrong ? NAN : static_cast<float>(reward[1]);
         }
     }
     __syncthreads();
-    if (!p.d_logprob) return;
-    const float c0 = coefficient[0], c1 = coefficient[1];
-    const auto write = [&](int64_t j, float weight) { p.d_logprob[place(j)] = weight == 0.0f ? 0.0f : weight * (j < length[0] ? c0 : c1); };
+    if (p.d_logprob) {
+        const float c0 = coefficient[0], c1 = coefficient[1];
 #pragma unroll
-    for (int k = 0; k < kKept; ++k)
-        if (first + k * stride < all) write(first + k * stride, kept[k]);
-#pragma unroll 4
-    for (int64_t j = first + kKept * stride; j < all; j += stride) write(j, token_at<R, kRef>(p, place(j)).weight);
+        for (int k = 0; k < kKept; ++k) {
+            const int64_t t = rank + k * ctas;
+            if (t >= tiles) break;
+            const Place x = place(t);
+            Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, kept[k], x.s ? c1 : c0);
+        }
+        each_tile([&](int64_t t) {
+            const Place x = place(t);
+            Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
+            double unused[2] = {0.0, 0.0};
+            tile.add(unused[0], unused[1]);
+            Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, tile.weight, x.s ? c1 : c0);
+        }, rank + kKept * ctas);
+    }
+    if (rank == 0 && tid == 0) p.loss[pair] = static_cast<float>(loss_at(p, h, e));
+}
+
+// How many clusters of 16 fit on the device at once (asked for once on each); such clusters need a permission.
+template <int NT, typename R, bool kRef>
+cudaError_t large_clusters(int* fit) {
+    static int known[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    if (known[dev] == 0) {
+        int found = 0;
+        const EarlyLaunch launch(kMaxCluster, NT, 0, kMaxCluster, nullptr);
+        cudaError_t e = cudaFuncSetAttribute(preference_kernel<NT, R, kRef>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&found, preference_kernel<NT, R, kRef>, &launch.cfg);
+        if (e != cudaSuccess) return e;
+        known[dev] = found < 1 ? -1 : found;
+    }
+    *fit = known[dev];
+    return cudaSuccess;
 }
 
 template <int NT, typename R, bool kRef>
@@ -184,15 +278,23 @@ cudaError_t launch_preference(const PreferenceParams& p, int ctas, cudaStream_t 
 
 template <typename R, bool kRef>
 cudaError_t launch_preference(const PreferenceParams& p, cudaStream_t st) {
-    // By the mean length of a pair (the lengths themselves are on the device): CTAs until the device is full or each has 512
-    // tokens, and threads for eight tokens each.
-    const int64_t mean = p.tokens / p.pairs;
+    // Threads for a pair, by its mean length (the lengths themselves are on the device): one for each eight tokens, as long as half of
+    // the threads that the device has (more do not fit beside their registers) are enough for all pairs.
+    const int64_t mean = p.tokens / p.pairs, room = 1024 * static_cast<int64_t>(qn_sm_count()) / p.pairs;
+    const int64_t threads = mean / kEach < room ? mean / kEach : room;
+    if (threads >= 128 * kMaxCluster) {
+        int fit = 0;
+        const cudaError_t e = large_clusters<512, R, kRef>(&fit);
+        if (e != cudaSuccess) return e;
+        if (p.pairs <= fit) return launch_preference<512, R, kRef>(p, kMaxCluster, st);
+    }
     int ctas = 1;
-    while (2 * ctas <= kMaxCluster && p.pairs * 2 * ctas <= 2 * qn_sm_count() && mean > 512 * ctas) ctas *= 2;
-    const int64_t per_cta = mean / ctas;
-    if (per_cta <= 512) return launch_preference<64, R, kRef>(p, ctas, st);
-    if (per_cta <= 2048) return launch_preference<256, R, kRef>(p, ctas, st);
-    return launch_preference<1024, R, kRef>(p, ctas, st);
+    while (ctas < 8 && p.pairs * ctas < qn_sm_count() && threads >= 128 * ctas) ctas *= 2;
+    const int64_t each = threads / ctas;
+    if (each < 96) return launch_preference<64, R, kRef>(p, ctas, st);
+    if (each < 192) return launch_preference<128, R, kRef>(p, ctas, st);
+    if (each < 384) return launch_preference<256, R, kRef>(p, ctas, st);
+    return launch_preference<512, R, kRef>(p, ctas, st);
 }
 
 }  // namespace
@@ -202,7 +304,7 @@ extern "C" qn_status qn_preference(int64_t pairs, int64_t tokens, const float* l
                                    const float* pair_weight, int32_t kind, double beta, double margin, double smoothing,
                                    int32_t normalise, float* loss, float* reward, float* d_logprob, void* cuda_stream) {
     if (pairs == 0) return QN_OK;
-    if (pairs < 0 || pairs > INT32_MAX / kMaxCluster || tokens < 0 || tokens > (int64_t(1) << 56)) return QN_ERR_INVALID;
+    if (pairs < 0 || pairs > INT32_MAX / 8 || tokens < 0 || tokens > (int64_t(1) << 56)) return QN_ERR_INVALID;
     if (!offsets || !loss || (tokens && !logprob)) return QN_ERR_INVALID;
     if (ref_dtype != QN_F32 && ref_dtype != QN_BF16) return QN_ERR_INVALID;
     if (kind != QN_PREFERENCE_LOGISTIC && kind != QN_PREFERENCE_HINGE && kind != QN_PREFERENCE_SQUARED) return QN_ERR_INVALID;
