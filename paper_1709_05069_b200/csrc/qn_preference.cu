@@ -14,7 +14,7 @@ namespace {
 
 constexpr int kMaxCluster = 16;
 constexpr int kEach = 8;  // tokens of a tile a thread
-constexpr int kKept = 2;  // tiles whose weights a thread keeps; it reads those of longer pairs again (from L2, mostly)
+constexpr int kKept = 4;  // tiles whose weights a thread keeps (in shared memory); it reads those of longer pairs again (from L2, mostly)
 
 struct PreferenceParams {
     int64_t pairs, tokens;
@@ -42,15 +42,15 @@ struct Tile {
     float l[kEach], ref[kEach], weight[kEach];
     // Loads without conditions, so that all are under way together: in a part of a tile, of its last token for those that are not there.
     template <bool kWhole>
-    __device__ __forceinline__ void load(const Sequence<R>& s, int64_t at, int count) {
+    __device__ __forceinline__ void load(const Sequence<R>& s, int64_t at, int count, bool all) {
         const float *l_at = s.l + at, *weight_at = s.weight + at;
         const R* ref_at = s.ref + at;
         const int tid = threadIdx.x;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
             const int i = kWhole ? k * NT + tid : min(k * NT + tid, count - 1);
-            l[k] = __ldg(l_at + i);
-            ref[k] = kRef ? Storage<R>::load1(ref_at + i) : 0.0f;
+            l[k] = all ? __ldg(l_at + i) : 0.0f;
+            ref[k] = kRef && all ? Storage<R>::load1(ref_at + i) : 0.0f;
             weight[k] = s.weight ? __ldg(weight_at + i) : 1.0f;
         }
         if (!kWhole)
@@ -58,20 +58,38 @@ struct Tile {
             for (int k = 0; k < kEach; ++k)
                 if (k * NT + tid >= count) weight[k] = 0.0f;
     }
-    __device__ __forceinline__ Tile(const Sequence<R>& s, int64_t at, int count) {
-        if (count == NT * kEach) load<true>(s, at, count);
-        else load<false>(s, at, count);
+    // all: not the weights alone
+    __device__ __forceinline__ Tile(const Sequence<R>& s, int64_t at, int count, bool all = true) {
+        if (count == NT * kEach) load<true>(s, at, count, all);
+        else load<false>(s, at, count, all);
     }
-    __device__ __forceinline__ void add(double& ratios, double& weights) {
+    // True if a token counts for nothing although its weight is not 0.
+    __device__ __forceinline__ bool add(double& ratios, double& weights, bool normalise) {
+        float most = 0.0f;  // of the magnitudes; NaN if there is one
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(l[k]), "f"(ref[k]));
+        bool dead = false;
+        if (!(most < INFINITY)) dead = clean();
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
-            if (kRef && l[k] == -INFINITY && ref[k] == -INFINITY) weight[k] = 0.0f;
-            // products of numbers in 32 bits are exact in 64
-            const double w = weight[k];
-            ratios += w * static_cast<double>(weight[k] == 0.0f ? 0.0f : l[k]);
-            if (kRef) ratios -= w * static_cast<double>(weight[k] == 0.0f ? 0.0f : ref[k]);
-            weights += w;
+            const double w = weight[k];  // products of numbers in 32 bits are exact in 64
+            ratios += w * static_cast<double>(l[k]);
+            if (kRef) ratios -= w * static_cast<double>(ref[k]);
+            if (normalise) weights += w;
         }
+        return dead;
+    }
+    // What does not count becomes 0.
+    __device__ __forceinline__ bool clean() {
+        bool dead = false;
+#pragma unroll
+        for (int k = 0; k < kEach; ++k) {
+            const bool both = kRef && weight[k] != 0.0f && l[k] == -INFINITY && ref[k] == -INFINITY;
+            dead = dead || both;
+            if (both) weight[k] = 0.0f;
+            if (weight[k] == 0.0f) l[k] = ref[k] = 0.0f;
+        }
+        return dead;
     }
     __device__ static __forceinline__ void write(const Sequence<R>& s, int64_t at, int count, const float (&w)[kEach], float coefficient) {
         float* d = s.d + at + threadIdx.x;
@@ -129,9 +147,10 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
     // tiles of the chosen sequence, then those of the rejected one, in turn for the CTAs
     constexpr int kTile = NT * kEach;
     const int64_t tiles0 = (sequence[0].length + kTile - 1) / kTile, tiles = tiles0 + (sequence[1].length + kTile - 1) / kTile;
-    const auto each_tile = [&](auto&& with, int64_t from) {
+    const auto each_tile = [&](auto&& with) {
+        int turn = 0;
 #pragma unroll 1
-        for (int64_t t = from; t < tiles; t += ctas) with(t);
+        for (int64_t t = rank; t < tiles; t += ctas, turn = turn < kKept ? turn + 1 : turn) with(t, turn);
     };
     struct Place {
         int s;
@@ -145,11 +164,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
     };
     if (unit == 0.0f) {  // padding
         if (p.d_logprob)
-            each_tile([&](int64_t t) {
+            each_tile([&](int64_t t, int) {
                 const Place x = place(t);
                 const float none[kEach] = {};
                 Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, none, 0.0f);
-            }, rank);
+            });
         if (rank == 0 && tid == 0) {
             p.loss[pair] = 0.0f;
             if (p.reward) p.reward[chosen] = p.reward[rejected] = 0.0f;
@@ -159,28 +178,22 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
         return;
     }
     double sums[4] = {0.0, 0.0, 0.0, 0.0};  // weighted ratios of the chosen and of the rejected, weights of both
-    float kept[kKept][kEach];
+    extern __shared__ float kept[];  // [tile][token of a thread][thread]: each thread its own
+    bool dead = false;
     const auto add = [&](const Place& x, Tile<NT, R, kRef>& tile) {
         double ratios = 0.0, weights = 0.0;
-        tile.add(ratios, weights);
+        dead = tile.add(ratios, weights, p.normalise) || dead;
         if (x.s) sums[1] += ratios, sums[3] += weights;
         else sums[0] += ratios, sums[2] += weights;
     };
-#pragma unroll
-    for (int k = 0; k < kKept; ++k) {
-        const int64_t t = rank + k * ctas;
-        if (t >= tiles) break;
+    each_tile([&](int64_t t, int turn) {
         const Place x = place(t);
         Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
         add(x, tile);
+        if (turn < kKept)
 #pragma unroll
-        for (int e = 0; e < kEach; ++e) kept[k][e] = tile.weight[e];
-    }
-    each_tile([&](int64_t t) {
-        const Place x = place(t);
-        Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
-        add(x, tile);
-    }, rank + kKept * ctas);
+            for (int e = 0; e < kEach; ++e) kept[(turn * kEach + e) * NT + tid] = tile.weight[e];
+    });
     const int count = p.normalise ? 4 : 2;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -234,23 +247,25 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
     __syncthreads();
     if (p.d_logprob) {
         const float c0 = coefficient[0], c1 = coefficient[1];
+        each_tile([&](int64_t t, int turn) {
+            const Place x = place(t);
+                if (turn < kKept) {
+                float weight[kEach];
 #pragma unroll
-        for (int k = 0; k < kKept; ++k) {
-            const int64_t t = rank + k * ctas;
-            if (t >= tiles) break;
-            const Place x = place(t);
-            Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, kept[k], x.s ? c1 : c0);
-        }
-        each_tile([&](int64_t t) {
-            const Place x = place(t);
-            Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
-            double unused[2] = {0.0, 0.0};
-            tile.add(unused[0], unused[1]);
-            Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, tile.weight, x.s ? c1 : c0);
-        }, rank + kKept * ctas);
+                for (int e = 0; e < kEach; ++e) weight[e] = kept[(turn * kEach + e) * NT + tid];
+                Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, weight, x.s ? c1 : c0);
+            } else {
+                Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count, dead);
+                if (dead) tile.clean();
+                Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, tile.weight, x.s ? c1 : c0);
+            }
+        });
     }
     if (rank == 0 && tid == 0) p.loss[pair] = static_cast<float>(loss_at(p, h, e));
 }
+
+template <int NT>
+constexpr int kShared = NT * kEach * kKept * 4;
 
 // How many clusters of 16 fit on the device at once (asked for once on each); such clusters need a permission.
 template <int NT, typename R, bool kRef>
@@ -260,8 +275,9 @@ cudaError_t large_clusters(int* fit) {
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (known[dev] == 0) {
         int found = 0;
-        const EarlyLaunch launch(kMaxCluster, NT, 0, kMaxCluster, nullptr);
+        const EarlyLaunch launch(kMaxCluster, NT, kShared<NT>, kMaxCluster, nullptr);
         cudaError_t e = cudaFuncSetAttribute(preference_kernel<NT, R, kRef>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(preference_kernel<NT, R, kRef>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<NT>);
         if (e == cudaSuccess) e = cudaOccupancyMaxActiveClusters(&found, preference_kernel<NT, R, kRef>, &launch.cfg);
         if (e != cudaSuccess) return e;
         known[dev] = found < 1 ? -1 : found;
@@ -272,7 +288,11 @@ cudaError_t large_clusters(int* fit) {
 
 template <int NT, typename R, bool kRef>
 cudaError_t launch_preference(const PreferenceParams& p, int ctas, cudaStream_t st) {
-    const EarlyLaunch launch(p.pairs * ctas, NT, 0, ctas, st);
+    if (kShared<NT> > (48 << 10)) {
+        const cudaError_t e = cudaFuncSetAttribute(preference_kernel<NT, R, kRef>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<NT>);
+        if (e != cudaSuccess) return e;
+    }
+    const EarlyLaunch launch(p.pairs * ctas, NT, kShared<NT>, ctas, st);
     return cudaLaunchKernelEx(&launch.cfg, preference_kernel<NT, R, kRef>, p);
 }
 
