@@ -17,6 +17,8 @@ __global__ void __launch_bounds__(kThreads) adam_norm_kernel(const Tensors all, 
     __shared__ int found;
     __shared__ bool last;
     const Share share(all.pieces);
+    start_after_last();
+    let_next_start();
     if (share.hi > share.lo) find_tensor(all, share.lo, &found);
     __syncthreads();
     double sum = 0.0;
@@ -77,6 +79,8 @@ template <typename T, typename S>
 __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all, T* m_out, T* root_out) {
     __shared__ int found;
     const Share share(all.pieces);
+    start_after_last();
+    let_next_start();
     if (share.hi > share.lo) find_tensor(all, share.lo, &found);
     __syncthreads();
     int tensor = found;

@@ -223,8 +223,8 @@ cudaError_t launch_over(void (*kernel)(P...), Resident& known, size_t shared, co
         resident = found < 1 ? 1 : found > kMostCtas ? kMostCtas : found;
     }
     const int64_t most = static_cast<int64_t>(resident) * qn_sm_count(), ctas = h.pieces < most ? h.pieces : most;
-    kernel<<<static_cast<unsigned>(ctas < 1 ? 1 : ctas), kThreads, shared, st>>>(h.tensors(), args...);
-    return cudaGetLastError();
+    const EarlyLaunch launch(ctas < 1 ? 1 : ctas, kThreads, shared, 1, st);
+    return cudaLaunchKernelEx(&launch.cfg, kernel, h.tensors(), args...);
 }
 
 }  // namespace

@@ -22,6 +22,7 @@ struct Hyper {
 
 // What is the same for all elements of a step.
 struct Common {
+    int64_t t;
     double lr, speed;           // learning rate, and lr / (1 - b1^t)
     float coefficient, spread;  // spread: 1 / sqrt(1 - b2^t)
     uint32_t key;
@@ -32,22 +33,31 @@ struct Setting {
     Common c;
 };
 
-__device__ __forceinline__ Common common_of(const Hyper& h, const int64_t* step, const float* lr, const double* sumsq) {
-    Common c;
-    const int64_t t = *step + 1;
-    c.lr = lr ? static_cast<double>(*lr) : h.lr;
-    c.speed = c.lr / -expm1(static_cast<double>(t) * h.log_beta1);
-    c.spread = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(t) * h.log_beta2)));
-    double coefficient = h.grad_scale;
-    c.skip = false;
-    if (sumsq) {
-        const double norm = sqrt(*sumsq) * fabs(h.grad_scale);
-        c.skip = !isfinite(norm);
-        if (h.max_norm > 0.0 && norm > h.max_norm) coefficient *= h.max_norm / norm;
+// By four threads, since each part is a chain of operations in 64 bits.
+__device__ __forceinline__ void make_common(const Hyper& h, const int64_t* step, const float* lr, const double* sumsq, Common& c) {
+    const int part = threadIdx.x / 32;
+    if (threadIdx.x % 32 != 0 || part > 3) return;
+    if (part == 2) {
+        double coefficient = h.grad_scale;
+        c.skip = false;
+        if (sumsq) {
+            const double norm = sqrt(*sumsq) * fabs(h.grad_scale);
+            c.skip = !isfinite(norm);
+            if (h.max_norm > 0.0 && norm > h.max_norm) coefficient *= h.max_norm / norm;
+        }
+        c.coefficient = static_cast<float>(coefficient);
+        return;
     }
-    c.coefficient = static_cast<float>(coefficient);
-    c.key = step_key(h.seed_low, h.seed_high, t);
-    return c;
+    const int64_t t = *step + 1;
+    if (part == 0) {
+        c.lr = lr ? static_cast<double>(*lr) : h.lr;
+        c.speed = c.lr / -expm1(static_cast<double>(t) * h.log_beta1);
+        c.t = t;
+    } else if (part == 1) {
+        c.spread = static_cast<float>(1.0 / sqrt(-expm1(static_cast<double>(t) * h.log_beta2)));
+    } else {
+        c.key = step_key(h.seed_low, h.seed_high, t);
+    }
 }
 
 // The same for all elements of a tensor.
@@ -481,7 +491,10 @@ __device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rate
     for (int base = i; base < min(i + 256, p.count); base += 32) {
         const int e = base + lane, block = base / QN_ADAM_BLOCK;
         Element x = {0.0f, 0.0f, 0.0f, 0.0f};
-        if (e < p.count) x = element_at(*set, rates, p, e, p.m_scale[block], p.v_scale[block]);
+        if (e < p.count) {
+            const float root = root_value(p.v[e], p.v_scale[block]);
+            x = stepped(set->h, set->c, rates, p.theta(e), Storage<G>::load1(p.grad + e), m_value(p.m[e], p.m_scale[block]), __fmul_rn(root, root));
+        }
         const uint32_t ms = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.m)));
         const uint32_t vs = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.root)));
         const uint32_t word = element_word(octet_word(set->c.key, p.octet + e / kOctet), e % kOctet);
@@ -554,15 +567,12 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
 
 // ---- the kernel ----------------------------------------------------------------------------------------------------------------
 
-// The last CTA to come here counts the step and leaves the ticket as it was.
-__device__ __forceinline__ void count_step(int64_t* step, unsigned* ticket) {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
-            *ticket = 0;
-            *step += 1;
-        }
+// By one thread of a CTA that has read the step's number: the last to come here counts it, and leaves the ticket as it was.
+__device__ __forceinline__ void count_step(int64_t* step, int64_t t, unsigned* ticket) {
+    __threadfence();
+    if (atomicAdd(ticket, 1u) == gridDim.x - 1) {
+        *ticket = 0;
+        *step = t;
     }
 }
 
@@ -575,12 +585,29 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
     __shared__ Setting set;
     __shared__ int found;
     const Share share(all.pieces);
+    start_after_last();
+    let_next_start();
     if (share.hi > share.lo) find_tensor(all, share.hi - 1, &found);
-    if (threadIdx.x == 0) set.h = h, set.c = common_of(h, step, lr, sumsq);
+    __syncthreads();
+    int tensor = found;
+    if (share.hi > share.lo && all.records[tensor].grad) {
+        // the first piece, on its way to L2 while the step's numbers are worked out
+        const Record r = all.records[tensor];
+        const int64_t i = (share.hi - 1 - all.first[tensor]) * kPiece + threadIdx.x * kOctet;
+        if (i < r.numel) {
+            const Part<P, G, kMaster, S> p(r, i, 0);
+            const auto warm = [](const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); };
+            warm(p.grad), warm(p.m), warm(p.v);
+            if constexpr (kMaster) warm(p.master);
+            else warm(p.param);
+        }
+    }
+    make_common(h, step, lr, sumsq, set.c);
+    if (threadIdx.x == 0) set.h = h;
     __syncthreads();
     const Common c = set.c;
     if (c.skip) return;
-    int tensor = found;
+    if (threadIdx.x == 0) count_step(step, c.t, ticket);
 #pragma unroll 1
     for (int64_t piece = share.hi; piece > share.lo;) {
         const Record r = all.records[tensor];
@@ -630,7 +657,6 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
             for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(&set, h, c, rates, p, i);
         }
     }
-    count_step(step, ticket);
 }
 
 template <typename P, typename G, bool kMaster, bool kChance>
