@@ -10,6 +10,9 @@
 // vectors go an element a lane, eight of them at a time, so that their loads are whole lines too.
 #include <nvtx3/nvToolsExt.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "qn_adam.cuh"
 
 namespace {
@@ -314,9 +317,12 @@ struct Raw {
 // The way of these elements through shared memory.  What a thread has under way in registers (some 40 bytes of an octet) is a
 // third of what it takes to cover the latency of a loaded memory, 2.5 us, so each thread copies its own eight elements of
 // the next pieces into slots of its own: asynchronously, and with nobody to wait for but itself.
-constexpr int kSlots = 4;
+// Slots: four, or three where an element takes so much that CTAs would be lost.
+template <typename P, typename G, bool kMaster>
+constexpr int kSlotsOf = (kMaster || sizeof(P) == 4) && sizeof(G) == 4 ? 3 : 4;
 template <typename P, typename G, bool kMaster>
 struct Slots {
+    static constexpr int kSlots = kSlotsOf<P, G, kMaster>;
     static constexpr int kTheta = kMaster || sizeof(P) == 4 ? 2 : 1, kGrad = sizeof(G) == 4 ? 2 : 1;  // units of 16 bytes
     uint4 theta[kSlots][kTheta][kThreads], grad[kSlots][kGrad][kThreads];
     uint2 m[kSlots][kThreads], v[kSlots][kThreads];
@@ -508,22 +514,96 @@ __device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rate
     }
 }
 
-template <bool kChance, typename P, typename G, bool kMaster>
+// A piece of a tensor that does not lie on vectors, in shared memory: as many bytes as it takes to copy whole units of 16.  (The tensor
+// has more elements on both sides of it.)
+template <typename P, typename G, bool kMaster>
+struct Window {
+    static constexpr int kTheta = kMaster || sizeof(P) == 4 ? 4 : 2, kScales = kPiece / QN_ADAM_BLOCK;
+    struct Slot {
+        uint4 theta[kPiece * kTheta / 16 + 1], grad[kPiece * sizeof(G) / 16 + 1], m[kPiece / 16 + 1], v[kPiece / 16 + 1];
+        uint4 m_scale[kScales / 16 + 1], v_scale[kScales / 16 + 1];
+    };
+    static constexpr int kSlots = kSlotsOf<P, G, kMaster>;
+    Slot slot[kSlots];
+
+    template <int N>
+    __device__ static __forceinline__ void copy(uint4 (&to)[N], const void* from) {
+        const char* at = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(from) & ~uintptr_t(15));
+        const int units = N - (at == from);
+#pragma unroll
+        for (int k = 0; k < N; k += kThreads) {
+            const int j = k + threadIdx.x;
+            if (j < units) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&to[j])), "l"(at + 16 * j) : "memory");
+        }
+    }
+    // By all threads; each call is a group, also if there is nothing to copy.
+    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int s, int i, bool any) {
+        if (any) {
+            copy(slot[s].theta, kMaster ? static_cast<const void*>(p.master + i) : static_cast<const void*>(p.param + i));
+            copy(slot[s].grad, p.grad + i);
+            copy(slot[s].m, p.m + i);
+            copy(slot[s].v, p.v + i);
+            copy(slot[s].m_scale, p.m_scale + i / QN_ADAM_BLOCK);
+            copy(slot[s].v_scale, p.v_scale + i / QN_ADAM_BLOCK);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ static __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
+};
+// Where elements come from: memory, or a window (elements counted from the piece's first).
+template <typename P, typename G, bool kMaster>
+struct FromMemory {
+    const Part<P, G, kMaster, uint8_t>& p;
+    __device__ __forceinline__ float theta(int e) const { return p.theta(e); }
+    __device__ __forceinline__ float grad(int e) const { return Storage<G>::load1(p.grad + e); }
+    __device__ __forceinline__ uint32_t m(int e) const { return p.m[e]; }
+    __device__ __forceinline__ uint32_t v(int e) const { return p.v[e]; }
+    __device__ __forceinline__ uint32_t m_scale(int block) const { return p.m_scale[block]; }
+    __device__ __forceinline__ uint32_t v_scale(int block) const { return p.v_scale[block]; }
+};
+template <typename P, typename G, bool kMaster>
+struct FromWindow {
+    using Theta = typename std::conditional<kMaster, float, P>::type;
+    const Theta* theta_at;
+    const G* grad_at;
+    const uint8_t *m_at, *v_at, *m_scale_at, *v_scale_at;
+    template <typename X>
+    __device__ static __forceinline__ const X* in(const uint4* to, const void* from) {
+        return reinterpret_cast<const X*>(reinterpret_cast<const char*>(to) + (reinterpret_cast<uintptr_t>(from) & 15));
+    }
+    __device__ __forceinline__ FromWindow(const typename Window<P, G, kMaster>::Slot& s, const Part<P, G, kMaster, uint8_t>& p)
+        : theta_at(in<Theta>(s.theta, kMaster ? static_cast<const void*>(p.master) : static_cast<const void*>(p.param))),
+          grad_at(in<G>(s.grad, p.grad)), m_at(in<uint8_t>(s.m, p.m)), v_at(in<uint8_t>(s.v, p.v)),
+          m_scale_at(in<uint8_t>(s.m_scale, p.m_scale)), v_scale_at(in<uint8_t>(s.v_scale, p.v_scale)) {}
+    __device__ __forceinline__ float theta(int e) const { return load_rw(theta_at + e); }
+    __device__ __forceinline__ float grad(int e) const { return load_rw(grad_at + e); }
+    __device__ __forceinline__ uint32_t m(int e) const { return m_at[e]; }
+    __device__ __forceinline__ uint32_t v(int e) const { return v_at[e]; }
+    __device__ __forceinline__ uint32_t m_scale(int block) const { return m_scale_at[block]; }
+    __device__ __forceinline__ uint32_t v_scale(int block) const { return v_scale_at[block]; }
+};
+
+// `from`: its element `offset` is the part's element i.
+template <bool kChance, typename P, typename G, bool kMaster, typename F>
 __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, uint8_t>& p, int i) {
+                                           const Part<P, G, kMaster, uint8_t>& p, int i, const F& from, int offset) {
     if (i >= p.count) return;
     if (i + 256 > p.count) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, i);
     const int lane = threadIdx.x & 31, at = i + lane, block = i / QN_ADAM_BLOCK;
     f32x2 m[4], r[4], g[4];
     float t[8];
+    uint32_t codes[8][2];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int e = offset + 32 * j + lane;
+        codes[j][0] = from.m(e), codes[j][1] = from.v(e), t[j] = from.theta(e);
+    }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int e = at + 64 * q;
-        const uint32_t m0 = p.m[e], m1 = p.m[e + 32], r0 = p.v[e], r1 = p.v[e + 32];
-        m[q] = m_values(m0 + m1 * 256u, pack2(power_of(p.m_scale[block + 2 * q]), power_of(p.m_scale[block + 2 * q + 1])));
-        r[q] = root_values(r0 + r1 * 65536u, pack2(root_unit(p.v_scale[block + 2 * q]), root_unit(p.v_scale[block + 2 * q + 1])));
-        g[q] = pack2(Storage<G>::load1(p.grad + e), Storage<G>::load1(p.grad + e + 32));
-        t[2 * q] = p.theta(e), t[2 * q + 1] = p.theta(e + 32);
+        const int e = offset + 64 * q + lane, b = offset / QN_ADAM_BLOCK + 2 * q;
+        g[q] = pack2(from.grad(e), from.grad(e + 32));
+        m[q] = m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u, pack2(power_of(from.m_scale(b)), power_of(from.m_scale(b + 1))));
+        r[q] = root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u, pack2(root_unit(from.v_scale(b)), root_unit(from.v_scale(b + 1))));
     }
     float top_m, top_v;
     const bool odd = !moments(h, c, m, r, g, top_m, top_v);
@@ -620,10 +700,39 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
         const Part<P, G, kMaster, S> p(r, begin, min(r.numel - begin, (to - from) * kPiece));
         const int last = static_cast<int>(to - from - 1) * kPiece;
         if (!p.whole_vectors()) {
+            const int mine = static_cast<int>(threadIdx.x / 32) * 256;  // of this warp in a piece
+            if constexpr (sizeof(S) == 4) {
 #pragma unroll 1
-            for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + static_cast<int>(threadIdx.x / 32) * 256);
+                for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine);
+            } else {
+                const FromMemory<P, G, kMaster> memory{p};
+                // pieces with more of the tensor on both sides go through shared memory
+                int base = last;
+                const int lowest = begin == 0 ? kPiece : 0;
+                for (; base >= 0 && begin + base + kPiece + 16 * QN_ADAM_BLOCK > r.numel; base -= kPiece)
+                    step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
+                Window<P, G, kMaster>& window = *reinterpret_cast<Window<P, G, kMaster>*>(shared);
+                constexpr int kSlots = Window<P, G, kMaster>::kSlots;
+                int slot = 0;
+#pragma unroll 1
+                for (int k = 0; k < kSlots - 1; ++k) window.fetch(p, k, base - k * kPiece, base - k * kPiece >= lowest);
+#pragma unroll 1
+                for (; base >= lowest; base -= kPiece) {
+                    window.wait();
+                    __syncthreads();  // all have their copies, and are through with the slot that is filled next
+                    const int ahead = base - (kSlots - 1) * kPiece;
+                    window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= lowest);
+                    const FromWindow<P, G, kMaster> from(window.slot[slot], p);
+                    step_lanes<kChance>(&set, h, c, rates, p, base + mine, from, mine);
+                    slot = slot == kSlots - 1 ? 0 : slot + 1;
+                }
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+                for (; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
+                __syncthreads();  // before the slots are filled again
+            }
         } else if constexpr (sizeof(S) == 1) {
             Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
+            constexpr int kSlots = Slots<P, G, kMaster>::kSlots;
             int i = last + threadIdx.x * kOctet, slot = 0;
             // scales are bytes at any address, and come through registers
             uint32_t m_scale[kSlots], v_scale[kSlots];
@@ -662,7 +771,8 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
 template <typename P, typename G, bool kMaster, bool kChance>
 cudaError_t launch_step(const qn_adam_plan& h, const Hyper& hyper, int64_t* step, const float* lr, const double* sumsq, cudaStream_t st) {
     static Resident resident[2];
-    return h.eight ? launch_over(adam_step_kernel<P, G, kMaster, uint8_t, kChance>, resident[1], sizeof(Slots<P, G, kMaster>), h, st, hyper, step, lr, sumsq, h.tickets)
+    constexpr size_t kShared = std::max(sizeof(Slots<P, G, kMaster>), sizeof(Window<P, G, kMaster>));
+    return h.eight ? launch_over(adam_step_kernel<P, G, kMaster, uint8_t, kChance>, resident[1], kShared, h, st, hyper, step, lr, sumsq, h.tickets)
                    : launch_over(adam_step_kernel<P, G, kMaster, float, kChance>, resident[0], 0, h, st, hyper, step, lr, sumsq, h.tickets);
 }
 
