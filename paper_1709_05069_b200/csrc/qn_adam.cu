@@ -16,40 +16,54 @@ __global__ void __launch_bounds__(kThreads) adam_norm_kernel(const Tensors all, 
     __shared__ double scratch[kThreads / 32];
     __shared__ int found;
     __shared__ bool last;
-    const Share share(all.pieces);
+    const Turns turns(all.pieces, 32, 8);
     start_after_last();
     let_next_start();
-    if (share.hi > share.lo) find_tensor(all, share.lo, &found);
-    __syncthreads();
     double sum = 0.0;
-    int tensor = found;
 #pragma unroll 1
-    for (int64_t piece = share.lo; piece < share.hi; ++tensor) {
-        const int64_t first = all.first[tensor], from = piece, to = min(share.hi, all.first[tensor + 1]);
-        const G* grad = static_cast<const G*>(all.records[tensor].grad);
-        piece = to;
-        if (to == from || !grad) continue;
-        const int64_t begin = (from - first) * kPiece, end = min(all.records[tensor].numel, (to - first) * kPiece);
-        int64_t i = begin + threadIdx.x;
-        if (reinterpret_cast<uintptr_t>(grad) % (kOctet * sizeof(G)) == 0) {  // eight elements a thread
+    for (int turn = 0; turn < turns.count; ++turn) {
+        const int64_t lo = turns.lo(turn), hi = turns.hi(turn);
+        __syncthreads();
+        if (hi > lo) find_tensor(all, lo, &found);
+        __syncthreads();
+        int tensor = found;
+#pragma unroll 1
+        for (int64_t piece = lo; piece < hi; ++tensor) {
+            const int64_t first = all.first[tensor], from = piece, to = min(hi, all.first[tensor + 1]);
+            const G* grad = static_cast<const G*>(all.records[tensor].grad);
+            piece = to;
+            if (to == from || !grad) continue;
+            const int64_t begin = (from - first) * kPiece, end = min(all.records[tensor].numel, (to - first) * kPiece);
+            int64_t i = begin + threadIdx.x;
+            if (reinterpret_cast<uintptr_t>(grad) % (kOctet * sizeof(G)) == 0) {  // eight elements a thread
 #pragma unroll 4
-            for (int64_t at = begin + threadIdx.x * kOctet; at + kOctet <= end; at += kPiece) {
-                uint32_t raw[sizeof(G) == 4 ? 8 : 4];
-                load8(grad + at, raw);
+                for (int64_t at = begin + threadIdx.x * kOctet; at + kOctet <= end; at += kPiece) {
+                    uint32_t raw[sizeof(G) == 4 ? 8 : 4];
+                    load8(grad + at, raw);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    float a, b;
-                    unpack2(two_of(raw, q), a, b);
-                    sum += static_cast<double>(a) * a;
-                    sum += static_cast<double>(b) * b;
+                    for (int q = 0; q < 4; ++q) {
+                        float a, b;
+                        unpack2(two_of(raw, q), a, b);
+                        sum += static_cast<double>(a) * a;
+                        sum += static_cast<double>(b) * b;
+                    }
                 }
+                i = end - (end - begin) % kOctet + threadIdx.x;
             }
-            i = end - (end - begin) % kOctet + threadIdx.x;
-        }
-#pragma unroll 8
-        for (; i < end; i += kThreads) {
-            const double g = Storage<G>::load1(grad + i);
-            sum += g * g;
+            // element by element, eight loads under way together
+#pragma unroll 1
+            for (; i + 7 * kThreads < end; i += 8 * kThreads) {
+                float g[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) g[e] = Storage<G>::load1(grad + i + e * kThreads);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum += static_cast<double>(g[e]) * g[e];
+            }
+#pragma unroll 1
+            for (; i < end; i += kThreads) {
+                const double g = Storage<G>::load1(grad + i);
+                sum += g * g;
+            }
         }
     }
     sum = block_reduce<double, add_op>(sum, scratch);
@@ -78,63 +92,84 @@ __device__ __forceinline__ void store_value(__nv_bfloat16* p, float x) { *p = __
 template <typename T, typename S>
 __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all, T* m_out, T* root_out) {
     __shared__ int found;
-    const Share share(all.pieces);
+    const Turns turns(all.pieces, 8, 32);
     start_after_last();
     let_next_start();
-    if (share.hi > share.lo) find_tensor(all, share.lo, &found);
-    __syncthreads();
-    int tensor = found;
 #pragma unroll 1
-    for (int64_t piece = share.lo; piece < share.hi; ++tensor) {
-        const Record r = all.records[tensor];
-        const int64_t first = all.first[tensor], from = piece, to = min(share.hi, all.first[tensor + 1]);
-        piece = to;
-        if (to == from) continue;
-        const S *m_at = static_cast<const S*>(r.m), *v_at = static_cast<const S*>(r.v);
-        T *m_to = m_out ? m_out + r.octet * kOctet : nullptr, *root_to = root_out ? root_out + r.octet * kOctet : nullptr;
-        const int64_t begin = (from - first) * kPiece, whole = (r.numel + QN_ADAM_BLOCK - 1) / QN_ADAM_BLOCK * QN_ADAM_BLOCK;
-        const int64_t end = min(whole, (to - first) * kPiece), full = min(end, r.numel / kOctet * kOctet);
-        int64_t i = begin + threadIdx.x;
-        const auto off = [](const void* p, uint32_t size) { return reinterpret_cast<uintptr_t>(p) & (8u * size - 1u); };
-        if ((off(m_out, sizeof(T)) | off(root_out, sizeof(T)) | off(r.m, sizeof(S)) | off(r.v, sizeof(S))) == 0) {
+    for (int turn = 0; turn < turns.count; ++turn) {
+        const int64_t lo = turns.lo(turn), hi = turns.hi(turn);
+        __syncthreads();
+        if (hi > lo) find_tensor(all, lo, &found);
+        __syncthreads();
+        int tensor = found;
+#pragma unroll 1
+        for (int64_t piece = lo; piece < hi; ++tensor) {
+            const Record r = all.records[tensor];
+            const int64_t first = all.first[tensor], from = piece, to = min(hi, all.first[tensor + 1]);
+            piece = to;
+            if (to == from) continue;
+            const S *m_at = static_cast<const S*>(r.m), *v_at = static_cast<const S*>(r.v);
+            T *m_to = m_out ? m_out + r.octet * kOctet : nullptr, *root_to = root_out ? root_out + r.octet * kOctet : nullptr;
+            const int64_t begin = (from - first) * kPiece, whole = (r.numel + QN_ADAM_BLOCK - 1) / QN_ADAM_BLOCK * QN_ADAM_BLOCK;
+            const int64_t end = min(whole, (to - first) * kPiece), full = min(end, r.numel / kOctet * kOctet);
+            int64_t i = begin + threadIdx.x;
+            const auto off = [](const void* p, uint32_t size) { return reinterpret_cast<uintptr_t>(p) & (8u * size - 1u); };
+            if ((off(m_out, sizeof(T)) | off(root_out, sizeof(T)) | off(r.m, sizeof(S)) | off(r.v, sizeof(S))) == 0) {
 #pragma unroll 2
-            for (int64_t a = begin + threadIdx.x * kOctet; a < full; a += kPiece) {
-                f32x2 m2[4], r2[4];
-                float m[8], root[8];
-                uint32_t m_raw[sizeof(S) == 1 ? 2 : 8], v_raw[sizeof(S) == 1 ? 2 : 8];
-                load8(m_at + a, m_raw);
-                load8(v_at + a, v_raw);
-                if constexpr (sizeof(S) == 1) {
-                    m_values(m_raw, r.m_scale[a / QN_ADAM_BLOCK], m2);
-                    root_values(v_raw, r.v_scale[a / QN_ADAM_BLOCK], r2);
-                } else {
+                for (int64_t a = begin + threadIdx.x * kOctet; a < full; a += kPiece) {
+                    f32x2 m2[4], r2[4];
+                    float m[8], root[8];
+                    uint32_t m_raw[sizeof(S) == 1 ? 2 : 8], v_raw[sizeof(S) == 1 ? 2 : 8];
+                    load8(m_at + a, m_raw);
+                    load8(v_at + a, v_raw);
+                    if constexpr (sizeof(S) == 1) {
+                        m_values(m_raw, r.m_scale[a / QN_ADAM_BLOCK], m2);
+                        root_values(v_raw, r.v_scale[a / QN_ADAM_BLOCK], r2);
+                    } else {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) m2[q] = two_of(m_raw, q), r2[q] = two_of(v_raw, q);
+                        for (int q = 0; q < 4; ++q) m2[q] = two_of(m_raw, q), r2[q] = two_of(v_raw, q);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) unpack2(m2[q], m[2 * q], m[2 * q + 1]), unpack2(r2[q], root[2 * q], root[2 * q + 1]);
+                    if constexpr (sizeof(S) == 4)
+#pragma unroll
+                        for (float& x : root) x = __fsqrt_rn(x);
+                    if (m_to) store8(m_to + a, m);
+                    if (root_to) store8(root_to + a, root);
                 }
-#pragma unroll
-                for (int q = 0; q < 4; ++q) unpack2(m2[q], m[2 * q], m[2 * q + 1]), unpack2(r2[q], root[2 * q], root[2 * q + 1]);
-                if constexpr (sizeof(S) == 4)
-#pragma unroll
-                    for (float& x : root) x = __fsqrt_rn(x);
-                if (m_to) store8(m_to + a, m);
-                if (root_to) store8(root_to + a, root);
+                i = max(begin, full) + threadIdx.x;
             }
-            i = max(begin, full) + threadIdx.x;
-        }
-#pragma unroll 4
-        for (; i < end; i += kThreads) {
-            float m = 0.0f, root = 0.0f;
-            if (i < r.numel) {
-                if constexpr (sizeof(S) == 1) {
-                    m = m_value(m_at[i], r.m_scale[i / QN_ADAM_BLOCK]);
-                    root = root_value(v_at[i], r.v_scale[i / QN_ADAM_BLOCK]);
-                } else {
-                    m = m_at[i];
-                    root = __fsqrt_rn(v_at[i]);
+            const auto value = [&](int64_t at, uint32_t m_code, uint32_t v_code, float& m, float& root) {
+                m = m_value(m_code, r.m_scale[at / QN_ADAM_BLOCK]);
+                root = root_value(v_code, r.v_scale[at / QN_ADAM_BLOCK]);
+            };
+            const auto put = [&](int64_t at, float m, float root) {
+                if (m_to) store_value(m_to + at, m);
+                if (root_to) store_value(root_to + at, root);
+            };
+            // element by element, eight loads of each under way together
+#pragma unroll 1
+            for (; i + 7 * kThreads < min(end, r.numel); i += 8 * kThreads) {
+                S m[8], v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) m[e] = m_at[i + e * kThreads], v[e] = v_at[i + e * kThreads];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float a, b;
+                    if constexpr (sizeof(S) == 1) value(i + e * kThreads, m[e], v[e], a, b);
+                    else a = m[e], b = __fsqrt_rn(v[e]);
+                    put(i + e * kThreads, a, b);
                 }
             }
-            if (m_to) store_value(m_to + i, m);
-            if (root_to) store_value(root_to + i, root);
+#pragma unroll 1
+            for (; i < end; i += kThreads) {
+                float m = 0.0f, root = 0.0f;
+                if (i < r.numel) {
+                    if constexpr (sizeof(S) == 1) value(i, m_at[i], v_at[i], m, root);
+                    else m = m_at[i], root = __fsqrt_rn(v_at[i]);
+                }
+                put(i, m, root);
+            }
         }
     }
 }

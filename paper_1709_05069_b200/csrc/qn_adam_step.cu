@@ -664,16 +664,17 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
     extern __shared__ __align__(16) unsigned char shared[];
     __shared__ Setting set;
     __shared__ int found;
-    const Share share(all.pieces);
+    const Turns turns(all.pieces, sizeof(S) == 4 ? 8 : 32, sizeof(S) == 4 ? 32 : 8);
+    int64_t lo = turns.lo(turns.count - 1), hi = turns.hi(turns.count - 1);
     start_after_last();
     let_next_start();
-    if (share.hi > share.lo) find_tensor(all, share.hi - 1, &found);
+    if (hi > lo) find_tensor(all, hi - 1, &found);
     __syncthreads();
     int tensor = found;
-    if (share.hi > share.lo && all.records[tensor].grad) {
+    if (hi > lo && all.records[tensor].grad) {
         // the first piece, on its way to L2 while the step's numbers are worked out
         const Record r = all.records[tensor];
-        const int64_t i = (share.hi - 1 - all.first[tensor]) * kPiece + threadIdx.x * kOctet;
+        const int64_t i = (hi - 1 - all.first[tensor]) * kPiece + threadIdx.x * kOctet;
         if (i < r.numel) {
             const Part<P, G, kMaster, S> p(r, i, 0);
             const auto warm = [](const void* at) { asm volatile("prefetch.global.L2 [%0];" ::"l"(at)); };
@@ -689,82 +690,91 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
     if (c.skip) return;
     if (threadIdx.x == 0) count_step(step, c.t, ticket);
 #pragma unroll 1
-    for (int64_t piece = share.hi; piece > share.lo;) {
-        const Record r = all.records[tensor];
-        const int64_t first = all.first[tensor], from = max(max(share.lo, first), piece - kMostPieces), to = piece;
-        piece = from;
-        if (piece == first) --tensor;
-        if (to == from || !r.grad) continue;
-        const Rates rates(c, r);
-        const int64_t begin = (from - first) * kPiece;
-        const Part<P, G, kMaster, S> p(r, begin, min(r.numel - begin, (to - from) * kPiece));
-        const int last = static_cast<int>(to - from - 1) * kPiece;
-        if (!p.whole_vectors()) {
-            const int mine = static_cast<int>(threadIdx.x / 32) * 256;  // of this warp in a piece
-            if constexpr (sizeof(S) == 4) {
+    for (int turn = turns.count - 1;;) {
 #pragma unroll 1
-                for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine);
-            } else {
-                const FromMemory<P, G, kMaster> memory{p};
-                // pieces with more of the tensor on both sides go through shared memory
-                int base = last;
-                const int lowest = begin == 0 ? kPiece : 0;
-                for (; base >= 0 && begin + base + kPiece + 16 * QN_ADAM_BLOCK > r.numel; base -= kPiece)
-                    step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
-                Window<P, G, kMaster>& window = *reinterpret_cast<Window<P, G, kMaster>*>(shared);
-                constexpr int kSlots = Window<P, G, kMaster>::kSlots;
-                int slot = 0;
+        for (int64_t piece = hi; piece > lo;) {
+            const Record r = all.records[tensor];
+            const int64_t first = all.first[tensor], from = max(max(lo, first), piece - kMostPieces), to = piece;
+            piece = from;
+            if (piece == first) --tensor;
+            if (to == from || !r.grad) continue;
+            const Rates rates(c, r);
+            const int64_t begin = (from - first) * kPiece;
+            const Part<P, G, kMaster, S> p(r, begin, min(r.numel - begin, (to - from) * kPiece));
+            const int last = static_cast<int>(to - from - 1) * kPiece;
+            if (!p.whole_vectors()) {
+                const int mine = static_cast<int>(threadIdx.x / 32) * 256;  // of this warp in a piece
+                if constexpr (sizeof(S) == 4) {
 #pragma unroll 1
-                for (int k = 0; k < kSlots - 1; ++k) window.fetch(p, k, base - k * kPiece, base - k * kPiece >= lowest);
+                    for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine);
+                } else {
+                    const FromMemory<P, G, kMaster> memory{p};
+                    // pieces with more of the tensor on both sides go through shared memory
+                    int base = last;
+                    const int lowest = begin == 0 ? kPiece : 0;
+                    for (; base >= 0 && begin + base + kPiece + 16 * QN_ADAM_BLOCK > r.numel; base -= kPiece)
+                        step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
+                    Window<P, G, kMaster>& window = *reinterpret_cast<Window<P, G, kMaster>*>(shared);
+                    constexpr int kSlots = Window<P, G, kMaster>::kSlots;
+                    int slot = 0;
 #pragma unroll 1
-                for (; base >= lowest; base -= kPiece) {
-                    window.wait();
-                    __syncthreads();  // all have their copies, and are through with the slot that is filled next
-                    const int ahead = base - (kSlots - 1) * kPiece;
-                    window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= lowest);
-                    const FromWindow<P, G, kMaster> from(window.slot[slot], p);
-                    step_lanes<kChance>(&set, h, c, rates, p, base + mine, from, mine);
+                    for (int k = 0; k < kSlots - 1; ++k) window.fetch(p, k, base - k * kPiece, base - k * kPiece >= lowest);
+#pragma unroll 1
+                    for (; base >= lowest; base -= kPiece) {
+                        window.wait();
+                        __syncthreads();  // all have their copies, and are through with the slot that is filled next
+                        const int ahead = base - (kSlots - 1) * kPiece;
+                        window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= lowest);
+                        const FromWindow<P, G, kMaster> from(window.slot[slot], p);
+                        step_lanes<kChance>(&set, h, c, rates, p, base + mine, from, mine);
+                        slot = slot == kSlots - 1 ? 0 : slot + 1;
+                    }
+                    asm volatile("cp.async.wait_group 0;" ::: "memory");
+                    for (; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
+                    __syncthreads();  // before the slots are filled again
+                }
+            } else if constexpr (sizeof(S) == 1) {
+                Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
+                constexpr int kSlots = Slots<P, G, kMaster>::kSlots;
+                int i = last + threadIdx.x * kOctet, slot = 0;
+                // scales are bytes at any address, and come through registers
+                uint32_t m_scale[kSlots], v_scale[kSlots];
+                const auto fetch = [&](int k, int ahead) {
+                    const int at = i - k * kPiece;
+                    slots.fetch(p, ahead, at, at >= 0 && at + kOctet <= p.count);
+                    const int block = at >= 0 && at < p.count ? at / QN_ADAM_BLOCK : 0;
+                    m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
+                };
+#pragma unroll
+                for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
+                bool first_one = true;
+#pragma unroll 1
+                for (int base = last; base >= 0; base -= kPiece, i -= kPiece) {
+                    Raw<P, G, kMaster> raw;
+                    slots.wait();
+                    slots.take(slot, raw);
+                    raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
+#pragma unroll
+                    for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
+                    fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
+                    m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
                     slot = slot == kSlots - 1 ? 0 : slot + 1;
+                    if (first_one) step_octet<kChance, false>(&set, h, c, rates, p, i, raw);  // the piece at the run's end may not be whole
+                    else step_octet<kChance, true>(&set, h, c, rates, p, i, raw);
+                    first_one = false;
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-                for (; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
-                __syncthreads();  // before the slots are filled again
-            }
-        } else if constexpr (sizeof(S) == 1) {
-            Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
-            constexpr int kSlots = Slots<P, G, kMaster>::kSlots;
-            int i = last + threadIdx.x * kOctet, slot = 0;
-            // scales are bytes at any address, and come through registers
-            uint32_t m_scale[kSlots], v_scale[kSlots];
-            const auto fetch = [&](int k, int ahead) {
-                const int at = i - k * kPiece;
-                slots.fetch(p, ahead, at, at >= 0 && at + kOctet <= p.count);
-                const int block = at >= 0 && at < p.count ? at / QN_ADAM_BLOCK : 0;
-                m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
-            };
-#pragma unroll
-            for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
-            bool first_one = true;
+            } else {
 #pragma unroll 1
-            for (int base = last; base >= 0; base -= kPiece, i -= kPiece) {
-                Raw<P, G, kMaster> raw;
-                slots.wait();
-                slots.take(slot, raw);
-                raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
-#pragma unroll
-                for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
-                fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
-                m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
-                slot = slot == kSlots - 1 ? 0 : slot + 1;
-                if (first_one) step_octet<kChance, false>(&set, h, c, rates, p, i, raw);  // the piece at the run's end may not be whole
-                else step_octet<kChance, true>(&set, h, c, rates, p, i, raw);
-                first_one = false;
+                for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(&set, h, c, rates, p, i);
             }
-            asm volatile("cp.async.wait_group 0;" ::: "memory");
-        } else {
-#pragma unroll 1
-            for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(&set, h, c, rates, p, i);
         }
+        if (--turn < 0) return;
+        lo = turns.lo(turn), hi = turns.hi(turn);
+        __syncthreads();
+        if (hi > lo) find_tensor(all, hi - 1, &found);
+        __syncthreads();
+        tensor = found;
     }
 }
 
