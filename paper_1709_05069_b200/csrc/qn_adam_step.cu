@@ -66,8 +66,12 @@ __device__ __forceinline__ void make_common(const Hyper& h, const int64_t* step,
 // The same for all elements of a tensor.
 struct Rates {
     float keep, speed;  // 1 - lr wd, lr / (1 - b1^t)
-    __device__ __forceinline__ Rates(const Common& c, const Record& r)
-        : keep(static_cast<float>(1.0 - c.lr * r.lr_scale * r.decay)), speed(static_cast<float>(c.speed * r.lr_scale)) {}
+    // 1 / sqrt(1 - b2^t) and eps in units of speed: speed / (r spread + eps) as one reciprocal.  For a speed of 0 they are infinite, and for
+    // r > 0 the step is 0, as it should be.
+    float spread, eps;
+    __device__ __forceinline__ Rates(const Hyper& h, const Common& c, const Record& r)
+        : keep(static_cast<float>(1.0 - c.lr * r.lr_scale * r.decay)), speed(static_cast<float>(c.speed * r.lr_scale)),
+          spread(c.spread / speed), eps(h.eps / speed) {}
 };
 
 // Where a run of a tensor's elements begins, and how many there are.  S: float, or uint8_t for codes.
@@ -122,11 +126,7 @@ __device__ __forceinline__ void store_param(__nv_bfloat16* p, float x, uint32_t 
     *p = kChance ? __ushort_as_bfloat16(static_cast<unsigned short>(chance_bits(x, word) >> 16)) : __float2bfloat16_rn(x);
 }
 
-// Element i from memory, with states in 32 bits; and with those in 8, whose block had the scales m_scale and v_scale.
-template <typename P, typename G, bool kMaster>
-__device__ __forceinline__ Element element_at(const Setting& set, const Rates& rates, const Part<P, G, kMaster, float>& p, int i) {
-    return stepped(set.h, set.c, rates, p.theta(i), Storage<G>::load1(p.grad + i), p.m[i], p.v[i]);
-}
+// Element i from memory, with states in 8 bits, whose block had the scales m_scale and v_scale.
 template <typename P, typename G, bool kMaster>
 __device__ __forceinline__ Element element_at(const Setting& set, const Rates& rates, const Part<P, G, kMaster, uint8_t>& p, int i,
                                               uint32_t m_scale, uint32_t v_scale) {
@@ -245,7 +245,9 @@ struct Coded {
     __device__ __forceinline__ Coded(const Hyper& h, const Common& c, const Rates& rates, f32x2 theta_, f32x2 m_, f32x2 minus_r, f32x2 ups_m,
                                      f32x2 ups_r, const uint32_t (&octets)[2], const uint32_t (&places)[2]) {
         float zm[2], zr[2], m1[2], t[2];
-        theta2 = moved(h, c, rates, theta_, m_, minus_r);
+        float d0, d1;
+        unpack2(fma2(minus_r, both(rates.spread), both(-rates.eps)), d0, d1);
+        theta2 = fma2(m_, pack2(rcp_approx(d0), rcp_approx(d1)), mul2(theta_, both(rates.keep)));
         unpack2(mul2(m_, ups_m), zm[0], zm[1]);
         unpack2(mul2(minus_r, ups_r), zr[0], zr[1]);
         unpack2(m_, m1[0], m1[1]);
@@ -265,21 +267,10 @@ struct Coded {
 
 // ---- tensors on vectors ----------------------------------------------------------------------------------------------------
 
-// Eight elements from i on, with states in 32 bits; element by element where there are fewer.
+// Eight elements from i on, with states in 32 bits.
 template <bool kChance, typename P, typename G, bool kMaster>
-__device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, float>& p, int i) {
+__device__ __forceinline__ void step_octet(const Hyper& h, const Common& c, const Rates& rates, const Part<P, G, kMaster, float>& p, int i) {
     const uint32_t word = kChance ? octet_word(c.key, p.octet + i / kOctet) : 0;
-    if (i + kOctet > p.count) {
-#pragma unroll 1
-        for (int e = i; e < p.count; ++e) {
-            const Element x = element_at(*set, rates, p, e);
-            p.m[e] = x.m, p.v[e] = x.v;
-            if constexpr (kMaster) p.master[e] = x.theta;
-            store_param<kChance>(p.param + e, x.theta, element_word(word, e - i));
-        }
-        return;
-    }
     uint32_t graw[sizeof(G) == 4 ? 8 : 4], traw[kMaster || sizeof(P) == 4 ? 8 : 4], mraw[8], vraw[8];
     load8(p.grad + i, graw);
     if constexpr (kMaster) load8(p.master + i, traw);
@@ -334,9 +325,9 @@ struct Slots {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory");
     }
     // Each call is a group, also if there is nothing to copy.
-    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int slot, int i, bool whole) {
+    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int slot, int i, bool any) {
         const int tid = threadIdx.x;
-        if (whole) {
+        if (any) {
             const char* at = kMaster ? reinterpret_cast<const char*>(p.master + i) : reinterpret_cast<const char*>(p.param + i);
 #pragma unroll
             for (int k = 0; k < kTheta; ++k) copy(&theta[slot][k][tid], at + 16 * k);
@@ -366,14 +357,14 @@ struct Slots {
     }
 };
 
-// For eight elements that are out of the ordinary, or fewer, from memory again: the bits of the largest finite m' and the exponent field
+// For eight elements that are out of the ordinary, from memory again: the bits of the largest finite m' and the exponent field
 // of the largest finite r'; and the step.
 template <typename P, typename G, bool kMaster>
 __device__ __noinline__ uint2 largest_of_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i, uint32_t m_scale,
                                               uint32_t v_scale) {
     uint2 top = {0, 0};
 #pragma unroll 1
-    for (int e = i; e < min(i + kOctet, p.count); ++e) {
+    for (int e = i; e < i + kOctet; ++e) {
         const Element x = element_at(*set, rates, p, e, m_scale, v_scale);
         top.x = max(top.x, finite_bits(x.m));
         top.y = max(top.y, finite_bits(x.root) >> 23);
@@ -385,7 +376,7 @@ __device__ __noinline__ void step_any(const Setting* set, const Rates rates, con
                                       uint32_t v_scale, uint32_t ms, uint32_t vs) {
     const uint32_t word = octet_word(set->c.key, p.octet + i / kOctet);
 #pragma unroll 1
-    for (int e = i; e < min(i + kOctet, p.count); ++e) {
+    for (int e = i; e < i + kOctet; ++e) {
         const uint32_t w = element_word(word, e - i);
         const Element x = element_at(*set, rates, p, e, m_scale, v_scale);
         p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), w));
@@ -395,8 +386,8 @@ __device__ __noinline__ void step_any(const Setting* set, const Rates rates, con
     }
 }
 
-// Eight elements from i on (unless kWhole: or what there is of them); all threads of a warp, four of which have a block.
-template <bool kChance, bool kWhole, typename P, typename G, bool kMaster>
+// Eight elements from i on; all threads of a warp, four of which have a block.
+template <bool kChance, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
                                            const Part<P, G, kMaster, uint8_t>& p, int i, const Raw<P, G, kMaster>& raw) {
     f32x2 m[4], r[4], g[4];
@@ -405,7 +396,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     root_values(raw.v, raw.v_scale, r);
 #pragma unroll
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
-    bool odd = !moments(h, c, m, r, g, top_m, top_v) || (!kWhole && i + kOctet > p.count);
+    bool odd = !moments(h, c, m, r, g, top_m, top_v);
     uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
     if (odd) {
         const uint2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
@@ -419,7 +410,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     // another one's element may be too large for this one's way
     odd = odd || most_m > __float_as_uint(kHigh) || field_r > (__float_as_uint(kHigh) >> 23);
     const uint32_t ms = scale_of(most_m), vs = scale_of(field_r << 23);
-    if ((kWhole || i < p.count) && (i / kOctet) % 4 == 0) {  // all four have read the old ones
+    if ((i / kOctet) % 4 == 0) {  // all four have read the old ones
         p.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(ms);
         p.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(vs);
     }
@@ -459,8 +450,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
 
 // 256 elements of a warp, from i on: element i + 32 j + lane is lane's j-th.  States in 32 bits.
 template <bool kChance, typename P, typename G, bool kMaster>
-__device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, float>& p, int i) {
+__device__ __forceinline__ void step_lanes(const Hyper& h, const Common& c, const Rates& rates, const Part<P, G, kMaster, float>& p, int i) {
     const int lane = threadIdx.x & 31;
     const uint32_t octet = kChance ? octet_word(c.key, p.octet + i / kOctet + lane) : 0;  // of the warp's lane-th eight
     float t[8], m[8], v[8], g[8];
@@ -486,7 +476,6 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
         if constexpr (kMaster) p.master[e] = t[j];
         store_param<kChance>(p.param + e, t[j], word);
     }
-    (void)set;
 }
 
 // The same for elements that are out of the ordinary, or fewer than 256, with states in 8 bits: a block at a time.
@@ -583,27 +572,30 @@ struct FromWindow {
     __device__ __forceinline__ uint32_t v_scale(int block) const { return v_scale_at[block]; }
 };
 
-// `from`: its element `offset` is the part's element i.
-template <bool kChance, typename P, typename G, bool kMaster, typename F>
+// `from`: its element `offset` is the part's element i.  kWhole: all 256 are there.
+template <bool kChance, bool kWhole, typename P, typename G, bool kMaster, typename F>
 __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
                                            const Part<P, G, kMaster, uint8_t>& p, int i, const F& from, int offset) {
-    if (i >= p.count) return;
-    if (i + 256 > p.count) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, i);
+    if (!kWhole && i >= p.count) return;
     const int lane = threadIdx.x & 31, at = i + lane, block = i / QN_ADAM_BLOCK;
+    // elements that are not there are ordinary ones that count for nothing and are not written
+    const auto here = [&](int j) { return kWhole || at + 32 * j < p.count; };
+    const auto last_block = [&](int b) { return kWhole ? b : min(b, (p.count - 1) / QN_ADAM_BLOCK); };
     f32x2 m[4], r[4], g[4];
     float t[8];
     uint32_t codes[8][2];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const int e = offset + 32 * j + lane;
-        codes[j][0] = from.m(e), codes[j][1] = from.v(e), t[j] = from.theta(e);
+        codes[j][0] = 0, codes[j][1] = 0x80, t[j] = 0.0f;
+        if (here(j)) codes[j][0] = from.m(e), codes[j][1] = from.v(e), t[j] = from.theta(e);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int e = offset + 64 * q + lane, b = offset / QN_ADAM_BLOCK + 2 * q;
-        g[q] = pack2(from.grad(e), from.grad(e + 32));
-        m[q] = m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u, pack2(power_of(from.m_scale(b)), power_of(from.m_scale(b + 1))));
-        r[q] = root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u, pack2(root_unit(from.v_scale(b)), root_unit(from.v_scale(b + 1))));
+        const int e = offset + 64 * q + lane, b0 = last_block(offset / QN_ADAM_BLOCK + 2 * q), b1 = last_block(offset / QN_ADAM_BLOCK + 2 * q + 1);
+        g[q] = pack2(here(2 * q) ? from.grad(e) : 1.0f, here(2 * q + 1) ? from.grad(e + 32) : 1.0f);
+        m[q] = m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u, pack2(power_of(from.m_scale(b0)), power_of(from.m_scale(b1))));
+        r[q] = root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u, pack2(root_unit(from.v_scale(b0)), root_unit(from.v_scale(b1))));
     }
     float top_m, top_v;
     const bool odd = !moments(h, c, m, r, g, top_m, top_v);
@@ -618,8 +610,8 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
         unpack2(r[q], r1[0], r1[1]);
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
-            most_m[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(m1[k]) & 0x7fffffffu);
-            most_r[k] = __reduce_max_sync(0xffffffffu, __float_as_uint(r1[k]) & 0x7fffffffu);
+            most_m[k] = __reduce_max_sync(0xffffffffu, here(2 * q + k) ? __float_as_uint(m1[k]) & 0x7fffffffu : 0u);
+            most_r[k] = __reduce_max_sync(0xffffffffu, here(2 * q + k) ? __float_as_uint(r1[k]) & 0x7fffffffu : 0u);
             octets[k] = __shfl_sync(0xffffffffu, octet, 4 * (2 * q + k) + lane / 8);
         }
         const Coded<kChance> two(h, c, rates, pack2(t[2 * q], t[2 * q + 1]), m[q], r[q], pack2(up_m(most_m[0] >> 23), up_m(most_m[1] >> 23)),
@@ -628,6 +620,7 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
             const int e = at + 64 * q + 32 * k;
+            if (!here(2 * q + k)) continue;
             p.m[e] = static_cast<uint8_t>(two.m[k] >> 24);
             p.v[e] = static_cast<uint8_t>(two.r[k] >> 24);
             if constexpr (kMaster) p.master[e] = t1[k];
@@ -698,75 +691,75 @@ __global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors al
             piece = from;
             if (piece == first) --tensor;
             if (to == from || !r.grad) continue;
-            const Rates rates(c, r);
+            const Rates rates(h, c, r);
             const int64_t begin = (from - first) * kPiece;
             const Part<P, G, kMaster, S> p(r, begin, min(r.numel - begin, (to - from) * kPiece));
             const int last = static_cast<int>(to - from - 1) * kPiece;
-            if (!p.whole_vectors()) {
-                const int mine = static_cast<int>(threadIdx.x / 32) * 256;  // of this warp in a piece
-                if constexpr (sizeof(S) == 4) {
+            const bool vectors = p.whole_vectors();
+            const int mine = static_cast<int>(threadIdx.x / 32) * 256;  // of this warp in a piece
+            if constexpr (sizeof(S) == 4) {
+                int base = last;
+                // element by element, all or what is left of a piece where the tensor ends
 #pragma unroll 1
-                    for (int base = last; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine);
-                } else {
-                    const FromMemory<P, G, kMaster> memory{p};
-                    // pieces with more of the tensor on both sides go through shared memory
-                    int base = last;
-                    const int lowest = begin == 0 ? kPiece : 0;
-                    for (; base >= 0 && begin + base + kPiece + 16 * QN_ADAM_BLOCK > r.numel; base -= kPiece)
-                        step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
+                for (; base >= 0 && (!vectors || base + kPiece > p.count); base -= kPiece) step_lanes<kChance>(h, c, rates, p, base + mine);
+#pragma unroll 1
+                for (int i = base + static_cast<int>(threadIdx.x) * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(h, c, rates, p, i);
+            } else {
+                // pieces from `top` down to `low` go through shared memory: whole ones, and off vectors those with more of the tensor on
+                // both sides.  The others come first.
+                int top = last;
+                const int low = !vectors && begin == 0 ? kPiece : 0;
+                while (top >= 0 && (vectors ? top + kPiece > p.count : begin + top + kPiece + 16 * QN_ADAM_BLOCK > r.numel)) top -= kPiece;
+#pragma unroll 1
+                for (int base = last; base >= 0; base -= kPiece) {
+                    if (base <= top && base >= low) base = low;
+                    else step_lanes<kChance, false>(&set, h, c, rates, p, base + mine, FromMemory<P, G, kMaster>{p}, base + mine);
+                }
+                constexpr int kSlots = kSlotsOf<P, G, kMaster>;
+                int base = top, slot = 0;
+                if (!vectors) {
                     Window<P, G, kMaster>& window = *reinterpret_cast<Window<P, G, kMaster>*>(shared);
-                    constexpr int kSlots = Window<P, G, kMaster>::kSlots;
-                    int slot = 0;
 #pragma unroll 1
-                    for (int k = 0; k < kSlots - 1; ++k) window.fetch(p, k, base - k * kPiece, base - k * kPiece >= lowest);
+                    for (int k = 0; k < kSlots - 1; ++k) window.fetch(p, k, base - k * kPiece, base - k * kPiece >= low);
 #pragma unroll 1
-                    for (; base >= lowest; base -= kPiece) {
+                    for (; base >= low; base -= kPiece) {
                         window.wait();
                         __syncthreads();  // all have their copies, and are through with the slot that is filled next
                         const int ahead = base - (kSlots - 1) * kPiece;
-                        window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= lowest);
+                        window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= low);
                         const FromWindow<P, G, kMaster> from(window.slot[slot], p);
-                        step_lanes<kChance>(&set, h, c, rates, p, base + mine, from, mine);
+                        step_lanes<kChance, true>(&set, h, c, rates, p, base + mine, from, mine);
                         slot = slot == kSlots - 1 ? 0 : slot + 1;
                     }
-                    asm volatile("cp.async.wait_group 0;" ::: "memory");
-                    for (; base >= 0; base -= kPiece) step_lanes<kChance>(&set, h, c, rates, p, base + mine, memory, base + mine);
-                    __syncthreads();  // before the slots are filled again
-                }
-            } else if constexpr (sizeof(S) == 1) {
-                Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
-                constexpr int kSlots = Slots<P, G, kMaster>::kSlots;
-                int i = last + threadIdx.x * kOctet, slot = 0;
-                // scales are bytes at any address, and come through registers
-                uint32_t m_scale[kSlots], v_scale[kSlots];
-                const auto fetch = [&](int k, int ahead) {
-                    const int at = i - k * kPiece;
-                    slots.fetch(p, ahead, at, at >= 0 && at + kOctet <= p.count);
-                    const int block = at >= 0 && at < p.count ? at / QN_ADAM_BLOCK : 0;
-                    m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
-                };
+                } else {
+                    Slots<P, G, kMaster>& slots = *reinterpret_cast<Slots<P, G, kMaster>*>(shared);
+                    int i = base + static_cast<int>(threadIdx.x) * kOctet;
+                    // scales are bytes at any address, and come through registers
+                    uint32_t m_scale[kSlots], v_scale[kSlots];
+                    const auto fetch = [&](int k, int to) {
+                        const int at = i - k * kPiece;
+                        slots.fetch(p, to, at, base >= k * kPiece);
+                        const int block = max(at, 0) / QN_ADAM_BLOCK;
+                        m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
+                    };
 #pragma unroll
-                for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
-                bool first_one = true;
+                    for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
 #pragma unroll 1
-                for (int base = last; base >= 0; base -= kPiece, i -= kPiece) {
-                    Raw<P, G, kMaster> raw;
-                    slots.wait();
-                    slots.take(slot, raw);
-                    raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
+                    for (; base >= 0; base -= kPiece, i -= kPiece) {
+                        Raw<P, G, kMaster> raw;
+                        slots.wait();
+                        slots.take(slot, raw);
+                        raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
 #pragma unroll
-                    for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
-                    fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
-                    m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
-                    slot = slot == kSlots - 1 ? 0 : slot + 1;
-                    if (first_one) step_octet<kChance, false>(&set, h, c, rates, p, i, raw);  // the piece at the run's end may not be whole
-                    else step_octet<kChance, true>(&set, h, c, rates, p, i, raw);
-                    first_one = false;
+                        for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
+                        fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
+                        m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
+                        slot = slot == kSlots - 1 ? 0 : slot + 1;
+                        step_octet<kChance>(&set, h, c, rates, p, i, raw);
+                    }
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
-            } else {
-#pragma unroll 1
-                for (int i = last + threadIdx.x * kOctet; i >= 0; i -= kPiece) step_octet<kChance>(&set, h, c, rates, p, i);
+                __syncthreads();  // before the slots are filled again
             }
         }
         if (--turn < 0) return;
