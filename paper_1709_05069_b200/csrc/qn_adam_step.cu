@@ -652,7 +652,7 @@ __device__ __forceinline__ void count_step(int64_t* step, int64_t t, unsigned* t
 constexpr int64_t kMostPieces = 1 << 19;  // of a run: its elements are counted in 32 bits
 
 template <typename P, typename G, bool kMaster, typename S, bool kChance>
-__global__ void __launch_bounds__(kThreads, 3) adam_step_kernel(const Tensors all, const Hyper h, int64_t* step, const float* lr,
+__global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_kernel(const Tensors all, const Hyper h, int64_t* step, const float* lr,
                                                              const double* sumsq, unsigned* ticket) {
     extern __shared__ __align__(16) unsigned char shared[];
     __shared__ Setting set;
