@@ -9,16 +9,28 @@ from . import qn  # noqa: F401
 from .qn import (  # noqa: F401
     QN_BF16,
     QN_F32,
+    QN_PREFERENCE_HINGE,
+    QN_PREFERENCE_LOGISTIC,
+    QN_PREFERENCE_SQUARED,
     QN_TEACHER_LOGITS,
     QN_TEACHER_LOGPROBS,
     QNError,
+    Adam,
     Handle,
+    qn_adam_create,
+    qn_adam_destroy,
+    qn_adam_grads,
+    qn_adam_norm,
+    qn_adam_state,
+    qn_adam_step,
     qn_create,
     qn_destroy,
     qn_distill,
     qn_gram,
     qn_logprobs,
     qn_logprobs_backward,
+    qn_policy,
+    qn_preference,
     qn_push,
     qn_rebuild,
     qn_status_sync,
