@@ -99,18 +99,24 @@ struct Part {
 
 // ---- one element -------------------------------------------------------------------------------------------------------
 
+__device__ __forceinline__ float rcp_approx(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 struct Element {
-    float theta, m, v, root;
+    float theta, m, root;
 };
-// m and v: before the step.
+// One element with states in 8 bits, whatever it is; m and v: before the step.  The same operations as those of the packed way below,
+// so that an element does not depend on which way its neighbours need.
 __device__ __forceinline__ Element stepped(const Hyper& h, const Common& c, const Rates& rates, float theta, float g, float m, float v) {
     Element e;
     g = __fmul_rn(g, c.coefficient);
     e.m = __fadd_rn(__fmul_rn(m, h.beta1), __fmul_rn(g, h.rest1));
-    e.v = __fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2));
-    e.root = __fsqrt_rn(e.v);
-    // 2 ulp of the step are far below the rounding of theta
-    e.theta = theta * rates.keep - __fdividef(e.m * rates.speed, e.root * c.spread + h.eps);
+    e.root = __fsqrt_rn(__fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2)));
+    const float down = e.root == 0.0f ? -rates.eps : __fmaf_rn(-e.root, rates.spread, -rates.eps);
+    e.theta = __fmaf_rn(e.m, rcp_approx(down), __fmul_rn(theta, rates.keep));
     return e;
 }
 
@@ -141,11 +147,6 @@ __device__ __forceinline__ Element element_at(const Setting& set, const Rates& r
 // not know it.
 __device__ __forceinline__ f32x2 product(f32x2 a, f32x2 b, f32x2 minus_zero) { return fma2(a, b, minus_zero); }
 
-__device__ __forceinline__ float rcp_approx(float x) {
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 // theta' from m' and -r', two elements.
 __device__ __forceinline__ f32x2 moved(const Hyper& h, const Common& c, const Rates& rates, f32x2 theta, f32x2 m, f32x2 minus_r) {
     float d0, d1;
@@ -485,7 +486,7 @@ __device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rate
 #pragma unroll 1
     for (int base = i; base < min(i + 256, p.count); base += 32) {
         const int e = base + lane, block = base / QN_ADAM_BLOCK;
-        Element x = {0.0f, 0.0f, 0.0f, 0.0f};
+        Element x = {0.0f, 0.0f, 0.0f};
         if (e < p.count) {
             const float root = root_value(p.v[e], p.v_scale[block]);
             x = stepped(set->h, set->c, rates, p.theta(e), Storage<G>::load1(p.grad + e), m_value(p.m[e], p.m_scale[block]), __fmul_rn(root, root));

@@ -133,7 +133,10 @@ class Case:
                 step_m = m1.abs() / 8 + 2.0 ** (ref.each(ms, n).double() - 127 - 9)
                 step_r = v1.sqrt() / 16 + 2.0 ** (ref.each(vs, n).double() - 127 - 10)
                 assert bool(((got_m - m1).abs() <= step_m * 1.001 + m_off).all())
-                assert bool(((got_r - v1.sqrt()).abs() <= step_r * 1.001 + 10 * ref.ULP * v1.sqrt()).all())
+                # the root lies between those of v' - v_off and v' + v_off; that is 5 ulp of it for ordinary numbers, and far more below
+                # 2^-126, where v' has steps of 2^-149: 3e-5 of v' = 5e-41
+                spread = (v1 + v_off).sqrt() - (v1 - v_off).clamp(min=0.0).sqrt()
+                assert bool(((got_r - v1.sqrt()).abs() <= step_r * 1.001 + spread + 2 * ref.ULP * v1.sqrt()).all())
             else:
                 assert bool(((self.m[i].double() - m1).abs() <= m_off).all())
                 assert bool(((self.v[i].double() - v1).abs() <= v_off).all())
@@ -255,19 +258,78 @@ def test_gradients_that_are_not_finite(qn, bits, bad):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
-def test_extreme_gradients(qn, bits):
-    """The least and the largest fp32 numbers beside ordinary ones, at the ends of the scales' range."""
-    n = 32 * 12
-    case = Case(qn, [n], F32, F32, False, bits)
+@pytest.mark.parametrize("repeats,each,offset", [(1, 32, 0), (16, 32, 0), (16, 32, 1), (60, 8, 0), (60, 8, 3), (25, 256, 0)])
+def test_extreme_gradients(qn, bits, repeats, each, offset):
+    """The least and the largest fp32 numbers beside ordinary ones, at the ends of the scales' range: in blocks of their own,
+    side by side in a block, and in blocks of zeros, in pieces that end and in whole ones."""
     values = [0.0, 1e-45, 1e-38, 1.2e-38, 1e-20, 1e-6, 1.0, 1e6, 1e15, 1e19, -1e19, 3e18]
-    g = torch.tensor(values, device="cuda").repeat_interleave(32)
-    g[::7] = 1e-3
+    n = each * len(values) * repeats
+    case = Case(qn, [n], F32, F32, False, bits, offset)
+    g = torch.tensor(values, device="cuda").repeat_interleave(each).repeat(repeats)
+    if each != 256:
+        g[::7] = 1e-3
     case.grad[0].copy_(g)
     for part in (case.m, case.v, case.m_scale, case.v_scale):
         if part is not None:
             part[0].zero_()
     for _ in range(2):
         case.check_step(beta1=0.5, beta2=0.5)
+
+
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("param,grad,master", TYPES)
+def test_numbers_that_are_not_finite_stay_in_their_places(qn, param, grad, master, offset):
+    """Infinite and NaN gradients, and parameters that are NaN already, in whole pieces and at ends: every other element is what it is
+    without them, but that codes of a block follow its scale."""
+    n = 9001
+    bad = [0, 100, 2047, 2048, 4100, 8191, 8999]
+    runs = []
+    for spoil in (False, True):
+        case = Case(qn, [n], param, grad, master, 8, offset)
+        if spoil:
+            case.grad[0][bad[:3]] = math.inf
+            case.grad[0][bad[3:5]] = math.nan
+            (case.master or case.theta)[0][bad[5:]] = math.nan
+        qn.qn_adam_step(case.plan, case.step, stochastic=True, seed=8)
+        case.guards_whole()
+        runs.append(case)
+    hit = torch.zeros(n, dtype=torch.bool, device="cuda")
+    hit[bad] = True
+    theta, want = runs[1].theta[0], runs[0].theta[0]
+    assert bool(torch.isnan(theta[hit]).all()) and torch.equal(theta[~hit], want[~hit])
+    m = ref.decode(runs[1].m[0], runs[1].m_scale[0], 3)
+    assert torch.isnan(m).nonzero()[:, 0].tolist() == bad[:5]
+    block = torch.zeros((n + 31) // 32, dtype=torch.bool, device="cuda")
+    block[torch.tensor(bad[:5], device="cuda") // 32] = True
+    elsewhere = ~block.repeat_interleave(32)[:n]
+    assert torch.equal(runs[1].m[0][elsewhere], runs[0].m[0][elsewhere]) and torch.equal(runs[1].v[0][elsewhere], runs[0].v[0][elsewhere])
+
+
+@pytest.mark.parametrize("bits,offset", [(32, 0), (8, 0), (8, 1)])
+def test_steps_in_a_row_are_those_one_by_one(qn, bits, offset):
+    """Launches whose set-up overlaps the end of the last one read what that has written."""
+    runs = []
+    for wait in (True, False):
+        case = Case(qn, [1_500_001, 33, 700_000], BF16, BF16, False, bits, offset)
+        sumsq = torch.zeros(1, dtype=torch.float64, device="cuda")
+        for _ in range(40):
+            qn.qn_adam_norm(case.plan, sumsq)
+            if wait:
+                torch.cuda.synchronize()
+            qn.qn_adam_step(case.plan, case.step, sumsq=sumsq, max_norm=1.0, stochastic=True, seed=4)
+            if wait:
+                torch.cuda.synchronize()
+        runs.append(case.everything())
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
+
+
+def test_many_small_tensors(qn):
+    sizes = [1 + (37 * i) % 90 for i in range(1500)]
+    for bits in (32, 8):
+        case = Case(qn, sizes, F32, F32, False, bits, offset=1, gap=0)
+        qn.qn_adam_grads(case.plan, [g.clone() for g in case.grad])
+        qn.qn_adam_grads(case.plan, case.grad)
+        case.check_step(max_norm=0.1)
 
 
 def test_tensors_without_gradients_and_empty_ones(qn):

@@ -316,6 +316,17 @@ def test_preference_masks_and_extremes(qn):
     check_preference(qn, l, big[1], None, None, None, beta=1.0)
 
 
+def test_preference_masks_in_long_sequences(qn):
+    """Tokens that both sides mask, and what does not count, past the tiles whose weights are kept."""
+    lengths = [400_000, 30, 300_001, 290_000]
+    l, offsets, reference, weight, pair_weight = preference_inputs(lengths, BF16, 5, lead=3, behind=2)
+    l[::1001] = -INF
+    reference[::1001] = -INF
+    l[500::999], weight[500::999] = math.nan, 0.0
+    for normalise in (False, True):
+        check_preference(qn, l, offsets, reference, weight, pair_weight, beta=0.001, normalise=normalise)
+
+
 def test_preference_offsets_that_are_wrong(qn):
     """Every way to leave [0, tokens] or to go backwards, with a good pair beside each; nothing outside is touched."""
     good = [(0, 4), (4, 9)]
