@@ -123,8 +123,11 @@ __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all,
                     load8(m_at + a, m_raw);
                     load8(v_at + a, v_raw);
                     if constexpr (sizeof(S) == 1) {
-                        m_values(m_raw, r.m_scale[a / QN_ADAM_BLOCK], m2);
-                        root_values(v_raw, r.v_scale[a / QN_ADAM_BLOCK], r2);
+                        m_values(m_raw, m2);
+                        root_values(v_raw, r2);
+                        const f32x2 m_unit = both(power_of(r.m_scale[a / QN_ADAM_BLOCK])), r_unit = both(root_unit(r.v_scale[a / QN_ADAM_BLOCK]));
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) m2[q] = mul2(m2[q], m_unit), r2[q] = mul2(r2[q], r_unit);
                     } else {
 #pragma unroll
                         for (int q = 0; q < 4; ++q) m2[q] = two_of(m_raw, q), r2[q] = two_of(v_raw, q);

@@ -171,27 +171,27 @@ __device__ __forceinline__ f32x2 two_of(const uint32_t (&x)[4], int q) {
 
 __device__ __forceinline__ f32x2 both(float x) { return pack2(x, x); }
 
-// What two codes of m (in the lower bytes), or of a root (in bytes 0 and 2), stand for.
-__device__ __forceinline__ f32x2 m_values(uint32_t codes, f32x2 unit) {
+// What two codes of m (in the lower bytes), or of a root (in bytes 0 and 2), stand for, but for the scale; a root's 2^8 too small: a
+// half has the same kind of fraction with five bits of exponent, so that a code moved up by 6 is one.
+__device__ __forceinline__ f32x2 m_values(uint32_t codes) {
     uint32_t halves;
     asm("{\n .reg .b16 lo;\n cvt.u16.u32 lo, %1;\n cvt.rn.f16x2.e4m3x2 %0, lo;\n}" : "=r"(halves) : "r"(codes));
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&halves));
-    return mul2(pack2(x.x, x.y), unit);
+    return pack2(x.x, x.y);
 }
-// A half has the same kind of fraction with five bits of exponent: a code moved up by 6 is one, 2^8 too small.
-__device__ __forceinline__ f32x2 root_values(uint32_t codes, f32x2 unit) {
+__device__ __forceinline__ f32x2 root_values(uint32_t codes) {
     const uint32_t halves = codes << 6;
     const float2 x = __half22float2(*reinterpret_cast<const __half2*>(&halves));
-    return mul2(pack2(x.x, x.y), unit);
+    return pack2(x.x, x.y);
 }
 __device__ __forceinline__ float root_unit(uint32_t scale) { return scale ? power_of(min(scale + 8u, 254u)) : 0.0f; }
-__device__ __forceinline__ void m_values(const uint32_t (&codes)[2], uint32_t scale, f32x2 (&m)[4]) {
+__device__ __forceinline__ void m_values(const uint32_t (&codes)[2], f32x2 (&m)[4]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) m[q] = m_values(codes[q / 2] >> (16 * (q & 1)), both(power_of(scale)));
+    for (int q = 0; q < 4; ++q) m[q] = m_values(codes[q / 2] >> (16 * (q & 1)));
 }
-__device__ __forceinline__ void root_values(const uint32_t (&codes)[2], uint32_t scale, f32x2 (&r)[4]) {
+__device__ __forceinline__ void root_values(const uint32_t (&codes)[2], f32x2 (&r)[4]) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) r[q] = root_values(__byte_perm(codes[q / 2], 0, q & 1 ? 0x4342 : 0x4140), both(root_unit(scale)));
+    for (int q = 0; q < 4; ++q) r[q] = root_values(__byte_perm(codes[q / 2], 0, q & 1 ? 0x4342 : 0x4140));
 }
 
 }  // namespace

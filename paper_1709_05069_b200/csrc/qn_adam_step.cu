@@ -195,18 +195,21 @@ __device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
     return fma2(fma2(s, s, minus_v), mul2(y, both(0.5f)), s);
 }
 
-// States in 8 bits: m and r before the step become m' and -r'.  top_m: the largest m'; top_v: the largest v'.  False where this way is
-// not the right one: a second moment is 0, or very small, or something is very large or not a number.
-__device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (&m)[4], f32x2 (&r)[4], const f32x2 (&grad)[4],
-                                        float& top_m, float& top_v) {
+// States in 8 bits: the codes' values become m' and -r'.  They may come without their scales: then keep_m is beta1 times the scale's
+// power of two, and keep_v -beta2 times that of r, squared: products with powers of two are exact, so that they may come before the rounding or after it.  (Where
+// keep_v underflows, what it stands for is below 2^-126, and below half a step of any v' that stays here; where keep_m
+// does, in blocks below 2^-112, the caller does not come here.)  top_m: the largest m'; top_v: the largest v'.  False where this way is not
+// the right one: a second moment is 0, or very small, or something is very large or not a number.
+__device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (&m)[4], f32x2 (&r)[4], const f32x2 (&keep_m)[4],
+                                        const f32x2 (&keep_v)[4], const f32x2 (&grad)[4], float& top_m, float& top_v) {
     const f32x2 none = both(h.minus_zero);
     float low_v = INFINITY;
     top_m = top_v = 0.0f;
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const f32x2 g = mul2(grad[q], both(c.coefficient));
-        m[q] = add2(product(m[q], both(h.beta1), none), product(g, both(h.rest1), none));
-        const f32x2 minus_v = add2(product(mul2(r[q], r[q]), both(-h.beta2), none), product(mul2(g, g), both(-h.rest2), none));
+        m[q] = add2(product(m[q], keep_m[q], none), product(g, both(h.rest1), none));
+        const f32x2 minus_v = add2(product(mul2(r[q], r[q]), keep_v[q], none), product(mul2(g, g), both(-h.rest2), none));
         float m0, m1, v0, v1;
         unpack2(m[q], m0, m1);
         unpack2(minus_v, v0, v1);
@@ -217,6 +220,13 @@ __device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (
     }
     return low_v >= kLow && top_v <= kHigh && top_m <= kHigh;
 }
+__device__ __forceinline__ float keep_of_m(const Hyper& h, uint32_t scale) { return h.beta1 * power_of(scale); }
+__device__ __forceinline__ float keep_of_v(const Hyper& h, uint32_t scale) {
+    const float unit = root_unit(scale);
+    return unit * unit * -h.beta2;
+}
+// keep_of_m is not exact: a small scale, but not that of a block of zeros.
+__device__ __forceinline__ bool tiny_scale(uint32_t scale) { return scale - 1u < 8u; }
 
 // 2^-e / 2^120 (see magnitude_bits; below kHigh this is a number, and one product does for the two there) from the exponent
 // field of a block's largest finite magnitude, which is not 0 (m: may be 0).
@@ -316,8 +326,11 @@ template <typename P, typename G, bool kMaster>
 struct Slots {
     static constexpr int kSlots = kSlotsOf<P, G, kMaster>;
     static constexpr int kTheta = kMaster || sizeof(P) == 4 ? 2 : 1, kGrad = sizeof(G) == 4 ? 2 : 1;  // units of 16 bytes
-    uint4 theta[kSlots][kTheta][kThreads], grad[kSlots][kGrad][kThreads];
-    uint2 m[kSlots][kThreads], v[kSlots][kThreads];
+    struct Slot {
+        uint4 theta[kTheta][kThreads], grad[kGrad][kThreads];
+        uint2 m[kThreads], v[kThreads];
+    };
+    Slot slot[kSlots];
 
     __device__ static __forceinline__ void copy(uint4* to, const void* from) {
         asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
@@ -326,34 +339,36 @@ struct Slots {
         asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(smem_u32(to)), "l"(from) : "memory");
     }
     // Each call is a group, also if there is nothing to copy.
-    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int slot, int i, bool any) {
+    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int s, int i, bool any) {
         const int tid = threadIdx.x;
+        Slot& to = slot[s];
         if (any) {
             const char* at = kMaster ? reinterpret_cast<const char*>(p.master + i) : reinterpret_cast<const char*>(p.param + i);
 #pragma unroll
-            for (int k = 0; k < kTheta; ++k) copy(&theta[slot][k][tid], at + 16 * k);
+            for (int k = 0; k < kTheta; ++k) copy(&to.theta[k][tid], at + 16 * k);
 #pragma unroll
-            for (int k = 0; k < kGrad; ++k) copy(&grad[slot][k][tid], reinterpret_cast<const char*>(p.grad + i) + 16 * k);
-            copy(&m[slot][tid], p.m + i);
-            copy(&v[slot][tid], p.v + i);
+            for (int k = 0; k < kGrad; ++k) copy(&to.grad[k][tid], reinterpret_cast<const char*>(p.grad + i) + 16 * k);
+            copy(&to.m[tid], p.m + i);
+            copy(&to.v[tid], p.v + i);
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
     // All groups but the last kSlots - 2 have arrived.
     __device__ static __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
-    __device__ __forceinline__ void take(int slot, Raw<P, G, kMaster>& raw) const {
+    __device__ __forceinline__ void take(int s, Raw<P, G, kMaster>& raw) const {
         const int tid = threadIdx.x;
+        const Slot& from = slot[s];
 #pragma unroll
         for (int k = 0; k < kTheta; ++k) {
-            const uint4 x = theta[slot][k][tid];
+            const uint4 x = from.theta[k][tid];
             raw.theta[4 * k] = x.x, raw.theta[4 * k + 1] = x.y, raw.theta[4 * k + 2] = x.z, raw.theta[4 * k + 3] = x.w;
         }
 #pragma unroll
         for (int k = 0; k < kGrad; ++k) {
-            const uint4 x = grad[slot][k][tid];
+            const uint4 x = from.grad[k][tid];
             raw.grad[4 * k] = x.x, raw.grad[4 * k + 1] = x.y, raw.grad[4 * k + 2] = x.z, raw.grad[4 * k + 3] = x.w;
         }
-        const uint2 a = m[slot][tid], b = v[slot][tid];
+        const uint2 a = from.m[tid], b = from.v[tid];
         raw.m[0] = a.x, raw.m[1] = a.y, raw.v[0] = b.x, raw.v[1] = b.y;
     }
 };
@@ -393,11 +408,13 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
                                            const Part<P, G, kMaster, uint8_t>& p, int i, const Raw<P, G, kMaster>& raw) {
     f32x2 m[4], r[4], g[4];
     float top_m, top_v;
-    m_values(raw.m, raw.m_scale, m);
-    root_values(raw.v, raw.v_scale, r);
+    const f32x2 keep_m = both(keep_of_m(h, raw.m_scale)), keep_v = both(keep_of_v(h, raw.v_scale));
+    const f32x2 keeps_m[4] = {keep_m, keep_m, keep_m, keep_m}, keeps_v[4] = {keep_v, keep_v, keep_v, keep_v};
+    m_values(raw.m, m);
+    root_values(raw.v, r);
 #pragma unroll
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
-    bool odd = !moments(h, c, m, r, g, top_m, top_v);
+    bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(raw.m_scale);
     uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
     if (odd) {
         const uint2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
@@ -582,6 +599,8 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
     // elements that are not there are ordinary ones that count for nothing and are not written
     const auto here = [&](int j) { return kWhole || at + 32 * j < p.count; };
     const auto last_block = [&](int b) { return kWhole ? b : min(b, (p.count - 1) / QN_ADAM_BLOCK); };
+    const f32x2 beta1 = both(h.beta1), minus_beta2 = both(-h.beta2);
+    const f32x2 keep_m[4] = {beta1, beta1, beta1, beta1}, keep_v[4] = {minus_beta2, minus_beta2, minus_beta2, minus_beta2};
     f32x2 m[4], r[4], g[4];
     float t[8];
     uint32_t codes[8][2];
@@ -595,11 +614,11 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
     for (int q = 0; q < 4; ++q) {
         const int e = offset + 64 * q + lane, b0 = last_block(offset / QN_ADAM_BLOCK + 2 * q), b1 = last_block(offset / QN_ADAM_BLOCK + 2 * q + 1);
         g[q] = pack2(here(2 * q) ? from.grad(e) : 1.0f, here(2 * q + 1) ? from.grad(e + 32) : 1.0f);
-        m[q] = m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u, pack2(power_of(from.m_scale(b0)), power_of(from.m_scale(b1))));
-        r[q] = root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u, pack2(root_unit(from.v_scale(b0)), root_unit(from.v_scale(b1))));
+        m[q] = mul2(m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u), pack2(power_of(from.m_scale(b0)), power_of(from.m_scale(b1))));
+        r[q] = mul2(root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u), pack2(root_unit(from.v_scale(b0)), root_unit(from.v_scale(b1))));
     }
     float top_m, top_v;
-    const bool odd = !moments(h, c, m, r, g, top_m, top_v);
+    const bool odd = !moments(h, c, m, r, keep_m, keep_v, g, top_m, top_v);
     if (__any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, i);
     const uint32_t octet = octet_word(c.key, p.octet + i / kOctet + lane);  // of the warp's lane-th eight
     const uint32_t place = (lane % 8) * kGolden, places[2] = {place, place};
