@@ -760,22 +760,23 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
                         const int at = i - k * kPiece;
                         slots.fetch(p, to, at, base >= k * kPiece);
                         const int block = max(at, 0) / QN_ADAM_BLOCK;
-                        m_scale[k] = p.m_scale[block], v_scale[k] = p.v_scale[block];
+                        m_scale[to] = p.m_scale[block], v_scale[to] = p.v_scale[block];
                     };
 #pragma unroll
                     for (int k = 0; k < kSlots - 1; ++k) fetch(k, k);
 #pragma unroll 1
-                    for (; base >= 0; base -= kPiece, i -= kPiece) {
-                        Raw<P, G, kMaster> raw;
-                        slots.wait();
-                        slots.take(slot, raw);
-                        raw.m_scale = m_scale[0], raw.v_scale = v_scale[0];
+                    while (base >= 0) {
 #pragma unroll
-                        for (int k = 0; k + 2 < kSlots; ++k) m_scale[k] = m_scale[k + 1], v_scale[k] = v_scale[k + 1];
-                        fetch(kSlots - 1, slot == 0 ? kSlots - 1 : slot - 1);
-                        m_scale[kSlots - 2] = m_scale[kSlots - 1], v_scale[kSlots - 2] = v_scale[kSlots - 1];
-                        slot = slot == kSlots - 1 ? 0 : slot + 1;
-                        step_octet<kChance>(&set, h, c, rates, p, i, raw);
+                        for (int s = 0; s < kSlots; ++s) {
+                            if (base < 0) break;
+                            Raw<P, G, kMaster> raw;
+                            slots.wait();
+                            slots.take(s, raw);
+                            raw.m_scale = m_scale[s], raw.v_scale = v_scale[s];
+                            fetch(kSlots - 1, s == 0 ? kSlots - 1 : s - 1);
+                            step_octet<kChance>(&set, h, c, rates, p, i, raw);
+                            base -= kPiece, i -= kPiece;
+                        }
                     }
                 }
                 asm volatile("cp.async.wait_group 0;" ::: "memory");
