@@ -34,35 +34,27 @@ __global__ void __launch_bounds__(kThreads) adam_norm_kernel(const Tensors all, 
             piece = to;
             if (to == from || !grad) continue;
             const int64_t begin = (from - first) * kPiece, end = min(all.records[tensor].numel, (to - first) * kPiece);
-            int64_t i = begin + threadIdx.x;
-            if (reinterpret_cast<uintptr_t>(grad) % (kOctet * sizeof(G)) == 0) {  // eight elements a thread
-#pragma unroll 4
-                for (int64_t at = begin + threadIdx.x * kOctet; at + kOctet <= end; at += kPiece) {
-                    uint32_t raw[sizeof(G) == 4 ? 8 : 4];
-                    load8(grad + at, raw);
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        float a, b;
-                        unpack2(two_of(raw, q), a, b);
-                        sum += static_cast<double>(a) * a;
-                        sum += static_cast<double>(b) * b;
-                    }
-                }
-                i = end - (end - begin) % kOctet + threadIdx.x;
-            }
-            // element by element, eight loads under way together
-#pragma unroll 1
-            for (; i + 7 * kThreads < end; i += 8 * kThreads) {
-                float g[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) g[e] = Storage<G>::load1(grad + i + e * kThreads);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) sum += static_cast<double>(g[e]) * g[e];
-            }
-#pragma unroll 1
-            for (; i < end; i += kThreads) {
+            // eight elements a thread from the first vector on; a few by themselves before it and after the last
+            constexpr int kBytes = kOctet * sizeof(G);
+            const int64_t head = (kBytes - reinterpret_cast<uintptr_t>(grad + begin) % kBytes) % kBytes / sizeof(G), full = min(begin + head, end);
+            const int64_t whole = (end - full) / kOctet * kOctet;
+            const auto add_one = [&](int64_t i) {
                 const double g = Storage<G>::load1(grad + i);
                 sum += g * g;
+            };
+            if (begin + threadIdx.x < full) add_one(begin + threadIdx.x);
+            if (full + whole + threadIdx.x < end) add_one(full + whole + threadIdx.x);
+#pragma unroll 4
+            for (int64_t at = full + threadIdx.x * kOctet; at < full + whole; at += kPiece) {
+                uint32_t raw[sizeof(G) == 4 ? 8 : 4];
+                load8(grad + at, raw);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    float a, b;
+                    unpack2(two_of(raw, q), a, b);
+                    sum += static_cast<double>(a) * a;
+                    sum += static_cast<double>(b) * b;
+                }
             }
         }
     }

@@ -50,7 +50,8 @@ struct Tensors {
 // or take one.  Within a run addresses only move on, but for the ends of tensors; the shorter the runs, the nearer to one another
 // in memory the CTAs are.  Measured with runs of whole shares, and of at least 32, 8 and 4 pieces (at most 8, 32 and 64 turns),
 // us for 2^28 parameters: the step with 32-bit states and master copies 1331, 1281, 1237, 1228; with 8-bit states, whose copies ahead end
-// with a run, 573, 571, 615, 673; the norm 88, 88, 94, 107; the states' values 315, 295, 286, 294.
+// with a run, 573, 571, 615, 673 (for 2^27 fp32 parameters with runs of whole shares, 32 and 16 pieces 549, 532, 519); the norm 88, 88,
+// 94, 107; the states' values 315, 295, 286, 294.
 struct Turns {
     int64_t pieces, each;
     int32_t count;

@@ -677,7 +677,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
     extern __shared__ __align__(16) unsigned char shared[];
     __shared__ Setting set;
     __shared__ int found;
-    const Turns turns(all.pieces, sizeof(S) == 4 ? 8 : 32, sizeof(S) == 4 ? 32 : 8);
+    // the fewer copies ahead an element leaves room for, the shorter the runs (see Turns)
+    constexpr int kTurns = sizeof(S) == 4 ? 32 : kMaster || sizeof(P) == 4 ? 16 : 8;
+    const Turns turns(all.pieces, 256 / kTurns, kTurns);
     int64_t lo = turns.lo(turns.count - 1), hi = turns.hi(turns.count - 1);
     start_after_last();
     let_next_start();
