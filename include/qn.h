@@ -531,7 +531,8 @@ QN_API qn_status qn_preference(int64_t pairs, int64_t tokens, const float* logpr
  * stream capture, for tensors that stay where they are.  Gradients that move are named again with qn_adam_grads.  Calls
  * on one plan share its workspace and must be ordered, as those on a qn_handle; so must replays of graphs that
  * captured them.  A call is one kernel launch that waits for nothing (qn_adam_grads: one for each 256 tensors), and can
- * be captured: step, lr_device and sumsq are read when the kernel runs.  The same inputs give the same bits.
+ * be captured: step, lr_device and sumsq are read when the kernel runs.  The same inputs give the same bits (of the norm: on
+ * the same kind of GPU, at the same addresses modulo 32).
  */
 #define QN_ADAM_BLOCK 32   /* elements that share a scale, where states are held in 8 bits */
 #define QN_STATE_F32 0     /* m and v in fp32 */
@@ -570,8 +571,8 @@ typedef struct {
 } qn_adam_tensor;
 
 /*
- * A plan for `count` tensors (HOST array), all on one device: no two arrays that a step writes may overlap, and no gradient may
- * overlap one of them.  Waits for the device.
+ * A plan for `count` tensors (HOST array; at most 2^20 of at most 2^40 elements each, 2^42 in all), all on one device: no two arrays
+ * that a step writes may overlap, and no gradient may overlap one of them.  Waits for the device.
  */
 QN_API qn_status qn_adam_create(int32_t count, const qn_adam_tensor* tensors, qn_dtype param, qn_dtype grad, int32_t state,
                                 qn_adam_handle* out);

@@ -6,7 +6,9 @@
 // has the form e_i (c0 + c1 d_i) and one more term at the token.  What a separate loss would read and write between the log
 // probabilities and their backward pass, and the second pass over the row, fall away: a row is read once and its
 // gradient written once.  As in qn_logprobs_backward ln p_i + H = ln 2 (d_i - E / S).
-// What bounds it and what it measured is in qn_vocab_grad.cuh.
+// What bounds it is in qn_vocab_grad.cuh.  Measured (the bytes alone at a copy's rate): 4096 x 131072 bf16 400 us (328); 2047 x 100003
+// bf16 with entropy, every eighth row padding 172 us (117); 61 x 20011 fp32 5.4 us of kernel, 11 us a call.  The log
+// probabilities, a separate loss and their backward pass would read the logits twice.
 #include <nvtx3/nvToolsExt.h>
 
 #include "qn_vocab_grad.cuh"
