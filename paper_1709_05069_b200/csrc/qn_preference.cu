@@ -7,11 +7,14 @@
 // its own tokens, whose weights it has kept.  So each token is read once and written once, 16 bytes, and there is one launch.
 // Sums and the pair's numbers are in 64 bits: h is the small difference of sums over thousands of tokens.
 //
-// Bound by latency: offsets, a pair's tiles one after the other, the exchange, exp and a division in 64 bits, the writes.  Measured, us of
-// kernel in a graph: 4 pairs of 64 tokens 3.8; 1024 pairs, 2.4 million tokens 11.7 (the bytes alone 5.8); 12 pairs, 1.8
-// million tokens 13.3 (4.7), with CTAs on all SMs only by clusters of 16.  Steps on the way: tokens of both sequences in
-// one index, a select for each sum, 39 and 21; conditions around loads, which then wait for one another, 18 and 21; tiles without
-// conditions 14 and 15; weights of four tiles in shared memory instead of two in registers 11.7 and 13.3.
+// Bound by latency: offsets, a pair's tiles one after the other, the exchange, exp and a division in 64 bits, the writes.
+// Measured, us of kernel in a graph: 4 pairs of 64 tokens at most 3.8; 1024 pairs, 2.4 million tokens 11.7 (the bytes alone
+// 5.8); 12 pairs, 1.8 million tokens 13.3 (4.7), with CTAs on all SMs only by clusters of 16.  Steps on the way, the last two
+// of these: tokens of both sequences in one index, a select for each sum, 39 and 21; conditions around loads, which then wait for
+// one another, 18 and 21; tiles without conditions 14 and 15; weights of four tiles in shared memory instead of two in
+// registers 11.7 and 13.3.  Thousands of short pairs are bound by the numbers of each pair, which one thread works out while the
+// others of its block wait: a warp a pair, and the eight pairs of a block by eight threads side by side, 4096 pairs of 72
+// tokens 14.2 -> 9.4 (4096 of 580 tokens 14.2 as a warp each or as before; 12 of 80 tokens 3.8 -> 4.9, so that these stay).
 #include <nvtx3/nvToolsExt.h>
 
 #include "qn_vocab.cuh"
@@ -46,14 +49,18 @@ struct Sequence {
 template <int NT, typename R, bool kRef>
 struct Tile {
     float l[kEach], ref[kEach], weight[kEach];
-    // Loads without conditions, so that all are under way together: in a part of a tile, of its last token for those that are not there.
+    // Loads without conditions, so that all are under way together: in a part of a tile, of its last token for those that are not
+    // there.  Where a warp has a pair, most tiles are short ones: what no thread has a token for is left out.
+    static __device__ __forceinline__ bool some(int k, int count) { return NT > 32 || k * NT < count; }
     template <bool kWhole>
     __device__ __forceinline__ void load(const Sequence<R>& s, int64_t at, int count, bool all) {
         const float *l_at = s.l + at, *weight_at = s.weight + at;
         const R* ref_at = s.ref + at;
-        const int tid = threadIdx.x;
+        const int tid = NT > 32 ? threadIdx.x : threadIdx.x % NT;
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
+            l[k] = ref[k] = weight[k] = 0.0f;
+            if (!kWhole && !some(k, count)) continue;
             const int i = kWhole ? k * NT + tid : min(k * NT + tid, count - 1);
             l[k] = all ? __ldg(l_at + i) : 0.0f;
             ref[k] = kRef && all ? Storage<R>::load1(ref_at + i) : 0.0f;
@@ -70,7 +77,7 @@ struct Tile {
         else load<false>(s, at, count, all);
     }
     // True if a token counts for nothing although its weight is not 0.
-    __device__ __forceinline__ bool add(double& ratios, double& weights, bool normalise) {
+    __device__ __forceinline__ bool add(double& ratios, double& weights, int count, bool normalise) {
         float most = 0.0f;  // of the magnitudes; NaN if there is one
 #pragma unroll
         for (int k = 0; k < kEach; ++k) asm("max.NaN.abs.f32 %0, %0, %1, %2;" : "+f"(most) : "f"(l[k]), "f"(ref[k]));
@@ -78,6 +85,7 @@ struct Tile {
         if (!(most < INFINITY)) dead = clean();
 #pragma unroll
         for (int k = 0; k < kEach; ++k) {
+            if (!some(k, count)) break;
             const double w = weight[k];  // products of numbers in 32 bits are exact in 64
             ratios += w * static_cast<double>(l[k]);
             if (kRef) ratios -= w * static_cast<double>(ref[k]);
@@ -98,10 +106,11 @@ struct Tile {
         return dead;
     }
     __device__ static __forceinline__ void write(const Sequence<R>& s, int64_t at, int count, const float (&w)[kEach], float coefficient) {
-        float* d = s.d + at + threadIdx.x;
+        const int tid = NT > 32 ? threadIdx.x : threadIdx.x % NT;
+        float* d = s.d + at + tid;
 #pragma unroll
         for (int k = 0; k < kEach; ++k)
-            if (k * NT + static_cast<int>(threadIdx.x) < count) d[k * NT] = w[k] == 0.0f ? 0.0f : w[k] * coefficient;
+            if (k * NT + tid < count) d[k * NT] = w[k] == 0.0f ? 0.0f : w[k] * coefficient;
     }
 };
 
@@ -126,19 +135,25 @@ __device__ __forceinline__ double loss_at(const PreferenceParams& p, double h, d
     return loss;
 }
 
+// Pairs of a CTA: short ones are a warp each.
+template <int NT>
+constexpr int kPairs = NT == 32 ? 8 : 1;
+
 template <int NT, typename R, bool kRef>
-__global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const PreferenceParams p) {
+__global__ void __launch_bounds__(NT * kPairs<NT>, 1024 / (NT * kPairs<NT>)) preference_kernel(const PreferenceParams p) {
     __shared__ double warp_sums[NT / 32][4];
     __shared__ uint64_t inbox[kMaxCluster][4];
     __shared__ float coefficient[2];
-    const uint32_t ctas = cluster_size(), rank = cluster_rank();
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t ctas = NT == 32 ? 1 : cluster_size(), rank = NT == 32 ? 0 : cluster_rank();
+    const int tid = NT > 32 ? threadIdx.x : threadIdx.x % NT, warp = tid >> 5, lane = tid & 31;
     start_after_last();
     let_next_start();
     if (ctas > 1) cluster_arrive();  // waited for before the first store into another CTA
-    const int64_t pair = blockIdx.x / ctas;
+    const int64_t mine = NT == 32 ? blockIdx.x * static_cast<int64_t>(kPairs<NT>) + threadIdx.x / NT : blockIdx.x / ctas;
+    const bool there = NT > 32 || mine < p.pairs;
+    const int64_t pair = there ? mine : p.pairs - 1;
     const int64_t chosen = p.split ? pair : 2 * pair, rejected = p.split ? p.pairs + pair : 2 * pair + 1;
-    const float unit = p.pair_weight ? p.pair_weight[pair] : 1.0f;
+    const float unit = !there ? 0.0f : p.pair_weight ? p.pair_weight[pair] : 1.0f;
     Sequence<R> sequence[2];
     bool wrong = false;
 #pragma unroll
@@ -169,30 +184,33 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
         return Place{s, at, static_cast<int>(min((s ? sequence[1].length : sequence[0].length) - at, static_cast<int64_t>(kTile)))};
     };
     if (unit == 0.0f) {  // padding
-        if (p.d_logprob)
+        if (p.d_logprob && there)
             each_tile([&](int64_t t, int) {
                 const Place x = place(t);
                 const float none[kEach] = {};
                 Tile<NT, R, kRef>::write(x.s ? sequence[1] : sequence[0], x.at, x.count, none, 0.0f);
             });
-        if (rank == 0 && tid == 0) {
+        if (rank == 0 && tid == 0 && there) {
             p.loss[pair] = 0.0f;
             if (p.reward) p.reward[chosen] = p.reward[rejected] = 0.0f;
         }
-        __syncwarp();
-        if (ctas > 1) cluster_wait();
-        return;
+        if (NT > 32) {
+            __syncwarp();
+            if (ctas > 1) cluster_wait();
+            return;
+        }
     }
     double sums[4] = {0.0, 0.0, 0.0, 0.0};  // weighted ratios of the chosen and of the rejected, weights of both
-    extern __shared__ float kept[];  // [tile][token of a thread][thread]: each thread its own
+    extern __shared__ float shared[];
+    float* kept = shared + (NT > 32 ? 0 : threadIdx.x / NT) * (kKept * kEach * NT);  // [tile][token of a thread][thread]: each thread its own
     bool dead = false;
     const auto add = [&](const Place& x, Tile<NT, R, kRef>& tile) {
         double ratios = 0.0, weights = 0.0;
-        dead = tile.add(ratios, weights, p.normalise) || dead;
+        dead = tile.add(ratios, weights, x.count, p.normalise) || dead;
         if (x.s) sums[1] += ratios, sums[3] += weights;
         else sums[0] += ratios, sums[2] += weights;
     };
-    each_tile([&](int64_t t, int turn) {
+    if (NT > 32 || unit != 0.0f) each_tile([&](int64_t t, int turn) {
         const Place x = place(t);
         Tile<NT, R, kRef> tile(x.s ? sequence[1] : sequence[0], x.at, x.count);
         add(x, tile);
@@ -201,61 +219,93 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
             for (int e = 0; e < kEach; ++e) kept[(turn * kEach + e) * NT + tid] = tile.weight[e];
     });
     const int count = p.normalise ? 4 : 2;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (q >= count) break;
-        const double x = warp_reduce<double, add_op>(sums[q]);
-        if (lane == 0) warp_sums[warp][q] = x;
-    }
-    __syncthreads();
-    if (warp == 0) {
-        double mine = 0.0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (q >= count) break;
-            const double x = warp_reduce<double, add_op>(lane < NT / 32 ? warp_sums[lane][q] : 0.0);
-            if (lane == q) mine = x;
-        }
-        __syncwarp();
-        if (ctas == 1) {
-            if (lane < 4) inbox[0][lane] = __double_as_longlong(mine);
-        } else {
-            cluster_wait();
-            if (lane < 4)
-                for (uint32_t c = 0; c < ctas; ++c) store_remote(&inbox[rank][lane], c, __double_as_longlong(mine));
-        }
-        __syncwarp();
-    }
-    if (ctas > 1) {
-        if (warp != 0) cluster_wait();
-        cluster_arrive();
-        cluster_wait();
-    }
     double h = 0.0, e = 0.0;
-    if (tid == 0) {
-        double total[4] = {0.0, 0.0, 0.0, 0.0};
-        for (uint32_t c = 0; c < ctas; ++c)
-            for (int q = 0; q < 4; ++q) total[q] += __longlong_as_double(inbox[c][q]);
+    float c0 = 0.0f, c1 = 0.0f;
+    const auto settle = [&](const double (&total)[4], float unit, bool wrong, int64_t chosen, int64_t rejected) {  // by one thread
         double each[2], reward[2];
+#pragma unroll
         for (int s = 0; s < 2; ++s) {
             each[s] = !p.normalise ? p.beta : total[2 + s] != 0.0 ? p.beta / total[2 + s] : 0.0;
             reward[s] = each[s] == 0.0 ? 0.0 : each[s] * total[s];
         }
         h = wrong ? NAN : reward[0] - reward[1] - p.margin;
         const double slope = unit * slope_at(p, h, e);
-        coefficient[0] = static_cast<float>(slope * each[0]);
-        coefficient[1] = static_cast<float>(-slope * each[1]);
+        c0 = static_cast<float>(slope * each[0]);
+        c1 = static_cast<float>(-slope * each[1]);
         if (rank == 0 && p.reward) {
             p.reward[chosen] = wrong ? NAN : static_cast<float>(reward[0]);
             p.reward[rejected] = wrong ? NAN : static_cast<float>(reward[1]);
         }
+    };
+    if constexpr (NT == 32) {
+        // the pairs' numbers side by side, by as many threads of the first warp
+        __shared__ double totals[kPairs<NT>][4];
+        __shared__ float units[kPairs<NT>], coefficients[kPairs<NT>][2];
+        __shared__ bool wrongs[kPairs<NT>];
+        const int group = threadIdx.x / NT;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const double x = q < count ? warp_reduce<double, add_op>(sums[q]) : 0.0;
+            if (lane == q) totals[group][q] = x;
+        }
+        if (lane == 0) units[group] = unit, wrongs[group] = wrong;
+        __syncthreads();
+        const int64_t theirs = blockIdx.x * static_cast<int64_t>(kPairs<NT>) + lane;
+        const bool one = group == 0 && lane < kPairs<NT> && units[lane % kPairs<NT>] != 0.0f;
+        if (one) {
+            const double total[4] = {totals[lane][0], totals[lane][1], totals[lane][2], totals[lane][3]};
+            settle(total, units[lane], wrongs[lane], p.split ? theirs : 2 * theirs, p.split ? p.pairs + theirs : 2 * theirs + 1);
+            coefficients[lane][0] = c0, coefficients[lane][1] = c1;
+        }
+        __syncthreads();
+        if (one) p.loss[theirs] = static_cast<float>(loss_at(p, h, e));
+        if (unit == 0.0f) return;
+        c0 = coefficients[group][0], c1 = coefficients[group][1];
+    } else {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (q >= count) break;
+            const double x = warp_reduce<double, add_op>(sums[q]);
+            if (lane == 0) warp_sums[warp][q] = x;
+        }
+        __syncthreads();
+        if (warp == 0) {
+            double mine = 0.0;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (q >= count) break;
+                const double x = warp_reduce<double, add_op>(lane < NT / 32 ? warp_sums[lane][q] : 0.0);
+                if (lane == q) mine = x;
+            }
+            __syncwarp();
+            if (ctas == 1) {
+                if (lane < 4) inbox[0][lane] = __double_as_longlong(mine);
+            } else {
+                cluster_wait();
+                if (lane < 4)
+                    for (uint32_t c = 0; c < ctas; ++c) store_remote(&inbox[rank][lane], c, __double_as_longlong(mine));
+            }
+            __syncwarp();
+        }
+        if (ctas > 1) {
+            if (warp != 0) cluster_wait();
+            cluster_arrive();
+            cluster_wait();
+        }
+        if (tid == 0) {
+            double total[4] = {0.0, 0.0, 0.0, 0.0};
+            for (uint32_t c = 0; c < ctas; ++c)
+                for (int q = 0; q < 4; ++q) total[q] += __longlong_as_double(inbox[c][q]);
+            settle(total, unit, wrong, chosen, rejected);
+            coefficient[0] = c0, coefficient[1] = c1;
+        }
+        __syncthreads();
+        c0 = coefficient[0], c1 = coefficient[1];
     }
-    __syncthreads();
     if (p.d_logprob) {
-        const float c0 = coefficient[0], c1 = coefficient[1];
         each_tile([&](int64_t t, int turn) {
             const Place x = place(t);
-                if (turn < kKept) {
+            if (turn < kKept) {
                 float weight[kEach];
 #pragma unroll
                 for (int e = 0; e < kEach; ++e) weight[e] = kept[(turn * kEach + e) * NT + tid];
@@ -267,11 +317,11 @@ __global__ void __launch_bounds__(NT, 1024 / NT) preference_kernel(const Prefere
             }
         });
     }
-    if (rank == 0 && tid == 0) p.loss[pair] = static_cast<float>(loss_at(p, h, e));
+    if (NT > 32 && rank == 0 && tid == 0) p.loss[pair] = static_cast<float>(loss_at(p, h, e));
 }
 
 template <int NT>
-constexpr int kShared = NT * kEach * kKept * 4;
+constexpr int kShared = NT * kPairs<NT> * kEach * kKept * 4;
 
 // How many clusters of 16 fit on the device at once (asked for once on each); such clusters need a permission.
 template <int NT, typename R, bool kRef>
@@ -298,7 +348,7 @@ cudaError_t launch_preference(const PreferenceParams& p, int ctas, cudaStream_t 
         const cudaError_t e = cudaFuncSetAttribute(preference_kernel<NT, R, kRef>, cudaFuncAttributeMaxDynamicSharedMemorySize, kShared<NT>);
         if (e != cudaSuccess) return e;
     }
-    const EarlyLaunch launch(p.pairs * ctas, NT, kShared<NT>, ctas, st);
+    const EarlyLaunch launch((p.pairs + kPairs<NT> - 1) / kPairs<NT> * ctas, NT * kPairs<NT>, kShared<NT>, ctas, st);
     return cudaLaunchKernelEx(&launch.cfg, preference_kernel<NT, R, kRef>, p);
 }
 
@@ -317,6 +367,8 @@ cudaError_t launch_preference(const PreferenceParams& p, cudaStream_t st) {
     int ctas = 1;
     while (ctas < 8 && p.pairs * ctas < qn_sm_count() && threads >= 128 * ctas) ctas *= 2;
     const int64_t each = threads / ctas;
+    // a warp a pair: short ones, of which there are more than there is room for blocks of 64 threads (8 an SM are their fair share)
+    if (mean < 32 * kEach && p.pairs > 8 * static_cast<int64_t>(qn_sm_count())) return launch_preference<32, R, kRef>(p, ctas, st);
     if (each < 96) return launch_preference<64, R, kRef>(p, ctas, st);
     if (each < 192) return launch_preference<128, R, kRef>(p, ctas, st);
     if (each < 384) return launch_preference<256, R, kRef>(p, ctas, st);

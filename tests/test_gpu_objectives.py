@@ -55,6 +55,7 @@ def check_policy(qn, z, tokens, old, reference, advantage, weight=None, temperat
     grad = torch.full_like(z, 9.0) if out is None else out
     args = dict(ref_logprob=reference if kl else None, weight=weight, clip_low=low, clip_high=high, dual=dual, kl=kl, entropy_bonus=bonus,
                 temperature=temperature, stream=stream)
+    torch.cuda.synchronize()  # `stream` waits for no other, and no other for it
     qn.qn_policy(z, tokens, old, advantage, loss, dlogits=grad, logprob=lp, entropy=ent if entropy else None, **args)
     torch.cuda.synchronize()
     want_loss, want_lp, want_ent, want, per, size, per_grad, ratio = ref.policy64(before, tokens, old, reference, advantage, weight,
@@ -81,7 +82,9 @@ def check_policy(qn, z, tokens, old, reference, advantage, weight=None, temperat
     # the loss alone gives the same numbers
     alone = torch.full((rows,), 9.0, device="cuda")
     if out is None:
+        torch.cuda.synchronize()
         qn.qn_policy(z, tokens, old, advantage, alone, logprob=lp, **args)
+        torch.cuda.synchronize()
         same = (alone == loss) | (torch.isnan(alone) & torch.isnan(loss))
         assert bool((same | ((alone - loss).abs() <= 2e-6 * (1 + loss.abs()) + 2 * (torch.nan_to_num(per, posinf=0.0) * off).float())).all())
         assert torch.equal(z, before) or bool(torch.isnan(z).any())
@@ -227,6 +230,7 @@ def check_preference(qn, l, offsets, reference, weight, pair_weight, kind=0, bet
     grad = torch.full((tokens,), 7.0, device="cuda")
     args = dict(ref_logprob=reference, weight=weight, pair_weight=pair_weight, kind=kind, beta=beta, margin=margin, smoothing=smoothing,
                 normalise=normalise, split=split, stream=stream)
+    torch.cuda.synchronize()  # `stream` waits for no other, and no other for it
     qn.qn_preference(l, offsets, loss, d_logprob=grad, reward=reward, **args)
     torch.cuda.synchronize()
     want_loss, want_reward, want, size = ref.preference64(l, offsets, reference, weight, pair_weight, kind, beta, margin, smoothing,
@@ -247,7 +251,9 @@ def check_preference(qn, l, offsets, reference, weight, pair_weight, kind=0, bet
     each = beta * (1.0 if not normalise else 10.0)
     close(grad, want, curve * float(off_h.max()) * largest * heavy * each + 1e-14 * largest * heavy * each)
     alone = torch.full((pairs,), 9.0, device="cuda")
+    torch.cuda.synchronize()
     qn.qn_preference(l, offsets, alone, **args)
+    torch.cuda.synchronize()
     assert bool(((alone == loss) | (torch.isnan(alone) & torch.isnan(loss))).all())
     return loss, reward, grad
 
@@ -325,6 +331,30 @@ def test_preference_masks_in_long_sequences(qn):
     l[500::999], weight[500::999] = math.nan, 0.0
     for normalise in (False, True):
         check_preference(qn, l, offsets, reference, weight, pair_weight, beta=0.001, normalise=normalise)
+
+
+@pytest.mark.parametrize("ref_dtype", [None, F32, BF16])
+@pytest.mark.parametrize("kind,smoothing,normalise,split", [(0, 0.1, False, True), (0, 0.0, True, False), (1, 0.0, True, False),
+                                                            (2, 0.0, False, True)])
+def test_preference_of_short_pairs_with_long_ones_between(qn, ref_dtype, kind, smoothing, normalise, split):
+    """More pairs than the device has room for blocks, short ones on average: one of nothing, one of nothing that counts, padding,
+    masked tokens, long sequences among them, and a pair out of place."""
+    pairs = 2501
+    lengths = [(11 * i * i + 5) % 90 for i in range(2 * pairs)]
+    lengths[7], lengths[2 * pairs - 3], lengths[2000], lengths[2001] = 9001, 5000, 0, 0
+    l, offsets, reference, weight, pair_weight = preference_inputs(lengths, ref_dtype, 12, lead=3, behind=4)
+    pair_weight[5::17] = 0.0
+    at = offsets.tolist()
+    weight[at[900]:at[902]] = 0.0
+    weight[at[7] + 17:at[8]:31] = 0.0
+    l[at[7] + 17:at[8]:31] = math.nan
+    if reference is not None:
+        l[1000::1013] = reference[1000::1013] = -INF
+    else:
+        weight[1000::1013] = 0.0
+    offsets[-1] += 5
+    loss, _, grad = check_preference(qn, l, offsets, reference, weight, pair_weight, kind, 0.3, 0.1, smoothing, normalise, split)
+    assert bool(torch.isnan(loss[-1])) and bool((grad[:3] == 7).all()) and int(torch.isnan(loss).sum()) == 1
 
 
 def test_preference_offsets_that_are_wrong(qn):
