@@ -79,13 +79,23 @@ __global__ void __launch_bounds__(kThreads) adam_norm_kernel(const Tensors all, 
 }
 
 // ---- what codes stand for -------------------------------------------------------------------------------------------
-// Bound by memory: 2^28 elements to bf16 286 us = 5.7 TB/s, two thirds of it written; off vectors 3 TB/s.
+// Bound by memory: 2^28 elements to bf16 282 us = 5.8 TB/s, two thirds of it written; 25.6 million whose codes lie off vectors
+// 32 us = 4.8 TB/s (a code a lane 52 us).  Six CTAs on an SM: with five, which the compiler would take, 313 and 35 us.
 
 __device__ __forceinline__ void store_value(float* p, float x) { *p = x; }
 __device__ __forceinline__ void store_value(__nv_bfloat16* p, float x) { *p = __float2bfloat16_rn(x); }
 
+// Eight codes at any address, from the words that they lie in: up to three bytes before them and four behind are read too.
+__device__ __forceinline__ void load_codes(const uint8_t* p, uint32_t (&x)[2]) {
+    const uint32_t shift = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) % 4 * 8;
+    const uint32_t* words = reinterpret_cast<const uint32_t*>(reinterpret_cast<uintptr_t>(p) & ~uintptr_t(3));
+    const uint32_t a = words[0], b = words[1], c = words[2];
+    x[0] = __funnelshift_r(a, b, shift);
+    x[1] = __funnelshift_r(b, c, shift);
+}
+
 template <typename T, typename S>
-__global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all, T* m_out, T* root_out) {
+__global__ void __launch_bounds__(kThreads, 6) adam_state_kernel(const Tensors all, T* m_out, T* root_out) {
     __shared__ int found;
     const Turns turns(all.pieces, 8, 32);
     start_after_last();
@@ -106,37 +116,9 @@ __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all,
             const S *m_at = static_cast<const S*>(r.m), *v_at = static_cast<const S*>(r.v);
             T *m_to = m_out ? m_out + r.octet * kOctet : nullptr, *root_to = root_out ? root_out + r.octet * kOctet : nullptr;
             const int64_t begin = (from - first) * kPiece, whole = (r.numel + QN_ADAM_BLOCK - 1) / QN_ADAM_BLOCK * QN_ADAM_BLOCK;
-            const int64_t end = min(whole, (to - first) * kPiece), full = min(end, r.numel / kOctet * kOctet);
+            const int64_t end = min(whole, (to - first) * kPiece);
             int64_t i = begin + threadIdx.x;
             const auto off = [](const void* p, uint32_t size) { return reinterpret_cast<uintptr_t>(p) & (8u * size - 1u); };
-            if ((off(m_out, sizeof(T)) | off(root_out, sizeof(T)) | off(r.m, sizeof(S)) | off(r.v, sizeof(S))) == 0) {
-#pragma unroll 2
-                for (int64_t a = begin + threadIdx.x * kOctet; a < full; a += kPiece) {
-                    f32x2 m2[4], r2[4];
-                    float m[8], root[8];
-                    uint32_t m_raw[sizeof(S) == 1 ? 2 : 8], v_raw[sizeof(S) == 1 ? 2 : 8];
-                    load8(m_at + a, m_raw);
-                    load8(v_at + a, v_raw);
-                    if constexpr (sizeof(S) == 1) {
-                        m_values(m_raw, m2);
-                        root_values(v_raw, r2);
-                        const f32x2 m_unit = both(power_of(r.m_scale[a / QN_ADAM_BLOCK])), r_unit = both(root_unit(r.v_scale[a / QN_ADAM_BLOCK]));
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) m2[q] = mul2(m2[q], m_unit), r2[q] = mul2(r2[q], r_unit);
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) m2[q] = two_of(m_raw, q), r2[q] = two_of(v_raw, q);
-                    }
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) unpack2(m2[q], m[2 * q], m[2 * q + 1]), unpack2(r2[q], root[2 * q], root[2 * q + 1]);
-                    if constexpr (sizeof(S) == 4)
-#pragma unroll
-                        for (float& x : root) x = __fsqrt_rn(x);
-                    if (m_to) store8(m_to + a, m);
-                    if (root_to) store8(root_to + a, root);
-                }
-                i = max(begin, full) + threadIdx.x;
-            }
             const auto value = [&](int64_t at, uint32_t m_code, uint32_t v_code, float& m, float& root) {
                 m = m_value(m_code, r.m_scale[at / QN_ADAM_BLOCK]);
                 root = root_value(v_code, r.v_scale[at / QN_ADAM_BLOCK]);
@@ -145,6 +127,54 @@ __global__ void __launch_bounds__(kThreads) adam_state_kernel(const Tensors all,
                 if (m_to) store_value(m_to + at, m);
                 if (root_to) store_value(root_to + at, root);
             };
+            const bool vectors = (off(r.m, sizeof(S)) | off(r.v, sizeof(S))) == 0;
+            if ((off(m_out, sizeof(T)) | off(root_out, sizeof(T))) == 0 && (vectors || sizeof(S) == 1)) {
+                // eight at a time; off vectors those with more of the tensor on both sides (see load_codes)
+                const int64_t low = vectors || begin > 0 ? begin : kOctet;
+                const int64_t full = min(end, vectors ? r.numel / kOctet * kOctet : (r.numel - 4) / kOctet * kOctet);
+                if (low > begin && threadIdx.x < kOctet) {
+                    float m = 0.0f, root = 0.0f;
+                    if constexpr (sizeof(S) == 1)
+                        if (threadIdx.x < r.numel) value(threadIdx.x, m_at[threadIdx.x], v_at[threadIdx.x], m, root);
+                    put(threadIdx.x, m, root);
+                }
+                const auto octets = [&](auto on_vectors) {
+                    constexpr bool kVectors = decltype(on_vectors)::value;
+#pragma unroll 2
+                    for (int64_t a = begin + threadIdx.x * kOctet; a < full; a += kPiece) {
+                        if (!kVectors && a < low) continue;
+                        f32x2 m2[4], r2[4];
+                        float m[8], root[8];
+                        uint32_t m_raw[sizeof(S) == 1 ? 2 : 8], v_raw[sizeof(S) == 1 ? 2 : 8];
+                        if constexpr (sizeof(S) == 1) {
+                            if (kVectors) load8(m_at + a, m_raw), load8(v_at + a, v_raw);
+                            else load_codes(m_at + a, m_raw), load_codes(v_at + a, v_raw);
+                        } else {
+                            load8(m_at + a, m_raw), load8(v_at + a, v_raw);
+                        }
+                        if constexpr (sizeof(S) == 1) {
+                            m_values(m_raw, m2);
+                            root_values(v_raw, r2);
+                            const f32x2 m_unit = both(power_of(r.m_scale[a / QN_ADAM_BLOCK])), r_unit = both(root_unit(r.v_scale[a / QN_ADAM_BLOCK]));
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) m2[q] = mul2(m2[q], m_unit), r2[q] = mul2(r2[q], r_unit);
+                        } else {
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) m2[q] = two_of(m_raw, q), r2[q] = two_of(v_raw, q);
+                        }
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) unpack2(m2[q], m[2 * q], m[2 * q + 1]), unpack2(r2[q], root[2 * q], root[2 * q + 1]);
+                        if constexpr (sizeof(S) == 4)
+#pragma unroll
+                            for (float& x : root) x = __fsqrt_rn(x);
+                        if (m_to) store8(m_to + a, m);
+                        if (root_to) store8(root_to + a, root);
+                    }
+                };
+                if (vectors) octets(std::true_type());
+                else if constexpr (sizeof(S) == 1) octets(std::false_type());
+                i = max(low, full) + threadIdx.x;
+            }
             // element by element, eight loads of each under way together
 #pragma unroll 1
             for (; i + 7 * kThreads < min(end, r.numel); i += 8 * kThreads) {

@@ -376,6 +376,21 @@ def test_learning_rate_on_the_device_and_seeds(qn):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("offset", range(8))
+def test_what_codes_stand_for_wherever_they_lie(qn, offset, dtype):
+    """Every place of a tensor's first code within a vector, the smallest sizes, and pieces' ends."""
+    sizes = [1, 3, 7, 8, 9, 11, 12, 13, 20, 31, 33, 2047, 2048, 2049, 2060, 70_001]
+    case = Case(qn, sizes, F32, BF16, False, 8, offset=offset, gap=1, seed=offset)
+    m, root = (torch.full((case.plan.places,), 9.0, dtype=dtype, device="cuda") for _ in range(2))
+    qn.qn_adam_state(case.plan, m, root)
+    for got, codes, scales, bits in ((m, case.m, case.m_scale, 3), (root, case.v, case.v_scale, 4)):
+        want = torch.zeros_like(got)
+        for i, n in enumerate(sizes):
+            want[case.begin[i]:case.begin[i] + n] = ref.decode(codes[i], scales[i], bits).to(dtype)
+        assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("bits", [32, 8])
 def test_what_states_stand_for(qn, bits, dtype):
     case = Case(qn, [33, 1, 5000, 64], F32, F32, False, bits, offset=1, gap=3)
