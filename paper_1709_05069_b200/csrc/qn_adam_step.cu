@@ -412,10 +412,156 @@ __device__ __noinline__ void step_any(const Setting* set, const Rates rates, con
     }
 }
 
-// Eight elements from i on; all threads of a warp, four of which have a block.
+// 256 elements of a warp from i on, or as many as there are, whatever they are: a block at a time.
 template <bool kChance, typename P, typename G, bool kMaster>
+__device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll 1
+    for (int base = i; base < min(i + 256, p.count); base += 32) {
+        const int e = base + lane, block = base / QN_ADAM_BLOCK;
+        Element x = {0.0f, 0.0f, 0.0f};
+        if (e < p.count) {
+            const float root = root_value(p.v[e], p.v_scale[block]);
+            x = stepped(set->h, set->c, rates, p.theta(e), Storage<G>::load1(p.grad + e), m_value(p.m[e], p.m_scale[block]), __fmul_rn(root, root));
+        }
+        const uint32_t ms = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.m)));
+        const uint32_t vs = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.root)));
+        const uint32_t word = element_word(octet_word(set->c.key, p.octet + e / kOctet), e % kOctet);
+        if (e < p.count) {
+            p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), word));
+            p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), word));
+            if constexpr (kMaster) p.master[e] = x.theta;
+            store_param<kChance>(p.param + e, x.theta, word);
+        }
+        if (lane == 0) p.m_scale[block] = static_cast<uint8_t>(ms), p.v_scale[block] = static_cast<uint8_t>(vs);
+    }
+}
+
+// A piece of a tensor that does not lie on vectors, in shared memory.  Numbers in 32 bits are copied word by word, so that there they
+// lie on vectors; those in 16 bits too, but for half a word; codes and scales in as many whole units of 16 bytes as it
+// takes.  (The tensor has more elements on both sides of the piece.)
+template <typename P, typename G, bool kMaster>
+struct Window {
+    using Theta = typename std::conditional<kMaster, float, P>::type;
+    static constexpr int kScales = kPiece / QN_ADAM_BLOCK;
+    template <typename X>
+    static constexpr int units() { return kPiece * sizeof(X) / 16 + (sizeof(X) == 2); }
+    struct Slot {
+        uint4 theta[units<Theta>()], grad[units<G>()], m[kPiece / 16 + 1], v[kPiece / 16 + 1], m_scale[kScales / 16 + 1], v_scale[kScales / 16 + 1];
+    };
+    static constexpr int kSlots = kSlotsOf<P, G, kMaster>;
+    Slot slot[kSlots];
+    uint4 out[sizeof(P) == 2 ? kThreads : 1];
+
+    __device__ static __forceinline__ uint32_t misplaced(const void* p, uint32_t unit) { return static_cast<uint32_t>(reinterpret_cast<uintptr_t>(p)) % unit; }
+    template <int N>
+    __device__ static __forceinline__ void copy_units(uint4 (&to)[N], const uint8_t* from) {
+        const uint8_t* at = from - misplaced(from, 16);
+        const int units = N - (at == from), j = threadIdx.x;
+        static_assert(N <= kThreads, "a unit for a thread");
+        if (j < units) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&to[j])), "l"(at + 16 * j) : "memory");
+    }
+    template <typename X>
+    __device__ static __forceinline__ void copy_words(uint4 (&to)[units<X>()], const X* from) {
+        constexpr int kWords = kPiece * sizeof(X) / 4;
+        const char* at = reinterpret_cast<const char*>(from) - misplaced(from, 4) + 4 * threadIdx.x;
+        const uint32_t into = smem_u32(to) + 4 * threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kWords; k += kThreads)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(into + 4 * k), "l"(at + 4 * k) : "memory");
+        if (sizeof(X) == 2 && misplaced(from, 4) && threadIdx.x == 0)
+            asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(into + 4 * kWords), "l"(at + 4 * kWords) : "memory");
+    }
+    // By all threads; each call is a group, also if there is nothing to copy.
+    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int s, int i, bool any) {
+        if (any) {
+            if constexpr (kMaster) copy_words<Theta>(slot[s].theta, p.master + i);
+            else copy_words<Theta>(slot[s].theta, p.param + i);
+            copy_words<G>(slot[s].grad, p.grad + i);
+            copy_units(slot[s].m, p.m + i);
+            copy_units(slot[s].v, p.v + i);
+            copy_units(slot[s].m_scale, p.m_scale + i / QN_ADAM_BLOCK);
+            copy_units(slot[s].v_scale, p.v_scale + i / QN_ADAM_BLOCK);
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ static __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
+
+    // This thread's eight elements.  (`p`: for where its arrays begin within units, which is the same for all pieces.)
+    __device__ static __forceinline__ void take8(const uint4* from, const float*, uint32_t (&x)[8]) {
+        const uint4 a = from[2 * threadIdx.x], b = from[2 * threadIdx.x + 1];
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+    }
+    __device__ static __forceinline__ void take8(const uint4* from, const __nv_bfloat16* at, uint32_t (&x)[4]) {
+        const uint4 a = from[threadIdx.x];
+        const uint32_t next = from[threadIdx.x + 1].x, shift = 8 * misplaced(at, 4);
+        x[0] = __funnelshift_r(a.x, a.y, shift), x[1] = __funnelshift_r(a.y, a.z, shift);
+        x[2] = __funnelshift_r(a.z, a.w, shift), x[3] = __funnelshift_r(a.w, next, shift);
+    }
+    __device__ static __forceinline__ void take8(const uint4* from, const uint8_t* at, uint32_t (&x)[2]) {
+        const uint32_t* words = reinterpret_cast<const uint32_t*>(from) + misplaced(at, 16) / 4 + 2 * threadIdx.x;
+        const uint32_t a = words[0], b = words[1], c = words[2], shift = 8 * misplaced(at, 4);
+        x[0] = __funnelshift_r(a, b, shift), x[1] = __funnelshift_r(b, c, shift);
+    }
+    __device__ __forceinline__ void take(int s, const Part<P, G, kMaster, uint8_t>& p, Raw<P, G, kMaster>& raw) const {
+        const Slot& from = slot[s];
+        if constexpr (kMaster) take8(from.theta, p.master, raw.theta);
+        else take8(from.theta, p.param, raw.theta);
+        take8(from.grad, p.grad, raw.grad);
+        take8(from.m, p.m, raw.m);
+        take8(from.v, p.v, raw.v);
+        const int block = threadIdx.x * kOctet / QN_ADAM_BLOCK;
+        raw.m_scale = reinterpret_cast<const uint8_t*>(from.m_scale)[misplaced(p.m_scale, 16) + block];
+        raw.v_scale = reinterpret_cast<const uint8_t*>(from.v_scale)[misplaced(p.v_scale, 16) + block];
+    }
+    // 256 elements of a warp, eight of each thread, to `to`: by way of shared memory, so that the stores of a warp lie together.
+    __device__ __forceinline__ void write_f32(int s, float* to, const uint32_t (&x)[8]) {
+        const int lane = threadIdx.x % 32;
+        uint4* mine = slot[s].theta + 2 * threadIdx.x;  // nobody else has read this
+        mine[0] = make_uint4(x[0], x[1], x[2], x[3]);
+        mine[1] = make_uint4(x[4], x[5], x[6], x[7]);
+        __syncwarp();
+        const float* from = reinterpret_cast<const float*>(mine - 2 * lane) + lane;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) to[32 * k + lane] = from[32 * k];
+    }
+    __device__ __forceinline__ void write_bf16(__nv_bfloat16* to, uint4 x) {
+        const int lane = threadIdx.x % 32;
+        const uint32_t off = misplaced(to, 4), before = __shfl_up_sync(0xffffffffu, x.w, 1);
+        out[threadIdx.x] = make_uint4(__funnelshift_l(before, x.x, 8 * off), __funnelshift_l(x.x, x.y, 8 * off),
+                                      __funnelshift_l(x.y, x.z, 8 * off), __funnelshift_l(x.z, x.w, 8 * off));
+        __syncwarp();
+        const uint32_t* from = reinterpret_cast<const uint32_t*>(out + (threadIdx.x - lane)) + lane;
+        uint32_t* words = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(to) - off) + lane;
+        // the halves of words at both ends by themselves
+        if (off && lane == 0) to[0] = __ushort_as_bfloat16(static_cast<unsigned short>(x.x));
+        else words[0] = from[0];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) words[32 * k] = from[32 * k];
+        if (off && lane == 31) to[255] = __ushort_as_bfloat16(static_cast<unsigned short>(x.w >> 16));
+    }
+};
+// Eight codes of each thread, at any address: in words, but for what is left of them at both ends of the warp's 256.
+__device__ __forceinline__ void write_codes(uint8_t* to, uint2 x) {
+    const int lane = threadIdx.x % 32;
+    const uint32_t off = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(to)) % 4, before = __shfl_up_sync(0xffffffffu, x.y, 1);
+    uint32_t* words = reinterpret_cast<uint32_t*>(to - off);
+    if (off == 0 || lane != 0) words[0] = __funnelshift_l(before, x.x, 8 * off);
+    words[1] = __funnelshift_l(x.x, x.y, 8 * off);
+    if (off != 0) {
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) {
+            if (lane == 0 && k + off < 4) to[k] = static_cast<uint8_t>(x.x >> (8 * k));
+            if (lane == 31 && k + off >= 4) to[4 + k] = static_cast<uint8_t>(x.y >> (8 * k));
+        }
+    }
+}
+// Eight elements from i on; all threads of a warp, four of which have a block.  `window`: if the tensor does not lie on vectors, which
+// is what writes it then; elements out of the ordinary send the whole warp the other way.
+template <bool kChance, bool kVectors, typename P, typename G, bool kMaster>
 __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, uint8_t>& p, int i, const Raw<P, G, kMaster>& raw) {
+                                           const Part<P, G, kMaster, uint8_t>& p, int i, const Raw<P, G, kMaster>& raw,
+                                           Window<P, G, kMaster>* window, int slot) {
     f32x2 m[4], r[4], g[4];
     float top_m, top_v;
     const f32x2 keep_m = both(keep_of_m(h, raw.m_scale)), keep_v = both(keep_of_v(h, raw.v_scale));
@@ -426,7 +572,9 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
     bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(raw.m_scale);
     uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
-    if (odd) {
+    const int warp_first = i - static_cast<int>(threadIdx.x % 32) * kOctet;
+    if (!kVectors && __any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, warp_first);
+    if (kVectors && odd) {
         const uint2 top = largest_of_any<P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale);
         most_m = top.x, field_r = top.y;
     }
@@ -436,12 +584,14 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
         field_r = max(field_r, __shfl_xor_sync(0xffffffffu, field_r, o));
     }
     // another one's element may be too large for this one's way
-    odd = odd || most_m > __float_as_uint(kHigh) || field_r > (__float_as_uint(kHigh) >> 23);
+    if (kVectors) odd = odd || most_m > __float_as_uint(kHigh) || field_r > (__float_as_uint(kHigh) >> 23);
     const uint32_t ms = scale_of(most_m), vs = scale_of(field_r << 23);
-    if ((i / kOctet) % 4 == 0) {  // all four have read the old ones
+    const auto write_scales = [&] {  // all four have read the old ones
+        if ((i / kOctet) % 4 != 0) return;
         p.m_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(ms);
         p.v_scale[i / QN_ADAM_BLOCK] = static_cast<uint8_t>(vs);
-    }
+    };
+    if (kVectors) write_scales();
     const f32x2 ups_m = both(up_m(most_m >> 23)), ups_r = both(-up_root(field_r));
     const uint32_t word = octet_word(c.key, p.octet + i / kOctet), octets[2] = {word, word};
     uint32_t a[8], b[8], x[8];
@@ -459,9 +609,28 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
         unpack2(not_finite, n0, n1);
         odd = odd || n0 + n1 != 0.0f;
     }
+    const uint2 m_codes = make_uint2(upper_bytes(a[0], a[1], a[2], a[3]), upper_bytes(a[4], a[5], a[6], a[7]));
+    const uint2 v_codes = make_uint2(upper_bytes(b[0], b[1], b[2], b[3]), upper_bytes(b[4], b[5], b[6], b[7]));
+    if constexpr (!kVectors) {
+        if (kChance && __any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, warp_first);
+        write_scales();
+        write_codes(p.m + i, m_codes);
+        write_codes(p.v + i, v_codes);
+        if constexpr (kMaster || sizeof(P) == 4) window->write_f32(slot, kMaster ? p.master + warp_first : reinterpret_cast<float*>(p.param + warp_first), x);
+        if constexpr (sizeof(P) == 2) {
+            float t1[8];
+#pragma unroll
+            for (int e = 0; e < kOctet; ++e) t1[e] = __uint_as_float(x[e]);
+            window->write_bf16(p.param + warp_first,
+                               kChance ? make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
+                                                    __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632))
+                                       : Storage<__nv_bfloat16>::pack(t1));
+        }
+        return;
+    }
     if (odd) return step_any<kChance, P, G, kMaster>(set, rates, p, i, raw.m_scale, raw.v_scale, ms, vs);
-    *reinterpret_cast<uint2*>(p.m + i) = make_uint2(upper_bytes(a[0], a[1], a[2], a[3]), upper_bytes(a[4], a[5], a[6], a[7]));
-    *reinterpret_cast<uint2*>(p.v + i) = make_uint2(upper_bytes(b[0], b[1], b[2], b[3]), upper_bytes(b[4], b[5], b[6], b[7]));
+    *reinterpret_cast<uint2*>(p.m + i) = m_codes;
+    *reinterpret_cast<uint2*>(p.v + i) = v_codes;
     if constexpr (kChance) {
         *reinterpret_cast<uint4*>(p.param + i) = make_uint4(__byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
                                                             __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
@@ -506,109 +675,15 @@ __device__ __forceinline__ void step_lanes(const Hyper& h, const Common& c, cons
     }
 }
 
-// The same for elements that are out of the ordinary, or fewer than 256, with states in 8 bits: a block at a time.
+// The same with states in 8 bits.
 template <bool kChance, typename P, typename G, bool kMaster>
-__device__ __noinline__ void step_lanes_any(const Setting* set, const Rates rates, const Part<P, G, kMaster, uint8_t> p, int i) {
-    const int lane = threadIdx.x & 31;
-#pragma unroll 1
-    for (int base = i; base < min(i + 256, p.count); base += 32) {
-        const int e = base + lane, block = base / QN_ADAM_BLOCK;
-        Element x = {0.0f, 0.0f, 0.0f};
-        if (e < p.count) {
-            const float root = root_value(p.v[e], p.v_scale[block]);
-            x = stepped(set->h, set->c, rates, p.theta(e), Storage<G>::load1(p.grad + e), m_value(p.m[e], p.m_scale[block]), __fmul_rn(root, root));
-        }
-        const uint32_t ms = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.m)));
-        const uint32_t vs = scale_of(__reduce_max_sync(0xffffffffu, finite_bits(x.root)));
-        const uint32_t word = element_word(octet_word(set->c.key, p.octet + e / kOctet), e % kOctet);
-        if (e < p.count) {
-            p.m[e] = static_cast<uint8_t>(m_code(x.m, up_by(ms), word));
-            p.v[e] = static_cast<uint8_t>(root_code(x.root, up_by(vs), word));
-            if constexpr (kMaster) p.master[e] = x.theta;
-            store_param<kChance>(p.param + e, x.theta, word);
-        }
-        if (lane == 0) p.m_scale[block] = static_cast<uint8_t>(ms), p.v_scale[block] = static_cast<uint8_t>(vs);
-    }
-}
-
-// A piece of a tensor that does not lie on vectors, in shared memory: as many bytes as it takes to copy whole units of 16.  (The tensor
-// has more elements on both sides of it.)
-template <typename P, typename G, bool kMaster>
-struct Window {
-    static constexpr int kTheta = kMaster || sizeof(P) == 4 ? 4 : 2, kScales = kPiece / QN_ADAM_BLOCK;
-    struct Slot {
-        uint4 theta[kPiece * kTheta / 16 + 1], grad[kPiece * sizeof(G) / 16 + 1], m[kPiece / 16 + 1], v[kPiece / 16 + 1];
-        uint4 m_scale[kScales / 16 + 1], v_scale[kScales / 16 + 1];
-    };
-    static constexpr int kSlots = kSlotsOf<P, G, kMaster>;
-    Slot slot[kSlots];
-
-    template <int N>
-    __device__ static __forceinline__ void copy(uint4 (&to)[N], const void* from) {
-        const char* at = reinterpret_cast<const char*>(reinterpret_cast<uintptr_t>(from) & ~uintptr_t(15));
-        const int units = N - (at == from);
-#pragma unroll
-        for (int k = 0; k < N; k += kThreads) {
-            const int j = k + threadIdx.x;
-            if (j < units) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(&to[j])), "l"(at + 16 * j) : "memory");
-        }
-    }
-    // By all threads; each call is a group, also if there is nothing to copy.
-    __device__ __forceinline__ void fetch(const Part<P, G, kMaster, uint8_t>& p, int s, int i, bool any) {
-        if (any) {
-            copy(slot[s].theta, kMaster ? static_cast<const void*>(p.master + i) : static_cast<const void*>(p.param + i));
-            copy(slot[s].grad, p.grad + i);
-            copy(slot[s].m, p.m + i);
-            copy(slot[s].v, p.v + i);
-            copy(slot[s].m_scale, p.m_scale + i / QN_ADAM_BLOCK);
-            copy(slot[s].v_scale, p.v_scale + i / QN_ADAM_BLOCK);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    }
-    __device__ static __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kSlots - 2) : "memory"); }
-};
-// Where elements come from: memory, or a window (elements counted from the piece's first).
-template <typename P, typename G, bool kMaster>
-struct FromMemory {
-    const Part<P, G, kMaster, uint8_t>& p;
-    __device__ __forceinline__ float theta(int e) const { return p.theta(e); }
-    __device__ __forceinline__ float grad(int e) const { return Storage<G>::load1(p.grad + e); }
-    __device__ __forceinline__ uint32_t m(int e) const { return p.m[e]; }
-    __device__ __forceinline__ uint32_t v(int e) const { return p.v[e]; }
-    __device__ __forceinline__ uint32_t m_scale(int block) const { return p.m_scale[block]; }
-    __device__ __forceinline__ uint32_t v_scale(int block) const { return p.v_scale[block]; }
-};
-template <typename P, typename G, bool kMaster>
-struct FromWindow {
-    using Theta = typename std::conditional<kMaster, float, P>::type;
-    const Theta* theta_at;
-    const G* grad_at;
-    const uint8_t *m_at, *v_at, *m_scale_at, *v_scale_at;
-    template <typename X>
-    __device__ static __forceinline__ const X* in(const uint4* to, const void* from) {
-        return reinterpret_cast<const X*>(reinterpret_cast<const char*>(to) + (reinterpret_cast<uintptr_t>(from) & 15));
-    }
-    __device__ __forceinline__ FromWindow(const typename Window<P, G, kMaster>::Slot& s, const Part<P, G, kMaster, uint8_t>& p)
-        : theta_at(in<Theta>(s.theta, kMaster ? static_cast<const void*>(p.master) : static_cast<const void*>(p.param))),
-          grad_at(in<G>(s.grad, p.grad)), m_at(in<uint8_t>(s.m, p.m)), v_at(in<uint8_t>(s.v, p.v)),
-          m_scale_at(in<uint8_t>(s.m_scale, p.m_scale)), v_scale_at(in<uint8_t>(s.v_scale, p.v_scale)) {}
-    __device__ __forceinline__ float theta(int e) const { return load_rw(theta_at + e); }
-    __device__ __forceinline__ float grad(int e) const { return load_rw(grad_at + e); }
-    __device__ __forceinline__ uint32_t m(int e) const { return m_at[e]; }
-    __device__ __forceinline__ uint32_t v(int e) const { return v_at[e]; }
-    __device__ __forceinline__ uint32_t m_scale(int block) const { return m_scale_at[block]; }
-    __device__ __forceinline__ uint32_t v_scale(int block) const { return v_scale_at[block]; }
-};
-
-// `from`: its element `offset` is the part's element i.  kWhole: all 256 are there.
-template <bool kChance, bool kWhole, typename P, typename G, bool kMaster, typename F>
 __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, const Common& c, const Rates& rates,
-                                           const Part<P, G, kMaster, uint8_t>& p, int i, const F& from, int offset) {
-    if (!kWhole && i >= p.count) return;
+                                           const Part<P, G, kMaster, uint8_t>& p, int i) {
+    if (i >= p.count) return;
     const int lane = threadIdx.x & 31, at = i + lane, block = i / QN_ADAM_BLOCK;
     // elements that are not there are ordinary ones that count for nothing and are not written
-    const auto here = [&](int j) { return kWhole || at + 32 * j < p.count; };
-    const auto last_block = [&](int b) { return kWhole ? b : min(b, (p.count - 1) / QN_ADAM_BLOCK); };
+    const auto here = [&](int j) { return at + 32 * j < p.count; };
+    const auto last_block = [&](int b) { return min(b, (p.count - 1) / QN_ADAM_BLOCK); };
     const f32x2 beta1 = both(h.beta1), minus_beta2 = both(-h.beta2);
     const f32x2 keep_m[4] = {beta1, beta1, beta1, beta1}, keep_v[4] = {minus_beta2, minus_beta2, minus_beta2, minus_beta2};
     f32x2 m[4], r[4], g[4];
@@ -616,16 +691,16 @@ __device__ __forceinline__ void step_lanes(const Setting* set, const Hyper& h, c
     uint32_t codes[8][2];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const int e = offset + 32 * j + lane;
+        const int e = at + 32 * j;
         codes[j][0] = 0, codes[j][1] = 0x80, t[j] = 0.0f;
-        if (here(j)) codes[j][0] = from.m(e), codes[j][1] = from.v(e), t[j] = from.theta(e);
+        if (here(j)) codes[j][0] = p.m[e], codes[j][1] = p.v[e], t[j] = p.theta(e);
     }
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        const int e = offset + 64 * q + lane, b0 = last_block(offset / QN_ADAM_BLOCK + 2 * q), b1 = last_block(offset / QN_ADAM_BLOCK + 2 * q + 1);
-        g[q] = pack2(here(2 * q) ? from.grad(e) : 1.0f, here(2 * q + 1) ? from.grad(e + 32) : 1.0f);
-        m[q] = mul2(m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u), pack2(power_of(from.m_scale(b0)), power_of(from.m_scale(b1))));
-        r[q] = mul2(root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u), pack2(root_unit(from.v_scale(b0)), root_unit(from.v_scale(b1))));
+        const int e = at + 64 * q, b0 = last_block(block + 2 * q), b1 = last_block(block + 2 * q + 1);
+        g[q] = pack2(here(2 * q) ? Storage<G>::load1(p.grad + e) : 1.0f, here(2 * q + 1) ? Storage<G>::load1(p.grad + e + 32) : 1.0f);
+        m[q] = mul2(m_values(codes[2 * q][0] + codes[2 * q + 1][0] * 256u), pack2(power_of(p.m_scale[b0]), power_of(p.m_scale[b1])));
+        r[q] = mul2(root_values(codes[2 * q][1] + codes[2 * q + 1][1] * 65536u), pack2(root_unit(p.v_scale[b0]), root_unit(p.v_scale[b1])));
     }
     float top_m, top_v;
     const bool odd = !moments(h, c, m, r, keep_m, keep_v, g, top_m, top_v);
@@ -745,7 +820,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
 #pragma unroll 1
                 for (int base = last; base >= 0; base -= kPiece) {
                     if (base <= top && base >= low) base = low;
-                    else step_lanes<kChance, false>(&set, h, c, rates, p, base + mine, FromMemory<P, G, kMaster>{p}, base + mine);
+                    else step_lanes<kChance>(&set, h, c, rates, p, base + mine);
                 }
                 constexpr int kSlots = kSlotsOf<P, G, kMaster>;
                 int base = top, slot = 0;
@@ -759,8 +834,9 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
                         __syncthreads();  // all have their copies, and are through with the slot that is filled next
                         const int ahead = base - (kSlots - 1) * kPiece;
                         window.fetch(p, slot == 0 ? kSlots - 1 : slot - 1, ahead, ahead >= low);
-                        const FromWindow<P, G, kMaster> from(window.slot[slot], p);
-                        step_lanes<kChance, true>(&set, h, c, rates, p, base + mine, from, mine);
+                        Raw<P, G, kMaster> raw;
+                        window.take(slot, p, raw);
+                        step_octet<kChance, false>(&set, h, c, rates, p, base + static_cast<int>(threadIdx.x) * kOctet, raw, &window, slot);
                         slot = slot == kSlots - 1 ? 0 : slot + 1;
                     }
                 } else {
@@ -786,7 +862,7 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
                             slots.take(s, raw);
                             raw.m_scale = m_scale[s], raw.v_scale = v_scale[s];
                             fetch(kSlots - 1, s == 0 ? kSlots - 1 : s - 1);
-                            step_octet<kChance>(&set, h, c, rates, p, i, raw);
+                            step_octet<kChance, true, P, G, kMaster>(&set, h, c, rates, p, i, raw, nullptr, 0);
                             base -= kPiece, i -= kPiece;
                         }
                     }
