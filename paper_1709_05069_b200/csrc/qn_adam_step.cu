@@ -5,19 +5,22 @@
 //     theta' = theta (1 - lr wd) - lr / (1 - b1^t) m' / (r' / sqrt(1 - b2^t) + eps)
 // Nothing is reused, so the floor is the bytes: each array once in and once out.
 //
-// CTAs stay and take turns at runs of pieces (see Turns), backwards: the last gradients that qn_adam_norm has read are the first to
-// be read again, from L2.  A thread has eight elements, in vectors of 8 to 32 bytes, and works on two at a time (packed fp32).
-// Tensors that do not lie on such vectors, and what is left of a piece where a tensor ends, go an element a lane, eight for each thread.
+// CTAs stay and take turns at runs of pieces (see Turns), backwards: the last gradients that qn_adam_norm has read are the
+// first to be read again, from L2.  A thread has eight elements, in vectors of 8 to 32 bytes, and works on two at a time
+// (packed fp32).  Where tensors do not lie on such vectors, states in 8 bits go by way of shared memory, where they do, and
+// states in 32 bits an element a lane, eight for each thread; so does, with both, what is left of a piece where a tensor ends.
 //
 // Measured on a B200 (a copy: 6.54 TB/s), bytes of the floor over time:
 //   states in 32 bits: bound by memory.  2^28 bf16 parameters with master copies 1210 us = 6.65 TB/s, 25.6 million fp32 ones 118 us
 //       = 6.1 TB/s; off vectors 4.4 to 5.1 TB/s.  With two CTAs on an SM and 88 registers 3 % less than with three and 80.
 //   states in 8 bits: 57 instructions an element, of which 27 go to the integer and comparison pipe; three quarters of the issue
-//       slots, two thirds of that pipe.  2^28 bf16 parameters 578 us = 4.75 TB/s; off vectors 93 instructions, 25.6 million fp32 ones 121 us.
-//   Steps on the way (2^28 bf16, 8 bits): an element a lane 4.3 ms; eight elements a thread in vectors 1106 us (81 instructions,
-//       two CTAs on an SM); the root by one correction instead of a call, reciprocals, codes put together from upper bytes 763; runs
-//       instead of chunks 726; copies ahead through shared memory 581 (three slots 619, six 605); turns, folded constants and
-//       slots by name 578.  The same constants from shared memory instead of registers changed nothing.
+//       slots, two thirds of that pipe.  2^28 bf16 parameters 578 us = 4.75 TB/s; off vectors 80 instructions, 2^27 bf16 ones
+//       428 us = 3.2 TB/s, 25.6 million fp32 ones 107 us (an element a lane 93, 558 and 120).
+//   Steps on the way (2^28 bf16, 8 bits): an element a lane 4.3 ms; eight elements a thread in vectors 1106 us (81
+//       instructions, two CTAs on an SM); the root by one correction instead of a call, reciprocals, codes put together from
+//       upper bytes 763; runs instead of chunks 726; copies ahead through shared memory 581 (three slots 619, six 605); turns,
+//       folded constants and slots by name 578.  The same constants from shared memory instead of registers changed nothing;
+//       nor did, off vectors, fewer instructions for the copies and for the ends of a warp's codes (107 and 439 us).
 #include <nvtx3/nvToolsExt.h>
 
 #include <algorithm>

@@ -257,6 +257,15 @@ def test_gradients_that_are_not_finite(qn, bits, bad):
     case.guards_whole()
 
 
+@pytest.mark.parametrize("param,grad,master", TYPES)
+@pytest.mark.parametrize("offset", range(1, 16))
+def test_codes_wherever_they_lie(qn, param, grad, master, offset):
+    """Every place within a vector, in tensors with whole pieces inside."""
+    case = Case(qn, [9001, 40, 16_385], param, grad, master, 8, offset, 0, seed=offset)
+    for k in range(2):
+        case.check_step(stochastic=k == 1)
+
+
 @pytest.mark.parametrize("bits", [32, 8])
 @pytest.mark.parametrize("repeats,each,offset", [(1, 32, 0), (16, 32, 0), (16, 32, 1), (60, 8, 0), (60, 8, 3), (25, 256, 0)])
 def test_extreme_gradients(qn, bits, repeats, each, offset):
