@@ -9,7 +9,7 @@
 //
 // Bound by latency: offsets, a pair's tiles one after the other, the exchange, exp and a division in 64 bits, the writes.
 // Measured, us of kernel in a graph: 4 pairs of 64 tokens at most 3.8; 1024 pairs, 2.4 million tokens 11.7 (the bytes alone
-// 5.8); 12 pairs, 1.8 million tokens 13.3 (4.7), with CTAs on all SMs only by clusters of 16.  Steps on the way, the last two
+// 5.8); 12 pairs, 2.2 million tokens 13.3 (4.7), with CTAs on all SMs only by clusters of 16.  Steps on the way, the last two
 // of these: tokens of both sequences in one index, a select for each sum, 39 and 21; conditions around loads, which then wait for
 // one another, 18 and 21; tiles without conditions 14 and 15; weights of four tiles in shared memory instead of two in
 // registers 11.7 and 13.3.  Thousands of short pairs are bound by the numbers of each pair, which one thread works out while the
