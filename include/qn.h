@@ -544,7 +544,7 @@ typedef struct qn_adam_plan* qn_adam_handle;
 
 /*
  * One tensor: contiguous arrays of numel elements, each aligned to its element type.  Arrays at multiples of 8 elements'
- * size (32 bytes of fp32, 16 of bf16, 8 of codes) are moved in vectors, others element by element.
+ * size (32 bytes of fp32, 16 of bf16, 8 of codes) are moved in vectors, which is the fastest; the results are the same.
  *   param       theta, of the plan's parameter type; read and written
  *   grad        g, of the plan's gradient type; read only.  NULL: the tensor has none, and is left alone with its states
  *   master      NULL, or (for all tensors of a plan, whose parameters are bf16) theta in fp32: the step is taken from it and

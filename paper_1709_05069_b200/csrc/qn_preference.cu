@@ -14,7 +14,7 @@
 // one another, 18 and 21; tiles without conditions 14 and 15; weights of four tiles in shared memory instead of two in
 // registers 11.7 and 13.3.  Thousands of short pairs are bound by the numbers of each pair, which one thread works out while the
 // others of its block wait: a warp a pair, and the eight pairs of a block by eight threads side by side, 4096 pairs of 72
-// tokens 14.2 -> 9.4 (4096 of 580 tokens 14.2 as a warp each or as before; 12 of 80 tokens 3.8 -> 4.9, so that these stay).
+// tokens 14.2 -> 9.4 (4096 of 580 tokens would go from 14.2 to 16.7, 12 of 80 from 3.8 to 4.9: these stay).
 #include <nvtx3/nvToolsExt.h>
 
 #include "qn_vocab.cuh"

@@ -257,6 +257,33 @@ def test_gradients_that_are_not_finite(qn, bits, bad):
     case.guards_whole()
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("param,grad,master", TYPES)
+@pytest.mark.parametrize("offset", [1, 6, 11])
+def test_results_do_not_depend_on_where_tensors_lie(qn, param, grad, master, bits, offset):
+    """The same bits on vectors and off them, in whole pieces too, with elements of every kind among them."""
+    runs = []
+    for off in (0, offset):
+        case = Case(qn, [30_000, 40, 9001, 2049], param, grad, master, bits, off, 0, seed=4)
+        for g in case.grad[::2]:
+            g[5::1031], g[6::2077], g[2500::4099], g[33::67] = 0.0, 1e20, 1e-30, 1e-12
+        case.grad[0][12_000], case.grad[0][12_700], case.grad[0][20_001] = math.inf, math.nan, -math.inf
+        case.theta[0][13_500], case.theta[0][14_001] = math.nan, math.inf
+        if master:
+            case.master[0][13_500], case.master[0][14_001] = math.nan, math.inf
+        if bits == 8:  # a block without history
+            for state in (case.m, case.m_scale, case.v, case.v_scale):
+                state[0][: 480 if state is case.m or state is case.v else 15] = 0
+            for x, n in ((case.m, 9600), (case.v, 9600)):
+                x[0][9000:n] = 0
+        for k in range(3):
+            qn.qn_adam_step(case.plan, case.step, lr=1e-2, stochastic=True, seed=k)
+        runs.append(case.everything())
+        case.guards_whole()
+    for a, b in zip(*runs):
+        assert bool(((a == b) | ((a != a) & (b != b))).all())
+
+
 @pytest.mark.parametrize("param,grad,master", TYPES)
 @pytest.mark.parametrize("offset", range(1, 16))
 def test_codes_wherever_they_lie(qn, param, grad, master, offset):
