@@ -587,7 +587,7 @@ QN_API qn_status qn_adam_norm(qn_adam_handle h, double* sumsq, void* cuda_stream
 /*
  * One step.
  *   step        DEVICE int64: steps taken so far; counted up by one
- *   lr          learning rate >= 0; lr_device (DEVICE fp32, may be NULL) takes its place
+ *   lr          learning rate >= 0; lr_device (DEVICE fp32, may be NULL) takes its place.  lr' / (1 - beta1^t) up to 2^64
  *   beta1, beta2 in [0, 1);  eps >= 2^-126
  *   sumsq       DEVICE, may be NULL: the norm's square (qn_adam_norm).  If it is not finite nothing is changed, *step neither
  *   max_norm    > 0: gradients whose norm (times |grad_scale|) is larger are scaled down to it; needs sumsq.  Otherwise no bound

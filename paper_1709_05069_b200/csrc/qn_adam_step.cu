@@ -122,14 +122,18 @@ struct Element {
     float theta, m, root;
 };
 // One element with states in 8 bits, whatever it is; m and v: before the step.  The same operations as those of the packed way below,
-// so that an element does not depend on which way its neighbours need.
+// so that an element does not depend on which way its neighbours need.  Only here a root may be 0 or so small that what is left, eps in
+// units of speed, is below 2^-126, which the reciprocal takes for 0: speed then stays outside (it is above 1, and r spread + eps is
+// 2^-126 at least).
 __device__ __forceinline__ Element stepped(const Hyper& h, const Common& c, const Rates& rates, float theta, float g, float m, float v) {
     Element e;
     g = __fmul_rn(g, c.coefficient);
     e.m = __fadd_rn(__fmul_rn(m, h.beta1), __fmul_rn(g, h.rest1));
     e.root = __fsqrt_rn(__fadd_rn(__fmul_rn(v, h.beta2), __fmul_rn(__fmul_rn(g, g), h.rest2)));
     const float down = e.root == 0.0f ? -rates.eps : __fmaf_rn(-e.root, rates.spread, -rates.eps);
-    e.theta = __fmaf_rn(e.m, rcp_approx(down), __fmul_rn(theta, rates.keep));
+    const float kept = __fmul_rn(theta, rates.keep);
+    if (fabsf(down) < 0x1p-126f) e.theta = __fmaf_rn(__fmul_rn(e.m, rates.speed), rcp_approx(-__fmaf_rn(e.root, c.spread, h.eps)), kept);
+    else e.theta = __fmaf_rn(e.m, rcp_approx(down), kept);
     return e;
 }
 

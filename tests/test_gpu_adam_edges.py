@@ -1,0 +1,34 @@
+"""qn_adam_*: constants and states at the ends of what the calls accept, and the ways that an element can take through the step."""
+import pytest
+import torch
+
+import adam_reference as ref
+from test_gpu_adam import BF16, F32, TYPES, Case, qn  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("offset", [0, 1])
+@pytest.mark.parametrize("eps,lr,lr_scale,done", [(2.0 ** -126, 1.0, 1.0, 0), (1e-37, 1.0, 1.0, 0), (1.2e-38, 0.5, 64.0, 3),
+                                                  (1e-30, 1e9, 1.0, 100), (2.0 ** -126, 1e12, 1.0, 0)])
+def test_eps_below_what_a_step_of_the_learning_rate_resolves(qn, bits, offset, eps, lr, lr_scale, done):  # noqa: F811
+    """eps / (lr / (1 - beta1^t)) below fp32's normal numbers: elements without history only decay, and those with v = 0 move by
+    m' / eps; in whole blocks, alone among ordinary ones, in whole pieces and at ends, on vectors and off them."""
+    case = Case(qn, [50, 12_345], F32, F32, False, bits, offset, lr_scale=lr_scale, spread=1.0)
+    case.step.fill_(done)
+    for i, n in enumerate(case.sizes):
+        at = torch.arange(n, device="cuda")
+        none = (at % 37 == 0) | ((at // 64) % 5 == 0)
+        case.grad[i][none] = 0.0
+        for part in (case.m, case.v):
+            part[i][none] = 0
+        if bits == 8:  # two blocks with m alone: E4M3's 1 at 2^-107
+            if n > 900:
+                case.m[i][640:704], case.m_scale[i][20:22] = 0x38, 20
+                case.v_scale[i][20:22] = 0
+        else:
+            case.m[i][640:704] = 2.0 ** -107
+    case.check_step(lr=lr, eps=eps)
+    for part in case.theta:
+        assert bool(torch.isfinite(part).all())
