@@ -118,7 +118,7 @@ __device__ __forceinline__ uint32_t m_code(float m, float up, uint32_t word) {
     const uint32_t bits = __float_as_uint(m);
     if ((bits & 0x7fffffffu) >= kInfinity) return 0x7fu;  // NaN
     const uint32_t chance = ((word >> 12) & 0xffff0u) | 8u;
-    return ((magnitude_bits(m, up) + chance) >> 20) | (m < 0.0f ? 0x80u : 0u);
+    return ((magnitude_bits(m, up) + chance) >> 20) | (bits >> 24 & 0x80u);  // -0 has its sign too, as in the packed ways
 }
 __device__ __forceinline__ uint32_t root_code(float r, float up, uint32_t word) {
     if (__float_as_uint(r) >= kInfinity) return 0xffu;  // the largest

@@ -32,3 +32,27 @@ def test_eps_below_what_a_step_of_the_learning_rate_resolves(qn, bits, offset, e
     case.check_step(lr=lr, eps=eps)
     for part in case.theta:
         assert bool(torch.isfinite(part).all())
+
+
+@pytest.mark.parametrize("param,grad,master", TYPES)
+def test_minus_zero_is_the_same_code_wherever_it_lies(qn, param, grad, master):  # noqa: F811
+    """m' = -0, from a code of -0 and gradients that are -0 or vanish beside it: the sign stays, whichever way the neighbours of an
+    element need (a root of 0 among them) and wherever the tensor lies."""
+    n, runs = 9001, []
+    at = torch.arange(n, device="cuda")
+    gone = (at % 3 == 1) & ((at // 32) % 2 == 0)
+    for offset in (0, 1, 6):
+        for apart in (8, 301, n):  # neighbours without history: in every octet, in every warp's elements, one
+            case = Case(qn, [n], param, grad, master, 8, offset, 0, seed=6)
+            case.m[0][gone] = 0x80
+            case.grad[0][gone] = -0.0
+            case.grad[0][gone & (at % 2 == 0)] = -1e-45
+            lone = (at % apart == 5) & ~gone
+            case.v[0][lone], case.grad[0][lone] = 0, 0.0
+            qn.qn_adam_step(case.plan, case.step, stochastic=True, seed=2)
+            assert bool((case.m[0][gone] == 0x80).all())
+            runs.append((apart, case.everything()))
+            case.guards_whole()
+    for apart, run in runs:
+        same = next(x for a, x in runs if a == apart)
+        assert all(torch.equal(x, y) for x, y in zip(run, same))
