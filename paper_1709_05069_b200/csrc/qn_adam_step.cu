@@ -34,6 +34,7 @@ struct Hyper {
     double lr, log_beta1, log_beta2, max_norm, grad_scale;
     float beta1, rest1, beta2, rest2, eps, minus_zero;
     uint32_t seed_low, seed_high;
+    uint32_t tiny_scales;  // see tiny_scale
 };
 
 // What is the same for all elements of a step.
@@ -214,8 +215,8 @@ __device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
 
 // States in 8 bits: the codes' values become m' and -r'.  They may come without their scales: then keep_m is beta1 times the scale's
 // power of two, and keep_v -beta2 times that of r, squared: products with powers of two are exact, so that they may come before the rounding or after it.  (Where
-// keep_v underflows, what it stands for is below 2^-126, and below half a step of any v' that stays here; where keep_m
-// does, in blocks below 2^-112, the caller does not come here.)  top_m: the largest m'; top_v: the largest v'.  False where this way is not
+// keep_v underflows, what it stands for is below 2^-126, and below half a step of any v' that stays here; where keep_m may,
+// the caller does not come here: see tiny_scale.)  top_m: the largest m'; top_v: the largest v'.  False where this way is not
 // the right one: a second moment is 0, or very small, or something is very large or not a number.
 __device__ __forceinline__ bool moments(const Hyper& h, const Common& c, f32x2 (&m)[4], f32x2 (&r)[4], const f32x2 (&keep_m)[4],
                                         const f32x2 (&keep_v)[4], const f32x2 (&grad)[4], float& top_m, float& top_v) {
@@ -242,8 +243,10 @@ __device__ __forceinline__ float keep_of_v(const Hyper& h, uint32_t scale) {
     const float unit = root_unit(scale);
     return unit * unit * -h.beta2;
 }
-// keep_of_m is not exact: a small scale, but not that of a block of zeros.
-__device__ __forceinline__ bool tiny_scale(uint32_t scale) { return scale - 1u < 8u; }
+// keep_of_m may not be exact: the scale s, but not that of a block of zeros, is so small that beta1 2^(s - 127) is below 2^-126.  With
+// beta1 in [2^-e, 2^(1 - e)) these are the scales from 1 to e.
+__device__ __forceinline__ bool tiny_scale(const Hyper& h, uint32_t scale) { return scale - 1u < h.tiny_scales; }
+uint32_t tiny_scales(float beta1) { return beta1 > 0.0f ? static_cast<uint32_t>(-ilogbf(beta1)) : 0u; }
 
 // 2^-e / 2^120 (see magnitude_bits; below kHigh this is a number, and one product does for the two there) from the exponent
 // field of a block's largest finite magnitude, which is not 0 (m: may be 0).
@@ -578,7 +581,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     root_values(raw.v, r);
 #pragma unroll
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
-    bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(raw.m_scale);
+    bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(h, raw.m_scale);
     uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
     const int warp_first = i - static_cast<int>(threadIdx.x % 32) * kOctet;
     if (!kVectors && __any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, warp_first);
@@ -912,7 +915,8 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     if (!guard.ok) return QN_ERR_CUDA;
     const Hyper hyper{lr, log(beta1), log(beta2), max_norm, grad_scale,
                       static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32)};
+                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32),
+                      tiny_scales(static_cast<float>(beta1))};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:adam_step");
     const auto by_grad = [&](auto grad) {

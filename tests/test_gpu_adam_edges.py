@@ -56,3 +56,21 @@ def test_minus_zero_is_the_same_code_wherever_it_lies(qn, param, grad, master): 
     for apart, run in runs:
         same = next(x for a, x in runs if a == apart)
         assert all(torch.equal(x, y) for x, y in zip(run, same))
+
+
+@pytest.mark.parametrize("beta1", [2.0 ** -8 * 0.99, 0.003, 2.0 ** -24 * 1.37, 2.0 ** -30 * 1.7, 2.0 ** -130 * 1.3, 2.0 ** -7 * 1.9,
+                                   0.0, 0.5, 0.9, 0.999])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_small_beta1_and_small_scales(qn, beta1, offset):  # noqa: F811
+    """beta1 times a block's power of two may lie below fp32's normal numbers where beta1 times the value that the code stands for does
+    not: m' is the latter, in whole pieces and at ends."""
+    n = 20_000
+    case = Case(qn, [n], F32, F32, False, 8, offset)
+    case.grad[0].zero_()
+    block = torch.arange((n + 31) // 32, device="cuda")
+    case.m_scale[0].copy_(1 + block % 160)
+    for seed in (1, 2, 3):
+        keep = [x.clone() for x in (case.m[0], case.m_scale[0])]
+        case.check_step(beta1=beta1, seed=seed)
+        case.m[0].copy_(keep[0])
+        case.m_scale[0].copy_(keep[1])
