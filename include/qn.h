@@ -610,6 +610,13 @@ QN_API int64_t qn_adam_places(qn_adam_handle h);
 QN_API qn_status qn_adam_state(qn_adam_handle h, qn_dtype dtype, void* m, void* root, void* cuda_stream);
 
 /*
+ * Self-test.  With states in 8 bits an element's codes and step are the same whichever way its neighbours need, which takes the fast
+ * way's square root to be the correctly rounded one for numbers from 2^-100 to 2^30 (others go another way).  Adds to *differ
+ * (DEVICE) how many of the fp32 numbers with the bits `first` to `last` (0 <= first <= last < 0x7f800000) have another root there.
+ */
+QN_API qn_status qn_selftest_roots(int64_t first, int64_t last, int64_t* differ, void* cuda_stream);
+
+/*
  * Per-kernel timing, for benchmarks.  Between qn_timing_begin and qn_timing_end every kernel the
  * handle launches (up to max_kernels of them) is bracketed by two CUDA events recorded on the
  * stream of the call.  qn_timing_end waits for those events and returns, per kind of kernel,

@@ -201,7 +201,7 @@ __device__ __forceinline__ float least(float a, float b, float c) {
 }
 
 // The root of a number in [kLow, kHigh] rounded to nearest: s + e / (2 sqrt(v)) with the exact remainder e = v - s^2 (Markstein's
-// correction of a root), which was compared with the library's root at every one of these numbers.  Numbers come and go
+// correction of a root): qn_selftest_roots compares it with the library's root at every one of these numbers.  Numbers come and go
 // with their signs changed, which spares the negations.
 constexpr float kLow = 0x1p-100f, kHigh = 0x1p30f;
 __device__ __forceinline__ f32x2 minus_roots(f32x2 minus_v) {
@@ -891,6 +891,20 @@ __global__ void __launch_bounds__(kThreads, sizeof(S) == 4 ? 2 : 3) adam_step_ke
     }
 }
 
+// How many of the numbers with the bits first to last have another root the packed way.
+__global__ void roots_kernel(uint32_t first, uint32_t last, unsigned long long* differ) {
+    unsigned count = 0;
+    for (uint64_t bits = first + 2ull * (blockIdx.x * blockDim.x + threadIdx.x); bits <= last; bits += 2ull * gridDim.x * blockDim.x) {
+        const float v0 = __uint_as_float(static_cast<uint32_t>(bits)), v1 = __uint_as_float(static_cast<uint32_t>(bits) + 1u);
+        float r0, r1;
+        unpack2(minus_roots(pack2(-v0, -v1)), r0, r1);
+        count += __float_as_uint(-r0) != __float_as_uint(__fsqrt_rn(v0));
+        count += bits < last && __float_as_uint(-r1) != __float_as_uint(__fsqrt_rn(v1));
+    }
+    count = __reduce_add_sync(0xffffffffu, count);
+    if (threadIdx.x % 32 == 0 && count) atomicAdd(differ, static_cast<unsigned long long>(count));
+}
+
 template <typename P, typename G, bool kMaster, bool kChance>
 cudaError_t launch_step(const qn_adam_plan& h, const Hyper& hyper, int64_t* step, const float* lr, const double* sumsq, cudaStream_t st) {
     static Resident resident[2];
@@ -929,4 +943,15 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     const cudaError_t e = h->grad == QN_F32 ? by_grad(float()) : by_grad(__nv_bfloat16());
     nvtxRangePop();
     return e == cudaSuccess ? QN_OK : QN_ERR_CUDA;
+}
+
+extern "C" qn_status qn_selftest_roots(int64_t first, int64_t last, int64_t* differ, void* cuda_stream) {
+    if (first < 0 || last < first || last >= 0x7f800000 || !differ || reinterpret_cast<uintptr_t>(differ) % 8) return QN_ERR_INVALID;
+    int dev = -1;
+    if (!device_of(differ, &dev)) return QN_ERR_INVALID;
+    DeviceGuard guard(dev);
+    if (!guard.ok) return QN_ERR_CUDA;
+    roots_kernel<<<4 * qn_sm_count(), kThreads, 0, static_cast<cudaStream_t>(cuda_stream)>>>(
+        static_cast<uint32_t>(first), static_cast<uint32_t>(last), reinterpret_cast<unsigned long long*>(differ));
+    return cudaGetLastError() == cudaSuccess ? QN_OK : QN_ERR_CUDA;
 }

@@ -47,6 +47,7 @@ EXPORTS = (
     "qn_gram_static", "qn_selftest_bounded_wait",
     "qn_logprobs", "qn_logprobs_backward", "qn_distill", "qn_policy", "qn_preference",
     "qn_adam_create", "qn_adam_destroy", "qn_adam_grads", "qn_adam_norm", "qn_adam_step", "qn_adam_places", "qn_adam_state",
+    "qn_selftest_roots",
 )
 TIME_KINDS = ("gram", "solve", "combine", "row")
 KERNEL_NAMES = {
@@ -121,6 +122,7 @@ def lib() -> ctypes.CDLL:
         for name in ("create", "destroy", "grads", "norm", "step", "state"):
             getattr(L, "qn_adam_" + name).restype = i32
         L.qn_adam_places.argtypes, L.qn_adam_places.restype = [vp], i64
+        L.qn_selftest_roots.argtypes, L.qn_selftest_roots.restype = [i64, i64, vp, vp], i32
         _lib = L
     return _lib
 
@@ -767,3 +769,13 @@ def qn_adam_state(h: Adam, m: Optional[torch.Tensor], root: Optional[torch.Tenso
     dtype = next((x.dtype for x in (m, root) if x is not None), torch.float32)
     _check(lib().qn_adam_state(h.ptr, dtype_code(dtype), _of_tensor(m, dtype, h.places, h.device, "m"),
                                _of_tensor(root, dtype, h.places, h.device, "root"), _stream_on(h.device, stream)), "qn_adam_state")
+
+
+def qn_selftest_roots(first: int, last: int, differ: torch.Tensor, stream=None) -> None:
+    """Adds to ``differ`` (int64, one element, on the device) how many float32 numbers with the bits ``first`` to ``last`` have a
+    root that is not the correctly rounded one in the AdamW step with states in 8 bits (none from 2^-100 to 2^30)."""
+    if differ is None or not differ.is_cuda:
+        raise ValueError("differ must be a CUDA tensor")
+    dev = differ.get_device()
+    _check(lib().qn_selftest_roots(first, last, _of_tensor(differ, torch.int64, 1, dev, "differ"), _stream_on(dev, stream)),
+           "qn_selftest_roots")

@@ -74,3 +74,22 @@ def test_small_beta1_and_small_scales(qn, beta1, offset):  # noqa: F811
         case.check_step(beta1=beta1, seed=seed)
         case.m[0].copy_(keep[0])
         case.m_scale[0].copy_(keep[1])
+
+
+def test_every_root_that_the_packed_way_takes_is_the_correctly_rounded_one(qn):  # noqa: F811
+    """All 130 * 2^23 + 1 numbers from 2^-100 to 2^30."""
+    def bits(x):
+        return int(torch.tensor(x, dtype=F32).view(torch.int32))
+
+    differ = torch.zeros(1, dtype=torch.int64, device="cuda")
+    qn.qn_selftest_roots(bits(2.0 ** -100), bits(2.0 ** 30), differ)
+    assert int(differ) == 0
+    qn.qn_selftest_roots(0, 0, differ)  # the packed way has no root of 0, and this says so
+    assert int(differ) == 1
+    qn.qn_selftest_roots(0, 6, differ)
+    assert 1 < int(differ) <= 8
+    for first, last in ((5, 4), (-1, 4), (0, 0x7F800000)):
+        with pytest.raises(qn.QNError):
+            qn.qn_selftest_roots(first, last, differ)
+    with pytest.raises(ValueError):
+        qn.qn_selftest_roots(0, 1, differ.cpu())
