@@ -93,3 +93,50 @@ def test_every_root_that_the_packed_way_takes_is_the_correctly_rounded_one(qn): 
             qn.qn_selftest_roots(first, last, differ)
     with pytest.raises(ValueError):
         qn.qn_selftest_roots(0, 1, differ.cpu())
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("sizes", [[0, 40, 0, 3000, 5], [0, 0, 1], [2049, 0], [33, 0, 0, 4100, 0, 0], [0, 9000, 0]])
+def test_empty_tensors_among_others(qn, bits, sizes):  # noqa: F811
+    """Tensors of no elements before, between and behind others, with 8-bit states too: the others' steps are those of a plan
+    without them."""
+    some = [n for n in sizes if n]
+    alone = Case(qn, some, F32, BF16, False, bits, seed=9)
+    beside = Case(qn, some, F32, BF16, False, bits, seed=9)
+    nothing = {dtype: torch.empty(0, dtype=dtype, device="cuda") for dtype in (F32, BF16, torch.uint8)}
+
+    def among(part):
+        rest = iter(part)
+        return [next(rest) if n else nothing[part[0].dtype] for n in sizes]
+
+    scales = dict(m_scale=among(beside.m_scale), v_scale=among(beside.v_scale)) if bits == 8 else {}
+    rest = iter(beside.decay)
+    sums = [torch.zeros(1, dtype=torch.float64, device="cuda") for _ in range(2)]
+    with qn.qn_adam_create(among(beside.theta), among(beside.grad), among(beside.m), among(beside.v), **scales,
+                           weight_decay=[next(rest) if n else 0.0 for n in sizes]) as plan:
+        assert plan.places == alone.plan.places
+        for k in range(2):
+            for p, case, sumsq in ((alone.plan, alone, sums[0]), (plan, beside, sums[1])):
+                qn.qn_adam_norm(p, sumsq)
+                qn.qn_adam_step(p, case.step, sumsq=sumsq, max_norm=0.25, seed=k)
+            assert abs(float(sums[0]) / float(sums[1]) - 1) < 1e-12
+            sums[1].copy_(sums[0])
+            assert all(torch.equal(a, b) for a, b in zip(alone.everything(), beside.everything()))
+        values = [[torch.full((plan.places,), 9.0, device="cuda") for _ in range(2)] for _ in range(2)]
+        qn.qn_adam_state(alone.plan, *values[0])
+        qn.qn_adam_state(plan, *values[1])
+        assert all(torch.equal(a, b) for a, b in zip(*values))
+    beside.guards_whole()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("master", [False, True])
+def test_tensors_without_gradients_stay_whole(qn, bits, master):  # noqa: F811
+    """Parameters, states, scales and master copies of a tensor without a gradient, with others on both sides."""
+    case = Case(qn, [40, 3000, 70, 5000], BF16, BF16, master, bits, offset=1, gap=0)
+    qn.qn_adam_grads(case.plan, [None if i in (1, 2) else g for i, g in enumerate(case.grad)])
+    parts = [p for p in (case.theta, case.master, case.m, case.v, case.m_scale, case.v_scale) if p is not None]
+    before = [[p[i].clone() for i in range(4)] for p in parts]
+    case.check_step(skip=(1, 2), max_norm=0.01, stochastic=True)
+    for p, old in zip(parts, before):
+        assert all(torch.equal(p[i], old[i]) for i in (1, 2))
