@@ -476,7 +476,8 @@ QN_API qn_status qn_distill(int64_t rows, int64_t vocab, qn_dtype dtype, const v
  *   dlogits       NULL (the loss alone), or placed as in qn_logprobs_backward
  * A token that the policy masks (and an empty row) has r = 0, and no gradient passes through its l; its KL term is +inf
  * unless the reference masks it too, which makes it 0.  An empty row's gradient is 0.  Inputs that are not numbers make their row's
- * outputs NaN.  No output but dlogits may overlap an input or another output.  vocab <= QN_GRAD_MAX_VOCAB.
+ * outputs NaN.  No output may overlap an input or another output, but that dlogits may take the logits' place.
+ * vocab <= QN_GRAD_MAX_VOCAB.
  */
 QN_API qn_status qn_policy(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
                            const int64_t* tokens, double temperature, const float* old_logprob, const float* ref_logprob,

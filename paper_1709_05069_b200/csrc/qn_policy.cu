@@ -175,9 +175,14 @@ extern "C" qn_status qn_policy(int64_t rows, int64_t vocab, qn_dtype dtype, cons
         !check_array(logprob, 4, dev) || !check_array(entropy, 4, dev))
         return QN_ERR_INVALID;
     if (dlogits && !check_gradient(rows, vocab, dtype, logits, row_stride, dlogits, dlogits_stride, dev)) return QN_ERR_INVALID;
-    // what is written touches nothing else
+    // what is written touches nothing else, but that the gradient may take the place of the logits
     float* const outputs[] = {loss, logprob, entropy};
     const float* const inputs[] = {old_logprob, ref_logprob, advantage, weight};
+    if (dlogits) {
+        if (overlaps_rows(tokens, rows * 8, dlogits, rows, vocab, dlogits_stride, dtype)) return QN_ERR_INVALID;
+        for (const float* in : inputs)
+            if (in && overlaps_rows(in, rows * 4, dlogits, rows, vocab, dlogits_stride, dtype)) return QN_ERR_INVALID;
+    }
     for (int i = 0; i < 3; ++i) {
         if (!outputs[i]) continue;
         if (overlaps(outputs[i], rows * 4, logits, matrix_bytes(rows, vocab, row_stride, dtype)) ||

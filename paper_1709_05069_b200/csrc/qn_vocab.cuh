@@ -38,6 +38,14 @@ inline size_t matrix_bytes(int64_t rows, int64_t vocab, int64_t row_stride, qn_d
     return static_cast<size_t>((rows - 1) * row_stride + vocab) * dtype_size(dtype);
 }
 
+// Whether an array touches a row of a matrix, and not only what lies between two of them.
+inline bool overlaps_rows(const void* a, size_t bytes, const void* matrix, int64_t rows, int64_t vocab, int64_t row_stride, qn_dtype dtype) {
+    if (!overlaps(a, bytes, matrix, matrix_bytes(rows, vocab, row_stride, dtype))) return false;
+    const int64_t from = reinterpret_cast<intptr_t>(a) - reinterpret_cast<intptr_t>(matrix);
+    const int64_t each = vocab * dtype_size(dtype), apart = row_stride * dtype_size(dtype);
+    return from < 0 || from % apart < each || from + static_cast<int64_t>(bytes) > (from / apart + 1) * apart;
+}
+
 // dlogits takes the place of the logits (same pointer and stride) or does not touch them: the two lie apart, or their rows
 // lie between one another's (same stride).
 inline bool check_gradient(int64_t rows, int64_t vocab, qn_dtype dtype, const void* logits, int64_t row_stride,
