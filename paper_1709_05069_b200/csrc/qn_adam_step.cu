@@ -34,7 +34,6 @@ struct Hyper {
     double lr, log_beta1, log_beta2, max_norm, grad_scale;
     float beta1, rest1, beta2, rest2, eps, minus_zero;
     uint32_t seed_low, seed_high;
-    uint32_t tiny_scales;  // see tiny_scale
 };
 
 // What is the same for all elements of a step.
@@ -243,10 +242,11 @@ __device__ __forceinline__ float keep_of_v(const Hyper& h, uint32_t scale) {
     const float unit = root_unit(scale);
     return unit * unit * -h.beta2;
 }
-// keep_of_m may not be exact: the scale s, but not that of a block of zeros, is so small that beta1 2^(s - 127) is below 2^-126.  With
-// beta1 in [2^-e, 2^(1 - e)) these are the scales from 1 to e.
-__device__ __forceinline__ bool tiny_scale(const Hyper& h, uint32_t scale) { return scale - 1u < h.tiny_scales; }
-uint32_t tiny_scales(float beta1) { return beta1 > 0.0f ? static_cast<uint32_t>(-ilogbf(beta1)) : 0u; }
+// keep_of_m may not be exact: a small scale, but not that of a block of zeros.  From scale 9 on it is above 2^-126 with a beta1 of 2^-8 and
+// more; a smaller one, but for 0, comes with a minus_zero of NaN, so that no element goes the packed way and a step takes several times as
+// long.  (Bounds that follow from beta1 cost all others: 2^28 bf16 parameters 557 -> 578 us.)
+__device__ __forceinline__ bool tiny_scale(uint32_t scale) { return scale - 1u < 8u; }
+float minus_zero_for(float beta1) { return beta1 > 0.0f && beta1 < 0x1p-8f ? NAN : -0.0f; }
 
 // 2^-e / 2^120 (see magnitude_bits; below kHigh this is a number, and one product does for the two there) from the exponent
 // field of a block's largest finite magnitude, which is not 0 (m: may be 0).
@@ -581,7 +581,7 @@ __device__ __forceinline__ void step_octet(const Setting* set, const Hyper& h, c
     root_values(raw.v, r);
 #pragma unroll
     for (int q = 0; q < 4; ++q) g[q] = two_of(raw.grad, q);
-    bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(h, raw.m_scale);
+    bool odd = !moments(h, c, m, r, keeps_m, keeps_v, g, top_m, top_v) || tiny_scale(raw.m_scale);
     uint32_t most_m = __float_as_uint(top_m), field_r = root_field(top_v);
     const int warp_first = i - static_cast<int>(threadIdx.x % 32) * kOctet;
     if (!kVectors && __any_sync(0xffffffffu, odd)) return step_lanes_any<kChance, P, G, kMaster>(set, rates, p, warp_first);
@@ -929,8 +929,8 @@ extern "C" qn_status qn_adam_step(qn_adam_handle h, int64_t* step, double lr, co
     if (!guard.ok) return QN_ERR_CUDA;
     const Hyper hyper{lr, log(beta1), log(beta2), max_norm, grad_scale,
                       static_cast<float>(beta1), static_cast<float>(1.0 - beta1), static_cast<float>(beta2), static_cast<float>(1.0 - beta2),
-                      static_cast<float>(eps), -0.0f, static_cast<uint32_t>(seed), static_cast<uint32_t>(seed >> 32),
-                      tiny_scales(static_cast<float>(beta1))};
+                      static_cast<float>(eps), minus_zero_for(static_cast<float>(beta1)), static_cast<uint32_t>(seed),
+                      static_cast<uint32_t>(seed >> 32)};
     cudaStream_t st = static_cast<cudaStream_t>(cuda_stream);
     nvtxRangePushA("qn:adam_step");
     const auto by_grad = [&](auto grad) {
