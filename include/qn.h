@@ -525,8 +525,8 @@ QN_API qn_status qn_preference(int64_t pairs, int64_t tokens, const float* logpr
  *     m' = beta1 m + (1 - beta1) g~               v' = beta2 v + (1 - beta2) g~^2
  *     theta' = theta (1 - lr' weight_decay) - lr' / (1 - beta1^t) * m' / (sqrt(v' / (1 - beta2^t)) + eps),   lr' = lr lr_scale
  *     c = grad_scale * min(1, max_norm / (|grad_scale| norm)),   norm^2 = *sumsq
- * Arithmetic: fp32, each product and sum that leads to m' and v' rounded by itself; what is the same for all elements of a tensor
- * is in fp64.
+ * Arithmetic: fp32; what is the same for all elements of a tensor is worked out in fp64 and rounded once.  With QN_STATE_8BIT each
+ * product and sum that leads to m' and v' is rounded by itself; with QN_STATE_F32 the last product and the sum are one fused operation.
  *
  * A plan holds the tensors' addresses and sizes on the device that has them (and a small workspace): it is made once, outside
  * stream capture, for tensors that stay where they are.  Gradients that move are named again with qn_adam_grads.  Calls
@@ -545,7 +545,8 @@ typedef struct qn_adam_plan* qn_adam_handle;
 
 /*
  * One tensor: contiguous arrays of numel elements, each aligned to its element type.  Arrays at multiples of 8 elements'
- * size (32 bytes of fp32, 16 of bf16, 8 of codes) are moved in vectors, which is the fastest; the results are the same.
+ * size (32 bytes of fp32, 16 of bf16, 8 of codes) are moved in vectors, which is the fastest; the results of a step are the
+ * same wherever they lie (given the same *sumsq, whose last bits depend on where the gradients lie).
  *   param       theta, of the plan's parameter type; read and written
  *   grad        g, of the plan's gradient type; read only.  NULL: the tensor has none, and is left alone with its states
  *   master      NULL, or (for all tensors of a plan, whose parameters are bf16) theta in fp32: the step is taken from it and
@@ -589,7 +590,8 @@ QN_API qn_status qn_adam_norm(qn_adam_handle h, double* sumsq, void* cuda_stream
  * One step.
  *   step        DEVICE int64: steps taken so far; counted up by one
  *   lr          learning rate >= 0; lr_device (DEVICE fp32, may be NULL) takes its place.  lr' / (1 - beta1^t) up to 2^64
- *   beta1, beta2 in [0, 1);  eps >= 2^-126
+ *   beta1, beta2 in [0, 1);  eps >= 2^-126.  (QN_STATE_8BIT: elements with v' = 0 and, for 0 < beta1 < 2^-8, all elements
+ *               take several times as long)
  *   sumsq       DEVICE, may be NULL: the norm's square (qn_adam_norm).  If it is not finite nothing is changed, *step neither
  *   max_norm    > 0: gradients whose norm (times |grad_scale|) is larger are scaled down to it; needs sumsq.  Otherwise no bound
  *   grad_scale  gradients are multiplied by it first (1 / a loss scale)

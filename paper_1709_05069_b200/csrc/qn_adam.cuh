@@ -72,8 +72,10 @@ __device__ __forceinline__ void find_tensor(const Tensors& all, int64_t piece, i
 
 // ---- random numbers ------------------------------------------------------------------------------------------------
 
-// A hash of 32 bits by multiplication and shifts.  The multipliers are the fractions of sqrt(3), sqrt(5) and sqrt(6) and of
-// the golden ratio, made odd; the means, pairwise correlations and two-dimensional histograms of what comes out were looked at.
+// A hash of 32 bits by multiplication and shifts; the shifts 15, 13 and 16 between products are those of the last steps of the published
+// hash XXH32.  The multipliers are the first 32 bits of the fractions of sqrt(3), sqrt(5) and sqrt(7), made odd, and for what is counted up
+// Knuth's for multiplicative hashing, the prime 2654435761 next to the golden ratio's fraction; the means, pairwise correlations and
+// two-dimensional histograms of what comes out were looked at.
 constexpr uint32_t kGolden = 0x9E3779B1u, kMix1 = 0xBB67AE85u, kMix2 = 0x3C6EF373u, kMix3 = 0xA54FF53Bu;
 
 __device__ __forceinline__ uint32_t mix(uint32_t x) {

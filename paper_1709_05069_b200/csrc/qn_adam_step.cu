@@ -11,11 +11,16 @@
 // states in 32 bits an element a lane, eight for each thread; so does, with both, what is left of a piece where a tensor ends.
 //
 // Measured on a B200 (a copy: 6.54 TB/s), bytes of the floor over time:
-//   states in 32 bits: bound by memory.  2^28 bf16 parameters with master copies 1210 us = 6.65 TB/s, 25.6 million fp32 ones 118 us
-//       = 6.1 TB/s; off vectors 4.4 to 5.1 TB/s.  With two CTAs on an SM and 88 registers 3 % less than with three and 80.
+//   states in 32 bits: bound by memory.  2^28 bf16 parameters with master copies (28 bytes an element) 1195 to 1210 us = 6.3 to 6.2 TB/s,
+//       without (22 bytes) 913 us = 6.5 TB/s to nearest and by chance, 25.6 million fp32 ones 118 us = 6.1 TB/s; off vectors 4.4 to
+//       5.1 TB/s: four-byte accesses.  With two CTAs on an SM and 88 registers 3 % less than with three and 80.
 //   states in 8 bits: 57 instructions an element, of which 27 go to the integer and comparison pipe; three quarters of the issue
-//       slots, two thirds of that pipe.  2^28 bf16 parameters 578 us = 4.75 TB/s; off vectors 80 instructions, 2^27 bf16 ones
+//       slots, two thirds of that pipe.  2^28 bf16 parameters 557 to 578 us = 4.9 to 4.7 TB/s, to nearest 528 us, with master copies
+//       895 us = 4.8 TB/s, 2^27 fp32 ones 500 us (bf16 gradients: 394 us) = 4.3 (4.8) TB/s; off vectors 80 instructions, 2^27 bf16 ones
 //       428 us = 3.2 TB/s, 25.6 million fp32 ones 107 us (an element a lane 93, 558 and 120).
+//       What the packed way does not take is slow, elements with v' = 0 above all: 2^27 bf16 parameters 266 us, with one of 64 elements or
+//       all without history 1150 us, with every other 1024 elements 885 us; off vectors, where a warp's 256 elements go together, 400 us, 3.0
+//       and 1.6 ms.
 //   Steps on the way (2^28 bf16, 8 bits): an element a lane 4.3 ms; eight elements a thread in vectors 1106 us (81
 //       instructions, two CTAs on an SM); the root by one correction instead of a call, reciprocals, codes put together from
 //       upper bytes 763; runs instead of chunks 726; copies ahead through shared memory 581 (three slots 619, six 605); turns,
